@@ -365,6 +365,125 @@ mp_status mp_replay_plan(const mp_batch *batch, const int64_t *offsets, const in
                          int64_t slab_bytes, int32_t *ok, int32_t *first_bad, int32_t *trace_status,
                          void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Key/value cache in 8 bits, in planned blocks
+ *
+ * The largest per-token state of a serving step is its key/value cache.  Here
+ * it lies in a pool of blocks of block_tokens tokens, so that a plan whose
+ * tensors are whole blocks (a request's cache: alloc_step = its first step,
+ * free_step = past its last, size = its blocks) gives every request its blocks
+ * by offset.  Keys and values are e4m3 bytes with one scale for each block and
+ * head: a stored byte stands for byte * scale.  mp_kv_write makes every scale a
+ * power of two, which costs an e4m3 value no precision.
+ *
+ * Inside a block and head (D = head_dim, t = token in the block, d = value)
+ *   key byte    ((t / 8) * (D / 16) + d / 16) * 128 + (t % 8) * 16 + d % 16
+ *   value byte  (t / 32) * 32 * D + (d / 8) * 256 + (t / 16 % 2) * 128 + (d % 8) * 16 + t % 16
+ * that is, tiles of 8 rows of 16 bytes, the summed-over axis of either product
+ * along the row.
+ *
+ * The conventions above hold, with sequences in the place of traces: per-sequence
+ * data errors go to seq_status[b] (MP_EINVAL), and a sequence that has one leaves
+ * the others untouched. */
+
+/* Type of the values of an mp_tokens. */
+typedef enum mp_dtype { MP_F16 = 0, MP_BF16 = 1, MP_F32 = 2 } mp_dtype;
+
+/* The pool.  n_blocks >= 0; block_tokens a multiple of 32, at most 256; n_heads
+ * >= 1 (key/value heads); head_dim 64 or 128.
+ *   k, v              uint8[n_blocks][n_heads][block_tokens * head_dim], 16-byte aligned
+ *   k_scale, v_scale  float[n_blocks][n_heads], finite and not negative */
+typedef struct mp_kv_cache {
+    int32_t n_blocks;
+    int32_t block_tokens;
+    int32_t n_heads;
+    int32_t head_dim;
+    uint8_t *k;
+    uint8_t *v;
+    float *k_scale;
+    float *v_scale;
+} mp_kv_cache;
+
+/* The sequences of one call.  Host scalars:
+ *   n_seqs      B >= 0
+ *   max_blocks  columns of table
+ *   max_tokens  upper bound on n_b = token_ptr[b+1] - token_ptr[b]
+ *   max_len     upper bound on lens[b], at most max_blocks * block_tokens
+ *   n_tokens    rows of the call's token arrays (= token_ptr[B])
+ * Device arrays:
+ *   table      int32[B][max_blocks]  pool block of positions [j * block_tokens, + block_tokens)
+ *              of sequence b; entries past its last block are not read
+ *   lens       int32[B]    tokens that sequence b holds, the call's included
+ *   token_ptr  int64[B+1]  rows [token_ptr[b], token_ptr[b+1]) of the token arrays are
+ *              positions [lens[b] - n_b, lens[b]) of sequence b
+ * MP_EINVAL in seq_status: a bad CSR range, a bound broken, a negative length, a
+ * table entry outside the pool (or, where tokens are stored or read, n_b > lens[b]). */
+typedef struct mp_kv_batch {
+    int32_t n_seqs;
+    int32_t max_blocks;
+    int32_t max_tokens;
+    int32_t max_len;
+    int64_t n_tokens;
+    const int32_t *table;
+    const int32_t *lens;
+    const int64_t *token_ptr;
+} mp_kv_batch;
+
+/* [n_tokens][n_heads][head_dim] values; strides in elements, the last axis
+ * dense; data aligned to its type (16-byte aligned rows are read faster). */
+typedef struct mp_tokens {
+    void *data;
+    int64_t token_stride;
+    int64_t head_stride;
+    int32_t n_heads;
+    int32_t dtype; /* mp_dtype */
+} mp_tokens;
+
+/* Quantises the call's keys and values into the blocks of their positions.  For
+ * each block and head touched, keys and values apart: with a = max |x| over the
+ * call's tokens in it and e the least integer in [-60, 120] with a <= 448 * 2^e,
+ * the scale becomes 2^e, or stays what it was where the block already held
+ * earlier tokens of the sequence under a larger one; bytes are x / scale rounded
+ * to the nearest e4m3 value (ties to even).  Where the scale grows, the block's
+ * earlier tokens are rounded anew under it.  Slots without a token are left alone.
+ * A NaN is stored as 0 and an infinity as the largest value (and neither counts
+ * in a); its sequence gets MP_EINVAL.  k, v: any mp_dtype, the same for both;
+ * n_heads as the cache's.  No two sequences of a call may share a block that it
+ * writes.  seq_status int32[B]. */
+mp_status mp_kv_write(const mp_kv_cache *cache, const mp_kv_batch *batch, const mp_tokens *k, const mp_tokens *v,
+                      int32_t *seq_status, void *stream);
+
+/* Reads positions [lens[b] - n_b, lens[b]) of every sequence back: byte * scale,
+ * rounded once to the outputs' type (any mp_dtype).  Outputs of a failed sequence
+ * are unspecified.  seq_status int32[B]. */
+mp_status mp_kv_read(const mp_kv_cache *cache, const mp_kv_batch *batch, const mp_tokens *k, const mp_tokens *v,
+                     int32_t *seq_status, void *stream);
+
+/* Bytes of device workspace mp_kv_attend needs for this cache, batch and number
+ * of query heads (depends on the host scalars only; 0 for a batch that the call
+ * rejects or that has no work). */
+size_t mp_kv_attend_workspace_bytes(const mp_kv_cache *cache, const mp_kv_batch *batch, int32_t n_q_heads);
+
+/* Attention of the call's tokens over what their sequences hold.  Query i of
+ * sequence b stands at position p = lens[b] - n_b + i and sees positions
+ *   j < lens[b];  with causal != 0 also j <= p;  with window > 0 (causal only)
+ *   also j > p - window.
+ * out = sum_j w_j v_j with w = softmax_j(scale * q . k_j), lse = log sum_j
+ * exp(scale * q . k_j) (natural); query head h reads cache head
+ * h / (q->n_heads / cache->n_heads).  A query that sees nothing gets out = 0 and
+ * lse = -inf.  Products of 16-bit values are summed in 32 bits, as are the
+ * softmax's sums; its weights are rounded to 16 bits (11 of precision) for the
+ * second product.
+ * q, out: MP_F16 or MP_BF16, the same for both; n_heads a multiple of the
+ * cache's.  scale > 0, finite.  lse: float[n_tokens][n_heads] or NULL.
+ * seq_status int32[B]; MP_ETIMEOUT there means that a wait inside a kernel gave
+ * up.  Outputs of a failed sequence are unspecified.  workspace: at least
+ * mp_kv_attend_workspace_bytes(cache, batch, q->n_heads) bytes, rules as for
+ * mp_plan_greedy_by_size. */
+mp_status mp_kv_attend(const mp_kv_cache *cache, const mp_kv_batch *batch, const mp_tokens *q, float scale,
+                       int32_t causal, int32_t window, const mp_tokens *out, float *lse, int32_t *seq_status,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
 /* Static, NUL-terminated name of a status code. */
 const char *mp_status_string(mp_status status);
 

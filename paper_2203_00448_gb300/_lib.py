@@ -34,6 +34,10 @@ EXPORTS = (
     "mp_slab_layout",
     "mp_replay_workspace_bytes",
     "mp_replay_plan",
+    "mp_kv_write",
+    "mp_kv_read",
+    "mp_kv_attend_workspace_bytes",
+    "mp_kv_attend",
     "mp_status_string",
     "mp_abi_version",
 )
@@ -63,6 +67,27 @@ class MpHostResults(ctypes.Structure):
 
     _fields_ = [(name, ctypes.c_void_p) for name in
                 ("profile", "peak_lb", "offsets", "plan_peak", "verdict", "conflict", "trace_status")]
+
+
+class MpKvCache(ctypes.Structure):
+    """Mirror of struct mp_kv_cache."""
+
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_blocks", "block_tokens", "n_heads", "head_dim")] + \
+        [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
+
+
+class MpKvBatch(ctypes.Structure):
+    """Mirror of struct mp_kv_batch."""
+
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_seqs", "max_blocks", "max_tokens", "max_len")] + \
+        [("n_tokens", ctypes.c_int64)] + [(n, ctypes.c_void_p) for n in ("table", "lens", "token_ptr")]
+
+
+class MpTokens(ctypes.Structure):
+    """Mirror of struct mp_tokens."""
+
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("n_heads", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
 HOST_PATH_MAX_CHUNKS = 64
@@ -127,6 +152,15 @@ def load(path: str = LIB_PATH):
     lib.mp_replay_workspace_bytes.restype = sz
     lib.mp_replay_plan.argtypes = [BP, P, P, P, ctypes.c_int64, P, P, P, P, sz, P]
     lib.mp_replay_plan.restype = i32
+    CP, KP, TP = (ctypes.POINTER(t) for t in (MpKvCache, MpKvBatch, MpTokens))
+    lib.mp_kv_write.argtypes = [CP, KP, TP, TP, P, P]
+    lib.mp_kv_write.restype = i32
+    lib.mp_kv_read.argtypes = [CP, KP, TP, TP, P, P]
+    lib.mp_kv_read.restype = i32
+    lib.mp_kv_attend_workspace_bytes.argtypes = [CP, KP, i32]
+    lib.mp_kv_attend_workspace_bytes.restype = sz
+    lib.mp_kv_attend.argtypes = [CP, KP, TP, ctypes.c_float, i32, i32, TP, P, P, P, sz, P]
+    lib.mp_kv_attend.restype = i32
     lib.mp_status_string.argtypes = [i32]
     lib.mp_status_string.restype = ctypes.c_char_p
     lib.mp_abi_version.argtypes = []

@@ -108,6 +108,38 @@ mp_status check_workspace(size_t need, const void* ws, size_t ws_bytes) {
     return MP_OK;
 }
 
+mp_status check_cache(const mp_kv_cache* c) {
+    if (c == nullptr || c->n_blocks < 0 || c->n_heads < 1 || (c->head_dim != 64 && c->head_dim != 128) ||
+        c->block_tokens < 32 || c->block_tokens > 256 || c->block_tokens % 32 != 0)
+        return MP_EINVAL;
+    const int64_t n = c->n_blocks;
+    if (!array_ok(c->k_scale, n) || !array_ok(c->v_scale, n)) return MP_EINVAL;
+    for (const uint8_t* p : {c->k, c->v})
+        if ((n > 0 && p == nullptr) || reinterpret_cast<uintptr_t>(p) % 16 != 0) return MP_EINVAL;
+    return MP_OK;
+}
+
+constexpr int64_t kKvMost = 1 << 28;  // positions, tokens, query rows: their sums and differences fit in 32 bits
+
+mp_status check_kv_batch(const mp_kv_cache* c, const mp_kv_batch* bt) {
+    if (bt == nullptr || bt->n_seqs < 0 || bt->max_blocks < 0 || bt->max_tokens < 0 || bt->max_len < 0 ||
+        bt->n_tokens < 0 || bt->max_len > (int64_t)bt->max_blocks * c->block_tokens || bt->max_len > kKvMost ||
+        bt->max_tokens > kKvMost)
+        return MP_EINVAL;
+    const int64_t B = bt->n_seqs;
+    if (!array_ok(bt->table, B * bt->max_blocks) || !array_ok(bt->lens, B) || !array_ok(bt->token_ptr, B ? B + 1 : 0))
+        return MP_EINVAL;
+    return MP_OK;
+}
+
+// Rows of n_heads heads (a multiple of them where `grouped`).
+mp_status check_tokens(const mp_tokens* t, const mp_kv_batch* bt, int32_t n_heads, bool grouped, int32_t max_dtype) {
+    if (t == nullptr || t->dtype < 0 || t->dtype > max_dtype || t->n_heads < 1) return MP_EINVAL;
+    if (grouped ? t->n_heads % n_heads != 0 : t->n_heads != n_heads) return MP_EINVAL;
+    if (bt->n_tokens > 0 && t->data == nullptr) return MP_EINVAL;
+    return reinterpret_cast<uintptr_t>(t->data) % (t->dtype == MP_F32 ? 4 : 2) == 0 ? MP_OK : MP_EINVAL;
+}
+
 mp_status from_cuda(cudaError_t e) { return e == cudaSuccess ? MP_OK : MP_ECUDA; }
 
 }  // namespace
@@ -314,6 +346,60 @@ __attribute__((visibility("default"))) mp_status mp_peak(const mp_batch* batch, 
         !array_ok(trace_status, batch->n_traces))
         return MP_EINVAL;
     return from_cuda(mp::launch_peak(*batch, offsets, plan_peak, trace_status, static_cast<cudaStream_t>(stream)));
+}
+
+__attribute__((visibility("default"))) mp_status mp_kv_write(const mp_kv_cache* cache, const mp_kv_batch* batch,
+                                                             const mp_tokens* k, const mp_tokens* v,
+                                                             int32_t* seq_status, void* stream) {
+    mp_status st = check_cache(cache);
+    if (st == MP_OK) st = check_kv_batch(cache, batch);
+    if (st == MP_OK) st = check_tokens(k, batch, cache->n_heads, false, MP_F32);
+    if (st == MP_OK) st = check_tokens(v, batch, cache->n_heads, false, MP_F32);
+    if (st != MP_OK) return st;
+    if (k->dtype != v->dtype || !array_ok(seq_status, batch->n_seqs)) return MP_EINVAL;
+    return from_cuda(mp::launch_kv_write(*cache, *batch, *k, *v, seq_status, static_cast<cudaStream_t>(stream)));
+}
+
+__attribute__((visibility("default"))) mp_status mp_kv_read(const mp_kv_cache* cache, const mp_kv_batch* batch,
+                                                            const mp_tokens* k, const mp_tokens* v,
+                                                            int32_t* seq_status, void* stream) {
+    mp_status st = check_cache(cache);
+    if (st == MP_OK) st = check_kv_batch(cache, batch);
+    if (st == MP_OK) st = check_tokens(k, batch, cache->n_heads, false, MP_F32);
+    if (st == MP_OK) st = check_tokens(v, batch, cache->n_heads, false, MP_F32);
+    if (st != MP_OK) return st;
+    if (k->dtype != v->dtype || !array_ok(seq_status, batch->n_seqs)) return MP_EINVAL;
+    return from_cuda(mp::launch_kv_read(*cache, *batch, *k, *v, seq_status, static_cast<cudaStream_t>(stream)));
+}
+
+__attribute__((visibility("default"))) size_t mp_kv_attend_workspace_bytes(const mp_kv_cache* cache,
+                                                                           const mp_kv_batch* batch,
+                                                                           int32_t n_q_heads) {
+    if (check_cache(cache) != MP_OK || check_kv_batch(cache, batch) != MP_OK || n_q_heads < 1 ||
+        n_q_heads % cache->n_heads != 0)
+        return 0;
+    return mp::kv_attend_workspace_bytes(*cache, *batch, n_q_heads);
+}
+
+__attribute__((visibility("default"))) mp_status mp_kv_attend(const mp_kv_cache* cache, const mp_kv_batch* batch,
+                                                              const mp_tokens* q, float scale, int32_t causal,
+                                                              int32_t window, const mp_tokens* out, float* lse,
+                                                              int32_t* seq_status, void* workspace,
+                                                              size_t workspace_bytes, void* stream) {
+    mp_status st = check_cache(cache);
+    if (st == MP_OK) st = check_kv_batch(cache, batch);
+    if (st == MP_OK) st = check_tokens(q, batch, cache->n_heads, true, MP_BF16);
+    if (st == MP_OK) st = check_tokens(out, batch, cache->n_heads, true, MP_BF16);
+    if (st != MP_OK) return st;
+    if (q->dtype != out->dtype || q->n_heads != out->n_heads || q->n_heads / cache->n_heads > 1024 ||
+        (int64_t)batch->max_tokens * (q->n_heads / cache->n_heads) > kKvMost || !(scale > 0.f && scale <= 3.402823466e38f) ||
+        window < 0 || (window > 0 && !causal) || !array_ok(seq_status, batch->n_seqs) ||
+        (lse != nullptr && !aligned(lse)))
+        return MP_EINVAL;
+    st = check_workspace(mp::kv_attend_workspace_bytes(*cache, *batch, q->n_heads), workspace, workspace_bytes);
+    if (st != MP_OK) return st;
+    return from_cuda(mp::launch_kv_attend(*cache, *batch, *q, scale, causal, window, *out, lse, seq_status, workspace,
+                                          static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

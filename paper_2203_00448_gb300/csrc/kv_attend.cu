@@ -1,0 +1,590 @@
+// kv_attend.cu -- mp_kv_attend for few query rows a sequence and head (single
+// tokens, a few proposed ones), and the joining of split sequences.
+//
+// A work unit is one granule (32 tokens) of one cache head under one tile of 8 * NT
+// query rows (rows = tokens x heads of a group, which share the cached head).  The
+// units of all sequences, tiles and heads lie on one line that is cut evenly among
+// the warps of the grid, so ragged batches and single long contexts keep every SM
+// at the memory alike; a warp walks its stretch with bulk copies into a ring of
+// its own, no warp waiting for another.  A (sequence, tile, head) that one warp holds
+// whole is written at once; the others leave (sum, reference, weighted values) and
+// k_kv_join adds them up.
+//
+// Per granule: scores S^T = K Q^T and O^T += V^T P^T on warp-level matrix products
+// in f16, rows of the stored tiles as the left operand, so that 8 query rows cost one
+// product column block and no query row is padding for a group of 8.  Stored bytes
+// become f16 exactly.  With x_j = scale * q.k_j * log2(e) * key scale + log2(value
+// scale), w_j = 2^(x_j - M) <= 1 under the running maximum M, the output is
+// sum w_j byte_j / sum (w_j / value scale): the value scale costs nothing per element
+// and products stay within f16's range whatever the scales.  Sums are f32; w is
+// rounded to f16 (11 bits, down to 2^-38 of the largest).
+#include <algorithm>
+#include <cmath>
+
+#include "kv_attend.cuh"
+
+namespace mp {
+namespace {
+
+constexpr int kFewWarps = 8;
+constexpr int kFewStages = 3;
+constexpr int kJoinThreads = 256;
+
+struct FewArgs {
+    mp_kv_cache c;
+    mp_kv_batch bt;
+    mp_tokens q, out;
+    float* lse;
+    int32_t* status;
+    float scale;
+    int32_t causal, window;
+    int32_t group;      // query heads a cache head
+    int32_t rows_skip;  // sequences of more rows than this are another kernel's (0: none are)
+    int32_t warps;      // of the grid
+    int64_t* base;      // [n_seqs + 1] first unit of each sequence, then units a warp
+    float* part;        // [2 * warps][rows * (D + 2)]
+    int32_t* gave_up;   // [warps]
+};
+
+// Granules [lo, hi) that the call's tokens of a sequence see.
+__device__ __forceinline__ void seq_granules(const FewArgs& a, const SeqView& s, int& lo, int& hi) {
+    const int start = s.len - s.n;
+    lo = a.window > 0 ? max(0, start - a.window + 1) / kGranule : 0;
+    hi = s.n > 0 ? (s.len + kGranule - 1) / kGranule : lo;
+}
+__device__ __forceinline__ bool seq_is_few(const FewArgs& a, const SeqView& s) {
+    return a.rows_skip == 0 || (int64_t)s.n * a.group <= a.rows_skip;
+}
+template <int kRows>
+__device__ __forceinline__ int seq_tiles(const FewArgs& a, const SeqView& s) {
+    return (int)(((int64_t)s.n * a.group + kRows - 1) / kRows);
+}
+template <int kRows>
+__device__ __forceinline__ int64_t seq_units(const FewArgs& a, int b) {
+    const SeqView s = load_seq(a.bt, b, false);
+    if (s.st != MP_OK || !seq_is_few(a, s)) return 0;
+    int lo, hi;
+    seq_granules(a, s, lo, hi);
+    return (int64_t)(hi - lo) * a.c.n_heads * seq_tiles<kRows>(a, s);
+}
+
+// A position on the line of units.
+struct Cursor {
+    int b, lo, hi, g;    // sequence, its granules, the granule
+    int slots, slot;     // tiles x heads, tile * heads + head
+    __device__ __forceinline__ void seek(int lo_, int hi_, int slots_, int64_t unit) {
+        lo = lo_, hi = hi_, slots = slots_;
+        slot = (int)(unit / (hi - lo));
+        g = lo + (int)(unit % (hi - lo));
+    }
+};
+template <int kRows>
+__device__ __forceinline__ bool enter(const FewArgs& a, Cursor& c, int64_t unit) {
+    const SeqView s = load_seq(a.bt, c.b, false);
+    if (s.st != MP_OK || !seq_is_few(a, s)) return false;
+    int lo, hi;
+    seq_granules(a, s, lo, hi);
+    const int slots = a.c.n_heads * seq_tiles<kRows>(a, s);
+    if (hi <= lo || slots == 0) return false;
+    c.seek(lo, hi, slots, unit);
+    return true;
+}
+template <int kRows>
+__device__ __forceinline__ void next(const FewArgs& a, Cursor& c) {
+    if (++c.g < c.hi) return;
+    c.g = c.lo;
+    if (++c.slot < c.slots) return;
+    do ++c.b;
+    while (c.b < a.bt.n_seqs && !enter<kRows>(a, c, 0));
+}
+__device__ __forceinline__ int page_of(const FewArgs& a, const Cursor& c) {
+    const int p = __ldg(a.bt.table + (int64_t)c.b * a.bt.max_blocks + c.g / (a.c.block_tokens / kGranule));
+    return p >= 0 && p < a.c.n_blocks ? p : 0;  // k_kv_join reports it; nothing outside the pool is read
+}
+
+__device__ __forceinline__ void mma(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                    uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
+
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(kFewWarps * 32, 1) k_kv_attend_few(FewArgs a) {
+    constexpr int kRows = 8 * NT;
+    constexpr int kBytes = kGranule * D;  // of either array
+    extern __shared__ __align__(128) uint8_t dyn[];
+    __shared__ int64_t strip_base[kFewWarps * 32 + 1];
+    __shared__ int64_t warp_sum[kFewWarps];
+    __shared__ __align__(8) uint64_t bars[kFewWarps * kFewStages];
+    __shared__ int pages[kFewWarps * kFewStages];
+    const int tid = threadIdx.x, lane = tid % 32, wid = tid / 32;
+    const int g = lane / 4, t = lane % 4;
+
+    // every CTA lays the line out for itself: thread i sums a strip of sequences
+    const int strip = (a.bt.n_seqs + kFewWarps * 32 - 1) / (kFewWarps * 32);
+    {
+        int64_t mine = 0;
+        for (int i = 0; i < strip; ++i) {
+            const int b = tid * strip + i;
+            if (b < a.bt.n_seqs) mine += seq_units<kRows>(a, b);
+        }
+        int64_t sum = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t x = __shfl_up_sync(~0u, sum, o);
+            if (lane >= o) sum += x;
+        }
+        if (lane == 31) warp_sum[wid] = sum;
+        if (tid < kFewWarps * kFewStages) mbar_init(&bars[tid], 1);
+        fence_mbar_init();
+        __syncthreads();
+        for (int w = 0; w < wid; ++w) sum += warp_sum[w];
+        strip_base[tid] = sum - mine;
+        if (tid == kFewWarps * 32 - 1) strip_base[kFewWarps * 32] = sum;
+        if (blockIdx.x == 0) {
+            int64_t at = sum - mine;
+            for (int i = 0; i < strip; ++i) {
+                const int b = tid * strip + i;
+                if (b < a.bt.n_seqs) {
+                    a.base[b] = at;
+                    at += seq_units<kRows>(a, b);
+                    if (b == a.bt.n_seqs - 1) a.base[b + 1] = at;
+                }
+            }
+        }
+        __syncthreads();
+    }
+    const int64_t total = strip_base[kFewWarps * 32];
+    const int64_t per_warp = (total + a.warps - 1) / a.warps;
+    // consecutive warps of the line are on different SMs: short lines reach them all
+    const int w = wid * gridDim.x + blockIdx.x;
+    if (w == 0 && lane == 0) a.base[a.bt.n_seqs + 1] = per_warp;
+    const int64_t u0 = min(total, w * per_warp), u1 = min(total, u0 + per_warp);
+    if (lane == 0) a.gave_up[w] = 0;
+    if (u0 >= u1) return;
+
+    Cursor cur;
+    {
+        // the strip that holds u0 (the last whose base is not past it), then the sequence
+        int lo = 0, hi = kFewWarps * 32;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (strip_base[mid] <= u0) lo = mid;
+            else hi = mid;
+        }
+        int64_t at = strip_base[lo];
+        cur.b = lo * strip;
+        for (;; ++cur.b) {
+            const int64_t n = seq_units<kRows>(a, cur.b);
+            if (u0 < at + n) break;
+            at += n;
+        }
+        enter<kRows>(a, cur, u0 - at);
+    }
+    uint8_t* ring = dyn + wid * kFewStages * 2 * kBytes;
+    uint64_t* bar = bars + wid * kFewStages;
+    int* ring_page = pages + wid * kFewStages;
+
+    Cursor ahead = cur;
+    int64_t issued = u0;
+    int page_ahead = page_of(a, ahead);
+    auto issue = [&]() {  // the next unit's bytes into its stage
+        if (issued >= u1) return;
+        const int st = (int)((issued - u0) % kFewStages);
+        const int64_t at = block_byte(a.c, page_ahead, ahead.slot % a.c.n_heads) +
+                           (int64_t)(ahead.g % (a.c.block_tokens / kGranule)) * kBytes;
+        if (lane == 0) {
+            ring_page[st] = page_ahead;
+            mbar_expect(&bar[st], 2 * kBytes);
+            bulk_load(ring + st * 2 * kBytes, a.c.k + at, kBytes, &bar[st]);
+            bulk_load(ring + st * 2 * kBytes + kBytes, a.c.v + at, kBytes, &bar[st]);
+        }
+        if (++issued < u1) {
+            next<kRows>(a, ahead);
+            page_ahead = page_of(a, ahead);
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < kFewStages; ++i) issue();
+    __syncwarp();
+
+    uint32_t qf[NT][D / 16][2];     // Q^T: 4 consecutive values of row 8 nt + g a lane and chunk
+    float unit[NT][2];              // of score columns 2t, 2t + 1: scale * log2(e) over the row's power of two
+    float top[NT][2], sum[NT][2];   // running maximum of x, this lane's part of the sum
+    float o[NT][D / 16][4];
+    int see_lo[NT][2], see_hi[NT][2];  // positions that the column's row sees
+    bool fresh = true;
+    int64_t lo_row = 0;
+    bool up = false;
+
+    for (int64_t u = u0; u < u1; ++u) {
+        const int head = cur.slot % a.c.n_heads, tile = cur.slot / a.c.n_heads;
+        if (fresh) {
+            fresh = false;
+            const SeqView s = load_seq(a.bt, cur.b, false);
+            const int rows = s.n * a.group;
+            lo_row = s.lo;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const int r = tile * kRows + nt * 8 + g;
+                float x[D / 16][4], most = 0.f;
+                const T* p = static_cast<const T*>(a.q.data) + (s.lo + r / a.group) * a.q.token_stride +
+                             (head * a.group + r % a.group) * a.q.head_stride;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        x[i][k] = r < rows ? to_f32(p[i * 16 + t * 4 + k]) : 0.f;
+                        most = fmaxf(most, fabsf(x[i][k]));
+                    }
+                }
+                most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
+                most = fmaxf(most, __shfl_xor_sync(~0u, most, 2));
+                const float f = row_factor(most);
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    qf[nt][i][0] = pack_f16(x[i][0] * f, x[i][1] * f);
+                    qf[nt][i][1] = pack_f16(x[i][2] * f, x[i][3] * f);
+                }
+                const float mine = __fdiv_rn(a.scale * 1.4426950408889634f, f);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    unit[nt][k] = __shfl_sync(~0u, mine, (2 * t + k) * 4);
+                    const int col = tile * kRows + nt * 8 + 2 * t + k;
+                    const int pos = s.len - s.n + col / a.group;
+                    see_hi[nt][k] = col >= rows ? 0 : a.causal ? min(s.len, pos + 1) : s.len;
+                    see_lo[nt][k] = a.window > 0 ? pos - a.window + 1 : 0;
+                    top[nt][k] = -INFINITY, sum[nt][k] = 0.f;
+                }
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
+            }
+        }
+        const int st = (int)((u - u0) % kFewStages);
+        if (!__all_sync(~0u, mbar_wait(&bar[st], (uint32_t)((u - u0) / kFewStages & 1)))) {
+            up = true;
+            break;
+        }
+        const int64_t sc = (int64_t)ring_page[st] * a.c.n_heads + head;
+        const float ks = __ldg(a.c.k_scale + sc), vs = value_scale(__ldg(a.c.v_scale + sc));
+        const uint8_t* kb = ring + st * 2 * kBytes;
+        const uint8_t* vb = kb + kBytes;
+
+        // scores: product row r of 16 is token 4 (r % 8 / 2) + r % 2 + 2 (r / 8), the order in which a
+        // lane's 4 stored value bytes meet the second product
+        float s[NT][2][4] = {};
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const int tok = 4 * (g / 2) + g % 2;
+            const uint8_t* row = kb + (m * 2 + tok / 8) * (D * 8) + tok % 8 * 16 + t * 4;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                uint32_t a0, a1, a2, a3;
+                e4m3_to_f16(*reinterpret_cast<const uint32_t*>(row + i * 128), a0, a2);
+                e4m3_to_f16(*reinterpret_cast<const uint32_t*>(row + i * 128 + 32), a1, a3);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma(s[nt][m], a0, a1, a2, a3, qf[nt][i][0], qf[nt][i][1]);
+            }
+        }
+        const float lv = log2f(vs), iv = __fdiv_rn(1.f, vs);
+        const int base = cur.g * kGranule;
+        uint32_t p[NT][2][2];
+        bool moved = false;
+        float fade[NT][2];
+        int last = 0;  // one past the last position that any row sees: stored bytes behind it mean nothing
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float unit_k = unit[nt][k] * ks;
+                float most = -INFINITY;
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int j = base + m * 16 + 4 * (g / 2) + g % 2 + 2 * h;
+                        const bool seen = j < see_hi[nt][k] && j >= see_lo[nt][k];
+                        float& x = s[nt][m][2 * h + k];
+                        x = seen ? fmaf(x, unit_k, lv) : -INFINITY;
+                        most = fmaxf(most, x);
+                    }
+                most = fmaxf(most, __shfl_xor_sync(~0u, most, 4));
+                most = fmaxf(most, __shfl_xor_sync(~0u, most, 8));
+                most = fmaxf(most, __shfl_xor_sync(~0u, most, 16));
+                const float now = fmaxf(top[nt][k], most);
+                const float ref = now == -INFINITY ? 0.f : now - kLift;
+                fade[nt][k] = exp2_approx(top[nt][k] - kLift - ref);
+                moved |= now != top[nt][k];
+                top[nt][k] = now;
+                float part = 0.f;
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float& x = s[nt][m][2 * h + k];
+                        x = exp2_approx(x - ref);
+                        part += x;
+                    }
+                sum[nt][k] = fmaf(part, iv, sum[nt][k] * fade[nt][k]);
+                last = max(last, see_hi[nt][k]);
+            }
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                p[nt][m][0] = transposed(pack_f16(s[nt][m][0], s[nt][m][1]));
+                p[nt][m][1] = transposed(pack_f16(s[nt][m][2], s[nt][m][3]));
+            }
+        }
+        if (__any_sync(~0u, moved)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) o[nt][i][k] *= fade[nt][k % 2];
+        }
+        last = __reduce_max_sync(~0u, last);
+        if (base + kGranule <= last) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    const uint8_t* at = vb + i * 512 + h * 128 + lane * 4;
+                    uint32_t a0, a1, a2, a3;
+                    e4m3_to_f16(*reinterpret_cast<const uint32_t*>(at), a0, a2);
+                    e4m3_to_f16(*reinterpret_cast<const uint32_t*>(at + 256), a1, a3);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma(o[nt][i], a0, a1, a2, a3, p[nt][h][0], p[nt][h][1]);
+                }
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int left = last - (base + h * 16 + t * 4);  // of this lane's 4 tokens
+                const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    const uint8_t* at = vb + i * 512 + h * 128 + lane * 4;
+                    uint32_t a0, a1, a2, a3;
+                    e4m3_to_f16(*reinterpret_cast<const uint32_t*>(at) & keep, a0, a2);
+                    e4m3_to_f16(*reinterpret_cast<const uint32_t*>(at + 256) & keep, a1, a3);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma(o[nt][i], a0, a1, a2, a3, p[nt][h][0], p[nt][h][1]);
+                }
+            }
+        }
+        __syncwarp();
+        issue();
+
+        const bool ends = cur.g + 1 == cur.hi;
+        if (ends || u + 1 == u1) {
+            const int64_t held = u + 1 - u0;  // units since the warp's start
+            const bool whole = ends && held >= cur.hi - cur.lo;
+            const SeqView sv = load_seq(a.bt, cur.b, false);
+            const int rows = sv.n * a.group;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    float l = sum[nt][k];
+                    l += __shfl_xor_sync(~0u, l, 4);
+                    l += __shfl_xor_sync(~0u, l, 8);
+                    l += __shfl_xor_sync(~0u, l, 16);
+                    const int in_tile = nt * 8 + 2 * t + k, r = tile * kRows + in_tile;
+                    const float m = top[nt][k];
+                    if (whole) {
+                        if (r < rows) {
+                            const int64_t tok = lo_row + r / a.group;
+                            const int qh = head * a.group + r % a.group;
+                            T* dst = static_cast<T*>(a.out.data) + tok * a.out.token_stride + qh * a.out.head_stride;
+                            const float inv = l == 0.f ? 0.f : __fdiv_rn(1.f, l);
+#pragma unroll
+                            for (int i = 0; i < D / 16; ++i) {
+                                dst[i * 16 + g] = from_f32<T>(o[nt][i][k] * inv);
+                                dst[i * 16 + g + 8] = from_f32<T>(o[nt][i][2 + k] * inv);
+                            }
+                            if (a.lse != nullptr && g == 0)
+                                a.lse[tok * a.q.n_heads + qh] =
+                                    m == -INFINITY ? -INFINITY : (m - kLift + log2f(l)) * 0.6931471805599453f;
+                        }
+                    } else {
+                        // a warp leaves at most two parts: of what began before it or with it, and of
+                        // what it begins and does not end
+                        const bool first = held <= cur.g - cur.lo + 1;
+                        float* part = a.part + ((int64_t)2 * w + (first ? 0 : 1)) * (kRows * (D + 2));
+                        float* dst = part + in_tile * D;
+#pragma unroll
+                        for (int i = 0; i < D / 16; ++i) {
+                            dst[i * 16 + g] = o[nt][i][k];
+                            dst[i * 16 + g + 8] = o[nt][i][2 + k];
+                        }
+                        if (g == 0) {
+                            part[kRows * D + 2 * in_tile] = m;
+                            part[kRows * D + 2 * in_tile + 1] = l;
+                        }
+                    }
+                }
+            fresh = true;
+        }
+        next<kRows>(a, cur);
+    }
+    if (up) {
+        if (lane == 0) a.gave_up[w] = 1;
+        // leave no copy in flight behind
+        for (int64_t u = max(u0, issued - kFewStages); u < issued; ++u)
+            mbar_wait(&bar[(u - u0) % kFewStages], (uint32_t)((u - u0) / kFewStages & 1));
+    }
+}
+
+// One CTA a query row: adds the parts of rows that several warps had, writes rows that
+// see nothing, and the sequences' status.
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(kJoinThreads) k_kv_join(FewArgs a) {
+    constexpr int kRows = 8 * NT, kWarps = kJoinThreads / 32, kPer = D / 32;
+    __shared__ float acc[kWarps][D];
+    __shared__ float weight[kWarps][2];
+    const int lane = threadIdx.x % 32, wid = threadIdx.x / 32;
+    const int64_t per_warp = a.base[a.bt.n_seqs + 1];
+    const int64_t rows_max = (int64_t)a.bt.max_tokens * a.group;
+    const int64_t work = a.bt.n_seqs * max(rows_max, (int64_t)1) * a.c.n_heads;
+    for (int64_t u = blockIdx.x; u < work; u += gridDim.x) {
+        const int head = (int)(u % a.c.n_heads);
+        const int64_t r = u / a.c.n_heads % max(rows_max, (int64_t)1);
+        const int b = (int)(u / a.c.n_heads / max(rows_max, (int64_t)1));
+        const SeqView s = load_seq(a.bt, b, false);
+        int lo, hi;
+        seq_granules(a, s, lo, hi);
+        const int cnt = hi - lo, rows = s.n * a.group;
+        const int64_t from = a.base[b], past = a.base[b + 1];
+        if (head == 0 && r == 0) {
+            bool ok = s.st == MP_OK, late = false;
+            if (cnt > 0) {
+                const int per = a.c.block_tokens / kGranule;
+                for (int col = lo / per + threadIdx.x; col <= (hi - 1) / per; col += kJoinThreads) {
+                    const int p = __ldg(a.bt.table + (int64_t)b * a.bt.max_blocks + col);
+                    ok &= p >= 0 && p < a.c.n_blocks;
+                }
+            }
+            if (past > from)
+                for (int64_t w = from / per_warp + threadIdx.x; w <= (past - 1) / per_warp; w += kJoinThreads)
+                    late |= a.gave_up[w] != 0;
+            ok = !__syncthreads_or(!ok);
+            late = __syncthreads_or(late);
+            if (threadIdx.x == 0) a.status[b] = !ok ? MP_EINVAL : late ? MP_ETIMEOUT : MP_OK;
+        }
+        if (r >= rows || s.st != MP_OK || !seq_is_few(a, s)) continue;
+        const int64_t tok = s.lo + r / a.group;
+        const int qh = head * a.group + (int)(r % a.group);
+        T* dst = static_cast<T*>(a.out.data) + tok * a.out.token_stride + qh * a.out.head_stride;
+        if (cnt <= 0) {
+            for (int d = threadIdx.x; d < D; d += kJoinThreads) dst[d] = from_f32<T>(0.f);
+            if (a.lse != nullptr && threadIdx.x == 0) a.lse[tok * a.q.n_heads + qh] = -INFINITY;
+            continue;
+        }
+        const int tile = (int)(r / kRows), in_tile = (int)(r % kRows);
+        const int64_t us = from + ((int64_t)tile * a.c.n_heads + head) * cnt;
+        const int64_t w0 = us / per_warp, w1 = (us + cnt - 1) / per_warp;
+        if (w0 == w1) continue;  // one warp had it all
+        float top = -INFINITY, l = 0.f, o[kPer] = {};
+        for (int64_t w = w0 + wid; w <= w1; w += kWarps) {
+            const float* part = a.part + (2 * w + (w * per_warp >= us ? 0 : 1)) * (kRows * (D + 2));
+            const float m = part[kRows * D + 2 * in_tile], lw = part[kRows * D + 2 * in_tile + 1];
+            float x[kPer];
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) x[i] = part[in_tile * D + i * 32 + lane];
+            const float now = fmaxf(top, m), ref = now == -INFINITY ? 0.f : now;
+            const float f = exp2_approx(top - ref), fw = exp2_approx(m - ref);
+            l = l * f + lw * fw;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) o[i] = o[i] * f + x[i] * fw;
+            top = now;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) acc[wid][i * 32 + lane] = o[i];
+        if (lane == 0) weight[wid][0] = top, weight[wid][1] = l;
+        __syncthreads();
+        float all = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) all = fmaxf(all, weight[w][0]);
+        const float ref = all == -INFINITY ? 0.f : all;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) sum += weight[w][1] * exp2_approx(weight[w][0] - ref);
+        const float inv = sum == 0.f ? 0.f : __fdiv_rn(1.f, sum);
+        for (int d = threadIdx.x; d < D; d += kJoinThreads) {
+            float x = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) x += acc[w][d] * exp2_approx(weight[w][0] - ref);
+            dst[d] = from_f32<T>(x * inv);
+        }
+        if (a.lse != nullptr && threadIdx.x == 0)
+            a.lse[tok * a.q.n_heads + qh] = all == -INFINITY ? -INFINITY : (all - kLift + log2f(sum)) * 0.6931471805599453f;
+    }
+}
+
+constexpr int kFewCtas = 152;  // one an SM: its rings take most of the shared memory
+constexpr int kFewRows = 16;   // most rows a tile
+
+struct Layout {
+    size_t base, gave_up, part, bytes;
+};
+Layout layout(const mp_kv_cache& c, const mp_kv_batch& bt) {
+    Layout l;
+    const size_t warps = (size_t)kFewCtas * kFewWarps;
+    l.base = 0;
+    l.gave_up = align_up(sizeof(int64_t) * ((size_t)bt.n_seqs + 2));
+    l.part = l.gave_up + align_up(sizeof(int32_t) * warps);
+    l.bytes = l.part + align_up(sizeof(float) * 2 * warps * kFewRows * (size_t)(c.head_dim + 2));
+    return l;
+}
+
+template <typename T, int D, int NT>
+cudaError_t few_as(const FewArgs& a, cudaStream_t stream) {
+    constexpr size_t smem = (size_t)kFewWarps * kFewStages * 2 * kGranule * D;
+    cudaError_t e = set_smem_limit((const void*)k_kv_attend_few<T, D, NT>, smem);
+    if (e != cudaSuccess) return e;
+    k_kv_attend_few<T, D, NT><<<kFewCtas, kFewWarps * 32, smem, stream>>>(a);
+    e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    const int64_t rows = std::max<int64_t>(1, (int64_t)a.bt.max_tokens * a.group);
+    const int64_t work = a.bt.n_seqs * rows * a.c.n_heads;
+    k_kv_join<T, D, NT><<<(unsigned)std::min<int64_t>(work, 1 << 20), kJoinThreads, 0, stream>>>(a);
+    return cudaGetLastError();
+}
+template <typename T, int D>
+cudaError_t few_rows(const FewArgs& a, cudaStream_t stream) {
+    return (int64_t)a.bt.max_tokens * a.group <= 8 ? few_as<T, D, 1>(a, stream) : few_as<T, D, 2>(a, stream);
+}
+
+}  // namespace
+
+size_t kv_attend_workspace_bytes(const mp_kv_cache& c, const mp_kv_batch& bt, int32_t) {
+    return bt.n_seqs == 0 ? 0 : layout(c, bt).bytes;
+}
+
+cudaError_t launch_kv_attend(const mp_kv_cache& c, const mp_kv_batch& bt, const mp_tokens& q, float scale,
+                             int32_t causal, int32_t window, const mp_tokens& out, float* lse, int32_t* status,
+                             void* workspace, cudaStream_t stream) {
+    if (bt.n_seqs == 0) return cudaSuccess;
+    const Layout l = layout(c, bt);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    FewArgs a;
+    a.c = c, a.bt = bt, a.q = q, a.out = out, a.lse = lse, a.status = status;
+    a.scale = scale, a.causal = causal, a.window = window < bt.max_len ? window : 0;
+    a.group = q.n_heads / c.n_heads;
+    a.rows_skip = 0;
+    a.warps = kFewCtas * kFewWarps;
+    a.base = reinterpret_cast<int64_t*>(ws + l.base);
+    a.gave_up = reinterpret_cast<int32_t*>(ws + l.gave_up);
+    a.part = reinterpret_cast<float*>(ws + l.part);
+    if (q.dtype == MP_F16)
+        return c.head_dim == 64 ? few_rows<__half, 64>(a, stream) : few_rows<__half, 128>(a, stream);
+    return c.head_dim == 64 ? few_rows<__nv_bfloat16, 64>(a, stream) : few_rows<__nv_bfloat16, 128>(a, stream);
+}
+
+}  // namespace mp

@@ -1,0 +1,81 @@
+// kv_attend.cuh -- what the attention kernels over the 8-bit cache share: barriers
+// with bounded waits, bulk copies, and the scaling that both products use.
+#pragma once
+
+#include "kv.cuh"
+
+namespace mp {
+
+#ifdef MP_TEST_SPIN_CYCLES
+constexpr long long kKvSpinCycles = MP_TEST_SPIN_CYCLES;
+#else
+constexpr long long kKvSpinCycles = 1ll << 31;  // about a second; a longer wait is a fault
+#endif
+
+// Weights are kept as 2^kLift times their value under the running maximum, so that in
+// f16 those down to 2^-38 of it are not lost.
+constexpr float kLift = 14.f;
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void mbar_init(uint64_t* bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(bar)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void fence_mbar_init() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
+__device__ __forceinline__ void mbar_expect(uint64_t* bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_addr(bar)), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+// Waits for the phase of that parity to end; false if it has not after kKvSpinCycles.
+__device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity) {
+    if (mbar_try(bar, parity)) return true;
+    const long long t0 = clock64();
+    while (clock64() - t0 < kKvSpinCycles)
+        if (mbar_try(bar, parity)) return true;
+    return false;
+}
+// bytes (a multiple of 16, both addresses on 16-byte boundaries) into shared memory.
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                     smem_addr(dst)),
+                 "l"(src), "r"(bytes), "r"(smem_addr(bar))
+                 : "memory");
+}
+
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// lo in the low half
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// The power of two that brings a query row's largest magnitude to [2^14, 2^15), so
+// that every bf16 and f16 row is an f16 row without loss (elements below 2^-28 of the
+// largest aside).  1 for rows of zeros, infinities or NaN.
+__device__ __forceinline__ float row_factor(float most) {
+    const int e = (int)(__float_as_uint(most) >> 23);
+    if (most == 0.f || e >= 255) return 1.f;
+    return __uint_as_float((uint32_t)min(268 - e, 254) << 23);
+}
+
+// The scale of a block of values as the kernels use it: they divide by it and take
+// its logarithm.
+__device__ __forceinline__ float value_scale(float s) { return fmaxf(s, 0x1p-100f); }
+
+}  // namespace mp

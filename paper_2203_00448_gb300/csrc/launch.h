@@ -132,4 +132,13 @@ cudaError_t launch_plan_fused(const mp_batch& bt, int32_t policy, int64_t* profi
                               int64_t* offsets, int64_t* plan_peak, int32_t* verdict, int32_t* conflict,
                               int32_t* status, void* workspace, cudaStream_t stream);
 
+cudaError_t launch_kv_write(const mp_kv_cache& c, const mp_kv_batch& bt, const mp_tokens& k, const mp_tokens& v,
+                            int32_t* status, cudaStream_t stream);
+cudaError_t launch_kv_read(const mp_kv_cache& c, const mp_kv_batch& bt, const mp_tokens& k, const mp_tokens& v,
+                           int32_t* status, cudaStream_t stream);
+size_t kv_attend_workspace_bytes(const mp_kv_cache& c, const mp_kv_batch& bt, int32_t n_q_heads);
+cudaError_t launch_kv_attend(const mp_kv_cache& c, const mp_kv_batch& bt, const mp_tokens& q, float scale,
+                             int32_t causal, int32_t window, const mp_tokens& out, float* lse, int32_t* status,
+                             void* workspace, cudaStream_t stream);
+
 }  // namespace mp

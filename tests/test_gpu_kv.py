@@ -1,0 +1,411 @@
+"""The key/value cache operators against plain 64-bit implementations, at the sizes, masks and layouts where they can go
+wrong: lengths of 0 and 1, blocks that end inside a granule or tile, queries that see nothing, unused slots full of bytes
+that stand for no number, groups that are no power of two, strided and unaligned rows, scales far apart."""
+import numpy as np
+import pytest
+import torch
+
+from tests import kv_refs as R
+
+pytestmark = pytest.mark.gpu
+F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
+
+
+def batch_of(mp, table, lens, new, **kw):
+    ptr = np.concatenate([[0], np.cumsum(new)]).astype(np.int64)
+    dev = [torch.from_numpy(np.asarray(x, t)).cuda() for x, t in ((table, np.int32), (lens, np.int32), (ptr, np.int64))]
+    kw.setdefault("max_tokens", max([0] + list(new)))
+    return mp.KvBatch(*dev, n_tokens=int(ptr[-1]), **kw)
+
+
+def rows(rng, tokens, heads, d, dtype, how="plain", scale=1.0):
+    """A tensor [tokens, heads, d] of `dtype`, laid out as asked, and its values in float64."""
+    x = torch.from_numpy(rng.standard_normal((tokens, heads, d)) * scale).to(dtype).cuda()
+    if how == "packed":  # columns of a wider projection
+        wide = torch.zeros(tokens, (heads + 3) * d, dtype=dtype, device="cuda")
+        view = wide[:, 2 * d:(heads + 2) * d].view(tokens, heads, d)
+    elif how == "odd":  # rows that start off any 16-byte boundary
+        wide = torch.zeros(tokens * (heads * d + 3) + 5, dtype=dtype, device="cuda")
+        view = wide[1:1 + tokens * (heads * d + 3)].view(tokens, -1)[:, :heads * d].view(tokens, heads, d)
+    elif how == "heads":  # heads before tokens
+        view = torch.zeros(heads, tokens, d, dtype=dtype, device="cuda").transpose(0, 1)
+    else:
+        return x, x.double().cpu().numpy()
+    view.copy_(x)
+    return view, x.double().cpu().numpy()
+
+
+WRITES = [
+    # block, heads, d, dtype, rows' layout, (held, new) of each sequence
+    (32, 8, 128, BF16, "plain", [(1, 1), (33, 1), (64, 1), (500, 1)]),
+    (64, 2, 64, F16, "packed", [(1, 1), (65, 2), (70, 7), (0, 0), (128, 16)]),
+    (96, 3, 128, F32, "odd", [(5, 5), (97, 3), (96, 1)]),
+    (256, 1, 64, BF16, "heads", [(300, 10)]),
+    (32, 2, 128, F16, "plain", [(17, 17), (500, 100), (333, 333), (40, 0), (33, 32)]),
+    (64, 5, 64, BF16, "odd", [(129, 129), (64, 64), (63, 62)]),
+    (128, 1, 128, F32, "heads", [(1000, 999), (20, 18)]),
+    (256, 2, 64, F32, "packed", [(511, 300)]),
+]
+
+
+@pytest.mark.parametrize("block,heads,d,dtype,how,seqs", WRITES)
+def test_write_and_read(cuda_lib, block, heads, d, dtype, how, seqs):
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(11)
+    lens, new = [s[0] for s in seqs], [s[1] for s in seqs]
+    table, n = R.make_table(lens, block, rng)
+    pool = R.Pool(n, block, heads, d, rng)
+    # sizes a thousandfold apart, so that some blocks' scales grow and some do not
+    size = np.exp2(rng.integers(-8, 4, (sum(new), heads, 1)))
+    k, kx = rows(rng, sum(new), heads, d, dtype, how)
+    v, vx = rows(rng, sum(new), heads, d, dtype, how)
+    s = torch.from_numpy(size).cuda()
+    k.copy_(k.double() * s)
+    v.copy_(v.double() * s * 0.03)
+    kx, vx = k.double().cpu().numpy(), v.double().cpu().numpy()
+    cache = pool.cache()
+    batch = batch_of(mp, table, lens, new)
+    status = mp.kv_write(cache, batch, k, v)
+    assert np.array_equal(R.write(pool, table, lens, new, kx, vx), status.cpu().numpy())
+    got = pool.from_stored(cache.k.cpu().numpy(), cache.v.cpu().numpy())
+    assert np.array_equal(cache.k_scale.cpu().numpy(), pool.ks) and np.array_equal(cache.v_scale.cpu().numpy(), pool.vs)
+    # the sign of a zero is kept, so bytes are equal, not only values
+    assert np.array_equal(got[0], pool.k) and np.array_equal(got[1], pool.v)
+    # a second call with the same tokens changes nothing
+    mp.kv_write(cache, batch, k, v)
+    again = pool.from_stored(cache.k.cpu().numpy(), cache.v.cpu().numpy())
+    assert np.array_equal(again[0], pool.k) and np.array_equal(again[1], pool.v)
+
+    for out_dtype in (F16, BF16, F32):
+        ko, _ = rows(rng, sum(new), heads, d, out_dtype, how)
+        vo, _ = rows(rng, sum(new), heads, d, out_dtype, how)
+        _, _, st = mp.kv_read(cache, batch, out_dtype, k=ko, v=vo)
+        assert not st.any()
+        want = [np.concatenate(x) for x in zip(*(R.held(pool, table, b, lens[b] - new[b], lens[b]) for b in range(len(lens))))]
+        for x, y in ((ko, want[0]), (vo, want[1])):
+            assert torch.equal(x.cpu(), torch.from_numpy(y).to(out_dtype))
+
+
+def test_read_everything_and_random_bytes(cuda_lib):
+    """All finite bytes under scales that are no power of two, read whole and from the middle of a block."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(3)
+    lens = [700, 1, 0, 63]
+    table, n = R.make_table(lens, 64, rng)
+    pool = R.Pool(n, 64, 3, 64, rng)
+    for x in (pool.k, pool.v):
+        x[:] = rng.integers(0, 256, x.shape)
+        x[x & 127 == 127] = 0x7E
+    pool.ks[:], pool.vs[:] = (rng.uniform(1e-3, 10, pool.ks.shape) for _ in range(2))
+    cache = pool.cache()
+    for new in ([700, 1, 0, 63], [13, 0, 0, 31]):
+        k, v, st = mp.kv_read(cache, batch_of(mp, table, lens, new), F32)
+        want = [np.concatenate(x) for x in zip(*(R.held(pool, table, b, lens[b] - new[b], lens[b]) for b in range(4)))]
+        assert torch.equal(k.cpu(), torch.from_numpy(want[0]).float()) and not st.any()
+        assert torch.equal(v.cpu(), torch.from_numpy(want[1]).float())
+
+
+def test_write_non_finite_and_extreme_values(cuda_lib):
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(5)
+    lens, new = [40, 40, 3, 40, 35], [8, 40, 3, 40, 20]
+    for dtype in (BF16, F32):
+        table, n = R.make_table(lens, 32, rng)
+        pool = R.Pool(n, 32, 2, 64, rng)
+        k, _ = rows(rng, sum(new), 2, 64, dtype)
+        v, _ = rows(rng, sum(new), 2, 64, dtype)
+        k[3, 0, 5], k[4, 1, 6] = float("nan"), float("inf")
+        v[9, 1, 7] = float("-inf")
+        k[48:51] = 0  # nothing but zeros
+        v[51:91] *= 3e38 if dtype == F32 else 1e38  # the largest values there are
+        v[60, 0, 0] = torch.finfo(dtype).max
+        k[91:] *= 1e-30  # below the least scale
+        kx, vx = k.double().cpu().numpy(), v.double().cpu().numpy()
+        cache, batch = pool.cache(), batch_of(mp, table, lens, new)
+        status = mp.kv_write(cache, batch, k, v)
+        want = R.write(pool, table, lens, new, kx, vx)
+        assert want[0] == 1 and want[1] == 1
+        assert np.array_equal(want, status.cpu().numpy())
+        got = pool.from_stored(cache.k.cpu().numpy(), cache.v.cpu().numpy())
+        assert np.array_equal(cache.k_scale.cpu().numpy(), pool.ks) and np.array_equal(cache.v_scale.cpu().numpy(), pool.vs)
+        assert np.array_equal(got[0], pool.k) and np.array_equal(got[1], pool.v)
+
+
+def check_attend(mp, pool, table, lens, new, q, qx, scale, causal, window, **kw):
+    cache, batch = pool.cache(), batch_of(mp, table, lens, new, **kw)
+    out, lse, status = mp.kv_attend(cache, batch, q, scale=scale, causal=causal, window=window, want_lse=True)
+    want, want_lse, mag, size = R.attend(pool, table, lens, new, qx, scale, causal, window)
+    bound, lse_bound = R.attend_bounds(q.dtype, want, want_lse, mag, size)
+    assert not status.any()
+    out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    assert np.array_equal(np.isneginf(lse), np.isneginf(want_lse))
+    assert (out[np.isneginf(want_lse)] == 0).all()
+    assert (np.abs(out - want) <= bound).all(), np.max(np.abs(out - want) / bound)
+    fine = np.isfinite(want_lse)
+    assert (np.abs(lse[fine] - want_lse[fine]) <= lse_bound[fine]).all()
+    return out
+
+
+ATTENDS = [
+    # block, query heads, heads, d, dtype, layout, causal, window, (held, new) of each sequence
+    (32, 8, 8, 128, BF16, "plain", True, 0, [(1, 1)]),
+    (32, 8, 8, 128, BF16, "packed", True, 0, [(512, 1)]),
+    (64, 32, 8, 128, BF16, "plain", True, 0, [(0, 1), (1, 1), (31, 1), (32, 1), (33, 1), (700, 1), (5, 0)]),
+    (96, 6, 2, 64, F16, "odd", True, 0, [(97, 2), (5, 2), (1, 2), (64, 1), (300, 2)]),  # one query before the start
+    (32, 20, 4, 64, F16, "heads", True, 40, [(100, 3), (45, 3), (41, 3), (40, 1), (2, 2)]),
+    (128, 5, 1, 128, F16, "plain", True, 1, [(200, 3), (1, 1)]),
+    (64, 16, 2, 64, BF16, "plain", True, 0, [(50, 2), (1000, 1), (64, 2)]),  # groups of 8: two tiles of rows
+    (256, 12, 4, 64, BF16, "packed", True, 100, [(513, 5), (99, 4)]),
+    (64, 8, 2, 128, F16, "plain", False, 0, [(130, 4), (1, 3), (0, 2), (64, 4)]),
+    # many rows: prompts, pieces of them, pieces before the start, no causal order
+    (64, 8, 2, 128, BF16, "packed", True, 0, [(200, 200)]),
+    (32, 4, 4, 64, F16, "plain", True, 0, [(127, 127), (129, 129), (128, 128), (1, 1), (0, 0)]),
+    (96, 6, 2, 128, F16, "odd", True, 0, [(400, 70), (60, 64), (300, 1)]),
+    (64, 3, 1, 128, BF16, "heads", True, 0, [(385, 100), (500, 33)]),
+    (32, 10, 2, 64, BF16, "plain", True, 50, [(300, 120), (49, 40), (400, 2)]),
+    (64, 4, 2, 128, F16, "plain", True, 130, [(600, 260)]),
+    (64, 8, 8, 64, F16, "packed", False, 0, [(37, 100), (300, 129), (1, 64), (0, 20)]),
+    (128, 7, 1, 128, BF16, "plain", False, 0, [(257, 61)]),
+]
+
+
+@pytest.mark.parametrize("block,hq,heads,d,dtype,how,causal,window,seqs", ATTENDS)
+def test_attend(cuda_lib, block, hq, heads, d, dtype, how, causal, window, seqs):
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(7)
+    lens, new = [s[0] for s in seqs], [s[1] for s in seqs]
+    table, n = R.make_table(lens, block, rng)
+    pool = R.Pool(n, block, heads, d, rng)
+    for b, length in enumerate(lens):  # slots past the end hold bytes that stand for no number
+        if length % block:
+            page = table[b, length // block]
+            pool.k[page, :, length % block:] = 0x7F
+            pool.v[page, :, length % block:] = 0xFF
+    q, qx = rows(rng, sum(new), hq, d, dtype, how)
+    check_attend(mp, pool, table, lens, new, q, qx, d ** -0.5, causal, window)
+
+
+def test_attend_sharp_and_flat_rows(cuda_lib):
+    """Scores hundreds apart, one token that outweighs thousands, and queries of zeros (all weights equal)."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(9)
+    lens, new = [3000, 700], [1, 90]
+    table, n = R.make_table(lens, 64, rng)
+    pool = R.Pool(n, 64, 2, 128, rng)
+    q, _ = rows(rng, sum(new), 4, 128, F16)
+    q[0] *= 60
+    q[1:30] = 0
+    q[30:60, 1] *= 1e-6
+    q[60:, 2:] *= 100
+    pool.v[:, 1] = R.to_byte(np.abs(R.VALUES[pool.v[:, 1]]))  # values of one sign: lost weights would show
+    check_attend(mp, pool, table, lens, new, q, q.double().cpu().numpy(), 128 ** -0.5, True, 0)
+
+
+def test_attend_scales_far_apart(cuda_lib):
+    """Blocks whose scales differ by 2^40, scales that are no power of two, and scales of zero."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(13)
+    for seqs in ([(300, 1), (33, 2)], [(300, 80), (65, 64)]):
+        lens, new = [s[0] for s in seqs], [s[1] for s in seqs]
+        table, n = R.make_table(lens, 32, rng)
+        pool = R.Pool(n, 32, 2, 64, rng)
+        pool.vs[:] = rng.uniform(0.5, 1, pool.vs.shape) * np.exp2(rng.integers(-20, 21, pool.vs.shape))
+        pool.ks[:] = rng.uniform(0.2, 1, pool.ks.shape) * 2.0 ** -5
+        pool.vs[table[0, 1]] = 0
+        pool.ks[table[0, 2]] = 0
+        q, qx = rows(rng, sum(new), 4, 64, BF16)
+        check_attend(mp, pool, table, lens, new, q, qx, 0.2, True, 0)
+
+
+def test_attend_many_short_sequences(cuda_lib):
+    """More sequences than threads of a CTA, some empty: each warp's stretch covers several."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(17)
+    lens = [int(x) for x in rng.integers(0, 70, 700)]
+    new = [int(x) for x in rng.integers(0, 3, 700)]
+    table, n = R.make_table(lens, 32, rng)
+    pool = R.Pool(n, 32, 1, 64, rng)
+    q, qx = rows(rng, sum(new), 2, 64, BF16)
+    check_attend(mp, pool, table, lens, new, q, qx, 0.125, True, 0)
+
+
+def test_non_finite_queries_stay_in_their_rows(cuda_lib):
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(19)
+    for lens, new in (([100, 50], [1, 2]), ([300, 100], [100, 70])):
+        table, n = R.make_table(lens, 64, rng)
+        pool = R.Pool(n, 64, 2, 64, rng)
+        cache, batch = pool.cache(), batch_of(mp, table, lens, new)
+        q, _ = rows(rng, sum(new), 4, 64, F16)
+        clean, _, _ = mp.kv_attend(cache, batch, q)
+        q[1, 2, 3] = float("nan")
+        q[0, 1, 5] = float("inf")
+        out, _, status = mp.kv_attend(cache, batch, q)
+        assert torch.isnan(out[1, 2]).all() and torch.isnan(out[0, 1]).all() and not status.any()
+        clean[1, 2] = clean[0, 1] = out[1, 2] = out[0, 1] = 0
+        assert torch.equal(out, clean)
+
+
+def test_attend_same_result_every_time(cuda_lib):
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(23)
+    lens, new = [5000, 333, 64], [1, 40, 1]
+    table, n = R.make_table(lens, 64, rng)
+    pool = R.Pool(n, 64, 2, 128, rng)
+    cache, batch = pool.cache(), batch_of(mp, table, lens, new)
+    q, _ = rows(rng, sum(new), 8, 128, BF16)
+    first, first_lse, _ = mp.kv_attend(cache, batch, q, want_lse=True)
+    for _ in range(20):
+        out, lse, _ = mp.kv_attend(cache, batch, q, want_lse=True)
+        assert torch.equal(out, first) and torch.equal(lse, first_lse)
+
+
+def test_pools_past_32_bit_offsets(cuda_lib):
+    """Blocks whose bytes lie past 2^32 in the pool."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(29)
+    block, heads, d = 128, 8, 128
+    n = (1 << 32) // (block * heads * d) + 40
+    cache = mp.KvCache(n, block, heads, d)
+    lens, new = [200, 300], [200, 1]
+    ids = np.array([[n - 1, n - 3, -1], [n - 2, n - 7, n - 5]], np.int32)
+    small = R.Pool(8, block, heads, d, rng)
+    local = np.array([[7, 5, -1], [6, 1, 3]], np.int32)
+    for x, y in zip((cache.k, cache.v), small.stored()):
+        x[n - 8:] = torch.from_numpy(y).cuda()
+    cache.k_scale[n - 8:] = torch.from_numpy(small.ks).cuda()
+    cache.v_scale[n - 8:] = torch.from_numpy(small.vs).cuda()
+    batch = batch_of(mp, ids, lens, new)
+    k, kx = rows(rng, 201, heads, d, BF16)
+    v, vx = rows(rng, 201, heads, d, BF16)
+    assert not mp.kv_write(cache, batch, k, v).any()
+    R.write(small, local, lens, new, kx, vx)
+    got = small.from_stored(cache.k[n - 8:].cpu().numpy(), cache.v[n - 8:].cpu().numpy())
+    assert np.array_equal(got[0], small.k) and np.array_equal(got[1], small.v)
+    ko, vo, _ = mp.kv_read(cache, batch, F32)
+    want = R.held(small, local, 0, 0, 200)
+    assert torch.equal(ko[:200].cpu(), torch.from_numpy(want[0]).float())
+    assert torch.equal(vo[:200].cpu(), torch.from_numpy(want[1]).float())
+    q, qx = rows(rng, 201, heads, d, BF16)
+    out, lse, status = mp.kv_attend(cache, batch, q, want_lse=True)
+    want, want_lse, mag, size = R.attend(small, local, lens, new, qx, d ** -0.5)
+    bound, _ = R.attend_bounds(BF16, want, want_lse, mag, size)
+    assert not status.any() and (np.abs(out.double().cpu().numpy() - want) <= bound).all()
+
+
+def test_bad_sequences_are_reported_and_leave_others_alone(cuda_lib):
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(31)
+    lens, new = [100, 90, 80, 70, 64, 60], [3, 3, 3, 3, 3, 3]
+    table, n = R.make_table(lens, 32, rng)
+    pool = R.Pool(n, 32, 2, 64, rng)
+    for many in (False, True):
+        if many:
+            new = [40, 40, 40, 40, 40, 40]
+        cache = pool.cache()
+        good = batch_of(mp, table, lens, new, max_len=100)
+        q, _ = rows(rng, sum(new), 4, 64, F16)
+        k, _ = rows(rng, sum(new), 2, 64, F16)
+        clean, _, _ = mp.kv_attend(cache, good, q)
+        bad_lens, bad_table = list(lens), table.copy()
+        bad_lens[1] = 101  # past max_len
+        bad_lens[2] = -1
+        bad_table[3, 1] = n  # outside the pool
+        bad_table[4, 1] = -1
+        ptr = np.concatenate([[0], np.cumsum(new)])
+        bad = batch_of(mp, bad_table, bad_lens, new, max_len=100)
+        out, _, status = mp.kv_attend(cache, bad, q)
+        assert status.tolist() == [0, 1, 1, 1, 1, 0]
+        for b in (0, 5):
+            assert torch.equal(out[ptr[b]:ptr[b + 1]], clean[ptr[b]:ptr[b + 1]])
+        # 3 tokens of sequence 3 lie past the block that is outside the pool: nothing is read or written there
+        _, _, status = mp.kv_read(cache, bad, F16)
+        assert status.tolist() == [0, 1, 1, int(many), 1, 0]
+        other = pool.cache()
+        assert mp.kv_write(cache, bad, k, k).tolist() == [0, 1, 1, int(many), 1, 0]
+        assert not mp.kv_write(other, good, k, k).any()
+        for b in (0, 5):
+            for page in table[b][table[b] >= 0]:
+                assert torch.equal(cache.k[page], other.k[page]) and torch.equal(cache.v[page], other.v[page])
+        # token ranges that go back or past the end, and more tokens than the declared bound or than are held
+        twisted = batch_of(mp, table, lens, new, max_len=100)
+        twisted.token_ptr[2] = ptr[1] - 1
+        status = mp.kv_attend(cache, twisted, q)[2]
+        assert status[1] == 1 and status[0] == 0
+        twisted.token_ptr.copy_(torch.from_numpy(ptr))
+        twisted.token_ptr[6] = int(ptr[-1]) + 1
+        assert mp.kv_attend(cache, twisted, q)[2].tolist() == [0, 0, 0, 0, 0, 1]
+        assert mp.kv_write(cache, twisted, k, k).tolist() == [0, 0, 0, 0, 0, 1]
+        held = torch.tensor([2, 100, 100, 100, 100, 100], dtype=torch.int32)
+        short = batch_of(mp, table, held.numpy(), new, max_len=100)
+        assert mp.kv_read(cache, short, F16)[2][0] == 1
+        assert mp.kv_write(cache, short, k, k)[0] == 1
+
+
+def test_empty_calls(cuda_lib):
+    import paper_2203_00448_gb300 as mp
+
+    cache = mp.KvCache(0, 32, 2, 64)
+    none = batch_of(mp, np.zeros((0, 1)), [], [])
+    q = torch.zeros(0, 4, 64, dtype=F16, device="cuda")
+    assert mp.kv_attend(cache, none, q)[0].shape == (0, 4, 64)
+    assert mp.kv_write(cache, none, q[:, :2], q[:, :2]).shape == (0,)
+    assert mp.kv_read(cache, none)[0].shape == (0, 2, 64)
+    idle = batch_of(mp, np.full((2, 1), -1), [0, 0], [0, 0])  # sequences, but no tokens
+    assert mp.kv_attend(cache, idle, q)[2].tolist() == [0, 0]
+    assert mp.kv_write(cache, idle, q[:, :2], q[:, :2]).tolist() == [0, 0]
+    assert mp.kv_read(cache, idle)[2].tolist() == [0, 0]
+    first = batch_of(mp, np.full((1, 1), -1), [0], [3], max_tokens=3)  # queries over nothing, no block at all
+    out, lse, st = mp.kv_attend(cache, first, torch.ones(3, 4, 64, dtype=F16, device="cuda"), causal=False, want_lse=True)
+    assert not out.any() and torch.isneginf(lse).all() and st.tolist() == [0]
+
+
+def test_streams_and_graphs(cuda_lib):
+    """Calls on two streams at once, each with its own scratch, and a captured step that follows lens on the device."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(37)
+    lens, new = [2000, 900], [1, 1]
+    table, n = R.make_table([2100, 1000], 64, rng)
+    pool = R.Pool(n, 64, 2, 128, rng)
+    cache, batch = pool.cache(), batch_of(mp, table, lens, new)
+    q, _ = rows(rng, 2, 8, 128, BF16)
+    r, _ = rows(rng, 2, 8, 128, BF16)
+    want, want_r = mp.kv_attend(cache, batch, q)[0], mp.kv_attend(cache, batch, r)[0]
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = [(mp.kv_attend(cache, batch, q, stream=s1)[0], mp.kv_attend(cache, batch, r, stream=s2)[0]) for _ in range(10)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, want) and torch.equal(b, want_r) for a, b in got)
+
+    k, _ = rows(rng, 2, 2, 128, BF16)
+    out, status = torch.empty_like(q), torch.empty(2, dtype=torch.int32, device="cuda")
+    ws = mp.Workspace("cuda")
+    mp.kv_attend(cache, batch, q, out=out, status=status, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        batch.lens += 1
+        mp.kv_write(cache, batch, k, k, status=status)
+        mp.kv_attend(cache, batch, q, out=out, status=status, workspace=ws)
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert batch.lens.tolist() == [2003, 903]
+    twin = pool.cache()
+    for step in range(1, 4):
+        at = batch_of(mp, table, [2000 + step, 900 + step], new)
+        mp.kv_write(twin, at, k, k)
+    assert torch.equal(twin.k, cache.k) and torch.equal(twin.v_scale, cache.v_scale)
+    assert torch.equal(mp.kv_attend(twin, at, q)[0], out)

@@ -1,0 +1,133 @@
+"""The key/value cache operators' checks of arguments and the tests' own plain forms, without a GPU."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2203_00448_gb300 as mp
+from paper_2203_00448_gb300 import _lib, build
+from tests import kv_refs as R
+
+P = 0x10000
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build()
+    return _lib.load()
+
+
+def cache(**kw):
+    c = _lib.MpKvCache(10, 32, 2, 64, P, P, P, P)
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return ctypes.byref(c)
+
+
+def batch(**kw):
+    b = _lib.MpKvBatch(4, 3, 8, 96, 20, P, P, P)
+    for k, v in kw.items():
+        setattr(b, k, v)
+    return ctypes.byref(b)
+
+
+def tokens(heads=2, dtype=1, data=P):
+    return ctypes.byref(_lib.MpTokens(data, heads * 64, 64, heads, dtype))
+
+
+BAD_CACHES = [dict(n_blocks=-1), dict(block_tokens=0), dict(block_tokens=48), dict(block_tokens=288), dict(n_heads=0),
+              dict(head_dim=96), dict(head_dim=256), dict(k=None), dict(v=P + 8), dict(k_scale=None), dict(v_scale=P + 2)]
+BAD_BATCHES = [dict(n_seqs=-1), dict(max_blocks=-1), dict(max_tokens=-1), dict(max_len=97), dict(max_len=-1),
+               dict(n_tokens=-1), dict(table=None), dict(lens=P + 1), dict(token_ptr=P + 4), dict(token_ptr=None),
+               dict(max_tokens=(1 << 28) + 1), dict(max_blocks=1 << 24, max_len=(1 << 28) + 1)]
+BAD_TOKENS = [tokens(3), tokens(0), tokens(dtype=3), tokens(dtype=-1), tokens(data=None), tokens(data=P + 1), None]
+
+
+def test_host_argument_errors(lib):
+    """Fake device addresses: every call fails its checks before anything could be enqueued."""
+    E = _lib.EINVAL
+    for c, b in [(cache(**x), batch()) for x in BAD_CACHES] + [(cache(), batch(**x)) for x in BAD_BATCHES] + \
+            [(None, batch()), (cache(), None)]:
+        assert lib.mp_kv_write(c, b, tokens(), tokens(), P, None) == E
+        assert lib.mp_kv_read(c, b, tokens(), tokens(), P, None) == E
+        assert lib.mp_kv_attend(c, b, tokens(4), 0.1, 1, 0, tokens(4), None, P, P, 1 << 40, None) == E
+        assert lib.mp_kv_attend_workspace_bytes(c, b, 4) == 0
+    for t in BAD_TOKENS:
+        for f in (lib.mp_kv_write, lib.mp_kv_read):
+            assert f(cache(), batch(), t, tokens(), P, None) == E
+            assert f(cache(), batch(), tokens(), t, P, None) == E
+        assert lib.mp_kv_attend(cache(), batch(), t, 0.1, 1, 0, tokens(4), None, P, P, 1 << 40, None) == E
+        assert lib.mp_kv_attend(cache(), batch(), tokens(4), 0.1, 1, 0, t, None, P, P, 1 << 40, None) == E
+    for f in (lib.mp_kv_write, lib.mp_kv_read):
+        assert f(cache(), batch(), tokens(dtype=0), tokens(dtype=1), P, None) == E  # two types
+        assert f(cache(), batch(), tokens(), tokens(), None, None) == E
+        assert f(cache(), batch(), tokens(), tokens(), P + 2, None) == E
+
+
+def test_attend_argument_errors(lib):
+    E = _lib.EINVAL
+
+    def call(q=None, scale=0.1, causal=1, window=0, out=None, lse=None, status=P, ws=P, room=1 << 40):
+        return lib.mp_kv_attend(cache(), batch(), q or tokens(4), scale, causal, window, out or tokens(4), lse, status, ws,
+                                room, None)
+
+    assert call(q=tokens(4, dtype=2), out=tokens(4, dtype=2)) == E  # 32-bit queries
+    assert call(q=tokens(4, dtype=0)) == E  # another type than the output's
+    assert call(out=tokens(2)) == E
+    assert call(q=tokens(5), out=tokens(5)) == E  # no whole groups
+    for scale in (0.0, -1.0, math.inf, math.nan):
+        assert call(scale=scale) == E
+    assert call(window=-1) == E and call(window=5, causal=0) == E
+    assert call(lse=P + 2) == E and call(status=None) == E
+    need = lib.mp_kv_attend_workspace_bytes(cache(), batch(), 4)
+    assert need > 0
+    assert call(room=need - 1) == _lib.ENOMEM
+    assert call(ws=None) == E and call(ws=P + 8) == E
+    assert lib.mp_kv_attend_workspace_bytes(cache(), batch(), 3) == 0
+    assert lib.mp_kv_attend_workspace_bytes(cache(), batch(n_seqs=0), 4) == 0
+
+
+def test_binding_refusals():
+    with pytest.raises(ValueError):
+        mp.KvCache(4, 48, 2, 64, "cpu")
+    with pytest.raises(ValueError):
+        mp.KvCache(4, 32, 2, 80, "cpu")
+    with pytest.raises(ValueError):
+        mp.KvCache(4, 32, 2, 64, k=torch.zeros(4, 2, 2047, dtype=torch.uint8))
+    with pytest.raises(ValueError):
+        mp.KvCache(4, 32, 2, 64, "cpu", k_scale=torch.zeros(4, 2, dtype=torch.float64))
+    c = mp.KvCache(4, 32, 2, 64, "cpu")
+    table, lens, ptr = torch.zeros(2, 2, dtype=torch.int32), torch.zeros(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int64)
+    for bad in ((table.long(), lens, ptr), (table[0], lens, ptr), (table, lens.long(), ptr), (table, lens, ptr.int()),
+                (table, lens, ptr[:2]), (table.t()[:, :1].expand(2, 2), lens, ptr)):
+        with pytest.raises(ValueError):
+            mp.KvBatch(*bad, n_tokens=2)
+    b = mp.KvBatch(table, lens, ptr, n_tokens=2)
+    x = torch.zeros(2, 2, 64)
+    for bad in (x[:1], x[0], x[..., :32], x.double(), torch.zeros(2, 3, 64), torch.zeros(2, 64, 2).transpose(1, 2)):
+        with pytest.raises(ValueError):
+            mp.kv_write(c, b, bad, x)
+        with pytest.raises(ValueError):
+            mp.kv_write(c, b, x, bad)
+    for bad in (x[:1], x[0], x[..., :32], x.double()):
+        with pytest.raises(ValueError):
+            mp.kv_attend(c, b, bad)
+
+
+def test_block_bytes():
+    c = mp.KvCache(3, 64, 5, 128, "cpu")
+    assert 3 * mp.KvCache.block_bytes(64, 5, 128) == sum(t.numel() * t.element_size() for t in (c.k, c.v, c.k_scale, c.v_scale))
+
+
+def test_plain_e4m3_rounding():
+    """The tests' own rounding against a brute-force search, and its ties."""
+    rng = np.random.default_rng(0)
+    grid = R.VALUES[np.isfinite(R.VALUES)]
+    x = np.concatenate([rng.standard_normal(2000) * np.exp2(rng.integers(-14, 9, 2000)), [0.0, 448.0, 500.0, -1e9, 2.0 ** -10]])
+    got = R.VALUES[R.to_byte(x)]
+    best = np.abs(np.minimum(np.abs(x), 448) * np.sign(x) - grid[:, None]).min(0)
+    assert np.array_equal(np.abs(np.clip(x, -448, 448) - got), best)
+    assert R.VALUES[R.to_byte(np.array([17.0, 19.0, 2.0 ** -10, 3 * 2.0 ** -10]))].tolist() == [16.0, 20.0, 0.0, 2.0 ** -8]
+    assert R.scale_of(448.0) == 1 and R.scale_of(448.1) == 2 and R.scale_of(224.0) == 0.5 and R.scale_of(0.0) == 2.0 ** -60
