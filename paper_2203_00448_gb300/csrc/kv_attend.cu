@@ -441,6 +441,12 @@ __global__ void __launch_bounds__(kFewWarps * 32, 1) k_kv_attend_few(FewArgs a) 
     }
 }
 
+// Most rows of a sequence that the kernel for few rows has.
+__host__ __device__ __forceinline__ int64_t join_rows(const FewArgs& a) {
+    const int64_t rows = (int64_t)a.bt.max_tokens * a.group;
+    return rows < 1 ? 1 : a.rows_skip > 0 && rows > a.rows_skip ? a.rows_skip : rows;
+}
+
 // One CTA a query row: adds the parts of rows that several warps had, writes rows that
 // see nothing, and the sequences' status.
 template <typename T, int D, int NT>
@@ -450,13 +456,13 @@ __global__ void __launch_bounds__(kJoinThreads) k_kv_join(FewArgs a) {
     __shared__ float weight[kWarps][2];
     const int lane = threadIdx.x % 32, wid = threadIdx.x / 32;
     const int64_t per_warp = a.base[a.bt.n_seqs + 1];
-    const int64_t rows_max = (int64_t)a.bt.max_tokens * a.group;
-    const int64_t work = a.bt.n_seqs * max(rows_max, (int64_t)1) * a.c.n_heads;
+    const int64_t rows_max = join_rows(a), work = a.bt.n_seqs * rows_max * a.c.n_heads;
     for (int64_t u = blockIdx.x; u < work; u += gridDim.x) {
         const int head = (int)(u % a.c.n_heads);
-        const int64_t r = u / a.c.n_heads % max(rows_max, (int64_t)1);
-        const int b = (int)(u / a.c.n_heads / max(rows_max, (int64_t)1));
+        const int64_t r = u / a.c.n_heads % rows_max;
+        const int b = (int)(u / a.c.n_heads / rows_max);
         const SeqView s = load_seq(a.bt, b, false);
+        if (!seq_is_few(a, s)) continue;
         int lo, hi;
         seq_granules(a, s, lo, hi);
         const int cnt = hi - lo, rows = s.n * a.group;
@@ -477,7 +483,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_kv_join(FewArgs a) {
             late = __syncthreads_or(late);
             if (threadIdx.x == 0) a.status[b] = !ok ? MP_EINVAL : late ? MP_ETIMEOUT : MP_OK;
         }
-        if (r >= rows || s.st != MP_OK || !seq_is_few(a, s)) continue;
+        if (r >= rows || s.st != MP_OK) continue;
         const int64_t tok = s.lo + r / a.group;
         const int qh = head * a.group + (int)(r % a.group);
         T* dst = static_cast<T*>(a.out.data) + tok * a.out.token_stride + qh * a.out.head_stride;
@@ -528,18 +534,41 @@ __global__ void __launch_bounds__(kJoinThreads) k_kv_join(FewArgs a) {
 }
 
 constexpr int kFewCtas = 152;  // one an SM: its rings take most of the shared memory
-constexpr int kFewRows = 16;   // most rows a tile
+constexpr int kFewRows = 16;   // most rows of a sequence and head
+
+// Which kernels a batch needs, by its host scalars: sequences of at most kFewRows rows are
+// bound by the cache's bytes, which k_kv_attend_few streams; above it the products count.
+// A batch whose sequences all have max_tokens has no sequence for the first.
+struct Route {
+    bool few, many;
+};
+Route route(const mp_kv_batch& bt, int32_t group) {
+    if ((int64_t)bt.max_tokens * group <= kFewRows) return {true, false};
+    return {bt.n_tokens != (int64_t)bt.n_seqs * bt.max_tokens, true};
+}
 
 struct Layout {
-    size_t base, gave_up, part, bytes;
+    size_t base, gave_up, part, starts, many_gave_up, many_part, bytes;
 };
-Layout layout(const mp_kv_cache& c, const mp_kv_batch& bt) {
-    Layout l;
+Layout layout(const mp_kv_cache& c, const mp_kv_batch& bt, int32_t group) {
+    Layout l = {};
+    const Route r = route(bt, group);
     const size_t warps = (size_t)kFewCtas * kFewWarps;
-    l.base = 0;
-    l.gave_up = align_up(sizeof(int64_t) * ((size_t)bt.n_seqs + 2));
-    l.part = l.gave_up + align_up(sizeof(int32_t) * warps);
-    l.bytes = l.part + align_up(sizeof(float) * 2 * warps * kFewRows * (size_t)(c.head_dim + 2));
+    auto take = [&](size_t bytes) {
+        const size_t at = l.bytes;
+        l.bytes += align_up(bytes);
+        return at;
+    };
+    if (r.few) {
+        l.base = take(sizeof(int64_t) * ((size_t)bt.n_seqs + 2));
+        l.gave_up = take(sizeof(int32_t) * warps);
+        l.part = take(sizeof(float) * 2 * warps * kFewRows * (size_t)(c.head_dim + 2));
+    }
+    if (r.many) {
+        l.starts = take(sizeof(ManyStart) * kManyCtas);
+        l.many_gave_up = take(sizeof(int32_t) * kManyCtas);
+        l.many_part = take(kv_many_part_bytes(c));
+    }
     return l;
 }
 
@@ -551,40 +580,57 @@ cudaError_t few_as(const FewArgs& a, cudaStream_t stream) {
     k_kv_attend_few<T, D, NT><<<kFewCtas, kFewWarps * 32, smem, stream>>>(a);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
-    const int64_t rows = std::max<int64_t>(1, (int64_t)a.bt.max_tokens * a.group);
-    const int64_t work = a.bt.n_seqs * rows * a.c.n_heads;
+    const int64_t work = a.bt.n_seqs * join_rows(a) * a.c.n_heads;
     k_kv_join<T, D, NT><<<(unsigned)std::min<int64_t>(work, 1 << 20), kJoinThreads, 0, stream>>>(a);
     return cudaGetLastError();
 }
 template <typename T, int D>
 cudaError_t few_rows(const FewArgs& a, cudaStream_t stream) {
-    return (int64_t)a.bt.max_tokens * a.group <= 8 ? few_as<T, D, 1>(a, stream) : few_as<T, D, 2>(a, stream);
+    return join_rows(a) <= 8 ? few_as<T, D, 1>(a, stream) : few_as<T, D, 2>(a, stream);
 }
 
 }  // namespace
 
-size_t kv_attend_workspace_bytes(const mp_kv_cache& c, const mp_kv_batch& bt, int32_t) {
-    return bt.n_seqs == 0 ? 0 : layout(c, bt).bytes;
+size_t kv_attend_workspace_bytes(const mp_kv_cache& c, const mp_kv_batch& bt, int32_t n_q_heads) {
+    return bt.n_seqs == 0 ? 0 : layout(c, bt, n_q_heads / c.n_heads).bytes;
 }
 
 cudaError_t launch_kv_attend(const mp_kv_cache& c, const mp_kv_batch& bt, const mp_tokens& q, float scale,
                              int32_t causal, int32_t window, const mp_tokens& out, float* lse, int32_t* status,
                              void* workspace, cudaStream_t stream) {
     if (bt.n_seqs == 0) return cudaSuccess;
-    const Layout l = layout(c, bt);
+    const int32_t group = q.n_heads / c.n_heads;
+    const Layout l = layout(c, bt, group);
+    const Route r = route(bt, group);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    FewArgs a;
+    if (window >= bt.max_len) window = 0;  // reaches back to every start
+    if (r.few) {
+        FewArgs a;
+        a.c = c, a.bt = bt, a.q = q, a.out = out, a.lse = lse, a.status = status;
+        a.scale = scale, a.causal = causal, a.window = window, a.group = group;
+        a.rows_skip = r.many ? kFewRows : 0;
+        a.warps = kFewCtas * kFewWarps;
+        a.base = reinterpret_cast<int64_t*>(ws + l.base);
+        a.gave_up = reinterpret_cast<int32_t*>(ws + l.gave_up);
+        a.part = reinterpret_cast<float*>(ws + l.part);
+        cudaError_t e;
+        if (q.dtype == MP_F16)
+            e = c.head_dim == 64 ? few_rows<__half, 64>(a, stream) : few_rows<__half, 128>(a, stream);
+        else
+            e = c.head_dim == 64 ? few_rows<__nv_bfloat16, 64>(a, stream) : few_rows<__nv_bfloat16, 128>(a, stream);
+        if (e != cudaSuccess) return e;
+    }
+    if (!r.many) return cudaSuccess;
+    ManyArgs a;
     a.c = c, a.bt = bt, a.q = q, a.out = out, a.lse = lse, a.status = status;
-    a.scale = scale, a.causal = causal, a.window = window < bt.max_len ? window : 0;
-    a.group = q.n_heads / c.n_heads;
-    a.rows_skip = 0;
-    a.warps = kFewCtas * kFewWarps;
-    a.base = reinterpret_cast<int64_t*>(ws + l.base);
-    a.gave_up = reinterpret_cast<int32_t*>(ws + l.gave_up);
-    a.part = reinterpret_cast<float*>(ws + l.part);
-    if (q.dtype == MP_F16)
-        return c.head_dim == 64 ? few_rows<__half, 64>(a, stream) : few_rows<__half, 128>(a, stream);
-    return c.head_dim == 64 ? few_rows<__nv_bfloat16, 64>(a, stream) : few_rows<__nv_bfloat16, 128>(a, stream);
+    a.scale = scale, a.causal = causal, a.window = window, a.group = group;
+    a.few_rows = r.few ? kFewRows : 0;
+    a.ctas = kManyCtas;
+    a.wide_q = rows_aligned(q), a.wide_out = rows_aligned(out);
+    a.part = reinterpret_cast<float*>(ws + l.many_part);
+    a.starts = reinterpret_cast<ManyStart*>(ws + l.starts);
+    a.gave_up = reinterpret_cast<int32_t*>(ws + l.many_gave_up);
+    return launch_kv_many(a, stream);
 }
 
 }  // namespace mp

@@ -78,4 +78,30 @@ __device__ __forceinline__ float row_factor(float most) {
 // its logarithm.
 __device__ __forceinline__ float value_scale(float s) { return fmaxf(s, 0x1p-100f); }
 
+// kv_attend_many.cu: where on the line of units a CTA began.
+struct ManyStart {
+    int32_t b, tile, head, cnt, k;  // cnt: units of that (sequence, pair of tiles, head); k: the first of this CTA
+    int32_t there;
+    int64_t per;  // units a CTA
+};
+constexpr int kManyCtas = 152;  // one an SM
+struct ManyArgs {
+    mp_kv_cache c;
+    mp_kv_batch bt;
+    mp_tokens q, out;
+    float* lse;
+    int32_t* status;
+    float scale;
+    int32_t causal, window;
+    int32_t group;
+    int32_t few_rows;  // sequences of at most this many rows are k_kv_attend_few's (0: none)
+    int32_t ctas;
+    bool wide_q, wide_out;
+    float* part;  // [2 * ctas][(D + 2) * 256]
+    ManyStart* starts;
+    int32_t* gave_up;
+};
+size_t kv_many_part_bytes(const mp_kv_cache& c);
+cudaError_t launch_kv_many(const ManyArgs& a, cudaStream_t stream);
+
 }  // namespace mp
