@@ -31,7 +31,12 @@ constexpr int kTokens = 128;    // of a unit
 constexpr int kGrans = kTokens / kGranule;
 constexpr int kStages = 2;      // of keys and of values
 constexpr int kScaleRing = 4;
-constexpr int kThreads = 13 * 32;
+constexpr int kLineRing = 4;
+constexpr int kSoftmaxWarps = 16;
+constexpr int kLineReaders = kSoftmaxWarps + 4 + 2;  // warps that read a stretch
+constexpr int kThreads = 24 * 32;
+// Registers a thread after the roles part: 512 x 80 + 128 x 112 + 128 x 48 = 768 x 80, the launch's.
+constexpr int kSoftmaxRegs = 80, kConvertRegs = 112, kProductRegs = 48;
 constexpr int kStrips = 1024;
 constexpr float kManyLift = 7.f;  // weights are at most 2^(8 + 7)
 constexpr float kGrow = 8.f;
@@ -55,6 +60,12 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
         "r"(a), "l"(b), "r"(what), "r"((uint32_t)add)
         : "memory");
 }
+// True in one lane of a whole warp, always the same one.
+__device__ __forceinline__ bool elected() {
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one != 0;
+}
 __device__ __forceinline__ void commit(uint64_t* bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar))
                  : "memory");
@@ -65,38 +76,48 @@ __device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-__device__ __forceinline__ void ld32(uint32_t addr, float* x) {
-    uint32_t* r = reinterpret_cast<uint32_t*>(x);
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
-        "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(addr));
-}
-__device__ __forceinline__ void st32(uint32_t addr, const float* x) {
-    const uint32_t* r = reinterpret_cast<const uint32_t*>(x);
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
-        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::"r"(r[0]),
-        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
-        "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
-        "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr));
+// n columns of this warp's 32 lanes of tensor memory, from and to registers.
+__device__ __forceinline__ void ld32(uint32_t addr, uint32_t* r) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(addr));
 }
 __device__ __forceinline__ void st16(uint32_t addr, const uint32_t* r) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"r"(r[0]),
-        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr));
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr));
+}
+__device__ __forceinline__ void ld16(uint32_t addr, uint32_t* r) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(addr));
+}
+__device__ __forceinline__ void fma2(float& x, float& y, float m, float o) {  // x, y = x m + o, y m + o
+    asm("{\n\t.reg .b64 v, w, z;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 w, {%2, %2};\n\tmov.b64 z, {%3, %3};\n\t"
+        "fma.rn.f32x2 v, v, w, z;\n\tmov.b64 {%0, %1}, v;\n\t}"
+        : "+f"(x), "+f"(y)
+        : "f"(m), "f"(o));
+}
+__device__ __forceinline__ void add2(float& x, float& y, float u, float v) {  // x, y = x + u, y + v
+    asm("{\n\t.reg .b64 p, q;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %3};\n\tadd.rn.f32x2 p, p, q;\n\t"
+        "mov.b64 {%0, %1}, p;\n\t}"
+        : "+f"(x), "+f"(y)
+        : "f"(u), "f"(v));
+}
+template <int kRegs>
+__device__ __forceinline__ void more_regs() {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs));
+}
+template <int kRegs>
+__device__ __forceinline__ void fewer_regs() {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs));
 }
 
 // A stretch of the line inside one (sequence, pair of row tiles, head).
 struct Stretch {
     int b, tile, head;
     int cnt, k;              // units of the whole, the first of this stretch
+    int units;               // of this stretch
+    int tiles;               // 1 or 2 of the pair have rows
+    int first;               // of its CTA
     int first_gran, grans;   // granules that the pair's rows see
     int rows;                // of the sequence and head
     int len, start;          // tokens held; position of the call's first
@@ -133,6 +154,7 @@ __device__ __forceinline__ void fill(const ManyArgs& a, const SeqView& s, Stretc
     pair_grans(a, s, x.tile, x.first_gran, x.grans);
     x.cnt = (x.grans + kGrans - 1) / kGrans;
     x.rows = s.n * a.group;
+    x.tiles = x.rows - x.tile * kPair > kRows ? 2 : 1;
     x.len = s.len, x.start = s.len - s.n, x.row = s.lo;
 }
 // The stretch that follows on the line (there is one: the caller has units left).
@@ -141,8 +163,9 @@ __device__ __forceinline__ void advance(const ManyArgs& a, Stretch& x) {
     if (++x.head < a.c.n_heads) return;
     x.head = 0;
     ++x.tile;
+    SeqView s;
+    s.lo = x.row, s.len = x.len, s.n = x.len - x.start, s.st = MP_OK;
     for (;;) {
-        const SeqView s = load_seq(a.bt, x.b, false);
         const int pairs = pairs_of(a, s);
         for (; x.tile < pairs; ++x.tile)
             if (pair_units(a, s, x.tile) > 0) {
@@ -151,13 +174,9 @@ __device__ __forceinline__ void advance(const ManyArgs& a, Stretch& x) {
             }
         ++x.b, x.tile = 0;
         if (x.b >= a.bt.n_seqs) return;
+        s = load_seq(a.bt, x.b, false);
     }
 }
-__device__ __forceinline__ int granule_page(const ManyArgs& a, int b, int gran) {
-    const int p = __ldg(a.bt.table + (int64_t)b * a.bt.max_blocks + gran / (a.c.block_tokens / kGranule));
-    return p >= 0 && p < a.c.n_blocks ? p : 0;  // k_kv_join_many reports it
-}
-
 template <int D>
 struct Smem {
     uint8_t q[2][kRows * D * 2];
@@ -166,7 +185,12 @@ struct Smem {
     int64_t strip[kStrips];
     float scales[kScaleRing][3][kGrans];  // key scale, log2 of the value scale, 1 / value scale
     uint64_t q_full[2], s_full[2], p_full[2], o_done[2], k_full[kStages], k_empty[kStages], v_full[kStages],
-        v_empty[kStages], drained;
+        v_empty[kStages], drained, line_full[kLineRing], line_empty[kLineRing],
+        scales_full[kScaleRing];
+    uint64_t traded[2];
+    float trade[2][2][2][kRows];  // [tile][exchange][half]: between the two threads of a row
+    float unit[2][2][kRows];      // [tile][stretch]: what a row's scores are to be multiplied by
+    Stretch line[kLineRing];  // the CTA's stretches as line_role lays them out
     Stretch first;
     int64_t total;
     uint32_t tmem;
@@ -194,27 +218,66 @@ __device__ __forceinline__ bool await_warp(uint64_t* bar, uint32_t parity, volat
 
 constexpr uint32_t kScoreCol = 0, kSumCol = 256;  // of tile 0; tile 1 has + 128 and + D
 
+// One thread walks the CTA's part of the line ahead of the roles.
+template <int D>
+__device__ void line_role(const ManyArgs& a, Smem<D>& m, int64_t left) {
+    Stretch x = m.first;
+    x.first = 1;
+    for (int seg = 0; left > 0; ++seg) {
+        x.units = (int)min((int64_t)(x.cnt - x.k), left);
+        if (!await(&m.line_empty[seg % kLineRing], (seg / kLineRing & 1) ^ 1, &m.gave_up)) return;
+        m.line[seg % kLineRing] = x;
+        mbar_arrive(&m.line_full[seg % kLineRing]);
+        left -= x.units;
+        x.first = 0;
+        if (left > 0) advance(a, x);
+    }
+}
+template <int D>
+__device__ __forceinline__ void release(Smem<D>& m, int seg) {
+    __syncwarp();
+    if (threadIdx.x % 32 == 0) mbar_arrive(&m.line_empty[seg % kLineRing]);
+}
+
 template <typename T, int D>
-__device__ void convert_role(const ManyArgs& a, Smem<D>& m, Stretch x, int64_t left) {
-    constexpr int kLoads = kTokens * D / 16 / 128;       // 16-byte loads a thread, of either array
-    constexpr int kPerGran = kGranule * D / 16 / 128;    // ... of which a granule is this many, 1 or 2
-    const int tid = threadIdx.x - 256;
+__device__ void convert_role(const ManyArgs& a, Smem<D>& m, int64_t left) {
+    constexpr int kLoads = kTokens * D / 16 / 128;     // 16-byte loads a thread, of either array
+    constexpr int kPerGran = kGranule * D / 16 / 128;  // ... of which a granule is this many, 1 or 2
+    const int tid = threadIdx.x - kSoftmaxWarps * 32;
     uint4 kr[kLoads], vr[kLoads];
-    int64_t at[kGrans];
-    int it = 0, tail = 0;
-    // the granules of the unit at hand: where they are, -1 past the last
-    auto locate = [&]() {
-#pragma unroll
-        for (int i = 0; i < kGrans; ++i) {
-            const int g = x.k * kGrans + i;
-            at[i] = -1;
-            if (g < x.grans) {
-                const int gran = x.first_gran + g, page = granule_page(a, x.b, gran);
-                at[i] = block_byte(a.c, page, x.head) +
-                        (int64_t)(gran % (a.c.block_tokens / kGranule)) * (kGranule * D);
-            }
+    const int lane = tid % 32, mine = lane % kGrans, per = a.c.block_tokens / kGranule;
+    int64_t at[kGrans];  // the granules of the unit at hand: where they are, -1 past the last
+    int seg = 0, u = 0, had = 0;
+    float ks = 0.f, vs = 1.f;
+    // a unit's table entries are read a unit ahead, a granule a lane
+    int page = -1, in_page = 0, head = 0, next_had = 0;
+    auto look_up = [&]() {
+        if (u == 0 && !await_warp(&m.line_full[seg % kLineRing], seg / kLineRing & 1, &m.gave_up)) return false;
+        const Stretch& x = m.line[seg % kLineRing];
+        const int g = (x.k + u) * kGrans + mine, gran = x.first_gran + g, col = gran / per;
+        page = -1, in_page = gran - col * per, head = x.head;
+        if (g < x.grans) {
+            page = __ldg(a.bt.table + (int64_t)x.b * a.bt.max_blocks + col);
+            if (page < 0 || page >= a.c.n_blocks) page = 0;  // k_kv_join_many reports it
         }
-        tail = x.len - (x.first_gran + x.k * kGrans) * kGranule;  // tokens of the unit that are held
+        next_had = x.len - (gran - mine) * kGranule;  // tokens of the unit that are held
+        if (++u == x.units) {
+            release(m, seg);
+            ++seg, u = 0;
+        }
+        return true;
+    };
+    auto locate = [&]() {
+        int64_t here = -1;
+        ks = 0.f, vs = 1.f;
+        if (page >= 0) {
+            here = block_byte(a.c, page, head) + in_page * (kGranule * D);
+            const int64_t sc = (int64_t)page * a.c.n_heads + head;
+            ks = __ldg(a.c.k_scale + sc), vs = __ldg(a.c.v_scale + sc);
+        }
+#pragma unroll
+        for (int i = 0; i < kGrans; ++i) at[i] = __shfl_sync(~0u, here, i);
+        had = next_had;
     };
     auto load = [&](const uint8_t* pool, uint4* r) {
 #pragma unroll
@@ -223,317 +286,359 @@ __device__ void convert_role(const ManyArgs& a, Smem<D>& m, Stretch x, int64_t l
                                         : __ldg(reinterpret_cast<const uint4*>(pool + at[i / kPerGran]) +
                                                 (i % kPerGran) * 128 + tid);
     };
-    auto widen = [](const uint4& w, uint4& lo, uint4& hi) {
+    auto widen = [](const uint4& w, uint4* dst) {
+        uint4 lo, hi;
         e4m3_to_f16(w.x, lo.x, lo.y), e4m3_to_f16(w.y, lo.z, lo.w);
         e4m3_to_f16(w.z, hi.x, hi.y), e4m3_to_f16(w.w, hi.z, hi.w);
+        dst[0] = lo, dst[8] = hi;
     };
-    if (left > 0) {
-        locate();
-        load(a.c.k, kr);
-    }
-    while (left > 0) {
-        const int st = it % kStages;
+    if (!look_up()) return;
+    locate();
+    load(a.c.k, kr);
+    if (left > 1 && !look_up()) return;
+#pragma unroll 1
+    for (int it = 0; left > 0; ++it, --left) {
+        const int st = it % kStages, held = had;
         const uint32_t empty = (it / kStages & 1) ^ 1;
         load(a.c.v, vr);
-        float ks = 0.f, vs = 1.f;
-        if (tid < kGrans && x.k * kGrans + tid < x.grans) {
-            const int64_t sc =
-                (int64_t)granule_page(a, x.b, x.first_gran + x.k * kGrans + tid) * a.c.n_heads + x.head;
-            ks = __ldg(a.c.k_scale + sc), vs = value_scale(__ldg(a.c.v_scale + sc));
-        }
         if (!await_warp(&m.k_empty[st], empty, &m.gave_up)) return;
         if (tid < kGrans) {
             // the slot's last readers are done: this stage's last scores were issued after sums that had
             // waited for the weights of the unit that had the slot
             float(*sc)[kGrans] = m.scales[it % kScaleRing];
-            sc[0][tid] = ks, sc[1][tid] = log2f(vs), sc[2][tid] = __fdiv_rn(1.f, vs);
+            const float s = value_scale(vs);
+            sc[0][tid] = ks, sc[1][tid] = log2f(s), sc[2][tid] = __fdiv_rn(1.f, s);
         }
+        __syncwarp();
+        if (tid == 0) mbar_arrive(&m.scales_full[it % kScaleRing]);
+        // stored tiles [token / 8][D / 16][8][16] become f16 tiles [token / 8][D / 8][8][8]
+        uint4* to = reinterpret_cast<uint4*>(m.k[st]) + (tid / 8) * 16 + tid % 8;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            // stored tiles [token / 8][D / 16][8][16] become f16 tiles [token / 8][D / 8][8][8]
-            const int q = i * 128 + tid;
-            uint4 lo, hi;
-            widen(kr[i], lo, hi);
-            uint4* dst = reinterpret_cast<uint4*>(m.k[st]) + (q / 8) * 16 + q % 8;
-            dst[0] = lo, dst[8] = hi;
-        }
+        for (int i = 0; i < kLoads; ++i) widen(kr[i], to + i * 256);
         fence_smem();
         mbar_arrive(&m.k_full[st]);
-        const int had = tail;
-        const bool more = left > 1;
-        if (more) {
-            if (++x.k == x.cnt) advance(a, x);
+        if (left > 1) {
             locate();
             load(a.c.k, kr);
+            if (left > 2 && !look_up()) return;
         }
         if (!await_warp(&m.v_empty[st], empty, &m.gave_up)) return;
+        // stored tiles [granule][D / 8][2][8][16] become [granule][D / 8][4][8][8]
+        to = reinterpret_cast<uint4*>(m.v[st]) + (tid / 8) * 16 + tid % 8;
+        if (held < kTokens) {  // bytes behind the last token mean nothing, NaN among them
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            // stored tiles [granule][D / 8][2][8][16] become [granule][D / 8][4][8][8]
-            const int q = i * 128 + tid;
-            uint4 w = vr[i], lo, hi;
-            const int t0 = i / kPerGran * kGranule + (q / 8 % 2) * 16;
-            if (had < t0 + 16) {  // bytes behind the last token mean nothing, NaN among them
-                uint32_t* p = reinterpret_cast<uint32_t*>(&w);
+            for (int i = 0; i < kLoads; ++i) {
+                const int left_here = held - (i / kPerGran * kGranule + (tid / 8 % 2) * 16);
+                uint32_t* p = reinterpret_cast<uint32_t*>(&vr[i]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const int n = had - t0 - 4 * j;
+                    const int n = left_here - 4 * j;
                     p[j] &= n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1;
                 }
             }
-            widen(w, lo, hi);
-            uint4* dst = reinterpret_cast<uint4*>(m.v[st]) + (q / 8) * 16 + q % 8;
-            dst[0] = lo, dst[8] = hi;
         }
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) widen(vr[i], to + i * 256);
         fence_smem();
         mbar_arrive(&m.v_full[st]);
-        ++it, --left;
     }
 }
 
+// One warp a tile, a lane of which issues: sums of a unit as its weights come, then the
+// next unit's scores over them.
 template <int D>
-__device__ void product_role(const ManyArgs& a, Smem<D>& m, Stretch x, int64_t left) {
+__device__ void product_role(const ManyArgs& a, Smem<D>& m, int64_t left, int tile) {
     constexpr uint32_t kScores = product_of(kRows, kTokens), kSums = product_of(kRows, D);
-    const uint32_t tm = m.tmem;
-    int it = 0, n[2] = {0, 0}, seg[2] = {0, 0};  // units, units of either tile, stretches of either tile
-    auto scores = [&](int i, int st) {
-        const uint32_t q = smem_addr(m.q[i]), k = smem_addr(m.k[st]);
+    constexpr uint32_t kStep = kTokens * D * 2 >> 4;  // between stages and between tiles, in descriptors
+    const uint32_t sc = __shfl_sync(~0u, m.tmem, 0) + kScoreCol + tile * 128;
+    const uint32_t su = __shfl_sync(~0u, m.tmem, 0) + kSumCol + tile * D;
+    const uint64_t q = operand(smem_addr(m.q[tile]), 128, D * 16);
+    const uint64_t k0 = operand(smem_addr(m.k[0]), 128, D * 16), v0 = operand(smem_addr(m.v[0]), 128, 512);
+    uint32_t it = 0, mine = 0, asked = 0;  // units of the CTA; units and stretches of this tile
+    int seg = 0;
+    // scores of unit it, which this tile has
+    auto scores = [&]() {
+        const uint64_t k = k0 + (it & 1) * kStep;
+        fence_after();
+        if (elected()) {
 #pragma unroll
-        for (int s = 0; s < D / 16; ++s)
-            mma_ss(tm + kScoreCol + i * 128, operand(q + s * 256, 128, D * 16), operand(k + s * 256, 128, D * 16), kScores,
-                   s > 0);
-        commit(&m.s_full[i]);
-    };
-    auto sums = [&](int i, int st, bool add) {
-        const uint32_t v = smem_addr(m.v[st]);
-#pragma unroll
-        for (int s = 0; s < kTokens / 16; ++s)
-            mma_ts(tm + kSumCol + i * D, tm + kScoreCol + i * 128 + s * 8,
-                   operand(v + (s / 2) * (kGranule * D * 2) + (s % 2) * 256, 128, 512), kSums, add || s > 0);
-        commit(&m.o_done[i]);
-    };
-    // the first unit's scores
-    {
-        const int tiles = x.rows - x.tile * kPair > kRows ? 2 : 1;
-        if (!await(&m.k_full[0], 0, &m.gave_up)) return;
-        for (int i = 0; i < tiles; ++i) {
-            if (!await(&m.q_full[i], seg[i]++ & 1, &m.gave_up)) return;
-            fence_after();
-            scores(i, 0);
+            for (int s = 0; s < D / 16; ++s) mma_ss(sc, q + s * 16, k + s * 16, kScores, s > 0);
+            commit(&m.s_full[tile]);
+            commit(&m.k_empty[it & 1]);
         }
-        commit(&m.k_empty[0]);
-    }
+        __syncwarp();
+    };
+#pragma unroll 1
     while (left > 0) {
-        const int tiles = x.rows - x.tile * kPair > kRows ? 2 : 1;
-        const bool add = n[0] > 0 && x.k > 0 && it > 0;
-        Stretch y = x;
-        bool fresh = false;
-        if (left > 1 && ++y.k == y.cnt) {
-            advance(a, y);
-            fresh = true;
-        }
-        const int next_tiles = left > 1 ? (y.rows - y.tile * kPair > kRows ? 2 : 1) : 0;
-        const int st = it % kStages, nst = (it + 1) % kStages;
-        if (!await(&m.v_full[st], it / kStages & 1, &m.gave_up)) return;
-        for (int i = 0; i < 2; ++i) {
-            if (i < tiles) {
-                if (!await(&m.p_full[i], n[i] & 1, &m.gave_up)) return;
-                fence_after();
-                sums(i, st, add);
-                if (i == tiles - 1) commit(&m.v_empty[st]);
-                ++n[i];
-            }
-            if (i < next_tiles) {
-                if (i == 0 && !await(&m.k_full[nst], (it + 1) / kStages & 1, &m.gave_up)) return;
-                if (fresh && !await(&m.q_full[i], seg[i]++ & 1, &m.gave_up)) return;
-                // its scores overwrite the weights that the product before reads: products of different
-                // sums are not ordered among themselves
-                if (n[i] > 0 && !await(&m.o_done[i], (n[i] - 1) & 1, &m.gave_up)) return;
-                fence_after();
-                scores(i, nst);
-                if (i == next_tiles - 1) commit(&m.k_empty[nst]);
-            }
-        }
-        x = y;
-        ++it, --left;
-    }
-}
-
-template <typename T, int D>
-__device__ void softmax_role(const ManyArgs& a, Smem<D>& m, Stretch x, int64_t left, int w) {
-    const int tile = threadIdx.x / 128, tid = threadIdx.x % 128, warp = tid / 32;
-    const uint32_t lanes = (uint32_t)(warp * 32) << 16;
-    const uint32_t sc = m.tmem + lanes + kScoreCol + tile * 128, su = m.tmem + lanes + kSumCol + tile * D;
-    int it = 0, n = 0;  // units of the CTA, of this tile
-    float unit = 0.f, next_unit = 0.f;
-    // a row of the tile into shared memory as f16, scaled; returns what scores are to be multiplied by
-    auto load_q = [&](const Stretch& y) {
-        const int r = y.tile * kPair + tile * kRows + tid;
-        const bool there = r < y.rows;
-        const T* p = static_cast<const T*>(a.q.data) + (y.row + r / a.group) * a.q.token_stride +
-                     (y.head * a.group + r % a.group) * a.q.head_stride;
-        float most = 0.f;
-#pragma unroll 4
-        for (int i = 0; i < D / 8; ++i) {
-            float v[8];
-            if (there) {
-                load_values<T, 8>(p + i * 8, a.wide_q, v);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(v[j]));
-            }
-        }
-        const float f = row_factor(most);
-#pragma unroll 4
-        for (int i = 0; i < D / 8; ++i) {
-            float v[8] = {};
-            if (there) load_values<T, 8>(p + i * 8, a.wide_q, v);
-            uint4 o;
-            o.x = pack_f16(v[0] * f, v[1] * f), o.y = pack_f16(v[2] * f, v[3] * f);
-            o.z = pack_f16(v[4] * f, v[5] * f), o.w = pack_f16(v[6] * f, v[7] * f);
-            reinterpret_cast<uint4*>(m.q[tile])[((tid / 8) * (D / 8) + i) * 8 + tid % 8] = o;
-        }
-        fence_smem();
-        mbar_arrive(&m.q_full[tile]);
-        return __fdiv_rn(a.scale * 1.4426950408889634f, f);
-    };
-    auto active = [&](const Stretch& y) { return tile == 0 || y.rows - y.tile * kPair > kRows; };
-
-    if (active(x)) next_unit = load_q(x);
-    const int64_t whole_line = left;
-    while (left > 0) {
-        const int units = (int)min((int64_t)(x.cnt - x.k), left);  // of this stretch
-        const bool mine = active(x);
-        if (!mine) {
-            it += units, left -= units;
-            if (left > 0) {
-                advance(a, x);
-                if (active(x)) next_unit = load_q(x);
+        if (!await_warp(&m.line_full[seg % kLineRing], seg / kLineRing & 1, &m.gave_up)) return;
+        const int units = m.line[seg % kLineRing].units;
+        const bool has = tile < m.line[seg % kLineRing].tiles;
+        release(m, seg++);
+        left -= units;
+        if (!has) {
+#pragma unroll 1
+            for (int u = 0; u < units; ++u, ++it) {
+                // this tile has nothing to do with the stages: it gives its part of them back as they fill
+                if (!await_warp(&m.k_full[it & 1], it >> 1 & 1, &m.gave_up)) return;
+                if (elected()) mbar_arrive(&m.k_empty[it & 1]);
+                if (!await_warp(&m.v_full[it & 1], it >> 1 & 1, &m.gave_up)) return;
+                if (elected()) mbar_arrive(&m.v_empty[it & 1]);
             }
             continue;
         }
-        unit = next_unit;
-        const int r = x.tile * kPair + tile * kRows + tid;
-        const int pos = x.start + r / a.group;
-        const int see_hi = r >= x.rows ? 0 : a.causal ? min(x.len, max(pos + 1, 0)) : x.len;
-        const int see_lo = a.window > 0 ? pos - a.window + 1 : 0;
-        float top = -INFINITY, sum = 0.f;
-        for (int u = 0; u < units; ++u, ++it, ++n) {
-            const int base = (x.first_gran + (x.k + u) * kGrans) * kGranule;
-            if (!await_warp(&m.s_full[tile], n & 1, &m.gave_up)) return;
+        if (!await_warp(&m.q_full[tile], asked++ & 1, &m.gave_up)) return;
+        if (!await_warp(&m.k_full[it & 1], it >> 1 & 1, &m.gave_up)) return;
+        if (mine > 0 && !await_warp(&m.o_done[tile], (mine - 1) & 1, &m.gave_up)) return;
+        scores();
+#pragma unroll 1
+        for (int u = 0; u < units; ++u) {
+            const uint64_t v = v0 + (it & 1) * kStep;
+            if (!await_warp(&m.v_full[it & 1], it >> 1 & 1, &m.gave_up)) return;
+            if (!await_warp(&m.p_full[tile], mine & 1, &m.gave_up)) return;
             fence_after();
-            const float(*scale)[kGrans] = m.scales[it % kScaleRing];
-            const bool edge = __any_sync(~0u, base + kTokens > see_hi || base < see_lo);
-            float most = -INFINITY;
-            float s[32];
+            if (elected()) {
 #pragma unroll
-            for (int c = 0; c < kGrans; ++c) {
-                ld32(sc + c * 32, s);
-                wait_ld();
-                float big = -INFINITY;
-                if (edge) {
+                for (int s = 0; s < kTokens / 16; ++s)
+                    mma_ts(su, sc + s / 4 * 64 + s % 4 * 8, v + (s / 2) * (kGranule * D * 2 >> 4) + (s % 2) * 16, kSums,
+                           u > 0 || s > 0);
+                commit(&m.o_done[tile]);
+                commit(&m.v_empty[it & 1]);
+            }
+            __syncwarp();
+            ++it;
+            if (u + 1 < units) {
+                if (!await_warp(&m.k_full[it & 1], it >> 1 & 1, &m.gave_up)) return;
+                // its scores overwrite the weights that the product before reads: products of different
+                // sums are not ordered among themselves
+                if (!await_warp(&m.o_done[tile], mine & 1, &m.gave_up)) return;
+                scores();
+            }
+            ++mine;
+        }
+    }
+}
+
+// 8 warps a tile: two threads a row, 64 of a unit's scores and half of the sums' columns each.
+template <typename T, int D>
+__device__ void softmax_role(const ManyArgs& a, Smem<D>& m, int64_t left, int w) {
+    const int tile = threadIdx.x / 256, half = threadIdx.x / 128 % 2, warp = threadIdx.x / 32 % 4, lane = threadIdx.x % 32;
+    const int in_tile = warp * 32 + lane;  // the row
+    const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+    const uint32_t sc = m.tmem + lanes + kScoreCol + tile * 128, su = m.tmem + lanes + kSumCol + tile * D + half * (D / 2);
+    uint32_t it = 0, n = 0, asked = 0, met = 0;  // units of the CTA; units, stretches and exchanges of this tile
+    float top = -INFINITY, sum = 0.f;
+    bool pending = false;
+    // x of the row's other thread; false if a wait gave up
+    auto exchange = [&](float& x) {
+        float* at = m.trade[tile][met & 1][half] + in_tile;
+        *at = x;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&m.traded[tile]);
+        const bool ok = await_warp(&m.traded[tile], met & 1, &m.gave_up);
+        x = m.trade[tile][met & 1][half ^ 1][in_tile];
+        ++met;
+        return ok;
+    };
+#pragma unroll 1
+    for (int seg = 0;; ++seg) {
+        // a stretch's queries go in before the sums of the one before it come out
+        if (left > 0 && !await_warp(&m.line_full[seg % kLineRing], seg / kLineRing & 1, &m.gave_up)) return;
+        const Stretch& x = m.line[seg % kLineRing];
+        const Stretch& done = m.line[(seg + kLineRing - 1) % kLineRing];
+        const bool mine = left > 0 && tile < x.tiles;
+        if (mine) {
+            // a warp has 16 rows, 8 rows x 4 chunks of 16 bytes a load
+            uint4 raw[2][D / 32];
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        const int t = base + c * 32 + j;
-                        if (t < see_hi && t >= see_lo) big = fmaxf(big, s[j]);
+            for (int g = 0; g < 2; ++g) {
+                const int row = x.tile * kPair + tile * kRows + warp * 32 + half * 16 + g * 8 + lane / 4;
+                const bool there = row < x.rows;
+                const T* p = static_cast<const T*>(a.q.data) + (x.row + row / a.group) * a.q.token_stride +
+                             (x.head * a.group + row % a.group) * a.q.head_stride + lane % 4 * 8;
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) {
+                    raw[g][i] = make_uint4(0, 0, 0, 0);
+                    if (there) {
+                        if (a.wide_q) {
+                            raw[g][i] = __ldg(reinterpret_cast<const uint4*>(p) + i * 4);
+                        } else {
+                            T* e = reinterpret_cast<T*>(&raw[g][i]);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) e[j] = p[i * 32 + j];
+                        }
                     }
-                    if (big > -INFINITY) most = fmaxf(most, fmaf(big, unit * scale[0][c], scale[1][c]));
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) big = fmaxf(big, s[j]);
-                    most = fmaxf(most, fmaf(big, unit * scale[0][c], scale[1][c]));
                 }
             }
-            const bool grows = most > top + kGrow || (top == -INFINITY && most > -INFINITY);
-            if (__any_sync(~0u, grows)) {
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                const int at = warp * 32 + half * 16 + g * 8 + lane / 4;
+                float most = 0.f;
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) {
+                    const T* e = reinterpret_cast<const T*>(&raw[g][i]);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(to_f32(e[j])));
+                }
+                most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
+                most = fmaxf(most, __shfl_xor_sync(~0u, most, 2));
+                const float f = row_factor(most);
+                if (lane % 4 == 0) m.unit[tile][seg & 1][at] = __fdiv_rn(a.scale * 1.4426950408889634f, f);
+                uint4* to = reinterpret_cast<uint4*>(m.q[tile]) + (at / 8 * (D / 8) + lane % 4) * 8 + at % 8;
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) {
+                    const T* e = reinterpret_cast<const T*>(&raw[g][i]);
+                    uint4 o;
+                    o.x = pack_f16(to_f32(e[0]) * f, to_f32(e[1]) * f), o.y = pack_f16(to_f32(e[2]) * f, to_f32(e[3]) * f);
+                    o.z = pack_f16(to_f32(e[4]) * f, to_f32(e[5]) * f), o.w = pack_f16(to_f32(e[6]) * f, to_f32(e[7]) * f);
+                    to[i * 32] = o;
+                }
+            }
+            fence_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&m.q_full[tile]);
+        }
+        if (pending) {
+            float both = sum;
+            if (!exchange(both)) return;
+            both += sum;
+            if (!await_warp(&m.o_done[tile], (n - 1) & 1, &m.gave_up)) return;
+            fence_after();
+            const bool whole = done.units == done.cnt;
+            const int dr = done.tile * kPair + tile * kRows + in_tile;
+            const int64_t tok = done.row + dr / a.group;
+            const int qh = done.head * a.group + dr % a.group;
+            const float inv = both == 0.f ? 0.f : __fdiv_rn(1.f, both);
+            // stretches that are not whole: at most the CTA's first and its last
+            float* part = a.part + ((int64_t)2 * w + (done.first ? 0 : 1)) * (kPair * (D + 2)) + tile * kRows + in_tile;
+            T* dst = static_cast<T*>(a.out.data) + tok * a.out.token_stride + qh * a.out.head_stride + half * (D / 2);
+#pragma unroll 1
+            for (int c = 0; c < D / 64; ++c) {
+                uint32_t o[32];
+                ld32(su + c * 32, o);
+                wait_ld();
+                if (whole) {
+                    if (dr < done.rows) {
+                        float v[32];
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(o[j]) * inv;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) store_values<T, 8>(dst + c * 32 + j * 8, a.wide_out, v + j * 8);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) part[(half * (D / 2) + c * 32 + j) * kPair] = __uint_as_float(o[j]);
+                }
+            }
+            if (half == 0) {
+                if (!whole) {
+                    part[D * kPair] = top;
+                    part[(D + 1) * kPair] = both;
+                } else if (dr < done.rows && a.lse != nullptr) {
+                    a.lse[tok * a.q.n_heads + qh] =
+                        top == -INFINITY ? -INFINITY : (top - kManyLift + log2f(both)) * 0.6931471805599453f;
+                }
+            }
+            pending = false;
+        }
+        if (seg > 0) release(m, seg - 1);
+        if (left <= 0) return;
+        const int units = x.units;
+        left -= units;
+        if (mine) {
+            const int r = x.tile * kPair + tile * kRows + in_tile;
+            const int pos = x.start + r / a.group;
+            const int first_token = (x.first_gran + x.k * kGrans) * kGranule + half * 64;
+            // seen: [lo, hi) counted from this thread's first score
+            int hi = (r >= x.rows ? 0 : a.causal ? min(x.len, max(pos + 1, 0)) : x.len) - first_token;
+            int lo = (a.window > 0 ? pos - a.window + 1 : 0) - first_token;
+            if (!await_warp(&m.q_full[tile], asked++ & 1, &m.gave_up)) return;
+            const float unit = m.unit[tile][seg & 1][in_tile];
+            top = -INFINITY, sum = 0.f;
+#pragma unroll 1
+            for (int u = 0; u < units; ++u, ++n, hi -= kTokens, lo -= kTokens) {
+                const float(*scale)[kGrans] = m.scales[(it + u) % kScaleRing];
+                if (!await_warp(&m.scales_full[(it + u) % kScaleRing], (it + u) / kScaleRing & 1, &m.gave_up)) return;
+                if (!await_warp(&m.s_full[tile], n & 1, &m.gave_up)) return;
+                fence_after();
+                uint32_t raw[32];
+                float* s = reinterpret_cast<float*>(raw);
+                // 32 of the scores, -inf where the row does not see
+                auto chunk = [&](int c) {
+                    ld32(sc + half * 64 + c * 32, raw);
+                    const int h = hi - c * 32, l = lo - c * 32;
+                    const bool some = h < 32 || l > 0;
+                    wait_ld();
+                    if (__any_sync(~0u, some)) {
+                        const uint32_t seen = (h >= 32 ? ~0u : h <= 0 ? 0u : (1u << h) - 1) &
+                                              (l <= 0 ? ~0u : l >= 32 ? 0u : ~0u << l);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (!(seen >> j & 1)) s[j] = -INFINITY;
+                    }
+                };
+                float most = -INFINITY;
+#pragma unroll 1
+                for (int c = 0; c < 2; ++c) {
+                    chunk(c);
+                    float big[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) big[j] = fmaxf(s[j], s[4 + j]);
+#pragma unroll
+                    for (int j = 8; j < 32; j += 8)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) big[i] = fmaxf(big[i], fmaxf(s[j + i], s[j + 4 + i]));
+                    const float b = fmaxf(fmaxf(big[0], big[1]), fmaxf(big[2], big[3]));
+                    // a factor that is not 0: what is not seen stays -inf
+                    most = fmaxf(most, fmaf(b, fmaxf(unit * scale[0][half * 2 + c], 0x1p-126f), scale[1][half * 2 + c]));
+                }
+                float other = most;
+                if (!exchange(other)) return;  
+                most = fmaxf(most, other);
+                const bool grows = most > top + kGrow;
                 const float now = grows ? most : top;
                 const float fade = top == -INFINITY ? 0.f : exp2_approx(top - now);
-                top = now;
+                const float ref = now == -INFINITY ? 0.f : now - kManyLift;
                 sum *= fade;
-                if (u > 0) {
+                top = now;
+#pragma unroll 1
+                for (int c = 0; c < 2; ++c) {
+                    chunk(c);
+                    const float mul = fmaxf(unit * scale[0][half * 2 + c], 0x1p-126f), off = scale[1][half * 2 + c] - ref;
+                    float p0 = 0.f, p1 = 0.f;
+                    uint32_t p[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        float &e0 = s[2 * j], &e1 = s[2 * j + 1];
+                        fma2(e0, e1, mul, off);
+                        e0 = exp2_approx(e0), e1 = exp2_approx(e1);
+                        add2(p0, p1, e0, e1);
+                        p[j] = pack_f16(e0, e1);
+                    }
+                    sum = fmaf(p0 + p1, scale[2][half * 2 + c], sum);
+                    // over scores that this thread has read: the first 32 columns of its 64
+                    st16(sc + half * 64 + c * 16, p);
+                }
+                if (u > 0 && __any_sync(~0u, grows)) {
                     if (!await_warp(&m.o_done[tile], (n - 1) & 1, &m.gave_up)) return;
                     fence_after();
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < D / 32; ++c) {
-                        ld32(su + c * 32, s);
+                        uint32_t o[16];
+                        ld16(su + c * 16, o);
                         wait_ld();
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) s[j] *= fade;
-                        st32(su + c * 32, s);
+                        for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * fade);
+                        st16(su + c * 16, o);
                     }
                 }
+                wait_st();
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&m.p_full[tile]);
             }
-            const float ref = top == -INFINITY ? 0.f : top - kManyLift;
-#pragma unroll
-            for (int c = 0; c < kGrans; ++c) {
-                ld32(sc + c * 32, s);
-                wait_ld();
-                const float mul = unit * scale[0][c], off = scale[1][c] - ref;
-                float part = 0.f;
-                uint32_t p[16];
-                if (edge) {
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        const int t = base + c * 32 + j;
-                        s[j] = t < see_hi && t >= see_lo ? exp2_approx(fmaf(s[j], mul, off)) : 0.f;
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) s[j] = exp2_approx(fmaf(s[j], mul, off));
-                }
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    part += s[2 * j] + s[2 * j + 1];
-                    p[j] = pack_f16(s[2 * j], s[2 * j + 1]);
-                }
-                sum = fmaf(part, scale[2][c], sum);
-                st16(sc + c * 16, p);
-            }
-            wait_st();
-            fence_before();
-            mbar_arrive(&m.p_full[tile]);
+            pending = true;
         }
-        // the next stretch's queries go in before this one's sums come out
-        const Stretch done = x;
-        left -= units;
-        if (left > 0) {
-            advance(a, x);
-            if (active(x)) next_unit = load_q(x);
-        }
-        if (!await_warp(&m.o_done[tile], (n - 1) & 1, &m.gave_up)) return;
-        fence_after();
-        const bool whole = done.k == 0 && units == done.cnt;
-        const bool first = whole_line - left - units == 0;  // of the CTA's stretches
-        const int64_t tok = done.row + r / a.group;
-        const int qh = done.head * a.group + r % a.group;
-        T* dst = static_cast<T*>(a.out.data) + tok * a.out.token_stride + qh * a.out.head_stride;
-        const float inv = sum == 0.f ? 0.f : __fdiv_rn(1.f, sum);
-        // stretches that are not whole: at most the CTA's first and its last
-        float* part = a.part + ((int64_t)2 * w + (first ? 0 : 1)) * (kPair * (D + 2));
-        const int pr = tile * kRows + tid;
-#pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-            float o[32];
-            ld32(su + c * 32, o);
-            wait_ld();
-            if (whole) {
-                if (r < done.rows) {
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) o[j] *= inv;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) store_values<T, 8>(dst + c * 32 + j * 8, a.wide_out, o + j * 8);
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 32; ++j) part[(c * 32 + j) * kPair + pr] = o[j];
-            }
-        }
-        if (whole) {
-            if (r < done.rows && a.lse != nullptr)
-                a.lse[tok * a.q.n_heads + qh] = top == -INFINITY ? -INFINITY : (top - kManyLift + log2f(sum)) * 0.6931471805599453f;
-        } else {
-            part[D * kPair + pr] = top;
-            part[(D + 1) * kPair + pr] = sum;
-        }
+        it += units;
     }
 }
 
@@ -544,18 +649,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend_many(ManyArgs a) {
     const int tid = threadIdx.x, lane = tid % 32, wid = tid / 32;
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&m.q_full[i], kRows), mbar_init(&m.s_full[i], 1);
-            mbar_init(&m.p_full[i], kRows), mbar_init(&m.o_done[i], 1);
+            mbar_init(&m.q_full[i], kSoftmaxWarps / 2), mbar_init(&m.s_full[i], 1);
+            mbar_init(&m.p_full[i], kSoftmaxWarps / 2), mbar_init(&m.o_done[i], 1);
+            mbar_init(&m.traded[i], kSoftmaxWarps / 2);
         }
         for (int i = 0; i < kStages; ++i) {
-            mbar_init(&m.k_full[i], 128), mbar_init(&m.k_empty[i], 1);
-            mbar_init(&m.v_full[i], 128), mbar_init(&m.v_empty[i], 1);
+            mbar_init(&m.k_full[i], 128), mbar_init(&m.k_empty[i], 2);
+            mbar_init(&m.v_full[i], 128), mbar_init(&m.v_empty[i], 2);
         }
-        mbar_init(&m.drained, 1);
+        for (int i = 0; i < kScaleRing; ++i) mbar_init(&m.scales_full[i], 1);
+        for (int i = 0; i < kLineRing; ++i) mbar_init(&m.line_full[i], 1), mbar_init(&m.line_empty[i], kLineReaders);
+        mbar_init(&m.drained, 2);
         m.gave_up = 0;
         fence_mbar_init();
     }
-    if (wid == 12) {
+    if (wid == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&m.tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
@@ -624,19 +732,28 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend_many(ManyArgs a) {
     fence_after();
     const int64_t per = (m.total + gridDim.x - 1) / gridDim.x;
     const int64_t u0 = min(m.total, blockIdx.x * per), left = min(m.total, u0 + per) - u0;
-    if (left > 0) {
-        if (wid < 8) softmax_role<T, D>(a, m, m.first, left, blockIdx.x);
-        else if (wid < 12) convert_role<T, D>(a, m, m.first, left);
-        else if (lane == 0) {
-            product_role<D>(a, m, m.first, left);
-            commit(&m.drained);  // nothing may be in flight when tensor memory goes
+    if (wid < kSoftmaxWarps) {
+        if (left > 0) softmax_role<T, D>(a, m, left, blockIdx.x);
+    } else if (wid < kSoftmaxWarps + 4) {
+        more_regs<kConvertRegs>();
+        if (left > 0) convert_role<T, D>(a, m, left);
+    } else {
+        fewer_regs<kProductRegs>();
+        const int role = wid - kSoftmaxWarps - 4;
+        if (role < 2 && left > 0) {
+            product_role<D>(a, m, left, role);
+            __syncwarp();
+            if (elected()) commit(&m.drained);  // nothing may be in flight when tensor memory goes
+            __syncwarp();
             mbar_wait(&m.drained, 0);
+        } else if (role == 2 && lane == 0 && left > 0) {
+            line_role<D>(a, m, left);
         }
     }
     fence_before();
     __syncthreads();
     fence_after();
-    if (wid == 12) {
+    if (wid == 0) {
         __syncwarp();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(m.tmem));
     }
