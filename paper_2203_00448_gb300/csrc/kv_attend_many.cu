@@ -32,11 +32,11 @@ constexpr int kGrans = kTokens / kGranule;
 constexpr int kStages = 2;      // of keys and of values
 constexpr int kScaleRing = 4;
 constexpr int kLineRing = 4;
-constexpr int kSoftmaxWarps = 16;
+constexpr int kSoftmaxWarps = 8;
 constexpr int kLineReaders = kSoftmaxWarps + 4 + 2;  // warps that read a stretch
-constexpr int kThreads = 24 * 32;
-// Registers a thread after the roles part: 512 x 80 + 128 x 112 + 128 x 48 = 768 x 80, the launch's.
-constexpr int kSoftmaxRegs = 80, kConvertRegs = 112, kProductRegs = 48;
+constexpr int kThreads = 16 * 32;
+// Registers a thread after the roles part: 256 x 168 + 128 x 112 + 128 x 64 = 512 x 128, the launch's.
+constexpr int kSoftmaxRegs = 168, kConvertRegs = 112, kProductRegs = 64;
 constexpr int kStrips = 1024;
 constexpr float kManyLift = 7.f;  // weights are at most 2^(8 + 7)
 constexpr float kGrow = 8.f;
@@ -89,6 +89,11 @@ __device__ __forceinline__ void ld16(uint32_t addr, uint32_t* r) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                  : "r"(addr));
+}
+__device__ __forceinline__ float max3(float x, float y, float z) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+    return r;
 }
 __device__ __forceinline__ void fma2(float& x, float& y, float m, float o) {  // x, y = x m + o, y m + o
     asm("{\n\t.reg .b64 v, w, z;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 w, {%2, %2};\n\tmov.b64 z, {%3, %3};\n\t"
@@ -187,9 +192,6 @@ struct Smem {
     uint64_t q_full[2], s_full[2], p_full[2], o_done[2], k_full[kStages], k_empty[kStages], v_full[kStages],
         v_empty[kStages], drained, line_full[kLineRing], line_empty[kLineRing],
         scales_full[kScaleRing];
-    uint64_t traded[2];
-    float trade[2][2][2][kRows];  // [tile][exchange][half]: between the two threads of a row
-    float unit[2][2][kRows];      // [tile][stretch]: what a row's scores are to be multiplied by
     Stretch line[kLineRing];  // the CTA's stretches as line_role lays them out
     Stretch first;
     int64_t total;
@@ -399,7 +401,7 @@ __device__ void product_role(const ManyArgs& a, Smem<D>& m, int64_t left, int ti
             if (elected()) {
 #pragma unroll
                 for (int s = 0; s < kTokens / 16; ++s)
-                    mma_ts(su, sc + s / 4 * 64 + s % 4 * 8, v + (s / 2) * (kGranule * D * 2 >> 4) + (s % 2) * 16, kSums,
+                    mma_ts(su, sc + s * 8, v + (s / 2) * (kGranule * D * 2 >> 4) + (s % 2) * 16, kSums,
                            u > 0 || s > 0);
                 commit(&m.o_done[tile]);
                 commit(&m.v_empty[it & 1]);
@@ -418,27 +420,15 @@ __device__ void product_role(const ManyArgs& a, Smem<D>& m, int64_t left, int ti
     }
 }
 
-// 8 warps a tile: two threads a row, 64 of a unit's scores and half of the sums' columns each.
+// 4 warps a tile, a thread a row.
 template <typename T, int D>
 __device__ void softmax_role(const ManyArgs& a, Smem<D>& m, int64_t left, int w) {
-    const int tile = threadIdx.x / 256, half = threadIdx.x / 128 % 2, warp = threadIdx.x / 32 % 4, lane = threadIdx.x % 32;
-    const int in_tile = warp * 32 + lane;  // the row
+    const int tile = threadIdx.x / 128, in_tile = threadIdx.x % 128, warp = in_tile / 32, lane = threadIdx.x % 32;
     const uint32_t lanes = (uint32_t)(warp * 32) << 16;
-    const uint32_t sc = m.tmem + lanes + kScoreCol + tile * 128, su = m.tmem + lanes + kSumCol + tile * D + half * (D / 2);
-    uint32_t it = 0, n = 0, asked = 0, met = 0;  // units of the CTA; units, stretches and exchanges of this tile
+    const uint32_t sc = m.tmem + lanes + kScoreCol + tile * 128, su = m.tmem + lanes + kSumCol + tile * D;
+    uint32_t it = 0, n = 0;  // units of the CTA, of this tile
     float top = -INFINITY, sum = 0.f;
     bool pending = false;
-    // x of the row's other thread; false if a wait gave up
-    auto exchange = [&](float& x) {
-        float* at = m.trade[tile][met & 1][half] + in_tile;
-        *at = x;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&m.traded[tile]);
-        const bool ok = await_warp(&m.traded[tile], met & 1, &m.gave_up);
-        x = m.trade[tile][met & 1][half ^ 1][in_tile];
-        ++met;
-        return ok;
-    };
 #pragma unroll 1
     for (int seg = 0;; ++seg) {
         // a stretch's queries go in before the sums of the one before it come out
@@ -446,12 +436,13 @@ __device__ void softmax_role(const ManyArgs& a, Smem<D>& m, int64_t left, int w)
         const Stretch& x = m.line[seg % kLineRing];
         const Stretch& done = m.line[(seg + kLineRing - 1) % kLineRing];
         const bool mine = left > 0 && tile < x.tiles;
+        float unit = 0.f;  // what the row's scores are to be multiplied by
         if (mine) {
-            // a warp has 16 rows, 8 rows x 4 chunks of 16 bytes a load
-            uint4 raw[2][D / 32];
+            // 8 rows x 4 chunks of 16 bytes a load
+            uint4 raw[4][D / 32];
 #pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                const int row = x.tile * kPair + tile * kRows + warp * 32 + half * 16 + g * 8 + lane / 4;
+            for (int g = 0; g < 4; ++g) {
+                const int row = x.tile * kPair + tile * kRows + warp * 32 + g * 8 + lane / 4;
                 const bool there = row < x.rows;
                 const T* p = static_cast<const T*>(a.q.data) + (x.row + row / a.group) * a.q.token_stride +
                              (x.head * a.group + row % a.group) * a.q.head_stride + lane % 4 * 8;
@@ -470,8 +461,8 @@ __device__ void softmax_role(const ManyArgs& a, Smem<D>& m, int64_t left, int w)
                 }
             }
 #pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                const int at = warp * 32 + half * 16 + g * 8 + lane / 4;
+            for (int g = 0; g < 4; ++g) {
+                const int at = warp * 32 + g * 8 + lane / 4;
                 float most = 0.f;
 #pragma unroll
                 for (int i = 0; i < D / 32; ++i) {
@@ -482,7 +473,8 @@ __device__ void softmax_role(const ManyArgs& a, Smem<D>& m, int64_t left, int w)
                 most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
                 most = fmaxf(most, __shfl_xor_sync(~0u, most, 2));
                 const float f = row_factor(most);
-                if (lane % 4 == 0) m.unit[tile][seg & 1][at] = __fdiv_rn(a.scale * 1.4426950408889634f, f);
+                const float owner = __shfl_sync(~0u, f, lane % 8 * 4);
+                if (lane / 8 == g) unit = __fdiv_rn(a.scale * 1.4426950408889634f, owner);
                 uint4* to = reinterpret_cast<uint4*>(m.q[tile]) + (at / 8 * (D / 8) + lane % 4) * 8 + at % 8;
 #pragma unroll
                 for (int i = 0; i < D / 32; ++i) {
@@ -498,21 +490,18 @@ __device__ void softmax_role(const ManyArgs& a, Smem<D>& m, int64_t left, int w)
             if (lane == 0) mbar_arrive(&m.q_full[tile]);
         }
         if (pending) {
-            float both = sum;
-            if (!exchange(both)) return;
-            both += sum;
             if (!await_warp(&m.o_done[tile], (n - 1) & 1, &m.gave_up)) return;
             fence_after();
             const bool whole = done.units == done.cnt;
             const int dr = done.tile * kPair + tile * kRows + in_tile;
             const int64_t tok = done.row + dr / a.group;
             const int qh = done.head * a.group + dr % a.group;
-            const float inv = both == 0.f ? 0.f : __fdiv_rn(1.f, both);
+            const float inv = sum == 0.f ? 0.f : __fdiv_rn(1.f, sum);
             // stretches that are not whole: at most the CTA's first and its last
             float* part = a.part + ((int64_t)2 * w + (done.first ? 0 : 1)) * (kPair * (D + 2)) + tile * kRows + in_tile;
-            T* dst = static_cast<T*>(a.out.data) + tok * a.out.token_stride + qh * a.out.head_stride + half * (D / 2);
+            T* dst = static_cast<T*>(a.out.data) + tok * a.out.token_stride + qh * a.out.head_stride;
 #pragma unroll 1
-            for (int c = 0; c < D / 64; ++c) {
+            for (int c = 0; c < D / 32; ++c) {
                 uint32_t o[32];
                 ld32(su + c * 32, o);
                 wait_ld();
@@ -526,17 +515,15 @@ __device__ void softmax_role(const ManyArgs& a, Smem<D>& m, int64_t left, int w)
                     }
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) part[(half * (D / 2) + c * 32 + j) * kPair] = __uint_as_float(o[j]);
+                    for (int j = 0; j < 32; ++j) part[(c * 32 + j) * kPair] = __uint_as_float(o[j]);
                 }
             }
-            if (half == 0) {
-                if (!whole) {
-                    part[D * kPair] = top;
-                    part[(D + 1) * kPair] = both;
-                } else if (dr < done.rows && a.lse != nullptr) {
-                    a.lse[tok * a.q.n_heads + qh] =
-                        top == -INFINITY ? -INFINITY : (top - kManyLift + log2f(both)) * 0.6931471805599453f;
-                }
+            if (!whole) {
+                part[D * kPair] = top;
+                part[(D + 1) * kPair] = sum;
+            } else if (dr < done.rows && a.lse != nullptr) {
+                a.lse[tok * a.q.n_heads + qh] =
+                    top == -INFINITY ? -INFINITY : (top - kManyLift + log2f(sum)) * 0.6931471805599453f;
             }
             pending = false;
         }
@@ -547,82 +534,84 @@ __device__ void softmax_role(const ManyArgs& a, Smem<D>& m, int64_t left, int w)
         if (mine) {
             const int r = x.tile * kPair + tile * kRows + in_tile;
             const int pos = x.start + r / a.group;
-            const int first_token = (x.first_gran + x.k * kGrans) * kGranule + half * 64;
-            // seen: [lo, hi) counted from this thread's first score
+            const int first_token = (x.first_gran + x.k * kGrans) * kGranule;
+            // seen: [lo, hi) counted from the unit's first score
             int hi = (r >= x.rows ? 0 : a.causal ? min(x.len, max(pos + 1, 0)) : x.len) - first_token;
             int lo = (a.window > 0 ? pos - a.window + 1 : 0) - first_token;
-            if (!await_warp(&m.q_full[tile], asked++ & 1, &m.gave_up)) return;
-            const float unit = m.unit[tile][seg & 1][in_tile];
             top = -INFINITY, sum = 0.f;
 #pragma unroll 1
             for (int u = 0; u < units; ++u, ++n, hi -= kTokens, lo -= kTokens) {
                 const float(*scale)[kGrans] = m.scales[(it + u) % kScaleRing];
                 if (!await_warp(&m.scales_full[(it + u) % kScaleRing], (it + u) / kScaleRing & 1, &m.gave_up)) return;
+                const bool edge = __any_sync(~0u, hi < kTokens || lo > 0);
+                float mul[kGrans], add[kGrans];
+#pragma unroll
+                for (int c = 0; c < kGrans; ++c) {
+                    mul[c] = fmaxf(unit * scale[0][c], 0x1p-126f);  // not 0: what is not seen stays -inf
+                    add[c] = scale[1][c];
+                }
                 if (!await_warp(&m.s_full[tile], n & 1, &m.gave_up)) return;
                 fence_after();
-                uint32_t raw[32];
+                uint32_t raw[kTokens];
                 float* s = reinterpret_cast<float*>(raw);
-                // 32 of the scores, -inf where the row does not see
-                auto chunk = [&](int c) {
-                    ld32(sc + half * 64 + c * 32, raw);
-                    const int h = hi - c * 32, l = lo - c * 32;
-                    const bool some = h < 32 || l > 0;
-                    wait_ld();
-                    if (__any_sync(~0u, some)) {
+#pragma unroll
+                for (int c = 0; c < kGrans; ++c) ld32(sc + c * 32, raw + c * 32);
+                wait_ld();
+                if (edge) {
+#pragma unroll
+                    for (int c = 0; c < kGrans; ++c) {
+                        const int h = hi - c * 32, l = lo - c * 32;
                         const uint32_t seen = (h >= 32 ? ~0u : h <= 0 ? 0u : (1u << h) - 1) &
                                               (l <= 0 ? ~0u : l >= 32 ? 0u : ~0u << l);
+                        if (__any_sync(~0u, seen != ~0u)) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (!(seen >> j & 1)) s[j] = -INFINITY;
+                            for (int j = 0; j < 32; ++j)
+                                if (!(seen >> j & 1)) s[c * 32 + j] = -INFINITY;
+                        }
                     }
-                };
-                float most = -INFINITY;
-#pragma unroll 1
-                for (int c = 0; c < 2; ++c) {
-                    chunk(c);
-                    float big[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) big[j] = fmaxf(s[j], s[4 + j]);
-#pragma unroll
-                    for (int j = 8; j < 32; j += 8)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) big[i] = fmaxf(big[i], fmaxf(s[j + i], s[j + 4 + i]));
-                    const float b = fmaxf(fmaxf(big[0], big[1]), fmaxf(big[2], big[3]));
-                    // a factor that is not 0: what is not seen stays -inf
-                    most = fmaxf(most, fmaf(b, fmaxf(unit * scale[0][half * 2 + c], 0x1p-126f), scale[1][half * 2 + c]));
                 }
-                float other = most;
-                if (!exchange(other)) return;  
-                most = fmaxf(most, other);
+                float most = -INFINITY;
+#pragma unroll
+                for (int c = 0; c < kGrans; ++c) {
+                    float b0 = max3(s[c * 32], s[c * 32 + 1], s[c * 32 + 2]);
+                    float b1 = max3(s[c * 32 + 3], s[c * 32 + 4], s[c * 32 + 5]);
+#pragma unroll
+                    for (int j = 6; j < 30; j += 4) {
+                        b0 = max3(b0, s[c * 32 + j], s[c * 32 + j + 1]);
+                        b1 = max3(b1, s[c * 32 + j + 2], s[c * 32 + j + 3]);
+                    }
+                    b0 = max3(b0, s[c * 32 + 30], s[c * 32 + 31]);
+                    most = fmaxf(most, fmaf(fmaxf(b0, b1), mul[c], add[c]));
+                }
                 const bool grows = most > top + kGrow;
                 const float now = grows ? most : top;
                 const float fade = top == -INFINITY ? 0.f : exp2_approx(top - now);
                 const float ref = now == -INFINITY ? 0.f : now - kManyLift;
                 sum *= fade;
                 top = now;
-#pragma unroll 1
-                for (int c = 0; c < 2; ++c) {
-                    chunk(c);
-                    const float mul = fmaxf(unit * scale[0][half * 2 + c], 0x1p-126f), off = scale[1][half * 2 + c] - ref;
-                    float p0 = 0.f, p1 = 0.f;
+#pragma unroll
+                for (int c = 0; c < kGrans; ++c) {
+                    const float off = add[c] - ref;
+                    float p0 = 0.f, p1 = 0.f, p2 = 0.f, p3 = 0.f;
                     uint32_t p[16];
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
-                        float &e0 = s[2 * j], &e1 = s[2 * j + 1];
-                        fma2(e0, e1, mul, off);
+                        float &e0 = s[c * 32 + 2 * j], &e1 = s[c * 32 + 2 * j + 1];
+                        fma2(e0, e1, mul[c], off);
                         e0 = exp2_approx(e0), e1 = exp2_approx(e1);
-                        add2(p0, p1, e0, e1);
+                        if (j % 2 == 0) add2(p0, p1, e0, e1);
+                        else add2(p2, p3, e0, e1);
                         p[j] = pack_f16(e0, e1);
                     }
-                    sum = fmaf(p0 + p1, scale[2][half * 2 + c], sum);
-                    // over scores that this thread has read: the first 32 columns of its 64
-                    st16(sc + half * 64 + c * 16, p);
+                    sum = fmaf((p0 + p1) + (p2 + p3), scale[2][c], sum);
+                    // over scores that have been read: 16 columns for 32
+                    st16(sc + c * 16, p);
                 }
                 if (u > 0 && __any_sync(~0u, grows)) {
                     if (!await_warp(&m.o_done[tile], (n - 1) & 1, &m.gave_up)) return;
                     fence_after();
 #pragma unroll 1
-                    for (int c = 0; c < D / 32; ++c) {
+                    for (int c = 0; c < D / 16; ++c) {
                         uint32_t o[16];
                         ld16(su + c * 16, o);
                         wait_ld();
@@ -651,7 +640,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend_many(ManyArgs a) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(&m.q_full[i], kSoftmaxWarps / 2), mbar_init(&m.s_full[i], 1);
             mbar_init(&m.p_full[i], kSoftmaxWarps / 2), mbar_init(&m.o_done[i], 1);
-            mbar_init(&m.traded[i], kSoftmaxWarps / 2);
         }
         for (int i = 0; i < kStages; ++i) {
             mbar_init(&m.k_full[i], 128), mbar_init(&m.k_empty[i], 2);
@@ -733,9 +721,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend_many(ManyArgs a) {
     const int64_t per = (m.total + gridDim.x - 1) / gridDim.x;
     const int64_t u0 = min(m.total, blockIdx.x * per), left = min(m.total, u0 + per) - u0;
     if (wid < kSoftmaxWarps) {
+        more_regs<kSoftmaxRegs>();
         if (left > 0) softmax_role<T, D>(a, m, left, blockIdx.x);
     } else if (wid < kSoftmaxWarps + 4) {
-        more_regs<kConvertRegs>();
+        fewer_regs<kConvertRegs>();
         if (left > 0) convert_role<T, D>(a, m, left);
     } else {
         fewer_regs<kProductRegs>();
