@@ -31,10 +31,10 @@ __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
 __device__ __forceinline__ bool mbar_try(uint64_t* bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
-        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 2000;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(ok)
         : "r"(smem_addr(bar)), "r"(parity)
-        : "memory");  // may sleep up to 2 us, and leaves the issue slots to others meanwhile
+        : "memory");
     return ok != 0;
 }
 // Waits for the phase of that parity to end; false if it has not after kKvSpinCycles.
@@ -80,9 +80,9 @@ __device__ __forceinline__ float value_scale(float s) { return fmaxf(s, 0x1p-100
 
 // kv_attend_many.cu: where on the line of units a CTA began.
 struct ManyStart {
-    int32_t b, tile, head, cnt, k;  // cnt: units of that (sequence, pair of tiles, head); k: the first of this CTA
+    int32_t b, tile, head, cnt, into;  // cnt: units of that (sequence, pair of tiles, head)
     int32_t there;
-    int64_t per;  // units a CTA
+    int64_t per;  // length of a CTA's part
 };
 constexpr int kManyCtas = 152;  // one an SM
 struct ManyArgs {

@@ -30,13 +30,15 @@ constexpr int kPair = 2 * kRows;
 constexpr int kTokens = 128;    // of a unit
 constexpr int kGrans = kTokens / kGranule;
 constexpr int kStages = 2;      // of keys and of values
+constexpr int kExtra = 3;  // units that a stretch costs beside its own: queries in, sums out
 constexpr int kScaleRing = 4;
 constexpr int kLineRing = 4;
 constexpr int kSoftmaxWarps = 8;
 constexpr int kLineReaders = kSoftmaxWarps + 4 + 2;  // warps that read a stretch
 constexpr int kThreads = 16 * 32;
-// Registers a thread after the roles part: 256 x 168 + 128 x 112 + 128 x 64 = 512 x 128, the launch's.
-constexpr int kSoftmaxRegs = 168, kConvertRegs = 112, kProductRegs = 64;
+// Registers a thread after the roles part: 256 x 176 + 128 x 112 + 128 x 48 = 512 x 128, the launch's.
+constexpr int kSoftmaxRegs = 176, kConvertRegs = 112, kProductRegs = 48;
+constexpr int kTries = (int)(kKvSpinCycles >> 10);
 constexpr int kStrips = 1024;
 constexpr float kManyLift = 7.f;  // weights are at most 2^(8 + 7)
 constexpr float kGrow = 8.f;
@@ -120,7 +122,7 @@ __device__ __forceinline__ void fewer_regs() {
 struct Stretch {
     int b, tile, head;
     int cnt, k;              // units of the whole, the first of this stretch
-    int units;               // of this stretch
+    int units;               // of this stretch; 0: the CTA has no more
     int tiles;               // 1 or 2 of the pair have rows
     int first;               // of its CTA
     int first_gran, grans;   // granules that the pair's rows see
@@ -140,48 +142,68 @@ __device__ __forceinline__ void pair_grans(const ManyArgs& a, const SeqView& s, 
     lo = a.window > 0 ? max(0, p0 - a.window + 1) / kGranule : 0;
     n = max(0, (past + kGranule - 1) / kGranule - lo);
 }
-__device__ __forceinline__ int pair_units(const ManyArgs& a, const SeqView& s, int tile) {
+__device__ __forceinline__ int units_of(int grans) { return (grans + kGrans - 1) / kGrans; }
+// Length on the line: its units and what beginning and ending a pair costs beside them.
+__device__ __forceinline__ int pair_length(const ManyArgs& a, const SeqView& s, int tile) {
     int lo, n;
     pair_grans(a, s, tile, lo, n);
-    return (n + kGrans - 1) / kGrans;
+    return n > 0 ? units_of(n) + kExtra : 0;
 }
-// Units of a sequence; a warp's lanes take its pairs in turn.
-__device__ __forceinline__ int64_t seq_units_warp(const ManyArgs& a, int b, int lane) {
+// Length of a sequence; a warp's lanes take its pairs in turn.
+__device__ __forceinline__ int64_t seq_length(const ManyArgs& a, int b, int lane) {
     const SeqView s = load_seq(a.bt, b, false);
     const int pairs = pairs_of(a, s);
     int64_t n = 0;
-    for (int i = lane; i < pairs; i += 32) n += pair_units(a, s, i);
+    for (int i = lane; i < pairs; i += 32) n += pair_length(a, s, i);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(~0u, n, o);
     return n * a.c.n_heads;
 }
 __device__ __forceinline__ void fill(const ManyArgs& a, const SeqView& s, Stretch& x) {
     pair_grans(a, s, x.tile, x.first_gran, x.grans);
-    x.cnt = (x.grans + kGrans - 1) / kGrans;
+    x.cnt = units_of(x.grans);
     x.rows = s.n * a.group;
     x.tiles = x.rows - x.tile * kPair > kRows ? 2 : 1;
     x.len = s.len, x.start = s.len - s.n, x.row = s.lo;
 }
-// The stretch that follows on the line (there is one: the caller has units left).
-__device__ __forceinline__ void advance(const ManyArgs& a, Stretch& x) {
-    x.k = 0;
-    if (++x.head < a.c.n_heads) return;
+// The next pair or head on the line; false at its end.
+__device__ __forceinline__ bool advance(const ManyArgs& a, Stretch& x) {
+    if (++x.head < a.c.n_heads) return true;
     x.head = 0;
     ++x.tile;
     SeqView s;
     s.lo = x.row, s.len = x.len, s.n = x.len - x.start, s.st = MP_OK;
     for (;;) {
         const int pairs = pairs_of(a, s);
-        for (; x.tile < pairs; ++x.tile)
-            if (pair_units(a, s, x.tile) > 0) {
-                fill(a, s, x);
-                return;
-            }
+        for (; x.tile < pairs; ++x.tile) {
+            fill(a, s, x);
+            if (x.cnt > 0) return true;
+        }
         ++x.b, x.tile = 0;
-        if (x.b >= a.bt.n_seqs) return;
+        if (x.b >= a.bt.n_seqs) return false;
         s = load_seq(a.bt, x.b, false);
     }
 }
+
+// 8 values of 16 bits from and to memory that is aligned to one.
+template <typename T>
+__device__ __forceinline__ uint4 load_narrow(const T* p) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint16_t* e = reinterpret_cast<const uint16_t*>(p) + 2 * i;
+        w[i] = (uint32_t)e[0] | (uint32_t)e[1] << 16;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <typename T>
+__device__ __forceinline__ void store_narrow(T* p, uint4 v) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint16_t* e = reinterpret_cast<uint16_t*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e[2 * i] = (uint16_t)w[i], e[2 * i + 1] = (uint16_t)(w[i] >> 16);
+}
+
 template <int D>
 struct Smem {
     uint8_t q[2][kRows * D * 2];
@@ -194,25 +216,22 @@ struct Smem {
         scales_full[kScaleRing];
     Stretch line[kLineRing];  // the CTA's stretches as line_role lays them out
     Stretch first;
-    int64_t total;
+    int64_t length;  // of the CTA's part of the line
+    int into;        // where in its first pair and head it begins, on the line
     uint32_t tmem;
     int gave_up;
 };
 
-// Waits until the phase ends; false if some wait of the CTA has given up.
+// Waits until the phase ends; false if some wait of the CTA has given up. A try sleeps for
+// up to 2 us, so that kTries of them are seconds.
 __device__ __forceinline__ bool await(uint64_t* bar, uint32_t parity, volatile int* gave_up) {
-    if (mbar_try(bar, parity)) return true;
-    const long long t0 = clock64();
-    while (!mbar_try(bar, parity)) {
-        if (*gave_up) return false;
-        if (clock64() - t0 > kKvSpinCycles) {
+    for (int i = 0; !mbar_try(bar, parity); ++i)
+        if (i > kTries || *gave_up) {
             *gave_up = 1;
             return false;
         }
-    }
     return true;
 }
-
 // ... by all lanes of a warp, with one answer for all.
 __device__ __forceinline__ bool await_warp(uint64_t* bar, uint32_t parity, volatile int* gave_up) {
     return __all_sync(~0u, await(bar, parity, gave_up));
@@ -222,17 +241,28 @@ constexpr uint32_t kScoreCol = 0, kSumCol = 256;  // of tile 0; tile 1 has + 128
 
 // One thread walks the CTA's part of the line ahead of the roles.
 template <int D>
-__device__ void line_role(const ManyArgs& a, Smem<D>& m, int64_t left) {
+__device__ void line_role(const ManyArgs& a, Smem<D>& m) {
     Stretch x = m.first;
+    int64_t left = m.length;
+    int into = m.into;
     x.first = 1;
-    for (int seg = 0; left > 0; ++seg) {
-        x.units = (int)min((int64_t)(x.cnt - x.k), left);
+#pragma unroll 1
+    for (int seg = 0;; ++seg) {
+        // units come last on a pair's part of the line
+        x.units = 0;
+        while (left > 0) {
+            const int span = (int)min((int64_t)(x.cnt + kExtra - into), left);
+            x.k = max(0, into - kExtra);
+            x.units = max(0, into + span - kExtra) - x.k;
+            left -= span;
+            if (x.units > 0) break;
+        }
         if (!await(&m.line_empty[seg % kLineRing], (seg / kLineRing & 1) ^ 1, &m.gave_up)) return;
         m.line[seg % kLineRing] = x;
         mbar_arrive(&m.line_full[seg % kLineRing]);
-        left -= x.units;
-        x.first = 0;
-        if (left > 0) advance(a, x);
+        if (x.units == 0) return;
+        x.first = into = 0;
+        if (left > 0 && !advance(a, x)) left = 0;
     }
 }
 template <int D>
@@ -242,7 +272,7 @@ __device__ __forceinline__ void release(Smem<D>& m, int seg) {
 }
 
 template <typename T, int D>
-__device__ void convert_role(const ManyArgs& a, Smem<D>& m, int64_t left) {
+__device__ void convert_role(const ManyArgs& a, Smem<D>& m) {
     constexpr int kLoads = kTokens * D / 16 / 128;     // 16-byte loads a thread, of either array
     constexpr int kPerGran = kGranule * D / 16 / 128;  // ... of which a granule is this many, 1 or 2
     const int tid = threadIdx.x - kSoftmaxWarps * 32;
@@ -253,9 +283,12 @@ __device__ void convert_role(const ManyArgs& a, Smem<D>& m, int64_t left) {
     float ks = 0.f, vs = 1.f;
     // a unit's table entries are read a unit ahead, a granule a lane
     int page = -1, in_page = 0, head = 0, next_had = 0;
+    bool more = true;  // that unit is one
     auto look_up = [&]() {
         if (u == 0 && !await_warp(&m.line_full[seg % kLineRing], seg / kLineRing & 1, &m.gave_up)) return false;
         const Stretch& x = m.line[seg % kLineRing];
+        more = x.units > 0;
+        if (!more) return true;
         const int g = (x.k + u) * kGrans + mine, gran = x.first_gran + g, col = gran / per;
         page = -1, in_page = gran - col * per, head = x.head;
         if (g < x.grans) {
@@ -294,12 +327,12 @@ __device__ void convert_role(const ManyArgs& a, Smem<D>& m, int64_t left) {
         e4m3_to_f16(w.z, hi.x, hi.y), e4m3_to_f16(w.w, hi.z, hi.w);
         dst[0] = lo, dst[8] = hi;
     };
-    if (!look_up()) return;
+    if (!look_up() || !more) return;
     locate();
     load(a.c.k, kr);
-    if (left > 1 && !look_up()) return;
+    if (!look_up()) return;
 #pragma unroll 1
-    for (int it = 0; left > 0; ++it, --left) {
+    for (int it = 0;; ++it) {
         const int st = it % kStages, held = had;
         const uint32_t empty = (it / kStages & 1) ^ 1;
         load(a.c.v, vr);
@@ -319,10 +352,11 @@ __device__ void convert_role(const ManyArgs& a, Smem<D>& m, int64_t left) {
         for (int i = 0; i < kLoads; ++i) widen(kr[i], to + i * 256);
         fence_smem();
         mbar_arrive(&m.k_full[st]);
-        if (left > 1) {
+        const bool again = more;
+        if (again) {
             locate();
             load(a.c.k, kr);
-            if (left > 2 && !look_up()) return;
+            if (!look_up()) return;
         }
         if (!await_warp(&m.v_empty[st], empty, &m.gave_up)) return;
         // stored tiles [granule][D / 8][2][8][16] become [granule][D / 8][4][8][8]
@@ -343,13 +377,14 @@ __device__ void convert_role(const ManyArgs& a, Smem<D>& m, int64_t left) {
         for (int i = 0; i < kLoads; ++i) widen(vr[i], to + i * 256);
         fence_smem();
         mbar_arrive(&m.v_full[st]);
+        if (!again) return;
     }
 }
 
 // One warp a tile, a lane of which issues: sums of a unit as its weights come, then the
 // next unit's scores over them.
 template <int D>
-__device__ void product_role(const ManyArgs& a, Smem<D>& m, int64_t left, int tile) {
+__device__ void product_role(Smem<D>& m, int tile) {
     constexpr uint32_t kScores = product_of(kRows, kTokens), kSums = product_of(kRows, D);
     constexpr uint32_t kStep = kTokens * D * 2 >> 4;  // between stages and between tiles, in descriptors
     const uint32_t sc = __shfl_sync(~0u, m.tmem, 0) + kScoreCol + tile * 128;
@@ -358,25 +393,13 @@ __device__ void product_role(const ManyArgs& a, Smem<D>& m, int64_t left, int ti
     const uint64_t k0 = operand(smem_addr(m.k[0]), 128, D * 16), v0 = operand(smem_addr(m.v[0]), 128, 512);
     uint32_t it = 0, mine = 0, asked = 0;  // units of the CTA; units and stretches of this tile
     int seg = 0;
-    // scores of unit it, which this tile has
-    auto scores = [&]() {
-        const uint64_t k = k0 + (it & 1) * kStep;
-        fence_after();
-        if (elected()) {
-#pragma unroll
-            for (int s = 0; s < D / 16; ++s) mma_ss(sc, q + s * 16, k + s * 16, kScores, s > 0);
-            commit(&m.s_full[tile]);
-            commit(&m.k_empty[it & 1]);
-        }
-        __syncwarp();
-    };
 #pragma unroll 1
-    while (left > 0) {
+    for (;;) {
         if (!await_warp(&m.line_full[seg % kLineRing], seg / kLineRing & 1, &m.gave_up)) return;
         const int units = m.line[seg % kLineRing].units;
         const bool has = tile < m.line[seg % kLineRing].tiles;
         release(m, seg++);
-        left -= units;
+        if (units == 0) return;
         if (!has) {
 #pragma unroll 1
             for (int u = 0; u < units; ++u, ++it) {
@@ -389,40 +412,41 @@ __device__ void product_role(const ManyArgs& a, Smem<D>& m, int64_t left, int ti
             continue;
         }
         if (!await_warp(&m.q_full[tile], asked++ & 1, &m.gave_up)) return;
-        if (!await_warp(&m.k_full[it & 1], it >> 1 & 1, &m.gave_up)) return;
-        if (mine > 0 && !await_warp(&m.o_done[tile], (mine - 1) & 1, &m.gave_up)) return;
-        scores();
 #pragma unroll 1
-        for (int u = 0; u < units; ++u) {
-            const uint64_t v = v0 + (it & 1) * kStep;
-            if (!await_warp(&m.v_full[it & 1], it >> 1 & 1, &m.gave_up)) return;
+        for (int u = 0; u < units; ++u, ++it, ++mine) {
+            const uint32_t st = it & 1, round = it >> 1 & 1;
+            if (!await_warp(&m.k_full[st], round, &m.gave_up)) return;
+            // scores overwrite the weights that the product before reads: products of different sums are not
+            // ordered among themselves
+            if (mine > 0 && !await_warp(&m.o_done[tile], (mine - 1) & 1, &m.gave_up)) return;
+            fence_after();
+            if (elected()) {
+                const uint64_t k = k0 + st * kStep;
+#pragma unroll
+                for (int s = 0; s < D / 16; ++s) mma_ss(sc, q + s * 16, k + s * 16, kScores, s > 0);
+                commit(&m.s_full[tile]);
+                commit(&m.k_empty[st]);
+            }
+            __syncwarp();
+            if (!await_warp(&m.v_full[st], round, &m.gave_up)) return;
             if (!await_warp(&m.p_full[tile], mine & 1, &m.gave_up)) return;
             fence_after();
             if (elected()) {
+                const uint64_t v = v0 + st * kStep;
 #pragma unroll
                 for (int s = 0; s < kTokens / 16; ++s)
-                    mma_ts(su, sc + s * 8, v + (s / 2) * (kGranule * D * 2 >> 4) + (s % 2) * 16, kSums,
-                           u > 0 || s > 0);
+                    mma_ts(su, sc + s * 8, v + (s / 2) * (kGranule * D * 2 >> 4) + (s % 2) * 16, kSums, u > 0 || s > 0);
                 commit(&m.o_done[tile]);
-                commit(&m.v_empty[it & 1]);
+                commit(&m.v_empty[st]);
             }
             __syncwarp();
-            ++it;
-            if (u + 1 < units) {
-                if (!await_warp(&m.k_full[it & 1], it >> 1 & 1, &m.gave_up)) return;
-                // its scores overwrite the weights that the product before reads: products of different
-                // sums are not ordered among themselves
-                if (!await_warp(&m.o_done[tile], mine & 1, &m.gave_up)) return;
-                scores();
-            }
-            ++mine;
         }
     }
 }
 
 // 4 warps a tile, a thread a row.
 template <typename T, int D>
-__device__ void softmax_role(const ManyArgs& a, Smem<D>& m, int64_t left, int w) {
+__device__ void softmax_role(const ManyArgs& a, Smem<D>& m, int w) {
     const int tile = threadIdx.x / 128, in_tile = threadIdx.x % 128, warp = in_tile / 32, lane = threadIdx.x % 32;
     const uint32_t lanes = (uint32_t)(warp * 32) << 16;
     const uint32_t sc = m.tmem + lanes + kScoreCol + tile * 128, su = m.tmem + lanes + kSumCol + tile * D;
@@ -432,58 +456,55 @@ __device__ void softmax_role(const ManyArgs& a, Smem<D>& m, int64_t left, int w)
 #pragma unroll 1
     for (int seg = 0;; ++seg) {
         // a stretch's queries go in before the sums of the one before it come out
-        if (left > 0 && !await_warp(&m.line_full[seg % kLineRing], seg / kLineRing & 1, &m.gave_up)) return;
+        if (!await_warp(&m.line_full[seg % kLineRing], seg / kLineRing & 1, &m.gave_up)) return;
         const Stretch& x = m.line[seg % kLineRing];
         const Stretch& done = m.line[(seg + kLineRing - 1) % kLineRing];
-        const bool mine = left > 0 && tile < x.tiles;
+        const int units = x.units;
+        const bool mine = units > 0 && tile < x.tiles;
         float unit = 0.f;  // what the row's scores are to be multiplied by
         if (mine) {
-            // 8 rows x 4 chunks of 16 bytes a load
-            uint4 raw[4][D / 32];
-#pragma unroll
+            // as they are into their places, 8 rows x 4 chunks of 16 bytes a step; then a thread its row
+            uint4* const q = reinterpret_cast<uint4*>(m.q[tile]);
+#pragma unroll 1
             for (int g = 0; g < 4; ++g) {
-                const int row = x.tile * kPair + tile * kRows + warp * 32 + g * 8 + lane / 4;
-                const bool there = row < x.rows;
+                const int at = warp * 32 + g * 8 + lane / 4, row = x.tile * kPair + tile * kRows + at;
                 const T* p = static_cast<const T*>(a.q.data) + (x.row + row / a.group) * a.q.token_stride +
                              (x.head * a.group + row % a.group) * a.q.head_stride + lane % 4 * 8;
+                uint4* to = q + (at / 8 * (D / 8) + lane % 4) * 8 + at % 8;
+                if (row >= x.rows) {
+#pragma unroll 1
+                    for (int i = 0; i < D / 32; ++i) to[i * 32] = make_uint4(0, 0, 0, 0);
+                } else if (a.wide_q) {
 #pragma unroll
-                for (int i = 0; i < D / 32; ++i) {
-                    raw[g][i] = make_uint4(0, 0, 0, 0);
-                    if (there) {
-                        if (a.wide_q) {
-                            raw[g][i] = __ldg(reinterpret_cast<const uint4*>(p) + i * 4);
-                        } else {
-                            T* e = reinterpret_cast<T*>(&raw[g][i]);
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) e[j] = p[i * 32 + j];
-                        }
-                    }
+                    for (int i = 0; i < D / 32; ++i)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(to + i * 32)), "l"(p + i * 32)
+                                     : "memory");
+                } else {
+#pragma unroll 1
+                    for (int i = 0; i < D / 32; ++i) to[i * 32] = load_narrow(p + i * 32);
                 }
             }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            __syncwarp();
+            uint4* const row = q + in_tile / 8 * D + in_tile % 8;
+            float most = 0.f;
+#pragma unroll 2
+            for (int i = 0; i < D / 8; ++i) {
+                const uint4 v = row[i * 8];
+                const T* e = reinterpret_cast<const T*>(&v);
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int at = warp * 32 + g * 8 + lane / 4;
-                float most = 0.f;
-#pragma unroll
-                for (int i = 0; i < D / 32; ++i) {
-                    const T* e = reinterpret_cast<const T*>(&raw[g][i]);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(to_f32(e[j])));
-                }
-                most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
-                most = fmaxf(most, __shfl_xor_sync(~0u, most, 2));
-                const float f = row_factor(most);
-                const float owner = __shfl_sync(~0u, f, lane % 8 * 4);
-                if (lane / 8 == g) unit = __fdiv_rn(a.scale * 1.4426950408889634f, owner);
-                uint4* to = reinterpret_cast<uint4*>(m.q[tile]) + (at / 8 * (D / 8) + lane % 4) * 8 + at % 8;
-#pragma unroll
-                for (int i = 0; i < D / 32; ++i) {
-                    const T* e = reinterpret_cast<const T*>(&raw[g][i]);
-                    uint4 o;
-                    o.x = pack_f16(to_f32(e[0]) * f, to_f32(e[1]) * f), o.y = pack_f16(to_f32(e[2]) * f, to_f32(e[3]) * f);
-                    o.z = pack_f16(to_f32(e[4]) * f, to_f32(e[5]) * f), o.w = pack_f16(to_f32(e[6]) * f, to_f32(e[7]) * f);
-                    to[i * 32] = o;
-                }
+                for (int j = 0; j < 8; j += 2) most = max3(most, fabsf(to_f32(e[j])), fabsf(to_f32(e[j + 1])));
+            }
+            const float f = row_factor(most);
+            unit = __fdiv_rn(a.scale * 1.4426950408889634f, f);
+#pragma unroll 2
+            for (int i = 0; i < D / 8; ++i) {
+                const uint4 v = row[i * 8];
+                const T* e = reinterpret_cast<const T*>(&v);
+                uint4 o;
+                o.x = pack_f16(to_f32(e[0]) * f, to_f32(e[1]) * f), o.y = pack_f16(to_f32(e[2]) * f, to_f32(e[3]) * f);
+                o.z = pack_f16(to_f32(e[4]) * f, to_f32(e[5]) * f), o.w = pack_f16(to_f32(e[6]) * f, to_f32(e[7]) * f);
+                row[i * 8] = o;
             }
             fence_smem();
             __syncwarp();
@@ -511,7 +532,14 @@ __device__ void softmax_role(const ManyArgs& a, Smem<D>& m, int64_t left, int w)
 #pragma unroll
                         for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(o[j]) * inv;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) store_values<T, 8>(dst + c * 32 + j * 8, a.wide_out, v + j * 8);
+                        for (int j = 0; j < 4; ++j) {
+                            Pack<T, 8> o8;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) o8.x[i] = from_f32<T>(v[j * 8 + i]);
+                            const uint4 w4 = *reinterpret_cast<const uint4*>(&o8);
+                            if (a.wide_out) reinterpret_cast<uint4*>(dst + c * 32)[j] = w4;
+                            else store_narrow(dst + c * 32 + j * 8, w4);
+                        }
                     }
                 } else {
 #pragma unroll
@@ -528,9 +556,7 @@ __device__ void softmax_role(const ManyArgs& a, Smem<D>& m, int64_t left, int w)
             pending = false;
         }
         if (seg > 0) release(m, seg - 1);
-        if (left <= 0) return;
-        const int units = x.units;
-        left -= units;
+        if (units == 0) return;
         if (mine) {
             const int r = x.tile * kPair + tile * kRows + in_tile;
             const int pos = x.start + r / a.group;
@@ -544,11 +570,11 @@ __device__ void softmax_role(const ManyArgs& a, Smem<D>& m, int64_t left, int w)
                 const float(*scale)[kGrans] = m.scales[(it + u) % kScaleRing];
                 if (!await_warp(&m.scales_full[(it + u) % kScaleRing], (it + u) / kScaleRing & 1, &m.gave_up)) return;
                 const bool edge = __any_sync(~0u, hi < kTokens || lo > 0);
-                float mul[kGrans], add[kGrans];
+                float mul[kGrans], add[kGrans], inverse[kGrans];
 #pragma unroll
                 for (int c = 0; c < kGrans; ++c) {
                     mul[c] = fmaxf(unit * scale[0][c], 0x1p-126f);  // not 0: what is not seen stays -inf
-                    add[c] = scale[1][c];
+                    add[c] = scale[1][c], inverse[c] = scale[2][c];
                 }
                 if (!await_warp(&m.s_full[tile], n & 1, &m.gave_up)) return;
                 fence_after();
@@ -603,7 +629,7 @@ __device__ void softmax_role(const ManyArgs& a, Smem<D>& m, int64_t left, int w)
                         else add2(p2, p3, e0, e1);
                         p[j] = pack_f16(e0, e1);
                     }
-                    sum = fmaf((p0 + p1) + (p2 + p3), scale[2][c], sum);
+                    sum = fmaf((p0 + p1) + (p2 + p3), inverse[c], sum);
                     // over scores that have been read: 16 columns for 32
                     st16(sc + c * 16, p);
                 }
@@ -656,41 +682,51 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend_many(ManyArgs a) {
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     // the line: strips of sequences, a warp a strip
-    const int strip = (a.bt.n_seqs + kStrips - 1) / kStrips;
-    for (int i = wid; i < kStrips; i += kThreads / 32) {
+    const int strip = (a.bt.n_seqs + kStrips - 1) / kStrips, strips = (a.bt.n_seqs + strip - 1) / strip;
+#pragma unroll 1
+    for (int i = wid; i < strips; i += kThreads / 32) {
         int64_t n = 0;
-        for (int b = i * strip; b < min((i + 1) * strip, a.bt.n_seqs); ++b) n += seq_units_warp(a, b, lane);
+#pragma unroll 1
+        for (int b = i * strip; b < min((i + 1) * strip, a.bt.n_seqs); ++b) n += seq_length(a, b, lane);
         if (lane == 0) m.strip[i] = n;
     }
     __syncthreads();
     if (wid == 0) {
-        // totals before each run of 32 strips, then the strip, sequence and pair of this CTA's first unit
+        // the strip, the sequence and the pair in which this CTA's part begins
+        const int each = (strips + 31) / 32;
         int64_t mine = 0;
-        for (int i = 0; i < kStrips / 32; ++i) mine += m.strip[lane * (kStrips / 32) + i];
+#pragma unroll 1
+        for (int i = lane * each; i < min((lane + 1) * each, strips); ++i) mine += m.strip[i];
         int64_t sum = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int64_t y = __shfl_up_sync(~0u, sum, o);
             if (lane >= o) sum += y;
         }
-        const int64_t total = __shfl_sync(~0u, sum, 31), per = (total + gridDim.x - 1) / gridDim.x;
+        const int64_t total = __shfl_sync(~0u, sum, 31);
+        const int64_t per = total < INT32_MAX ? ((uint32_t)total + gridDim.x - 1) / gridDim.x
+                                              : (total + gridDim.x - 1) / gridDim.x;
         const int64_t u0 = min(total, blockIdx.x * per);
         Stretch x = {};
+        int into = 0;
         if (u0 < total) {
             const int run = __popc(__ballot_sync(~0u, sum <= u0));
             int64_t at = __shfl_sync(~0u, sum - mine, run);
-            int i = run * (kStrips / 32);
+            int i = run * each;
+#pragma unroll 1
             while (at + m.strip[i] <= u0) at += m.strip[i++];
             int b = i * strip;
-            for (;; ++b) {
-                const int64_t n = seq_units_warp(a, b, lane);
+#pragma unroll 1
+            while (strip > 1) {
+                const int64_t n = seq_length(a, b, lane);
                 if (u0 < at + n) break;
-                at += n;
+                at += n, ++b;
             }
             const SeqView s = load_seq(a.bt, b, false);
             const int pairs = pairs_of(a, s);
+#pragma unroll 1
             for (int t0 = 0;; t0 += 32) {
-                const int64_t n = t0 + lane < pairs ? (int64_t)pair_units(a, s, t0 + lane) * a.c.n_heads : 0;
+                const int64_t n = t0 + lane < pairs ? (int64_t)pair_length(a, s, t0 + lane) * a.c.n_heads : 0;
                 int64_t up = n;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) {
@@ -706,37 +742,35 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend_many(ManyArgs a) {
                 at += __shfl_sync(~0u, up, 31);
             }
             fill(a, s, x);
-            x.head = (int)((u0 - at) / x.cnt);
-            x.k = (int)((u0 - at) % x.cnt);
+            x.head = (int)((uint32_t)(u0 - at) / (uint32_t)(x.cnt + kExtra));
+            into = (int)((uint32_t)(u0 - at) % (uint32_t)(x.cnt + kExtra));
         }
         if (lane == 0) {
-            m.first = x, m.total = total;
-            ManyStart st = {x.b, x.tile, x.head, x.cnt, x.k, u0 < total, per};
+            m.first = x, m.length = min(total, u0 + per) - u0, m.into = into;
+            const ManyStart st = {x.b, x.tile, x.head, x.cnt, into, u0 < total, per};
             a.starts[blockIdx.x] = st;
         }
     }
     fence_before();
     __syncthreads();
     fence_after();
-    const int64_t per = (m.total + gridDim.x - 1) / gridDim.x;
-    const int64_t u0 = min(m.total, blockIdx.x * per), left = min(m.total, u0 + per) - u0;
     if (wid < kSoftmaxWarps) {
         more_regs<kSoftmaxRegs>();
-        if (left > 0) softmax_role<T, D>(a, m, left, blockIdx.x);
+        softmax_role<T, D>(a, m, blockIdx.x);
     } else if (wid < kSoftmaxWarps + 4) {
         fewer_regs<kConvertRegs>();
-        if (left > 0) convert_role<T, D>(a, m, left);
+        convert_role<T, D>(a, m);
     } else {
         fewer_regs<kProductRegs>();
         const int role = wid - kSoftmaxWarps - 4;
-        if (role < 2 && left > 0) {
-            product_role<D>(a, m, left, role);
+        if (role < 2) {
+            product_role<D>(m, role);
             __syncwarp();
             if (elected()) commit(&m.drained);  // nothing may be in flight when tensor memory goes
             __syncwarp();
             mbar_wait(&m.drained, 0);
-        } else if (role == 2 && lane == 0 && left > 0) {
-            line_role<D>(a, m, left);
+        } else if (role == 2 && lane == 0) {
+            line_role<D>(a, m);
         }
     }
     fence_before();
@@ -761,15 +795,15 @@ __global__ void __launch_bounds__(kPair) k_kv_join_many(ManyArgs a) {
     if (blockIdx.x < cuts) {
         const int w = blockIdx.x / (D / kJoinCols), y = blockIdx.x % (D / kJoinCols);
         const ManyStart st = a.starts[w];
-        if (!st.there || st.k == 0) return;
-        const int64_t us = w * st.per - st.k;  // the stretch's first unit
-        if (us < (w - 1) * st.per) return;
-        const int last = (int)((us + st.cnt - 1) / st.per);
+        if (!st.there || st.into <= kExtra) return;  // (it began with the pair's first unit)
+        const int64_t us = w * st.per - st.into;     // the pair and head on the line
+        const int begun = (int)((us + kExtra) / st.per), last = (int)((us + kExtra + st.cnt - 1) / st.per);
+        if (w != begun + 1) return;  // another CTA cut it before
         const SeqView s = load_seq(a.bt, st.b, false);
         const int r = st.tile * kPair + tid;
         if (r >= s.n * a.group) return;
         float top = -INFINITY, sum = 0.f, o[kJoinCols] = {};
-        for (int v = w - 1; v <= last; ++v) {
+        for (int v = begun; v <= last; ++v) {
             const float* part = a.part + ((int64_t)2 * v + (v * st.per >= us ? 0 : 1)) * (kPair * (D + 2));
             const float m = part[D * kPair + tid], l = part[(D + 1) * kPair + tid];
             const float now = fmaxf(top, m), ref = now == -INFINITY ? 0.f : now;
