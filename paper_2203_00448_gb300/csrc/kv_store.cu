@@ -15,24 +15,70 @@ namespace mp {
 namespace {
 
 constexpr int kWriteWarps = 16;          // few tokens: one CTA a sequence, a warp a block, head and array
-constexpr int kWriteThreads = 128;       // many tokens: one CTA a block, head and array
-constexpr int32_t kWriteFewTokens = 16;  // ... above this many tokens a sequence
+constexpr int32_t kWriteFewTokens = 16;  // ... up to this many tokens a sequence
+constexpr int kWriteThreads = 128;
+constexpr int kWriteCtas = 152 * 12;
 constexpr int kReadThreads = 256;
 
-// The larger of all lanes' values, over a warp or a CTA of kGroup threads.
+// Magnitudes are compared as the integers that their bits are (without the sign): one operation a value or a pair,
+// and infinities and NaN come out above everything finite.
+template <typename T>
+constexpr uint32_t kInfBits = 0x7f800000u;
+template <>
+constexpr uint32_t kInfBits<__half> = 0x7c00u;
+template <>
+constexpr uint32_t kInfBits<__nv_bfloat16> = 0x7f80u;
+template <typename T>
+__device__ __forceinline__ float value_of(uint32_t bits) {
+    if (sizeof(T) == 4) return __uint_as_float(bits);
+    const uint16_t h = (uint16_t)bits;
+    return to_f32(*reinterpret_cast<const T*>(&h));
+}
+// The largest magnitude of the values in a word (4-byte types: one, else two) joins top (two halves for two).
+template <typename T>
+__device__ __forceinline__ uint32_t join_word(uint32_t top, uint32_t w) {
+    return sizeof(T) == 4 ? max(top, w & 0x7fffffffu) : __vmaxu2(top, w & 0x7fff7fffu);
+}
+// ... only finite ones.
+template <typename T>
+__device__ __forceinline__ uint32_t join_finite(uint32_t top, uint32_t w) {
+    if (sizeof(T) == 4) return (w & 0x7fffffffu) < kInfBits<T> ? max(top, w & 0x7fffffffu) : top;
+    const uint32_t lo = w & 0x7fffu, hi = w & 0x7fff0000u;
+    if (lo < kInfBits<T>) top = __vmaxu2(top, lo);
+    if (hi < kInfBits<T> << 16) top = __vmaxu2(top, hi);
+    return top;
+}
+template <typename T>
+__device__ __forceinline__ uint32_t join_end(uint32_t top) {
+    return sizeof(T) == 4 ? top : max(top & 0xffffu, top >> 16);
+}
+// The largest of all threads' integers, over a warp (kGroup 32) or a CTA (0).
 template <int kGroup>
-__device__ __forceinline__ float group_max(float x, float* smem) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(~0u, x, o));
-    if (kGroup > 32) {
+__device__ __forceinline__ uint32_t group_max(uint32_t x, uint32_t* smem) {
+    x = __reduce_max_sync(~0u, x);
+    if (kGroup == 0) {
         __syncthreads();  // smem's last use
         if (threadIdx.x % 32 == 0) smem[threadIdx.x / 32] = x;
         __syncthreads();
-        x = smem[0];
-#pragma unroll
-        for (int w = 1; w < kGroup / 32; ++w) x = fmaxf(x, smem[w]);
+        x = smem[threadIdx.x % (kWriteThreads / 32)];
+        x = __reduce_max_sync(~0u, x);
     }
     return x;
+}
+// The values in a word, times the inverse of the scale; `odd`: some value of the block is not finite (NaN is stored as 0).
+template <typename T>
+__device__ __forceinline__ void scaled(uint32_t w, float inverse, bool odd, float* y) {
+    if (sizeof(T) == 4) {
+        y[0] = __uint_as_float(w);
+    } else {
+        const uint16_t lo = (uint16_t)w, hi = (uint16_t)(w >> 16);
+        y[0] = to_f32(*reinterpret_cast<const T*>(&lo)), y[1] = to_f32(*reinterpret_cast<const T*>(&hi));
+    }
+#pragma unroll
+    for (int i = 0; i < 4 / (int)sizeof(T); ++i) {
+        if (odd) y[i] = y[i] == y[i] ? y[i] : 0.f;
+        y[i] *= inverse;
+    }
 }
 
 // 2^e with the least e in [-60, 120] such that a <= 448 * 2^e = 1.75 * 2^(e + 8).
@@ -43,9 +89,6 @@ __device__ __forceinline__ float scale_of(float a) {
     return __uint_as_float((uint32_t)(e + 127) << 23);
 }
 
-// NaN counts as 0 where it is stored; ok is cleared for it and for infinities.
-__device__ __forceinline__ float storable(float x) { return x == x ? x : 0.f; }
-
 // 4 stored bytes under another scale (ratio: the old one over the new one).
 __device__ __forceinline__ uint32_t rescale(uint32_t w, float ratio) {
     float x[4];
@@ -55,113 +98,128 @@ __device__ __forceinline__ uint32_t rescale(uint32_t w, float ratio) {
     return f32_to_e4m3(x);
 }
 
-// kGroup threads put n tokens (x: the first one's values of this head) into slots
-// [first, first + n) of one block and head of one array; slots below first hold
-// earlier tokens.  Returns whether this thread met only finite values.
-template <typename T, int D, bool kValues, int kGroup>
-__device__ bool store_block(const T* x, int64_t stride, bool wide, int first, int n, uint8_t* bytes, float* scale_at,
-                            int rank, float* smem) {
-    bool ok = true;
-    float top = 0.f;
-    const float old = first > 0 ? *scale_at : 0.f;
-    for (int i = rank; i < n * (D / 16); i += kGroup) {
-        float v[16];
-        load_values<T, 16>(x + (i / (D / 16)) * stride + i % (D / 16) * 16, wide, v);
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            const float a = fabsf(v[k]);
-            const bool fine = a <= 3.402823466e38f;
-            ok = ok && fine;
-            top = fmaxf(top, fine ? a : 0.f);
+// The earlier tokens (slots below first) of one block and head under a larger scale; kGroup threads.
+template <int D, bool kValues>
+__device__ __noinline__ void rescale_block(uint8_t* bytes, int first, float ratio, int rank, int group) {
+    uint32_t* const word = reinterpret_cast<uint32_t*>(bytes);
+    const int words = (first + kGranule - 1) / kGranule * kGranule * D / 4;
+    for (int i = rank; i < words; i += group) {
+        const int byte = i * 4;
+        if (!kValues) {
+            if (byte / 128 / (D / 16) * 8 + byte % 128 / 16 < first) word[i] = rescale(word[i], ratio);
+        } else {
+            const int t = byte / (32 * D) * 32 + byte / 128 % 2 * 16 + byte % 16, n = first - t;
+            if (n <= 0) continue;
+            const uint32_t keep = n >= 4 ? ~0u : (1u << (8 * n)) - 1, had = word[i];
+            word[i] = (rescale(had, ratio) & keep) | (had & ~keep);
         }
     }
-    top = group_max<kGroup>(top, smem);
-    const float fresh = scale_of(top), scale = fmaxf(fresh, old), inverse = __fdiv_rn(1.f, scale);
-    const bool grows = first > 0 && scale > old;
-    const float ratio = grows ? __fdiv_rn(old, scale) : 1.f;
-    if (rank == 0 && !(first > 0 && scale == old)) *scale_at = scale;
-    const int past = first + n;
-    if (!kValues) {
-        const int from = grows ? 0 : first;
-        for (int i = rank; i < (past - from) * (D / 16); i += kGroup) {
-            const int t = from + i / (D / 16), d = i % (D / 16) * 16;
-            uint4* at = reinterpret_cast<uint4*>(bytes + key_byte<D>(t, d));
-            uint4 w;
-            if (t < first) {
-                w = *at;
-                w.x = rescale(w.x, ratio), w.y = rescale(w.y, ratio), w.z = rescale(w.z, ratio), w.w = rescale(w.w, ratio);
-            } else {
-                float v[16];
-                load_values<T, 16>(x + (t - first) * stride + d, wide, v);
-#pragma unroll
-                for (int k = 0; k < 16; ++k) v[k] = storable(v[k]) * inverse;
-                w = make_uint4(f32_to_e4m3(v), f32_to_e4m3(v + 4), f32_to_e4m3(v + 8), f32_to_e4m3(v + 12));
-            }
-            *at = w;
-        }
-        return ok;
-    }
-    // a thread has 16 tokens of 2 neighbouring values, 2 x 16 stored bytes
-    const int from = grows ? 0 : first / 16;
-    for (int i = rank; i < ((past + 15) / 16 - from) * (D / 2); i += kGroup) {
-        const int t0 = (from + i / (D / 2)) * 16, d = i % (D / 2) * 2;
-        uint8_t* at = bytes + value_byte<D>(t0, d);
-        float v[2][16];
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            float pair[2] = {0.f, 0.f};
-            if (t0 + k >= first && t0 + k < past) load_values<T, 2>(x + (t0 + k - first) * stride + d, wide, pair);
-            v[0][k] = storable(pair[0]) * inverse, v[1][k] = storable(pair[1]) * inverse;
-        }
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            uint32_t w[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] = f32_to_e4m3(v[r] + 4 * k);
-            uint4* row = reinterpret_cast<uint4*>(at + 16 * r);
-            if (t0 < first || t0 + 16 > past) {
-                // part of it only: earlier tokens under the new scale, slots without a token as they were
-                const uint4 had = *row;
-                const uint32_t h[4] = {had.x, had.y, had.z, had.w};
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint32_t again = grows ? rescale(h[k], ratio) : h[k];
-                    uint32_t m = 0, o = 0;  // bytes of new tokens, of earlier ones
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int t = t0 + 4 * k + j;
-                        if (t < first) o |= 0xffu << (8 * j);
-                        else if (t < past) m |= 0xffu << (8 * j);
-                    }
-                    w[k] = (w[k] & m) | (again & o) | (h[k] & ~(m | o));
-                }
-            }
-            *row = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-    }
-    return ok;
 }
 
-// One block, head and array of sequence b; j counts the blocks that the call touches.
-template <typename T, int D, int kGroup>
-__device__ bool write_unit(const mp_kv_cache& c, const mp_kv_batch& bt, const SeqView& s, int b, int j, int head,
-                           bool values, const mp_tokens& k, const mp_tokens& v, bool wide, int rank, float* smem) {
+// What the tokens of a block and head are stored under, given the largest new magnitude; earlier tokens are brought
+// under it too.  Every thread of the group calls it, after top is known to all; returns the scale's inverse.
+template <int D, bool kValues, int kGroup>
+__device__ __forceinline__ float settle(float top, float old, int first, uint8_t* bytes, float* scale_at, int rank) {
+    const float scale = fmaxf(scale_of(top), old);
+    if (first > 0 && scale > old) {
+        rescale_block<D, kValues>(bytes, first, __fdiv_rn(old, scale), rank, kGroup == 32 ? 32 : blockDim.x);
+        // a new token's bytes may share words with earlier ones
+        if (kGroup == 32) __syncwarp();
+        else __syncthreads();
+    }
+    if (rank == 0 && !(first > 0 && scale == old)) *scale_at = scale;
+    return __fdiv_rn(1.f, scale);
+}
+
+// Where a block, head and array of the call lies.
+struct Place {
+    const void* x;  // its first new token's values
+    int64_t stride;
+    int first, n;  // slots [first, first + n)
+    uint8_t* bytes;
+    float* scale;
+};
+// j counts the blocks that the call touches; false if the table is wrong there.
+template <typename T>
+__device__ __forceinline__ bool find(const mp_kv_cache& c, const mp_kv_batch& bt, const SeqView& s, int b, int j, int head,
+                                     bool values, const mp_tokens& k, const mp_tokens& v, Place& p) {
     const int start = s.len - s.n, col = start / c.block_tokens + j, base = col * c.block_tokens;
     const int page = __ldg(bt.table + (int64_t)b * bt.max_blocks + col);
     if (page < 0 || page >= c.n_blocks) return false;
-    const int first = max(start - base, 0), n = min(s.len - base, c.block_tokens) - first;
+    p.first = max(start - base, 0), p.n = min(s.len - base, c.block_tokens) - p.first;
     const mp_tokens& t = values ? v : k;
-    const T* x = static_cast<const T*>(t.data) + (s.lo + (base + first - start)) * t.token_stride + head * t.head_stride;
+    p.stride = t.token_stride;
+    p.x = static_cast<const T*>(t.data) + (s.lo + (base + p.first - start)) * t.token_stride + head * t.head_stride;
     const int64_t at = block_byte(c, page, head), sc = (int64_t)page * c.n_heads + head;
-    return values ? store_block<T, D, true, kGroup>(x, t.token_stride, wide, first, n, c.v + at, c.v_scale + sc, rank, smem)
-                  : store_block<T, D, false, kGroup>(x, t.token_stride, wide, first, n, c.k + at, c.k_scale + sc, rank, smem);
+    p.bytes = (values ? c.v : c.k) + at, p.scale = (values ? c.v_scale : c.k_scale) + sc;
+    return true;
 }
 
 __device__ __forceinline__ int blocks_touched(const mp_kv_cache& c, const SeqView& s) {
     return s.n == 0 ? 0 : (s.len - 1) / c.block_tokens - (s.len - s.n) / c.block_tokens + 1;
 }
 
-// Few tokens a sequence: one CTA a sequence, so that its status has one writer.
+// A lane's D / 32 values of a token as words.
+template <typename T, int D>
+__device__ __forceinline__ void read_lane(const T* at, bool wide, uint32_t* w) {
+    constexpr int kWords = D / 32 * sizeof(T) / 4;
+    if (wide) {
+        const Pack<uint32_t, kWords> v = *reinterpret_cast<const Pack<uint32_t, kWords>*>(at);
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = v.x[i];
+    } else if (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = reinterpret_cast<const uint32_t*>(at)[i];
+    } else {
+        const uint16_t* h = reinterpret_cast<const uint16_t*>(at);
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = (uint32_t)h[2 * i] | (uint32_t)h[2 * i + 1] << 16;
+    }
+}
+
+// A warp stores n tokens one after another, a lane D / 32 values of each.
+template <typename T, int D, bool kValues>
+__device__ __forceinline__ bool store_few(const Place& p, bool wide, int lane) {
+    constexpr int kPer = D / 32, kWords = kPer * sizeof(T) / 4, kIn = 4 / sizeof(T);
+    const T* x = static_cast<const T*>(p.x) + lane * kPer;
+    const float old = p.first > 0 ? *p.scale : 0.f;
+    uint32_t w[kWords], top = 0;
+    for (int i = 0; i < p.n; ++i) {
+        read_lane<T, D>(x + i * p.stride, wide, w);
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) top = join_word<T>(top, w[k]);
+    }
+    top = group_max<32>(join_end<T>(top), nullptr);
+    const bool odd = top >= kInfBits<T>;
+    if (odd) {
+        top = 0;
+        for (int i = 0; i < p.n; ++i) {
+            read_lane<T, D>(x + i * p.stride, wide, w);
+            for (int k = 0; k < kWords; ++k) top = join_finite<T>(top, w[k]);
+        }
+        top = group_max<32>(join_end<T>(top), nullptr);
+    }
+    const float inverse = settle<D, kValues, 32>(value_of<T>(top), old, p.first, p.bytes, p.scale, lane);
+    for (int i = 0; i < p.n; ++i) {
+        if (p.n > 1) read_lane<T, D>(x + i * p.stride, wide, w);
+        float v[4] = {};
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) scaled<T>(w[k], inverse, odd, v + k * kIn);
+        const uint32_t out = f32_to_e4m3(v);
+        const int t = p.first + i, d = lane * kPer;
+        if (!kValues) {
+            uint8_t* at = p.bytes + key_byte<D>(t, d);
+            if (kPer == 4) *reinterpret_cast<uint32_t*>(at) = out;
+            else *reinterpret_cast<uint16_t*>(at) = (uint16_t)out;
+        } else {
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) p.bytes[value_byte<D>(t, d + k)] = (uint8_t)(out >> (8 * k));
+        }
+    }
+    return !odd;
+}
+
+// Few tokens a sequence: one CTA a sequence, so that its status has one writer; a warp a block, head and array.
 template <typename T, int D>
 __global__ void __launch_bounds__(kWriteWarps * 32)
     k_kv_write_few(mp_kv_cache c, mp_kv_batch bt, mp_tokens k, mp_tokens v, bool wide, int32_t* status) {
@@ -169,30 +227,149 @@ __global__ void __launch_bounds__(kWriteWarps * 32)
         const SeqView s = load_seq(bt, b, true);
         const int tasks = blocks_touched(c, s) * c.n_heads * 2;
         bool ok = s.st == MP_OK;
-        for (int u = threadIdx.x / 32; u < tasks; u += kWriteWarps)
-            ok &= write_unit<T, D, 32>(c, bt, s, b, u / (2 * c.n_heads), u / 2 % c.n_heads, u % 2, k, v, wide,
-                                       threadIdx.x % 32, nullptr);
+        for (int u = threadIdx.x / 32; u < tasks; u += kWriteWarps) {
+            Place p;
+            if (!find<T>(c, bt, s, b, u / (2 * c.n_heads), u / 2 % c.n_heads, u % 2, k, v, p)) ok = false;
+            else if (u % 2) ok &= store_few<T, D, true>(p, wide, threadIdx.x % 32);
+            else ok &= store_few<T, D, false>(p, wide, threadIdx.x % 32);
+        }
         const bool bad = __syncthreads_or(!ok);
         if (threadIdx.x == 0) status[b] = bad ? MP_EINVAL : MP_OK;
     }
 }
 
-// Many tokens: units of one block, head and array over the whole grid; status is
-// cleared before.
+// Bytes of shared memory for a unit's values, and how many such stages a CTA has.
+__host__ __device__ constexpr size_t stage_bytes(int block_tokens, int dim, size_t size) { return (size_t)block_tokens * dim * size; }
+__host__ __device__ constexpr int stages_of(size_t bytes) { return bytes <= 48 * 1024 ? 2 : 1; }
+
+// Many tokens: a CTA a block and `heads` of its heads, keys and values; the next unit's values come into shared memory
+// while one is scaled and stored (a lane takes 16 values of a token, or 16 tokens of 2 neighbouring values, to store 16
+// bytes at once).  status is cleared before.
 template <typename T, int D>
 __global__ void __launch_bounds__(kWriteThreads)
-    k_kv_write_many(mp_kv_cache c, mp_kv_batch bt, mp_tokens k, mp_tokens v, bool wide, int32_t* status, int per_seq) {
-    __shared__ float smem[kWriteThreads / 32];
-    const int64_t units = (int64_t)bt.n_seqs * per_seq * c.n_heads * 2;
-    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const bool values = u % 2;
-        const int64_t r = u / 2;
-        const int head = (int)(r % c.n_heads), j = (int)(r / c.n_heads % per_seq), b = (int)(r / c.n_heads / per_seq);
+    k_kv_write_many(mp_kv_cache c, mp_kv_batch bt, mp_tokens k, mp_tokens v, bool wide, int32_t* status, int per_seq,
+                    int heads) {
+    extern __shared__ __align__(16) uint8_t dyn[];
+    __shared__ uint32_t smem[kWriteThreads / 32];
+    const int rank = threadIdx.x, groups = (c.n_heads + heads - 1) / heads;
+    const size_t bytes = stage_bytes(c.block_tokens, D, sizeof(T));
+    const int stages = stages_of(bytes);
+    const int64_t work = (int64_t)bt.n_seqs * per_seq * groups;
+    for (int64_t w = blockIdx.x; w < work; w += gridDim.x) {
+        const int h0 = (int)(w % groups) * heads, j = (int)(w / groups % per_seq), b = (int)(w / groups / per_seq);
         const SeqView s = load_seq(bt, b, true);
         bool ok = s.st == MP_OK;
-        if (j < blocks_touched(c, s))
-            ok &= write_unit<T, D, kWriteThreads>(c, bt, s, b, j, head, values, k, v, wide, threadIdx.x, smem);
-        if (!ok) status[b] = MP_EINVAL;  // whoever writes it writes the same
+        const int units = j < blocks_touched(c, s) ? 2 * min(heads, c.n_heads - h0) : 0;
+        Place p, q;
+        if (!ok || (units > 0 && !find<T>(c, bt, s, b, j, h0, false, k, v, p))) {
+            status[b] = MP_EINVAL;  // whoever writes it writes the same
+            continue;
+        }
+        constexpr int kIn = 16 / sizeof(T);  // values in 16 bytes
+        const int step = kWriteThreads / (D / kIn), t_in = rank / (D / kIn), d_in = rank % (D / kIn) * kIn;
+        auto fetch = [&](int u) {  // unit u's values into its stage: [tokens][D]
+            find<T>(c, bt, s, b, j, h0 + u / 2, u % 2, k, v, q);
+            T* to = reinterpret_cast<T*>(dyn + (u % stages) * bytes) + rank * kIn;
+            const T* at = static_cast<const T*>(q.x) + t_in * q.stride + d_in;
+            for (int t = t_in; t < q.n; t += step, at += step * q.stride, to += kWriteThreads * kIn) {
+                if (wide) {
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(
+                                     (uint32_t)__cvta_generic_to_shared(to)),
+                                 "l"(at)
+                                 : "memory");
+                } else {
+#pragma unroll
+                    for (int e = 0; e < kIn; ++e) to[e] = at[e];
+                }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        if (units > 0) fetch(0);
+        for (int u = 0; u < units; ++u) {
+            p = q;
+            if (stages == 2 && u + 1 < units) {
+                fetch(u + 1);
+                asm volatile("cp.async.wait_group 1;" ::: "memory");
+            } else {
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+            }
+            const float old = p.first > 0 ? *p.scale : 0.f;
+            __syncthreads();
+            const uint4* x = reinterpret_cast<const uint4*>(dyn + (u % stages) * bytes);
+            const int chunks = p.n * (D / kIn);  // of 16 bytes
+            uint32_t top = 0;
+            for (int i = rank; i < chunks; i += kWriteThreads) {
+                const uint4 w = x[i];
+                top = join_word<T>(join_word<T>(top, w.x), w.y);
+                top = join_word<T>(join_word<T>(top, w.z), w.w);
+            }
+            top = group_max<0>(join_end<T>(top), smem);
+            const bool odd = top >= kInfBits<T>;
+            if (odd) {
+                ok = false;
+                top = 0;
+                for (int i = rank; i < chunks; i += kWriteThreads) {
+                    const uint4 w = x[i];
+                    top = join_finite<T>(join_finite<T>(top, w.x), w.y);
+                    top = join_finite<T>(join_finite<T>(top, w.z), w.w);
+                }
+                top = group_max<0>(join_end<T>(top), smem);
+            }
+            if (u % 2 == 0) {
+                const float inverse = settle<D, false, 0>(value_of<T>(top), old, p.first, p.bytes, p.scale, rank);
+                for (int i = rank; i < p.n * (D / 16); i += kWriteThreads) {
+                    constexpr int kFour = 16 / kIn;  // 16-byte chunks in 16 values
+                    float y[16];
+#pragma unroll
+                    for (int e = 0; e < kFour; ++e) {
+                        const uint4 w = x[i * kFour + e];
+                        scaled<T>(w.x, inverse, odd, y + e * kIn), scaled<T>(w.y, inverse, odd, y + e * kIn + kIn / 4);
+                        scaled<T>(w.z, inverse, odd, y + e * kIn + kIn / 2);
+                        scaled<T>(w.w, inverse, odd, y + e * kIn + kIn / 4 * 3);
+                    }
+                    *reinterpret_cast<uint4*>(p.bytes + key_byte<D>(p.first + i / (D / 16), i % (D / 16) * 16)) =
+                        make_uint4(f32_to_e4m3(y), f32_to_e4m3(y + 4), f32_to_e4m3(y + 8), f32_to_e4m3(y + 12));
+                }
+            } else {
+                const float inverse = settle<D, true, 0>(value_of<T>(top), old, p.first, p.bytes, p.scale, rank);
+                const int past = p.first + p.n, from = p.first / 16;
+                for (int i = rank; i < ((past + 15) / 16 - from) * (D / 2); i += kWriteThreads) {
+                    const int t0 = (from + i / (D / 2)) * 16, d = i % (D / 2) * 2;
+                    // two values of 16 tokens; past the ends of the new tokens the nearest one's
+                    const T* col = reinterpret_cast<const T*>(x) + (t0 - p.first) * D + d;
+                    const int lo = max(p.first - t0, 0), hi = min(past - t0, 16);
+                    uint32_t out[2][4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float y[2][4];
+#pragma unroll
+                        for (int f = 0; f < 4; ++f) {
+                            const int t = min(max(4 * e + f, lo), hi - 1);
+                            const uint32_t* at = reinterpret_cast<const uint32_t*>(col + t * D);
+                            float pair[2];
+                            scaled<T>(at[0], inverse, odd, pair);
+                            if (sizeof(T) == 4) scaled<T>(at[1], inverse, odd, pair + 1);
+                            y[0][f] = pair[0], y[1][f] = pair[1];
+                        }
+                        out[0][e] = f32_to_e4m3(y[0]), out[1][e] = f32_to_e4m3(y[1]);
+                    }
+                    uint8_t* at = p.bytes + value_byte<D>(t0, d);
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        if (lo == 0 && hi == 16) {
+                            *reinterpret_cast<uint4*>(at + 16 * r) = make_uint4(out[r][0], out[r][1], out[r][2], out[r][3]);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 16; ++e)
+                                if (e >= lo && e < hi) at[16 * r + e] = (uint8_t)(out[r][e / 4] >> (8 * (e % 4)));
+                        }
+                    }
+                }
+            }
+            __syncthreads();  // the stage's next values may come
+            if (stages == 1 && u + 1 < units) fetch(u + 1);
+        }
+        if (!ok) status[b] = MP_EINVAL;
     }
 }
 
@@ -278,9 +455,15 @@ cudaError_t write_as(const mp_kv_cache& c, const mp_kv_batch& bt, const mp_token
     cudaError_t e = cudaMemsetAsync(status, 0, sizeof(int32_t) * (size_t)bt.n_seqs, stream);
     if (e != cudaSuccess) return e;
     const int per_seq = (int)(((int64_t)bt.max_tokens + 2 * c.block_tokens - 2) / c.block_tokens);
-    const int64_t units = (int64_t)bt.n_seqs * per_seq * c.n_heads * 2;
-    k_kv_write_many<T, D>
-        <<<(unsigned)std::min<int64_t>(units, 1 << 20), kWriteThreads, 0, stream>>>(c, bt, k, v, wide, status, per_seq);
+    // as many heads a CTA as leave CTAs enough to fill the GPU several times over
+    int heads = c.n_heads;
+    while (heads > 1 && (int64_t)bt.n_seqs * per_seq * ((c.n_heads + heads - 1) / heads) < kWriteCtas) heads = (heads + 1) / 2;
+    const int64_t work = (int64_t)bt.n_seqs * per_seq * ((c.n_heads + heads - 1) / heads);
+    const size_t bytes = stage_bytes(c.block_tokens, D, sizeof(T)), smem = bytes * stages_of(bytes);
+    e = set_smem_limit((const void*)k_kv_write_many<T, D>, smem);
+    if (e != cudaSuccess) return e;
+    k_kv_write_many<T, D><<<(unsigned)std::min<int64_t>(work, 1 << 20), kWriteThreads, smem, stream>>>(c, bt, k, v, wide, status,
+                                                                                                    per_seq, heads);
     return cudaGetLastError();
 }
 
