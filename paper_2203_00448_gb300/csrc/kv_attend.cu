@@ -26,41 +26,18 @@
 namespace mp {
 namespace {
 
-constexpr int kFewWarps = 8;
-constexpr int kFewStages = 3;
+// Warps of a CTA, and granules that the ring of each holds: 192 KB in all (D = 128).
+constexpr int few_warps(int nt) { return nt == 1 ? 12 : 8; }
+constexpr int few_stages(int nt) { return nt == 1 ? 2 : 3; }
+constexpr int kFewRows = 16;  // most rows of a sequence and head
 constexpr int kJoinThreads = 256;
 
-struct FewArgs {
-    mp_kv_cache c;
-    mp_kv_batch bt;
-    mp_tokens q, out;
-    float* lse;
-    int32_t* status;
-    float scale;
-    int32_t causal, window;
-    int32_t group;      // query heads a cache head
-    int32_t rows_skip;  // sequences of more rows than this are another kernel's (0: none are)
-    int32_t warps;      // of the grid
-    int64_t* base;      // [n_seqs + 1] first unit of each sequence, then units a warp
-    float* part;        // [2 * warps][rows * (D + 2)]
-    int32_t* gave_up;   // [warps]
-};
-
-// Granules [lo, hi) that the call's tokens of a sequence see.
-__device__ __forceinline__ void seq_granules(const FewArgs& a, const SeqView& s, int& lo, int& hi) {
-    const int start = s.len - s.n;
-    lo = a.window > 0 ? max(0, start - a.window + 1) / kGranule : 0;
-    hi = s.n > 0 ? (s.len + kGranule - 1) / kGranule : lo;
-}
-__device__ __forceinline__ bool seq_is_few(const FewArgs& a, const SeqView& s) {
-    return a.rows_skip == 0 || (int64_t)s.n * a.group <= a.rows_skip;
-}
 template <int kRows>
-__device__ __forceinline__ int seq_tiles(const FewArgs& a, const SeqView& s) {
+__device__ __forceinline__ int seq_tiles(const AttendArgs& a, const SeqView& s) {
     return (int)(((int64_t)s.n * a.group + kRows - 1) / kRows);
 }
 template <int kRows>
-__device__ __forceinline__ int64_t seq_units(const FewArgs& a, int b) {
+__device__ __forceinline__ int64_t seq_units(const AttendArgs& a, int b) {
     const SeqView s = load_seq(a.bt, b, false);
     if (s.st != MP_OK || !seq_is_few(a, s)) return 0;
     int lo, hi;
@@ -74,12 +51,12 @@ struct Cursor {
     int slots, slot;     // tiles x heads, tile * heads + head
     __device__ __forceinline__ void seek(int lo_, int hi_, int slots_, int64_t unit) {
         lo = lo_, hi = hi_, slots = slots_;
-        slot = (int)(unit / (hi - lo));
-        g = lo + (int)(unit % (hi - lo));
+        slot = (int)quotient(unit, hi - lo);
+        g = lo + (int)(unit - (int64_t)slot * (hi - lo));
     }
 };
 template <int kRows>
-__device__ __forceinline__ bool enter(const FewArgs& a, Cursor& c, int64_t unit) {
+__device__ __forceinline__ bool enter(const AttendArgs& a, Cursor& c, int64_t unit) {
     const SeqView s = load_seq(a.bt, c.b, false);
     if (s.st != MP_OK || !seq_is_few(a, s)) return false;
     int lo, hi;
@@ -90,14 +67,14 @@ __device__ __forceinline__ bool enter(const FewArgs& a, Cursor& c, int64_t unit)
     return true;
 }
 template <int kRows>
-__device__ __forceinline__ void next(const FewArgs& a, Cursor& c) {
+__device__ __forceinline__ void next(const AttendArgs& a, Cursor& c) {
     if (++c.g < c.hi) return;
     c.g = c.lo;
     if (++c.slot < c.slots) return;
     do ++c.b;
     while (c.b < a.bt.n_seqs && !enter<kRows>(a, c, 0));
 }
-__device__ __forceinline__ int page_of(const FewArgs& a, const Cursor& c) {
+__device__ __forceinline__ int page_of(const AttendArgs& a, const Cursor& c) {
     const int p = __ldg(a.bt.table + (int64_t)c.b * a.bt.max_blocks + c.g / (a.c.block_tokens / kGranule));
     return p >= 0 && p < a.c.n_blocks ? p : 0;  // k_kv_join reports it; nothing outside the pool is read
 }
@@ -116,7 +93,8 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
 }
 
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(kFewWarps * 32, 1) k_kv_attend_few(FewArgs a) {
+__global__ void __launch_bounds__(few_warps(NT) * 32, 1) k_kv_attend_few(AttendArgs a, FewWork work) {
+    constexpr int kFewWarps = few_warps(NT), kFewStages = few_stages(NT);
     constexpr int kRows = 8 * NT;
     constexpr int kBytes = kGranule * D;  // of either array
     extern __shared__ __align__(128) uint8_t dyn[];
@@ -127,6 +105,8 @@ __global__ void __launch_bounds__(kFewWarps * 32, 1) k_kv_attend_few(FewArgs a) 
     const int tid = threadIdx.x, lane = tid % 32, wid = tid / 32;
     const int g = lane / 4, t = lane % 4;
 
+    after_previous();
+    let_next_begin();
     // every CTA lays the line out for itself: thread i sums a strip of sequences
     const int strip = (a.bt.n_seqs + kFewWarps * 32 - 1) / (kFewWarps * 32);
     {
@@ -148,26 +128,27 @@ __global__ void __launch_bounds__(kFewWarps * 32, 1) k_kv_attend_few(FewArgs a) 
         for (int w = 0; w < wid; ++w) sum += warp_sum[w];
         strip_base[tid] = sum - mine;
         if (tid == kFewWarps * 32 - 1) strip_base[kFewWarps * 32] = sum;
-        if (blockIdx.x == 0) {
+        __syncthreads();
+        if (blockIdx.x == gridDim.x - 1) {  // the one with the shortest part
             int64_t at = sum - mine;
             for (int i = 0; i < strip; ++i) {
                 const int b = tid * strip + i;
                 if (b < a.bt.n_seqs) {
-                    a.base[b] = at;
-                    at += seq_units<kRows>(a, b);
-                    if (b == a.bt.n_seqs - 1) a.base[b + 1] = at;
+                    work.base[b] = at;
+                    at += strip == 1 ? mine : seq_units<kRows>(a, b);
+                    if (b == a.bt.n_seqs - 1) work.base[b + 1] = at;
                 }
             }
         }
-        __syncthreads();
     }
+    const int warps = gridDim.x * kFewWarps;
     const int64_t total = strip_base[kFewWarps * 32];
-    const int64_t per_warp = (total + a.warps - 1) / a.warps;
+    const int64_t per_warp = quotient(total + warps - 1, warps);
     // consecutive warps of the line are on different SMs: short lines reach them all
     const int w = wid * gridDim.x + blockIdx.x;
-    if (w == 0 && lane == 0) a.base[a.bt.n_seqs + 1] = per_warp;
+    if (w == 0 && lane == 0) work.base[a.bt.n_seqs + 1] = per_warp;
     const int64_t u0 = min(total, w * per_warp), u1 = min(total, u0 + per_warp);
-    if (lane == 0) a.gave_up[w] = 0;
+    if (lane == 0) work.gave_up[w] = 0;
     if (u0 >= u1) return;
 
     Cursor cur;
@@ -181,10 +162,10 @@ __global__ void __launch_bounds__(kFewWarps * 32, 1) k_kv_attend_few(FewArgs a) 
         }
         int64_t at = strip_base[lo];
         cur.b = lo * strip;
-        for (;; ++cur.b) {
+        while (strip > 1) {
             const int64_t n = seq_units<kRows>(a, cur.b);
             if (u0 < at + n) break;
-            at += n;
+            at += n, ++cur.b;
         }
         enter<kRows>(a, cur, u0 - at);
     }
@@ -416,7 +397,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, 1) k_kv_attend_few(FewArgs a) 
                         // a warp leaves at most two parts: of what began before it or with it, and of
                         // what it begins and does not end
                         const bool first = held <= cur.g - cur.lo + 1;
-                        float* part = a.part + ((int64_t)2 * w + (first ? 0 : 1)) * (kRows * (D + 2));
+                        float* part = work.part + ((int64_t)2 * w + (first ? 0 : 1)) * (kRows * (D + 2));
                         float* dst = part + in_tile * D;
 #pragma unroll
                         for (int i = 0; i < D / 16; ++i) {
@@ -434,107 +415,189 @@ __global__ void __launch_bounds__(kFewWarps * 32, 1) k_kv_attend_few(FewArgs a) 
         next<kRows>(a, cur);
     }
     if (up) {
-        if (lane == 0) a.gave_up[w] = 1;
+        if (lane == 0) work.gave_up[w] = 1;
         // leave no copy in flight behind
         for (int64_t u = max(u0, issued - kFewStages); u < issued; ++u)
             mbar_wait(&bar[(u - u0) % kFewStages], (uint32_t)((u - u0) / kFewStages & 1));
     }
 }
 
-// Most rows of a sequence that the kernel for few rows has.
-__host__ __device__ __forceinline__ int64_t join_rows(const FewArgs& a) {
+// Rows of a sequence and head that k_kv_attend_few may have.
+__host__ __device__ __forceinline__ int join_rows(const AttendArgs& a) {
     const int64_t rows = (int64_t)a.bt.max_tokens * a.group;
-    return rows < 1 ? 1 : a.rows_skip > 0 && rows > a.rows_skip ? a.rows_skip : rows;
+    return (int)(rows < 1 ? 1 : rows > a.few_rows ? a.few_rows : rows);
 }
 
-// One CTA a query row: adds the parts of rows that several warps had, writes rows that
-// see nothing, and the sequences' status.
-template <typename T, int D, int NT>
-__global__ void __launch_bounds__(kJoinThreads) k_kv_join(FewArgs a) {
-    constexpr int kRows = 8 * NT, kWarps = kJoinThreads / 32, kPer = D / 32;
-    __shared__ float acc[kWarps][D];
-    __shared__ float weight[kWarps][2];
-    const int lane = threadIdx.x % 32, wid = threadIdx.x / 32;
-    const int64_t per_warp = a.base[a.bt.n_seqs + 1];
-    const int64_t rows_max = join_rows(a), work = a.bt.n_seqs * rows_max * a.c.n_heads;
-    for (int64_t u = blockIdx.x; u < work; u += gridDim.x) {
-        const int head = (int)(u % a.c.n_heads);
-        const int64_t r = u / a.c.n_heads % rows_max;
-        const int b = (int)(u / a.c.n_heads / rows_max);
-        const SeqView s = load_seq(a.bt, b, false);
-        if (!seq_is_few(a, s)) continue;
-        int lo, hi;
-        seq_granules(a, s, lo, hi);
-        const int cnt = hi - lo, rows = s.n * a.group;
-        const int64_t from = a.base[b], past = a.base[b + 1];
-        if (head == 0 && r == 0) {
-            bool ok = s.st == MP_OK, late = false;
-            if (cnt > 0) {
-                const int per = a.c.block_tokens / kGranule;
-                for (int col = lo / per + threadIdx.x; col <= (hi - 1) / per; col += kJoinThreads) {
-                    const int p = __ldg(a.bt.table + (int64_t)b * a.bt.max_blocks + col);
-                    ok &= p >= 0 && p < a.c.n_blocks;
-                }
-            }
-            if (past > from)
-                for (int64_t w = from / per_warp + threadIdx.x; w <= (past - 1) / per_warp; w += kJoinThreads)
-                    late |= a.gave_up[w] != 0;
-            ok = !__syncthreads_or(!ok);
-            late = __syncthreads_or(late);
-            if (threadIdx.x == 0) a.status[b] = !ok ? MP_EINVAL : late ? MP_ETIMEOUT : MP_OK;
+constexpr int kJoinCols = 16;  // of D, a CTA's share of a pair of tiles
+struct JoinPlan {
+    int cuts, checks, row_ctas;  // CTAs: of k_kv_attend_many's cuts, of the sequences' status, of k_kv_attend_few's rows
+};
+
+// Adds up the 16 columns y of the (sequence, pair, head) in which CTA w of k_kv_attend_many began, if w is the first to
+// begin inside it: a thread a row.
+template <typename T, int D>
+__device__ void join_cut(const AttendArgs& a, const ManyWork& work, int w, int y) {
+    const ManyStart st = work.starts[w];
+    if (!st.there || st.into <= kExtra) return;  // (it began with the pair's first unit)
+    const int64_t us = w * st.per - st.into;     // the pair and head on the line
+    const int begun = (int)quotient(us + kExtra, st.per), last = (int)quotient(us + kExtra + st.cnt - 1, st.per);
+    if (w != begun + 1) return;  // another CTA cut it before
+    const SeqView s = load_seq(a.bt, st.b, false);
+    const int in_pair = threadIdx.x, r = st.tile * kPair + in_pair;
+    if (r >= s.n * a.group) return;
+    float top = -INFINITY, sum = 0.f, o[kJoinCols] = {};
+#pragma unroll 1
+    for (int v = begun; v <= last; ++v) {
+        const float* part = work.part + ((int64_t)2 * v + (v * st.per >= us ? 0 : 1)) * (kPair * (D + 2)) + in_pair;
+        float x[kJoinCols];
+        const float m = part[D * kPair], l = part[(D + 1) * kPair];
+#pragma unroll
+        for (int j = 0; j < kJoinCols; ++j) x[j] = part[(y * kJoinCols + j) * kPair];
+        const float now = fmaxf(top, m), ref = now == -INFINITY ? 0.f : now;
+        const float f = exp2_approx(top - ref), g = exp2_approx(m - ref);
+        sum = sum * f + l * g;
+#pragma unroll
+        for (int j = 0; j < kJoinCols; ++j) o[j] = o[j] * f + x[j] * g;
+        top = now;
+    }
+    const int64_t tok = s.lo + r / a.group;
+    const int qh = st.head * a.group + r % a.group;
+    const float inv = sum == 0.f ? 0.f : __fdiv_rn(1.f, sum);
+    T* dst = static_cast<T*>(a.out.data) + tok * a.out.token_stride + qh * a.out.head_stride + y * kJoinCols;
+#pragma unroll
+    for (int j = 0; j < kJoinCols; ++j) o[j] *= inv;
+    store_values<T, 8>(dst, a.wide_out, o);
+    store_values<T, 8>(dst + 8, a.wide_out, o + 8);
+    if (y == 0 && a.lse != nullptr)
+        a.lse[tok * a.q.n_heads + qh] =
+            top == -INFINITY ? -INFINITY : (top - kManyLift + log2f(sum)) * 0.6931471805599453f;
+}
+
+// A sequence's status, and its rows that see nothing (no kernel has units of theirs).
+template <typename T, int D>
+__device__ void check_seq(const AttendArgs& a, const FewWork& few, bool late, int b) {
+    const SeqView s = load_seq(a.bt, b, false);
+    int lo, hi;
+    seq_granules(a, s, lo, hi);
+    bool ok = s.st == MP_OK;
+    if (ok && hi > lo) {
+        const int per = a.c.block_tokens / kGranule;
+        for (int col = lo / per + threadIdx.x; col <= (hi - 1) / per; col += kJoinThreads) {
+            const int p = __ldg(a.bt.table + (int64_t)b * a.bt.max_blocks + col);
+            ok &= p >= 0 && p < a.c.n_blocks;
         }
-        if (r >= rows || s.st != MP_OK) continue;
-        const int64_t tok = s.lo + r / a.group;
-        const int qh = head * a.group + (int)(r % a.group);
-        T* dst = static_cast<T*>(a.out.data) + tok * a.out.token_stride + qh * a.out.head_stride;
-        if (cnt <= 0) {
-            for (int d = threadIdx.x; d < D; d += kJoinThreads) dst[d] = from_f32<T>(0.f);
-            if (a.lse != nullptr && threadIdx.x == 0) a.lse[tok * a.q.n_heads + qh] = -INFINITY;
-            continue;
-        }
-        const int tile = (int)(r / kRows), in_tile = (int)(r % kRows);
-        const int64_t us = from + ((int64_t)tile * a.c.n_heads + head) * cnt;
-        const int64_t w0 = us / per_warp, w1 = (us + cnt - 1) / per_warp;
-        if (w0 == w1) continue;  // one warp had it all
-        float top = -INFINITY, l = 0.f, o[kPer] = {};
-        for (int64_t w = w0 + wid; w <= w1; w += kWarps) {
-            const float* part = a.part + (2 * w + (w * per_warp >= us ? 0 : 1)) * (kRows * (D + 2));
-            const float m = part[kRows * D + 2 * in_tile], lw = part[kRows * D + 2 * in_tile + 1];
-            float x[kPer];
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) x[i] = part[in_tile * D + i * 32 + lane];
-            const float now = fmaxf(top, m), ref = now == -INFINITY ? 0.f : now;
-            const float f = exp2_approx(top - ref), fw = exp2_approx(m - ref);
-            l = l * f + lw * fw;
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) o[i] = o[i] * f + x[i] * fw;
-            top = now;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) acc[wid][i * 32 + lane] = o[i];
-        if (lane == 0) weight[wid][0] = top, weight[wid][1] = l;
-        __syncthreads();
-        float all = -INFINITY, sum = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) all = fmaxf(all, weight[w][0]);
-        const float ref = all == -INFINITY ? 0.f : all;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) sum += weight[w][1] * exp2_approx(weight[w][0] - ref);
-        const float inv = sum == 0.f ? 0.f : __fdiv_rn(1.f, sum);
-        for (int d = threadIdx.x; d < D; d += kJoinThreads) {
-            float x = 0.f;
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) x += acc[w][d] * exp2_approx(weight[w][0] - ref);
-            dst[d] = from_f32<T>(x * inv);
-        }
-        if (a.lse != nullptr && threadIdx.x == 0)
-            a.lse[tok * a.q.n_heads + qh] = all == -INFINITY ? -INFINITY : (all - kLift + log2f(sum)) * 0.6931471805599453f;
+    }
+    if (ok && few.base != nullptr && seq_is_few(a, s)) {
+        const int64_t from = few.base[b], past = few.base[b + 1], per = few.base[a.bt.n_seqs + 1];
+        if (past > from)
+            for (int64_t w = quotient(from, per) + threadIdx.x; w <= quotient(past - 1, per); w += kJoinThreads)
+                late |= few.gave_up[w] != 0;
+    }
+    ok = !__syncthreads_or(!ok);
+    late = __syncthreads_or(late);
+    if (threadIdx.x == 0) a.status[b] = !ok ? MP_EINVAL : late ? MP_ETIMEOUT : MP_OK;
+    // queries before the first position, or of an empty sequence
+    const int blind = s.st != MP_OK ? 0 : s.len == 0 ? s.n : a.causal ? min(s.n, max(s.n - s.len, 0)) : 0;
+    for (int64_t i = threadIdx.x; i < (int64_t)blind * a.q.n_heads * (D / 2); i += kJoinThreads) {
+        const int64_t tok = s.lo + i / (D / 2) / a.q.n_heads;
+        const int qh = (int)(i / (D / 2) % a.q.n_heads), d = (int)(i % (D / 2)) * 2;
+        T* dst = static_cast<T*>(a.out.data) + tok * a.out.token_stride + qh * a.out.head_stride + d;
+        dst[0] = dst[1] = from_f32<T>(0.f);
+        if (d == 0 && a.lse != nullptr) a.lse[tok * a.q.n_heads + qh] = -INFINITY;
     }
 }
 
-constexpr int kFewCtas = 152;  // one an SM: its rings take most of the shared memory
-constexpr int kFewRows = 16;   // most rows of a sequence and head
+// kPer warps a query row add up what several warps of k_kv_attend_few had of it.
+template <typename T, int D, int NT, int kPer>
+__device__ void join_row(const AttendArgs& a, const FewWork& work, int64_t u, bool there) {
+    constexpr int kRows = 8 * NT, kCols = D / 32, kAhead = 4;
+    __shared__ float acc[kJoinThreads / 32][D + 2];
+    const int lane = threadIdx.x % 32, wid = threadIdx.x / 32;
+    const int head = (int)(u % a.c.n_heads), rows_max = join_rows(a);
+    const int r = (int)(u / a.c.n_heads % rows_max), b = (int)(u / a.c.n_heads / rows_max);
+    SeqView s = {};
+    int lo = 0, hi = 0;
+    int64_t from = 0, per = 1;
+    if (there) {
+        s = load_seq(a.bt, b, false);
+        from = work.base[b], per = work.base[a.bt.n_seqs + 1];
+        seq_granules(a, s, lo, hi);
+        there = s.st == MP_OK && seq_is_few(a, s) && r < s.n * a.group && hi > lo;
+    }
+    const int tile = r / kRows, in_tile = r % kRows, cnt = hi - lo;
+    const int64_t us = from + ((int64_t)tile * a.c.n_heads + head) * cnt;
+    const int64_t w0 = there ? quotient(us, per) : 0, w1 = there ? quotient(us + cnt - 1, per) : 0;
+    there = there && w0 != w1;  // else one warp had it all
+    float top = -INFINITY, l = 0.f, o[kCols] = {};
+    if (there) {
+        auto part_of = [&](int64_t w) { return work.part + (2 * w + (w * per >= us ? 0 : 1)) * (kRows * (D + 2)); };
+        // the largest reference first, so that the sums do not depend on one another
+        for (int64_t w = w0 + lane; w <= w1; w += 32) top = fmaxf(top, part_of(w)[kRows * D + 2 * in_tile]);
+#pragma unroll
+        for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, k));
+        const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll kAhead
+        for (int64_t w = w0 + wid % kPer; w <= w1; w += kPer) {
+            const float* part = part_of(w);
+            const float f = exp2_approx(part[kRows * D + 2 * in_tile] - ref);
+            l += part[kRows * D + 2 * in_tile + 1] * f;
+            const Pack<float, kCols> x = *reinterpret_cast<const Pack<float, kCols>*>(part + in_tile * D + lane * kCols);
+#pragma unroll
+            for (int i = 0; i < kCols; ++i) o[i] += x.x[i] * f;
+        }
+    }
+    if (kPer > 1) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kCols; ++i) acc[wid][lane * kCols + i] = o[i];
+        if (lane == 0) acc[wid][D] = l;
+        __syncthreads();
+        if (wid > 0 || !there) return;
+        l = 0.f;
+#pragma unroll
+        for (int i = 0; i < kCols; ++i) o[i] = 0.f;
+#pragma unroll
+        for (int v = 0; v < kPer; ++v) {
+            l += acc[v][D];
+#pragma unroll
+            for (int i = 0; i < kCols; ++i) o[i] += acc[v][lane * kCols + i];
+        }
+    }
+    if (!there) return;
+    const int64_t tok = s.lo + r / a.group;
+    const int qh = head * a.group + r % a.group;
+    T* dst = static_cast<T*>(a.out.data) + tok * a.out.token_stride + qh * a.out.head_stride;
+    const float inv = l == 0.f ? 0.f : __fdiv_rn(1.f, l);
+#pragma unroll
+    for (int i = 0; i < kCols; ++i) o[i] *= inv;
+    store_values<T, kCols>(dst + lane * kCols, a.wide_out, o);
+    if (a.lse != nullptr && lane == 0)
+        a.lse[tok * a.q.n_heads + qh] = top == -INFINITY ? -INFINITY : (top - kLift + log2f(l)) * 0.6931471805599453f;
+}
+
+// After both kernels: what more than one CTA or warp had of a row, and the sequences' status.  kPer: warps a row.
+template <typename T, int D, int NT, int kPer>
+__global__ void __launch_bounds__(kJoinThreads) k_kv_join(AttendArgs a, FewWork few, ManyWork many, JoinPlan plan) {
+    after_previous();
+    let_next_begin();
+    int cta = blockIdx.x;
+    if (cta < plan.cuts) return join_cut<T, D>(a, many, cta / (D / kJoinCols), cta % (D / kJoinCols));
+    cta -= plan.cuts;
+    if (cta < plan.checks) {
+        bool late = false;
+        if (many.part != nullptr)
+            for (int i = threadIdx.x; i < kManyCtas; i += kJoinThreads) late |= many.gave_up[i] != 0;
+        for (int b = cta; b < a.bt.n_seqs; b += plan.checks) check_seq<T, D>(a, few, late, b);
+        return;
+    }
+    cta -= plan.checks;
+    constexpr int kRowsCta = kJoinThreads / 32 / kPer;
+    const int64_t rows = (int64_t)a.bt.n_seqs * join_rows(a) * a.c.n_heads;
+    for (int64_t u = (int64_t)cta * kRowsCta; u < rows; u += (int64_t)plan.row_ctas * kRowsCta) {
+        const int64_t mine = u + threadIdx.x / 32 / kPer;
+        join_row<T, D, NT, kPer>(a, few, mine < rows ? mine : 0, mine < rows);
+    }
+}
 
 // Which kernels a batch needs, by its host scalars: sequences of at most kFewRows rows are
 // bound by the cache's bytes, which k_kv_attend_few streams; above it the products count.
@@ -553,7 +616,7 @@ struct Layout {
 Layout layout(const mp_kv_cache& c, const mp_kv_batch& bt, int32_t group) {
     Layout l = {};
     const Route r = route(bt, group);
-    const size_t warps = (size_t)kFewCtas * kFewWarps;
+    const size_t warps = (size_t)kFewCtas * few_warps(1);
     auto take = [&](size_t bytes) {
         const size_t at = l.bytes;
         l.bytes += align_up(bytes);
@@ -562,7 +625,7 @@ Layout layout(const mp_kv_cache& c, const mp_kv_batch& bt, int32_t group) {
     if (r.few) {
         l.base = take(sizeof(int64_t) * ((size_t)bt.n_seqs + 2));
         l.gave_up = take(sizeof(int32_t) * warps);
-        l.part = take(sizeof(float) * 2 * warps * kFewRows * (size_t)(c.head_dim + 2));
+        l.part = take(sizeof(float) * 2 * kFewCtas * std::max(8 * few_warps(1), 16 * few_warps(2)) * (size_t)(c.head_dim + 2));
     }
     if (r.many) {
         l.starts = take(sizeof(ManyStart) * kManyCtas);
@@ -573,20 +636,39 @@ Layout layout(const mp_kv_cache& c, const mp_kv_batch& bt, int32_t group) {
 }
 
 template <typename T, int D, int NT>
-cudaError_t few_as(const FewArgs& a, cudaStream_t stream) {
-    constexpr size_t smem = (size_t)kFewWarps * kFewStages * 2 * kGranule * D;
-    cudaError_t e = set_smem_limit((const void*)k_kv_attend_few<T, D, NT>, smem);
-    if (e != cudaSuccess) return e;
-    k_kv_attend_few<T, D, NT><<<kFewCtas, kFewWarps * 32, smem, stream>>>(a);
-    e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
-    const int64_t work = a.bt.n_seqs * join_rows(a) * a.c.n_heads;
-    k_kv_join<T, D, NT><<<(unsigned)std::min<int64_t>(work, 1 << 20), kJoinThreads, 0, stream>>>(a);
-    return cudaGetLastError();
+cudaError_t attend_as(const AttendArgs& a, const FewWork& few, const ManyWork& many, cudaStream_t stream) {
+    cudaError_t e;
+    JoinPlan plan = {};
+    plan.checks = std::min(a.bt.n_seqs, 1024);
+    int64_t rows = 0;
+    if (few.base != nullptr) {
+        constexpr size_t smem = (size_t)few_warps(NT) * few_stages(NT) * 2 * kGranule * D;
+        e = set_smem_limit((const void*)k_kv_attend_few<T, D, NT>, smem);
+        if (e == cudaSuccess)
+            e = launch_close(k_kv_attend_few<T, D, NT>, kFewCtas, few_warps(NT) * 32, smem, stream, a, few);
+        if (e != cudaSuccess) return e;
+        rows = (int64_t)a.bt.n_seqs * join_rows(a) * a.c.n_heads;
+    }
+    if (many.part != nullptr) {
+        e = launch_kv_many(a, many, stream);
+        if (e != cudaSuccess) return e;
+        plan.cuts = kManyCtas * (D / kJoinCols);
+    }
+    // few rows in all are cut into many parts each, which a CTA's warps share (64 rows of 76 parts: 18 -> 5 us); many rows
+    // into two or three, a warp a row (2,048 rows: 12 -> 7 us)
+    constexpr int kWarps = kJoinThreads / 32;
+    if (rows <= 4 * kFewCtas) {
+        plan.row_ctas = (int)rows;
+        return launch_close(k_kv_join<T, D, NT, kWarps>, plan.cuts + plan.checks + plan.row_ctas, kJoinThreads, 0, stream, a,
+                            few, many, plan);
+    }
+    plan.row_ctas = (int)std::min<int64_t>((rows + kWarps - 1) / kWarps, 1 << 20);
+    return launch_close(k_kv_join<T, D, NT, 1>, plan.cuts + plan.checks + plan.row_ctas, kJoinThreads, 0, stream, a, few, many,
+                        plan);
 }
 template <typename T, int D>
-cudaError_t few_rows(const FewArgs& a, cudaStream_t stream) {
-    return join_rows(a) <= 8 ? few_as<T, D, 1>(a, stream) : few_as<T, D, 2>(a, stream);
+cudaError_t attend_rows(const AttendArgs& a, const FewWork& few, const ManyWork& many, cudaStream_t stream) {
+    return join_rows(a) <= 8 ? attend_as<T, D, 1>(a, few, many, stream) : attend_as<T, D, 2>(a, few, many, stream);
 }
 
 }  // namespace
@@ -603,34 +685,29 @@ cudaError_t launch_kv_attend(const mp_kv_cache& c, const mp_kv_batch& bt, const 
     const Layout l = layout(c, bt, group);
     const Route r = route(bt, group);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    if (window >= bt.max_len) window = 0;  // reaches back to every start
-    if (r.few) {
-        FewArgs a;
-        a.c = c, a.bt = bt, a.q = q, a.out = out, a.lse = lse, a.status = status;
-        a.scale = scale, a.causal = causal, a.window = window, a.group = group;
-        a.rows_skip = r.many ? kFewRows : 0;
-        a.warps = kFewCtas * kFewWarps;
-        a.base = reinterpret_cast<int64_t*>(ws + l.base);
-        a.gave_up = reinterpret_cast<int32_t*>(ws + l.gave_up);
-        a.part = reinterpret_cast<float*>(ws + l.part);
-        cudaError_t e;
-        if (q.dtype == MP_F16)
-            e = c.head_dim == 64 ? few_rows<__half, 64>(a, stream) : few_rows<__half, 128>(a, stream);
-        else
-            e = c.head_dim == 64 ? few_rows<__nv_bfloat16, 64>(a, stream) : few_rows<__nv_bfloat16, 128>(a, stream);
-        if (e != cudaSuccess) return e;
-    }
-    if (!r.many) return cudaSuccess;
-    ManyArgs a;
+    AttendArgs a;
     a.c = c, a.bt = bt, a.q = q, a.out = out, a.lse = lse, a.status = status;
-    a.scale = scale, a.causal = causal, a.window = window, a.group = group;
-    a.few_rows = r.few ? kFewRows : 0;
-    a.ctas = kManyCtas;
+    a.scale = scale, a.causal = causal, a.window = window >= bt.max_len ? 0 : window;  // (reaches back to every start)
+    a.group = group;
+    a.few_rows = r.few ? kFewRows : -1;
     a.wide_q = rows_aligned(q), a.wide_out = rows_aligned(out);
-    a.part = reinterpret_cast<float*>(ws + l.many_part);
-    a.starts = reinterpret_cast<ManyStart*>(ws + l.starts);
-    a.gave_up = reinterpret_cast<int32_t*>(ws + l.many_gave_up);
-    return launch_kv_many(a, stream);
+    FewWork few = {};
+    ManyWork many = {};
+    if (r.few) {
+        few.base = reinterpret_cast<int64_t*>(ws + l.base);
+        few.gave_up = reinterpret_cast<int32_t*>(ws + l.gave_up);
+        few.part = reinterpret_cast<float*>(ws + l.part);
+    }
+    if (r.many) {
+        many.starts = reinterpret_cast<ManyStart*>(ws + l.starts);
+        many.gave_up = reinterpret_cast<int32_t*>(ws + l.many_gave_up);
+        many.part = reinterpret_cast<float*>(ws + l.many_part);
+    }
+    if (q.dtype == MP_F16)
+        return c.head_dim == 64 ? attend_rows<__half, 64>(a, few, many, stream)
+                                : attend_rows<__half, 128>(a, few, many, stream);
+    return c.head_dim == 64 ? attend_rows<__nv_bfloat16, 64>(a, few, many, stream)
+                            : attend_rows<__nv_bfloat16, 128>(a, few, many, stream);
 }
 
 }  // namespace mp

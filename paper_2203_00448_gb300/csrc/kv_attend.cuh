@@ -78,14 +78,8 @@ __device__ __forceinline__ float row_factor(float most) {
 // its logarithm.
 __device__ __forceinline__ float value_scale(float s) { return fmaxf(s, 0x1p-100f); }
 
-// kv_attend_many.cu: where on the line of units a CTA began.
-struct ManyStart {
-    int32_t b, tile, head, cnt, into;  // cnt: units of that (sequence, pair of tiles, head)
-    int32_t there;
-    int64_t per;  // length of a CTA's part
-};
-constexpr int kManyCtas = 152;  // one an SM
-struct ManyArgs {
+// What both kernels and the joining need of a call.
+struct AttendArgs {
     mp_kv_cache c;
     mp_kv_batch bt;
     mp_tokens q, out;
@@ -93,15 +87,68 @@ struct ManyArgs {
     int32_t* status;
     float scale;
     int32_t causal, window;
-    int32_t group;
-    int32_t few_rows;  // sequences of at most this many rows are k_kv_attend_few's (0: none)
-    int32_t ctas;
+    int32_t group;     // query heads a cache head
+    int32_t few_rows;  // sequences of at most this many rows (tokens x group) are k_kv_attend_few's, the others k_kv_attend_many's
     bool wide_q, wide_out;
+};
+__device__ __forceinline__ bool seq_is_few(const AttendArgs& a, const SeqView& s) {
+    return (int64_t)s.n * a.group <= a.few_rows;
+}
+// Granules [lo, hi) that the call's tokens of a sequence see.
+__device__ __forceinline__ void seq_granules(const AttendArgs& a, const SeqView& s, int& lo, int& hi) {
+    const int start = s.len - s.n;
+    lo = a.window > 0 ? max(0, start - a.window + 1) / kGranule : 0;
+    hi = s.n > 0 ? (s.len + kGranule - 1) / kGranule : lo;
+}
+
+// k_kv_attend_few: warps share the line of units; what is left to add up.
+constexpr int kFewCtas = 152;  // one an SM: its rings take most of the shared memory
+struct FewWork {
+    int64_t* base;     // [n_seqs + 1] first unit of each sequence, then units a warp
+    float* part;       // [2 * warps][rows * (D + 2)]
+    int32_t* gave_up;  // [warps]
+};
+
+// k_kv_attend_many: pairs of tiles of 128 rows, units of 128 tokens; where on the line a CTA began.
+constexpr int kManyCtas = 152;
+constexpr int kPair = 256;
+constexpr int kExtra = 3;           // units that a stretch costs beside its own: queries in, sums out
+constexpr float kManyLift = 7.f;    // weights are at most 2^(8 + 7)
+struct ManyStart {
+    int32_t b, tile, head, cnt, into;  // cnt: units of that (sequence, pair of tiles, head)
+    int32_t there;
+    int64_t per;  // length of a CTA's part
+};
+struct ManyWork {
     float* part;  // [2 * ctas][(D + 2) * 256]
     ManyStart* starts;
-    int32_t* gave_up;
+    int32_t* gave_up;  // [ctas]
 };
+
+// x / y for both below 2^63, mostly below 2^32: a 64-bit division takes a hundred instructions.
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
+    return ((x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
+}
+
+// A kernel's launch may begin while the one before it in the stream ends; it touches memory after this.
+__device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_begin() { asm volatile("griddepcontrol.launch_dependents;"); }
+template <typename... K, typename... A>
+inline cudaError_t launch_close(void (*kernel)(K...), int grid, int threads, size_t smem, cudaStream_t stream, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 size_t kv_many_part_bytes(const mp_kv_cache& c);
-cudaError_t launch_kv_many(const ManyArgs& a, cudaStream_t stream);
+cudaError_t launch_kv_many(const AttendArgs& a, const ManyWork& w, cudaStream_t stream);
 
 }  // namespace mp

@@ -16,7 +16,7 @@
 // (sequence, row tile pair, head, 128 tokens) units lie on a line that is cut evenly
 // among 152 CTAs, so that causal rows, ragged prompts and a short piece over a long
 // context all end together; what a CTA does not hold whole is added up by
-// k_kv_join_many.
+// k_kv_join.
 #include <algorithm>
 #include <cmath>
 
@@ -26,11 +26,10 @@ namespace mp {
 namespace {
 
 constexpr int kRows = 128;      // of one tile
-constexpr int kPair = 2 * kRows;
+static_assert(kPair == 2 * kRows, "a pair of tiles");
 constexpr int kTokens = 128;    // of a unit
 constexpr int kGrans = kTokens / kGranule;
 constexpr int kStages = 2;      // of keys and of values
-constexpr int kExtra = 3;  // units that a stretch costs beside its own: queries in, sums out
 constexpr int kScaleRing = 4;
 constexpr int kLineRing = 4;
 constexpr int kSoftmaxWarps = 8;
@@ -40,7 +39,6 @@ constexpr int kThreads = 16 * 32;
 constexpr int kSoftmaxRegs = 176, kConvertRegs = 112, kProductRegs = 48;
 constexpr int kTries = (int)(kKvSpinCycles >> 10);
 constexpr int kStrips = 1024;
-constexpr float kManyLift = 7.f;  // weights are at most 2^(8 + 7)
 constexpr float kGrow = 8.f;
 
 __device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lead, uint32_t stride) {
@@ -131,11 +129,11 @@ struct Stretch {
     int64_t row;             // its first row of the token arrays
 };
 
-__device__ __forceinline__ int pairs_of(const ManyArgs& a, const SeqView& s) {
-    if (s.st != MP_OK || (a.few_rows > 0 && (int64_t)s.n * a.group <= a.few_rows)) return 0;
+__device__ __forceinline__ int pairs_of(const AttendArgs& a, const SeqView& s) {
+    if (s.st != MP_OK || seq_is_few(a, s)) return 0;
     return (s.n * a.group + kPair - 1) / kPair;
 }
-__device__ __forceinline__ void pair_grans(const ManyArgs& a, const SeqView& s, int tile, int& lo, int& n) {
+__device__ __forceinline__ void pair_grans(const AttendArgs& a, const SeqView& s, int tile, int& lo, int& n) {
     const int start = s.len - s.n, rows = s.n * a.group;
     const int p0 = start + tile * kPair / a.group, p1 = start + (min(rows, (tile + 1) * kPair) - 1) / a.group;
     const int past = a.causal ? min(s.len, max(p1 + 1, 0)) : s.len;
@@ -144,13 +142,13 @@ __device__ __forceinline__ void pair_grans(const ManyArgs& a, const SeqView& s, 
 }
 __device__ __forceinline__ int units_of(int grans) { return (grans + kGrans - 1) / kGrans; }
 // Length on the line: its units and what beginning and ending a pair costs beside them.
-__device__ __forceinline__ int pair_length(const ManyArgs& a, const SeqView& s, int tile) {
+__device__ __forceinline__ int pair_length(const AttendArgs& a, const SeqView& s, int tile) {
     int lo, n;
     pair_grans(a, s, tile, lo, n);
     return n > 0 ? units_of(n) + kExtra : 0;
 }
 // Length of a sequence; a warp's lanes take its pairs in turn.
-__device__ __forceinline__ int64_t seq_length(const ManyArgs& a, int b, int lane) {
+__device__ __forceinline__ int64_t seq_length(const AttendArgs& a, int b, int lane) {
     const SeqView s = load_seq(a.bt, b, false);
     const int pairs = pairs_of(a, s);
     int64_t n = 0;
@@ -159,7 +157,7 @@ __device__ __forceinline__ int64_t seq_length(const ManyArgs& a, int b, int lane
     for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(~0u, n, o);
     return n * a.c.n_heads;
 }
-__device__ __forceinline__ void fill(const ManyArgs& a, const SeqView& s, Stretch& x) {
+__device__ __forceinline__ void fill(const AttendArgs& a, const SeqView& s, Stretch& x) {
     pair_grans(a, s, x.tile, x.first_gran, x.grans);
     x.cnt = units_of(x.grans);
     x.rows = s.n * a.group;
@@ -167,7 +165,7 @@ __device__ __forceinline__ void fill(const ManyArgs& a, const SeqView& s, Stretc
     x.len = s.len, x.start = s.len - s.n, x.row = s.lo;
 }
 // The next pair or head on the line; false at its end.
-__device__ __forceinline__ bool advance(const ManyArgs& a, Stretch& x) {
+__device__ __forceinline__ bool advance(const AttendArgs& a, Stretch& x) {
     if (++x.head < a.c.n_heads) return true;
     x.head = 0;
     ++x.tile;
@@ -241,7 +239,7 @@ constexpr uint32_t kScoreCol = 0, kSumCol = 256;  // of tile 0; tile 1 has + 128
 
 // One thread walks the CTA's part of the line ahead of the roles.
 template <int D>
-__device__ void line_role(const ManyArgs& a, Smem<D>& m) {
+__device__ void line_role(const AttendArgs& a, Smem<D>& m) {
     Stretch x = m.first;
     int64_t left = m.length;
     int into = m.into;
@@ -272,7 +270,7 @@ __device__ __forceinline__ void release(Smem<D>& m, int seg) {
 }
 
 template <typename T, int D>
-__device__ void convert_role(const ManyArgs& a, Smem<D>& m) {
+__device__ void convert_role(const AttendArgs& a, Smem<D>& m) {
     constexpr int kLoads = kTokens * D / 16 / 128;     // 16-byte loads a thread, of either array
     constexpr int kPerGran = kGranule * D / 16 / 128;  // ... of which a granule is this many, 1 or 2
     const int tid = threadIdx.x - kSoftmaxWarps * 32;
@@ -293,7 +291,7 @@ __device__ void convert_role(const ManyArgs& a, Smem<D>& m) {
         page = -1, in_page = gran - col * per, head = x.head;
         if (g < x.grans) {
             page = __ldg(a.bt.table + (int64_t)x.b * a.bt.max_blocks + col);
-            if (page < 0 || page >= a.c.n_blocks) page = 0;  // k_kv_join_many reports it
+            if (page < 0 || page >= a.c.n_blocks) page = 0;  // k_kv_join reports it
         }
         next_had = x.len - (gran - mine) * kGranule;  // tokens of the unit that are held
         if (++u == x.units) {
@@ -446,7 +444,7 @@ __device__ void product_role(Smem<D>& m, int tile) {
 
 // 4 warps a tile, a thread a row.
 template <typename T, int D>
-__device__ void softmax_role(const ManyArgs& a, Smem<D>& m, int w) {
+__device__ void softmax_role(const AttendArgs& a, const ManyWork& work, Smem<D>& m) {
     const int tile = threadIdx.x / 128, in_tile = threadIdx.x % 128, warp = in_tile / 32, lane = threadIdx.x % 32;
     const uint32_t lanes = (uint32_t)(warp * 32) << 16;
     const uint32_t sc = m.tmem + lanes + kScoreCol + tile * 128, su = m.tmem + lanes + kSumCol + tile * D;
@@ -519,7 +517,7 @@ __device__ void softmax_role(const ManyArgs& a, Smem<D>& m, int w) {
             const int qh = done.head * a.group + dr % a.group;
             const float inv = sum == 0.f ? 0.f : __fdiv_rn(1.f, sum);
             // stretches that are not whole: at most the CTA's first and its last
-            float* part = a.part + ((int64_t)2 * w + (done.first ? 0 : 1)) * (kPair * (D + 2)) + tile * kRows + in_tile;
+            float* part = work.part + ((int64_t)2 * blockIdx.x + (done.first ? 0 : 1)) * (kPair * (D + 2)) + tile * kRows + in_tile;
             T* dst = static_cast<T*>(a.out.data) + tok * a.out.token_stride + qh * a.out.head_stride;
 #pragma unroll 1
             for (int c = 0; c < D / 32; ++c) {
@@ -658,7 +656,7 @@ __device__ void softmax_role(const ManyArgs& a, Smem<D>& m, int w) {
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, 1) k_kv_attend_many(ManyArgs a) {
+__global__ void __launch_bounds__(kThreads, 1) k_kv_attend_many(AttendArgs a, ManyWork work) {
     extern __shared__ __align__(1024) uint8_t dyn[];
     Smem<D>& m = *reinterpret_cast<Smem<D>*>(dyn);
     const int tid = threadIdx.x, lane = tid % 32, wid = tid / 32;
@@ -681,6 +679,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend_many(ManyArgs a) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&m.tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
+    after_previous();
+    let_next_begin();
     // the line: strips of sequences, a warp a strip
     const int strip = (a.bt.n_seqs + kStrips - 1) / kStrips, strips = (a.bt.n_seqs + strip - 1) / strip;
 #pragma unroll 1
@@ -748,7 +748,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend_many(ManyArgs a) {
         if (lane == 0) {
             m.first = x, m.length = min(total, u0 + per) - u0, m.into = into;
             const ManyStart st = {x.b, x.tile, x.head, x.cnt, into, u0 < total, per};
-            a.starts[blockIdx.x] = st;
+            work.starts[blockIdx.x] = st;
         }
     }
     fence_before();
@@ -756,7 +756,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend_many(ManyArgs a) {
     fence_after();
     if (wid < kSoftmaxWarps) {
         more_regs<kSoftmaxRegs>();
-        softmax_role<T, D>(a, m, blockIdx.x);
+        softmax_role<T, D>(a, work, m);
     } else if (wid < kSoftmaxWarps + 4) {
         fewer_regs<kConvertRegs>();
         convert_role<T, D>(a, m);
@@ -780,99 +780,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend_many(ManyArgs a) {
         __syncwarp();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(m.tmem));
     }
-    if (tid == 0) a.gave_up[blockIdx.x] = m.gave_up;
-}
-
-constexpr int kJoinCols = 16;  // of D, a CTA of 256 rows
-
-// CTA (w, y): adds up the 16 columns y of the stretch in which CTA w of the line began,
-// if w is the first to begin inside it; the last CTAs write what sees nothing and the
-// sequences' status.
-template <typename T, int D>
-__global__ void __launch_bounds__(kPair) k_kv_join_many(ManyArgs a) {
-    const int tid = threadIdx.x;
-    const int cuts = a.ctas * (D / kJoinCols);
-    if (blockIdx.x < cuts) {
-        const int w = blockIdx.x / (D / kJoinCols), y = blockIdx.x % (D / kJoinCols);
-        const ManyStart st = a.starts[w];
-        if (!st.there || st.into <= kExtra) return;  // (it began with the pair's first unit)
-        const int64_t us = w * st.per - st.into;     // the pair and head on the line
-        const int begun = (int)((us + kExtra) / st.per), last = (int)((us + kExtra + st.cnt - 1) / st.per);
-        if (w != begun + 1) return;  // another CTA cut it before
-        const SeqView s = load_seq(a.bt, st.b, false);
-        const int r = st.tile * kPair + tid;
-        if (r >= s.n * a.group) return;
-        float top = -INFINITY, sum = 0.f, o[kJoinCols] = {};
-        for (int v = begun; v <= last; ++v) {
-            const float* part = a.part + ((int64_t)2 * v + (v * st.per >= us ? 0 : 1)) * (kPair * (D + 2));
-            const float m = part[D * kPair + tid], l = part[(D + 1) * kPair + tid];
-            const float now = fmaxf(top, m), ref = now == -INFINITY ? 0.f : now;
-            const float f = exp2_approx(top - ref), g = exp2_approx(m - ref);
-            sum = sum * f + l * g;
-#pragma unroll
-            for (int j = 0; j < kJoinCols; ++j) o[j] = o[j] * f + part[(y * kJoinCols + j) * kPair + tid] * g;
-            top = now;
-        }
-        const int64_t tok = s.lo + r / a.group;
-        const int qh = st.head * a.group + r % a.group;
-        const float inv = sum == 0.f ? 0.f : __fdiv_rn(1.f, sum);
-        T* dst = static_cast<T*>(a.out.data) + tok * a.out.token_stride + qh * a.out.head_stride + y * kJoinCols;
-#pragma unroll
-        for (int j = 0; j < kJoinCols; ++j) o[j] *= inv;
-        store_values<T, 8>(dst, a.wide_out, o);
-        store_values<T, 8>(dst + 8, a.wide_out, o + 8);
-        if (y == 0 && a.lse != nullptr)
-            a.lse[tok * a.q.n_heads + qh] = top == -INFINITY ? -INFINITY : (top - kManyLift + log2f(sum)) * 0.6931471805599453f;
-        return;
-    }
-    bool late = false;
-    for (int i = tid; i < a.ctas; i += kPair) late |= a.gave_up[i] != 0;
-    late = __syncthreads_or(late);
-    for (int b = blockIdx.x - cuts; b < a.bt.n_seqs; b += gridDim.x - cuts) {
-        const SeqView s = load_seq(a.bt, b, false);
-        const int pairs = pairs_of(a, s);
-        if (pairs == 0 && a.few_rows > 0) continue;  // the other kernel's
-        bool ok = s.st == MP_OK;
-        int lo = INT32_MAX, hi = 0;
-        for (int t = 0; t < pairs; ++t) {
-            int g, n;
-            pair_grans(a, s, t, g, n);
-            if (n > 0) {
-                lo = min(lo, g), hi = max(hi, g + n);
-                continue;
-            }
-            for (int i = tid; i < kPair * a.c.n_heads; i += kPair) {
-                const int r = t * kPair + i % kPair, head = i / kPair;
-                if (r >= s.n * a.group) continue;
-                const int64_t tok = s.lo + r / a.group;
-                const int qh = head * a.group + r % a.group;
-                T* dst = static_cast<T*>(a.out.data) + tok * a.out.token_stride + qh * a.out.head_stride;
-                for (int d = 0; d < D; ++d) dst[d] = from_f32<T>(0.f);
-                if (a.lse != nullptr) a.lse[tok * a.q.n_heads + qh] = -INFINITY;
-            }
-        }
-        if (hi > 0) {
-            const int in = a.c.block_tokens / kGranule;
-            for (int col = lo / in + tid; col <= (hi - 1) / in; col += kPair) {
-                const int p = __ldg(a.bt.table + (int64_t)b * a.bt.max_blocks + col);
-                ok &= p >= 0 && p < a.c.n_blocks;
-            }
-        }
-        ok = !__syncthreads_or(!ok);
-        if (tid == 0) a.status[b] = !ok ? MP_EINVAL : late ? MP_ETIMEOUT : MP_OK;
-    }
+    if (tid == 0) work.gave_up[blockIdx.x] = m.gave_up;
 }
 
 template <typename T, int D>
-cudaError_t many_as(const ManyArgs& a, cudaStream_t stream) {
-    cudaError_t e = set_smem_limit((const void*)k_kv_attend_many<T, D>, sizeof(Smem<D>) + 16);
+cudaError_t many_as(const AttendArgs& a, const ManyWork& w, cudaStream_t stream) {
+    cudaError_t e = set_smem_limit((const void*)k_kv_attend_many<T, D>, sizeof(Smem<D>));
     if (e != cudaSuccess) return e;
-    k_kv_attend_many<T, D><<<a.ctas, kThreads, sizeof(Smem<D>), stream>>>(a);
-    e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
-    const int cuts = a.ctas * (D / kJoinCols);
-    k_kv_join_many<T, D><<<cuts + std::min(a.bt.n_seqs, 1024), kPair, 0, stream>>>(a);
-    return cudaGetLastError();
+    return launch_close(k_kv_attend_many<T, D>, kManyCtas, kThreads, sizeof(Smem<D>), stream, a, w);
 }
 
 }  // namespace
@@ -881,9 +796,10 @@ size_t kv_many_part_bytes(const mp_kv_cache& c) {
     return sizeof(float) * 2 * kManyCtas * kPair * (size_t)(c.head_dim + 2);
 }
 
-cudaError_t launch_kv_many(const ManyArgs& a, cudaStream_t stream) {
-    if (a.q.dtype == MP_F16) return a.c.head_dim == 64 ? many_as<__half, 64>(a, stream) : many_as<__half, 128>(a, stream);
-    return a.c.head_dim == 64 ? many_as<__nv_bfloat16, 64>(a, stream) : many_as<__nv_bfloat16, 128>(a, stream);
+cudaError_t launch_kv_many(const AttendArgs& a, const ManyWork& w, cudaStream_t stream) {
+    if (a.q.dtype == MP_F16)
+        return a.c.head_dim == 64 ? many_as<__half, 64>(a, w, stream) : many_as<__half, 128>(a, w, stream);
+    return a.c.head_dim == 64 ? many_as<__nv_bfloat16, 64>(a, w, stream) : many_as<__nv_bfloat16, 128>(a, w, stream);
 }
 
 }  // namespace mp
