@@ -49,6 +49,8 @@ __device__ __forceinline__ int64_t seq_units(const AttendArgs& a, int b) {
 struct Cursor {
     int b, lo, hi, g;    // sequence, its granules, the granule
     int slots, slot;     // tiles x heads, tile * heads + head
+    int64_t row;         // first row of the token arrays
+    int n, len;          // the call's tokens, tokens held
     __device__ __forceinline__ void seek(int lo_, int hi_, int slots_, int64_t unit) {
         lo = lo_, hi = hi_, slots = slots_;
         slot = (int)quotient(unit, hi - lo);
@@ -63,6 +65,7 @@ __device__ __forceinline__ bool enter(const AttendArgs& a, Cursor& c, int64_t un
     seq_granules(a, s, lo, hi);
     const int slots = a.c.n_heads * seq_tiles<kRows>(a, s);
     if (hi <= lo || slots == 0) return false;
+    c.row = s.lo, c.n = s.n, c.len = s.len;
     c.seek(lo, hi, slots, unit);
     return true;
 }
@@ -201,223 +204,224 @@ __global__ void __launch_bounds__(few_warps(NT) * 32, 1) k_kv_attend_few(AttendA
     float top[NT][2], sum[NT][2];   // running maximum of x, this lane's part of the sum
     float o[NT][D / 16][4];
     int see_lo[NT][2], see_hi[NT][2];  // positions that the column's row sees
-    bool fresh = true;
-    int64_t lo_row = 0;
     bool up = false;
+    int done = 0;  // units
 
-    for (int64_t u = u0; u < u1; ++u) {
+    for (int left = (int)(u1 - u0); left > 0 && !up;) {
+        // one (sequence, tile, head) or what this warp has of it
         const int head = cur.slot % a.c.n_heads, tile = cur.slot / a.c.n_heads;
-        if (fresh) {
-            fresh = false;
-            const SeqView s = load_seq(a.bt, cur.b, false);
-            const int rows = s.n * a.group;
-            lo_row = s.lo;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                const int r = tile * kRows + nt * 8 + g;
-                float x[D / 16][4], most = 0.f;
-                const T* p = static_cast<const T*>(a.q.data) + (s.lo + r / a.group) * a.q.token_stride +
-                             (head * a.group + r % a.group) * a.q.head_stride;
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        x[i][k] = r < rows ? to_f32(p[i * 16 + t * 4 + k]) : 0.f;
-                        most = fmaxf(most, fabsf(x[i][k]));
-                    }
-                }
-                most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
-                most = fmaxf(most, __shfl_xor_sync(~0u, most, 2));
-                const float f = row_factor(most);
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-                    qf[nt][i][0] = pack_f16(x[i][0] * f, x[i][1] * f);
-                    qf[nt][i][1] = pack_f16(x[i][2] * f, x[i][3] * f);
-                }
-                const float mine = __fdiv_rn(a.scale * 1.4426950408889634f, f);
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    unit[nt][k] = __shfl_sync(~0u, mine, (2 * t + k) * 4);
-                    const int col = tile * kRows + nt * 8 + 2 * t + k;
-                    const int pos = s.len - s.n + col / a.group;
-                    see_hi[nt][k] = col >= rows ? 0 : a.causal ? min(s.len, pos + 1) : s.len;
-                    see_lo[nt][k] = a.window > 0 ? pos - a.window + 1 : 0;
-                    top[nt][k] = -INFINITY, sum[nt][k] = 0.f;
-                }
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
-            }
-        }
-        const int st = (int)((u - u0) % kFewStages);
-        if (!__all_sync(~0u, mbar_wait(&bar[st], (uint32_t)((u - u0) / kFewStages & 1)))) {
-            up = true;
-            break;
-        }
-        const int64_t sc = (int64_t)ring_page[st] * a.c.n_heads + head;
-        const float ks = __ldg(a.c.k_scale + sc), vs = value_scale(__ldg(a.c.v_scale + sc));
-        const uint8_t* kb = ring + st * 2 * kBytes;
-        const uint8_t* vb = kb + kBytes;
-
-        // scores: product row r of 16 is token 4 (r % 8 / 2) + r % 2 + 2 (r / 8), the order in which a
-        // lane's 4 stored value bytes meet the second product
-        float s[NT][2][4] = {};
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const int tok = 4 * (g / 2) + g % 2;
-            const uint8_t* row = kb + (m * 2 + tok / 8) * (D * 8) + tok % 8 * 16 + t * 4;
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i) {
-                uint32_t a0, a1, a2, a3;
-                e4m3_to_f16(*reinterpret_cast<const uint32_t*>(row + i * 128), a0, a2);
-                e4m3_to_f16(*reinterpret_cast<const uint32_t*>(row + i * 128 + 32), a1, a3);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma(s[nt][m], a0, a1, a2, a3, qf[nt][i][0], qf[nt][i][1]);
-            }
-        }
-        const float lv = log2f(vs), iv = __fdiv_rn(1.f, vs);
-        const int base = cur.g * kGranule;
-        uint32_t p[NT][2][2];
-        bool moved = false;
-        float fade[NT][2];
-        int last = 0;  // one past the last position that any row sees: stored bytes behind it mean nothing
+        const int rows = cur.n * a.group, units = min(cur.hi - cur.g, left);
+        const bool whole = units == cur.hi - cur.lo;
+        const bool first = done == 0;
+        left -= units;
+        int last = 0;  // stored bytes from this position on mean nothing
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
+            const int r = tile * kRows + nt * 8 + g, there = min(r, rows - 1);
+            const T* p = static_cast<const T*>(a.q.data) + (cur.row + there / a.group) * a.q.token_stride +
+                         (head * a.group + there % a.group) * a.q.head_stride + t * 4;
+            // all loads at once: a branch in between would have each wait for the one before
+            Pack<T, 4> raw[D / 16];
+            if (a.wide_q) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const float unit_k = unit[nt][k] * ks;
-                float most = -INFINITY;
-#pragma unroll
-                for (int m = 0; m < 2; ++m)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int j = base + m * 16 + 4 * (g / 2) + g % 2 + 2 * h;
-                        const bool seen = j < see_hi[nt][k] && j >= see_lo[nt][k];
-                        float& x = s[nt][m][2 * h + k];
-                        x = seen ? fmaf(x, unit_k, lv) : -INFINITY;
-                        most = fmaxf(most, x);
-                    }
-                most = fmaxf(most, __shfl_xor_sync(~0u, most, 4));
-                most = fmaxf(most, __shfl_xor_sync(~0u, most, 8));
-                most = fmaxf(most, __shfl_xor_sync(~0u, most, 16));
-                const float now = fmaxf(top[nt][k], most);
-                const float ref = now == -INFINITY ? 0.f : now - kLift;
-                fade[nt][k] = exp2_approx(top[nt][k] - kLift - ref);
-                moved |= now != top[nt][k];
-                top[nt][k] = now;
-                float part = 0.f;
-#pragma unroll
-                for (int m = 0; m < 2; ++m)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        float& x = s[nt][m][2 * h + k];
-                        x = exp2_approx(x - ref);
-                        part += x;
-                    }
-                sum[nt][k] = fmaf(part, iv, sum[nt][k] * fade[nt][k]);
-                last = max(last, see_hi[nt][k]);
-            }
-#pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                p[nt][m][0] = transposed(pack_f16(s[nt][m][0], s[nt][m][1]));
-                p[nt][m][1] = transposed(pack_f16(s[nt][m][2], s[nt][m][3]));
-            }
-        }
-        if (__any_sync(~0u, moved)) {
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+                for (int i = 0; i < D / 16; ++i) raw[i] = *reinterpret_cast<const Pack<T, 4>*>(p + i * 16);
+            } else {
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) o[nt][i][k] *= fade[nt][k % 2];
+                    for (int k = 0; k < 4; ++k) raw[i].x[k] = p[i * 16 + k];
+            }
+            float most = 0.f;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) most = fmaxf(most, fabsf(to_f32(raw[i].x[k])));
+            most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
+            most = fmaxf(most, __shfl_xor_sync(~0u, most, 2));
+            const float f = row_factor(most);
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                qf[nt][i][0] = pack_f16(to_f32(raw[i].x[0]) * f, to_f32(raw[i].x[1]) * f);
+                qf[nt][i][1] = pack_f16(to_f32(raw[i].x[2]) * f, to_f32(raw[i].x[3]) * f);
+            }
+            const float mine = __fdiv_rn(a.scale * 1.4426950408889634f, f);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                unit[nt][k] = __shfl_sync(~0u, mine, (2 * t + k) * 4);
+                const int col = tile * kRows + nt * 8 + 2 * t + k;
+                const int pos = cur.len - cur.n + col / a.group;
+                // columns past the last row repeat it and see all that is held: no one reads them
+                see_hi[nt][k] = col < rows && a.causal ? min(cur.len, pos + 1) : cur.len;
+                see_lo[nt][k] = col < rows && a.window > 0 ? pos - a.window + 1 : 0;
+                last = max(last, see_hi[nt][k]);
+                top[nt][k] = -INFINITY, sum[nt][k] = 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
         }
         last = __reduce_max_sync(~0u, last);
-        if (base + kGranule <= last) {
+#pragma unroll 1
+        for (int i = 0; i < units; ++i, ++done, ++cur.g) {
+            const int st = done % kFewStages;
+            if (!__all_sync(~0u, mbar_wait(&bar[st], (uint32_t)(done / kFewStages & 1)))) {
+                up = true;
+                break;
+            }
+            const int64_t sc = (int64_t)ring_page[st] * a.c.n_heads + head;
+            const float ks = __ldg(a.c.k_scale + sc), vs = value_scale(__ldg(a.c.v_scale + sc));
+            const uint8_t* kb = ring + st * 2 * kBytes;
+            const uint8_t* vb = kb + kBytes;
+
+            // scores: product row r of 16 is token 4 (r % 8 / 2) + r % 2 + 2 (r / 8), the order in which a
+            // lane's 4 stored value bytes meet the second product
+            float s[NT][2][4] = {};
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int m = 0; m < 2; ++m) {
+                const int tok = 4 * (g / 2) + g % 2;
+                const uint8_t* row = kb + (m * 2 + tok / 8) * (D * 8) + tok % 8 * 16 + t * 4;
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) {
-                    const uint8_t* at = vb + i * 512 + h * 128 + lane * 4;
                     uint32_t a0, a1, a2, a3;
-                    e4m3_to_f16(*reinterpret_cast<const uint32_t*>(at), a0, a2);
-                    e4m3_to_f16(*reinterpret_cast<const uint32_t*>(at + 256), a1, a3);
+                    e4m3_to_f16(*reinterpret_cast<const uint32_t*>(row + i * 128), a0, a2);
+                    e4m3_to_f16(*reinterpret_cast<const uint32_t*>(row + i * 128 + 32), a1, a3);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma(o[nt][i], a0, a1, a2, a3, p[nt][h][0], p[nt][h][1]);
-                }
-        } else {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int left = last - (base + h * 16 + t * 4);  // of this lane's 4 tokens
-                const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-                    const uint8_t* at = vb + i * 512 + h * 128 + lane * 4;
-                    uint32_t a0, a1, a2, a3;
-                    e4m3_to_f16(*reinterpret_cast<const uint32_t*>(at) & keep, a0, a2);
-                    e4m3_to_f16(*reinterpret_cast<const uint32_t*>(at + 256) & keep, a1, a3);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma(o[nt][i], a0, a1, a2, a3, p[nt][h][0], p[nt][h][1]);
+                    for (int nt = 0; nt < NT; ++nt) mma(s[nt][m], a0, a1, a2, a3, qf[nt][i][0], qf[nt][i][1]);
                 }
             }
-        }
-        __syncwarp();
-        issue();
-
-        const bool ends = cur.g + 1 == cur.hi;
-        if (ends || u + 1 == u1) {
-            const int64_t held = u + 1 - u0;  // units since the warp's start
-            const bool whole = ends && held >= cur.hi - cur.lo;
-            const SeqView sv = load_seq(a.bt, cur.b, false);
-            const int rows = sv.n * a.group;
+            const float lv = log2f(vs), iv = __fdiv_rn(1.f, vs);
+            const int base = cur.g * kGranule;
+            uint32_t p[NT][2][2];
+            bool moved = false;
+            float fade[NT][2];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    float l = sum[nt][k];
-                    l += __shfl_xor_sync(~0u, l, 4);
-                    l += __shfl_xor_sync(~0u, l, 8);
-                    l += __shfl_xor_sync(~0u, l, 16);
-                    const int in_tile = nt * 8 + 2 * t + k, r = tile * kRows + in_tile;
-                    const float m = top[nt][k];
-                    if (whole) {
-                        if (r < rows) {
-                            const int64_t tok = lo_row + r / a.group;
-                            const int qh = head * a.group + r % a.group;
-                            T* dst = static_cast<T*>(a.out.data) + tok * a.out.token_stride + qh * a.out.head_stride;
-                            const float inv = l == 0.f ? 0.f : __fdiv_rn(1.f, l);
+                    const float unit_k = unit[nt][k] * ks;
+                    float most = -INFINITY;
 #pragma unroll
-                            for (int i = 0; i < D / 16; ++i) {
-                                dst[i * 16 + g] = from_f32<T>(o[nt][i][k] * inv);
-                                dst[i * 16 + g + 8] = from_f32<T>(o[nt][i][2 + k] * inv);
-                            }
-                            if (a.lse != nullptr && g == 0)
-                                a.lse[tok * a.q.n_heads + qh] =
-                                    m == -INFINITY ? -INFINITY : (m - kLift + log2f(l)) * 0.6931471805599453f;
-                        }
-                    } else {
-                        // a warp leaves at most two parts: of what began before it or with it, and of
-                        // what it begins and does not end
-                        const bool first = held <= cur.g - cur.lo + 1;
-                        float* part = work.part + ((int64_t)2 * w + (first ? 0 : 1)) * (kRows * (D + 2));
-                        float* dst = part + in_tile * D;
+                    for (int m = 0; m < 2; ++m)
 #pragma unroll
-                        for (int i = 0; i < D / 16; ++i) {
-                            dst[i * 16 + g] = o[nt][i][k];
-                            dst[i * 16 + g + 8] = o[nt][i][2 + k];
+                        for (int h = 0; h < 2; ++h) {
+                            const int j = base + m * 16 + 4 * (g / 2) + g % 2 + 2 * h;
+                            const bool seen = j < see_hi[nt][k] && j >= see_lo[nt][k];
+                            float& x = s[nt][m][2 * h + k];
+                            x = seen ? fmaf(x, unit_k, lv) : -INFINITY;
+                            most = fmaxf(most, x);
                         }
-                        if (g == 0) {
-                            part[kRows * D + 2 * in_tile] = m;
-                            part[kRows * D + 2 * in_tile + 1] = l;
+                    most = fmaxf(most, __shfl_xor_sync(~0u, most, 4));
+                    most = fmaxf(most, __shfl_xor_sync(~0u, most, 8));
+                    most = fmaxf(most, __shfl_xor_sync(~0u, most, 16));
+                    const float now = fmaxf(top[nt][k], most);
+                    const float ref = now == -INFINITY ? 0.f : now - kLift;
+                    fade[nt][k] = exp2_approx(top[nt][k] - kLift - ref);
+                    moved |= now != top[nt][k];
+                    top[nt][k] = now;
+                    float part = 0.f;
+#pragma unroll
+                    for (int m = 0; m < 2; ++m)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            float& x = s[nt][m][2 * h + k];
+                            x = exp2_approx(x - ref);
+                            part += x;
                         }
+                    sum[nt][k] = fmaf(part, iv, sum[nt][k] * fade[nt][k]);
+                }
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    p[nt][m][0] = transposed(pack_f16(s[nt][m][0], s[nt][m][1]));
+                    p[nt][m][1] = transposed(pack_f16(s[nt][m][2], s[nt][m][3]));
+                }
+            }
+            if (__any_sync(~0u, moved)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) o[nt][i][k] *= fade[nt][k % 2];
+            }
+            if (base + kGranule <= last) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) {
+                        const uint8_t* at = vb + i * 512 + h * 128 + lane * 4;
+                        uint32_t a0, a1, a2, a3;
+                        e4m3_to_f16(*reinterpret_cast<const uint32_t*>(at), a0, a2);
+                        e4m3_to_f16(*reinterpret_cast<const uint32_t*>(at + 256), a1, a3);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) mma(o[nt][i], a0, a1, a2, a3, p[nt][h][0], p[nt][h][1]);
+                    }
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int left = last - (base + h * 16 + t * 4);  // of this lane's 4 tokens
+                    const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) {
+                        const uint8_t* at = vb + i * 512 + h * 128 + lane * 4;
+                        uint32_t a0, a1, a2, a3;
+                        e4m3_to_f16(*reinterpret_cast<const uint32_t*>(at) & keep, a0, a2);
+                        e4m3_to_f16(*reinterpret_cast<const uint32_t*>(at + 256) & keep, a1, a3);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) mma(o[nt][i], a0, a1, a2, a3, p[nt][h][0], p[nt][h][1]);
                     }
                 }
-            fresh = true;
+            }
+            __syncwarp();
+            issue();
         }
-        next<kRows>(a, cur);
+        if (up) break;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                float l = sum[nt][k];
+                l += __shfl_xor_sync(~0u, l, 4);
+                l += __shfl_xor_sync(~0u, l, 8);
+                l += __shfl_xor_sync(~0u, l, 16);
+                const int in_tile = nt * 8 + 2 * t + k, r = tile * kRows + in_tile;
+                const float m = top[nt][k];
+                if (whole) {
+                    if (r < rows) {
+                        const int64_t tok = cur.row + r / a.group;
+                        const int qh = head * a.group + r % a.group;
+                        T* dst = static_cast<T*>(a.out.data) + tok * a.out.token_stride + qh * a.out.head_stride;
+                        const float inv = l == 0.f ? 0.f : __fdiv_rn(1.f, l);
+#pragma unroll
+                        for (int i = 0; i < D / 16; ++i) {
+                            dst[i * 16 + g] = from_f32<T>(o[nt][i][k] * inv);
+                            dst[i * 16 + g + 8] = from_f32<T>(o[nt][i][2 + k] * inv);
+                        }
+                        if (a.lse != nullptr && g == 0)
+                            a.lse[tok * a.q.n_heads + qh] =
+                                m == -INFINITY ? -INFINITY : (m - kLift + log2f(l)) * 0.6931471805599453f;
+                    }
+                } else {
+                    // a warp leaves at most two parts: of what began before it or with it, and of
+                    // what it begins and does not end
+                    float* part = work.part + ((int64_t)2 * w + (first ? 0 : 1)) * (kRows * (D + 2));
+                    float* dst = part + in_tile * D;
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) {
+                        dst[i * 16 + g] = o[nt][i][k];
+                        dst[i * 16 + g + 8] = o[nt][i][2 + k];
+                    }
+                    if (g == 0) {
+                        part[kRows * D + 2 * in_tile] = m;
+                        part[kRows * D + 2 * in_tile + 1] = l;
+                    }
+                }
+            }
+        --cur.g;
+        if (left > 0) next<kRows>(a, cur);
     }
     if (up) {
         if (lane == 0) work.gave_up[w] = 1;
         // leave no copy in flight behind
-        for (int64_t u = max(u0, issued - kFewStages); u < issued; ++u)
+        for (int64_t u = max(u0 + done, issued - kFewStages); u < issued; ++u)
             mbar_wait(&bar[(u - u0) % kFewStages], (uint32_t)((u - u0) / kFewStages & 1));
     }
 }
