@@ -566,6 +566,9 @@ __device__ void softmax_role(const AttendArgs& a, const ManyWork& work, Smem<D>&
 #pragma unroll 1
             for (int u = 0; u < units; ++u, ++n, hi -= kTokens, lo -= kTokens) {
                 const float(*scale)[kGrans] = m.scales[(it + u) % kScaleRing];
+                // a tile that sat stretches out is ahead of the ring, where an old phase looks like the one to come:
+                // its first scores say that the unit is at hand
+                if (u == 0 && !await_warp(&m.s_full[tile], n & 1, &m.gave_up)) return;
                 if (!await_warp(&m.scales_full[(it + u) % kScaleRing], (it + u) / kScaleRing & 1, &m.gave_up)) return;
                 const bool edge = __any_sync(~0u, hi < kTokens || lo > 0);
                 float mul[kGrans], add[kGrans], inverse[kGrans];
@@ -574,7 +577,7 @@ __device__ void softmax_role(const AttendArgs& a, const ManyWork& work, Smem<D>&
                     mul[c] = fmaxf(unit * scale[0][c], 0x1p-126f);  // not 0: what is not seen stays -inf
                     add[c] = scale[1][c], inverse[c] = scale[2][c];
                 }
-                if (!await_warp(&m.s_full[tile], n & 1, &m.gave_up)) return;
+                if (u > 0 && !await_warp(&m.s_full[tile], n & 1, &m.gave_up)) return;
                 fence_after();
                 uint32_t raw[kTokens];
                 float* s = reinterpret_cast<float*>(raw);

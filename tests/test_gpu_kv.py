@@ -189,6 +189,50 @@ def test_attend(cuda_lib, block, hq, heads, d, dtype, how, causal, window, seqs)
     check_attend(mp, pool, table, lens, new, q, qx, d ** -0.5, causal, window)
 
 
+@pytest.mark.parametrize("group,d,dtype", [(4, 128, BF16), (4, 64, F16), (3, 128, F16), (1, 64, BF16)])
+def test_attend_many_ragged_prompts(cuda_lib, group, d, dtype):
+    """Pairs of row tiles with one tile in use follow and precede pairs with both, in batches whose work is cut between
+    CTAs, from scratch memory that holds anything; the definition in 64 bits on the GPU."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(group * d)
+    heads, block = 3, 32
+    for seqs in ([(500, 460), (1300, 408), (700, 300)], [(int(n) + int(x), int(n)) for n, x in
+                                                      zip(rng.integers(30, 700, 24), rng.integers(0, 900, 24))]):
+        lens, new = [s[0] for s in seqs], [s[1] for s in seqs]
+        table, n = R.make_table(lens, block, rng)
+        pool = R.Pool(n, block, heads, d, rng)
+        pool.vs[:] = np.exp2(rng.integers(-12, 3, pool.vs.shape))  # scales that are not the next unit's
+        pool.ks[:] = np.exp2(rng.integers(-9, -5, pool.ks.shape))
+        cache, batch = pool.cache(), batch_of(mp, table, lens, new)
+        q, qx = rows(rng, sum(new), heads * group, d, dtype)
+        k, v, _ = mp.kv_read(cache, batch_of(mp, table, lens, lens), F32)
+        want, mag, row, past = [], [], 0, 0
+        want_lse, size = [], []
+        for length, m in seqs:
+            kk, vv = (x[past:past + length].double().repeat_interleave(group, 1).transpose(0, 1) for x in (k, v))
+            qq = q[row:row + m].double().transpose(0, 1)
+            x = qq @ kk.transpose(1, 2) * d ** -0.5
+            j = torch.arange(length, device="cuda")
+            x = x.masked_fill(j > (length - m + torch.arange(m, device="cuda"))[:, None], -torch.inf)
+            w = torch.softmax(x, -1)
+            want.append((w @ vv).transpose(0, 1)), mag.append((w @ vv.abs()).transpose(0, 1))
+            want_lse.append(torch.logsumexp(x, -1).transpose(0, 1))
+            size.append(((qq.abs() @ kk.abs().transpose(1, 2)).amax(-1) * d ** -0.5).transpose(0, 1))
+            row, past = row + m, past + length
+        want, mag, want_lse, size = (torch.cat(x).cpu().numpy() for x in (want, mag, want_lse, size))
+        bound, lse_bound = R.attend_bounds(dtype, want, want_lse, mag, size)
+        for fill in (0, 255, 0, 255):
+            ws = mp.Workspace("cuda")
+            need = mp.kv_attend_workspace_bytes(cache, batch, heads * group)
+            ws.get(need)
+            ws.buf.fill_(fill)
+            out, lse, status = mp.kv_attend(cache, batch, q, want_lse=True, workspace=ws)
+            assert not status.any()
+            assert (np.abs(out.double().cpu().numpy() - want) <= bound).all()
+            assert (np.abs(lse.double().cpu().numpy() - want_lse) <= lse_bound).all()
+
+
 def test_attend_sharp_and_flat_rows(cuda_lib):
     """Scores hundreds apart, one token that outweighs thousands, and queries of zeros (all weights equal)."""
     import paper_2203_00448_gb300 as mp
