@@ -81,7 +81,7 @@ class KvBatch:
         self.max_tokens = self.n_tokens if max_tokens is None else int(max_tokens)
         self.max_len = max_len
         self.n_seqs, self.device = B, table.device
-        self._structs = {}
+        self._structs, self._needs = {}, {}
 
     def _ref(self, cache: KvCache):
         ref = self._structs.get(cache.block_tokens)
@@ -110,6 +110,10 @@ def _tokens(name, t, cache, batch, n_heads=None):
     return _lib.MpTokens(t.data_ptr() or None, strides[0], strides[1], shape[1], dtype)
 
 
+def _fresh(t, heads, dim):  # a dense tensor that this module has made
+    return _lib.MpTokens(t.data_ptr() or None, heads * dim, dim, heads, _DTYPES[t.dtype])
+
+
 def _status(status, batch):
     if status is None:
         return torch.empty_like(batch.lens)
@@ -126,7 +130,7 @@ _workspaces = {}
 
 def _workspace_of(stream_ptr, device):
     # calls on different streams may overlap: each stream has its own
-    key = (device, stream_ptr)
+    key = (device.index, stream_ptr)
     ws = _workspaces.get(key)
     if ws is None:
         ws = _workspaces[key] = Workspace(device)
@@ -152,19 +156,29 @@ def kv_read(cache: KvCache, batch: KvBatch, dtype=torch.bfloat16, k=None, v=None
     if stream is not None:
         with torch.cuda.stream(stream):
             return kv_read(cache, batch, dtype, k, v, status)
-    shape = (batch.n_tokens, cache.n_heads, cache.head_dim)
-    k = torch.empty(shape, dtype=dtype, device=cache.device) if k is None else k
-    v = torch.empty(shape, dtype=dtype, device=cache.device) if v is None else v
+    heads, dim = cache.n_heads, cache.head_dim
+    outs = []
+    for name, t in (("k", k), ("v", v)):
+        if t is None:
+            if dtype not in _DTYPES:
+                raise ValueError(f"float16, bfloat16 or float32 can be read, not {dtype}")
+            t = torch.empty((batch.n_tokens, heads, dim), dtype=dtype, device=cache.device)
+            outs += [t, _fresh(t, heads, dim)]
+        else:
+            outs += [t, _tokens(name, t, cache, batch, heads)]
+    k, kt, v, vt = outs
     status = _status(status, batch)
-    _check("mp_kv_read", _lib.load().mp_kv_read(cache._ref, batch._ref(cache),
-                                                _tokens("k", k, cache, batch, cache.n_heads),
-                                                _tokens("v", v, cache, batch, cache.n_heads),
-                                                status.data_ptr() or None, _stream(cache.device)))
+    _check("mp_kv_read", _lib.load().mp_kv_read(cache._ref, batch._ref(cache), kt, vt, status.data_ptr() or None,
+                                                _stream(cache.device)))
     return k, v, status
 
 
 def kv_attend_workspace_bytes(cache: KvCache, batch: KvBatch, n_q_heads: int) -> int:
-    return int(_lib.load().mp_kv_attend_workspace_bytes(cache._ref, batch._ref(cache), n_q_heads))
+    key = (n_q_heads, cache.n_heads, cache.head_dim, cache.block_tokens)
+    need = batch._needs.get(key)
+    if need is None:
+        need = batch._needs[key] = int(_lib.load().mp_kv_attend_workspace_bytes(cache._ref, batch._ref(cache), n_q_heads))
+    return need
 
 
 def kv_attend(cache: KvCache, batch: KvBatch, q: torch.Tensor, scale: float | None = None, causal: bool = True,
@@ -181,6 +195,9 @@ def kv_attend(cache: KvCache, batch: KvBatch, q: torch.Tensor, scale: float | No
     heads = q.shape[1]
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        ot = _fresh(out, heads, cache.head_dim)
+    else:
+        ot = _tokens("out", out, cache, batch, heads)
     if lse is not None:
         _tensor("lse", lse, torch.float32, (batch.n_tokens, heads), cache.device)
     elif want_lse:
@@ -188,10 +205,10 @@ def kv_attend(cache: KvCache, batch: KvBatch, q: torch.Tensor, scale: float | No
     status = _status(status, batch)
     stream_ptr = _stream(cache.device)
     ref = batch._ref(cache)
-    ws = workspace or _workspace_of(stream_ptr, cache.device)
-    wptr, wbytes = ws.get(lib.mp_kv_attend_workspace_bytes(cache._ref, ref, heads))
+    need = kv_attend_workspace_bytes(cache, batch, heads)
+    wptr, wbytes = (workspace or _workspace_of(stream_ptr, cache.device)).get(need) if need else (None, 0)
     _check("mp_kv_attend",
            lib.mp_kv_attend(cache._ref, ref, qt, cache.head_dim ** -0.5 if scale is None else scale, 1 if causal else 0,
-                            window, _tokens("out", out, cache, batch, heads), _ptr(lse), status.data_ptr() or None, wptr, wbytes,
-                            stream_ptr))
+                            window, ot, None if lse is None else lse.data_ptr() or None, status.data_ptr() or None, wptr,
+                            wbytes, stream_ptr))
     return out, lse, status

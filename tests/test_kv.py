@@ -69,8 +69,10 @@ def test_host_argument_errors(lib):
 def test_attend_argument_errors(lib):
     E = _lib.EINVAL
 
+    long = dict(max_blocks=1000, max_len=32000)  # a context that is shared among CTAs, which takes scratch
+
     def call(q=None, scale=0.1, causal=1, window=0, out=None, lse=None, status=P, ws=P, room=1 << 40):
-        return lib.mp_kv_attend(cache(), batch(), q or tokens(4), scale, causal, window, out or tokens(4), lse, status, ws,
+        return lib.mp_kv_attend(cache(), batch(**long), q or tokens(4), scale, causal, window, out or tokens(4), lse, status, ws,
                                 room, None)
 
     assert call(q=tokens(4, dtype=2), out=tokens(4, dtype=2)) == E  # 32-bit queries
@@ -81,7 +83,7 @@ def test_attend_argument_errors(lib):
         assert call(scale=scale) == E
     assert call(window=-1) == E and call(window=5, causal=0) == E
     assert call(lse=P + 2) == E and call(status=None) == E
-    need = lib.mp_kv_attend_workspace_bytes(cache(), batch(), 4)
+    need = lib.mp_kv_attend_workspace_bytes(cache(), batch(**long), 4)
     assert need > 0
     assert call(room=need - 1) == _lib.ENOMEM
     assert call(ws=None) == E and call(ws=P + 8) == E
