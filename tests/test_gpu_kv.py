@@ -453,3 +453,15 @@ def test_streams_and_graphs(cuda_lib):
         mp.kv_write(twin, at, k, k)
     assert torch.equal(twin.k, cache.k) and torch.equal(twin.v_scale, cache.v_scale)
     assert torch.equal(mp.kv_attend(twin, at, q)[0], out)
+
+
+def test_example_serves_planned_requests(cuda_lib):
+    """The example's loop: requests' blocks from one plan, prompts and single tokens mixed in a call.  An output may be off
+    by bf16's last rounding, 2^-9 of it, and by the weights' 2^-11 (both at most, in the 2-norm)."""
+    from examples.serve_requests import serve
+
+    for kw in (dict(n=12, prompt=150, generate=8, spread=15, heads=2, group=4, dim=64, block_tokens=32),
+               dict(n=6, prompt=400, generate=5, spread=4, heads=1, group=3, dim=128, block_tokens=96, dtype=F16)):
+        done = serve(check=True, **kw)
+        assert done["pool_blocks"] < done["blocks"] or kw["spread"] < 10
+        assert 0 < done["worst"] <= 2.0 ** -9 + 2.0 ** -11
