@@ -731,9 +731,10 @@ constexpr int64_t kShortCtas = 304;
 struct Route {
     bool few, many, brief;
 };
-Route route(const mp_kv_cache& c, const mp_kv_batch& bt, int32_t group) {
+Route route(const mp_kv_cache& c, const mp_kv_batch& bt, int32_t group, int32_t window) {
     if ((int64_t)bt.max_tokens * group <= kFewRows) {
-        const bool brief = bt.max_len <= kShortLen && (int64_t)bt.n_seqs * c.n_heads <= kShortCtas;
+        const int32_t span = window > 0 ? std::min(bt.max_len, window + bt.max_tokens) : bt.max_len;
+        const bool brief = span <= kShortLen && (int64_t)bt.n_seqs * c.n_heads <= kShortCtas;
         return {!brief, false, brief};
     }
     return {bt.n_tokens != (int64_t)bt.n_seqs * bt.max_tokens, true, false};
@@ -742,9 +743,10 @@ Route route(const mp_kv_cache& c, const mp_kv_batch& bt, int32_t group) {
 struct Layout {
     size_t base, gave_up, part, starts, many_gave_up, many_part, bytes;
 };
+// (The scratch is asked for before the window is known: a window can only leave it unused.)
 Layout layout(const mp_kv_cache& c, const mp_kv_batch& bt, int32_t group) {
     Layout l = {};
-    const Route r = route(c, bt, group);
+    const Route r = route(c, bt, group, 0);
     const size_t warps = (size_t)kFewCtas * few_warps(1);
     auto take = [&](size_t bytes) {
         const size_t at = l.bytes;
@@ -822,11 +824,12 @@ cudaError_t launch_kv_attend(const mp_kv_cache& c, const mp_kv_batch& bt, const 
     if (bt.n_seqs == 0) return cudaSuccess;
     const int32_t group = q.n_heads / c.n_heads;
     const Layout l = layout(c, bt, group);
-    const Route r = route(c, bt, group);
+    if (window >= bt.max_len) window = 0;  // reaches back to every start
+    const Route r = route(c, bt, group, window);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     AttendArgs a;
     a.c = c, a.bt = bt, a.q = q, a.out = out, a.lse = lse, a.status = status;
-    a.scale = scale, a.causal = causal, a.window = window >= bt.max_len ? 0 : window;  // (reaches back to every start)
+    a.scale = scale, a.causal = causal, a.window = window;
     a.group = group;
     a.few_rows = r.few || r.brief ? kFewRows : -1;
     a.wide_q = rows_aligned(q), a.wide_out = rows_aligned(out);

@@ -65,9 +65,9 @@ __device__ __forceinline__ uint32_t group_max(uint32_t x, uint32_t* smem) {
     }
     return x;
 }
-// The values in a word, times the inverse of the scale; `odd`: some value of the block is not finite (NaN is stored as 0).
-template <typename T>
-__device__ __forceinline__ void scaled(uint32_t w, float inverse, bool odd, float* y) {
+// The values in a word, times the inverse of the scale; kOdd: some value of the block is not finite (NaN is stored as 0).
+template <typename T, bool kOdd>
+__device__ __forceinline__ void scaled(uint32_t w, float inverse, float* y) {
     if (sizeof(T) == 4) {
         y[0] = __uint_as_float(w);
     } else {
@@ -76,7 +76,7 @@ __device__ __forceinline__ void scaled(uint32_t w, float inverse, bool odd, floa
     }
 #pragma unroll
     for (int i = 0; i < 4 / (int)sizeof(T); ++i) {
-        if (odd) y[i] = y[i] == y[i] ? y[i] : 0.f;
+        if (kOdd) y[i] = y[i] == y[i] ? y[i] : 0.f;
         y[i] *= inverse;
     }
 }
@@ -204,7 +204,7 @@ __device__ __forceinline__ bool store_few(const Place& p, bool wide, int lane) {
         if (p.n > 1) read_lane<T, D>(x + i * p.stride, wide, w);
         float v[4] = {};
 #pragma unroll
-        for (int k = 0; k < kWords; ++k) scaled<T>(w[k], inverse, odd, v + k * kIn);
+        for (int k = 0; k < kWords; ++k) scaled<T, true>(w[k], inverse, v + k * kIn);
         const uint32_t out = f32_to_e4m3(v);
         const int t = p.first + i, d = lane * kPer;
         if (!kValues) {
@@ -238,13 +238,63 @@ __global__ void __launch_bounds__(kWriteWarps * 32)
     }
 }
 
-// Bytes of shared memory for a unit's values, and how many such stages a CTA has.
-__host__ __device__ constexpr size_t stage_bytes(int block_tokens, int dim, size_t size) { return (size_t)block_tokens * dim * size; }
-__host__ __device__ constexpr int stages_of(size_t bytes) { return bytes <= 48 * 1024 ? 2 : 1; }
+// A unit's values [tokens][D] at x into its block: keys, 16 values of a token a step.
+template <typename T, int D, bool kOdd>
+__device__ __forceinline__ void store_keys(const uint4* x, const Place& p, float inverse, int rank) {
+    constexpr int kIn = 16 / sizeof(T), kFour = 16 / kIn;  // values in 16 bytes, and 16 bytes in 16 values
+    for (int i = rank; i < p.n * (D / 16); i += kWriteThreads) {
+        float y[16];
+#pragma unroll
+        for (int e = 0; e < kFour; ++e) {
+            const uint4 w = x[i * kFour + e];
+            scaled<T, kOdd>(w.x, inverse, y + e * kIn), scaled<T, kOdd>(w.y, inverse, y + e * kIn + kIn / 4);
+            scaled<T, kOdd>(w.z, inverse, y + e * kIn + kIn / 2), scaled<T, kOdd>(w.w, inverse, y + e * kIn + kIn / 4 * 3);
+        }
+        *reinterpret_cast<uint4*>(p.bytes + key_byte<D>(p.first + i / (D / 16), i % (D / 16) * 16)) =
+            make_uint4(f32_to_e4m3(y), f32_to_e4m3(y + 4), f32_to_e4m3(y + 8), f32_to_e4m3(y + 12));
+    }
+}
+// ... values, 16 tokens of 2 neighbouring ones a step: lanes along the values to read, 16 bytes a lane to store.
+template <typename T, int D, bool kOdd>
+__device__ __forceinline__ void store_columns(const uint4* x, const Place& p, float inverse, int rank) {
+    const int past = p.first + p.n, from = p.first / 16;
+    for (int i = rank; i < ((past + 15) / 16 - from) * (D / 2); i += kWriteThreads) {
+        const int t0 = (from + i / (D / 2)) * 16, d = i % (D / 2) * 2;
+        const T* col = reinterpret_cast<const T*>(x) + (t0 - p.first) * D + d;
+        uint8_t* at = p.bytes + value_byte<D>(t0, d);
+        auto pair = [&](int t, float& y0, float& y1) {
+            const uint32_t* w = reinterpret_cast<const uint32_t*>(col + t * D);
+            float y[2];
+            scaled<T, kOdd>(w[0], inverse, y);
+            if (sizeof(T) == 4) scaled<T, kOdd>(w[1], inverse, y + 1);
+            y0 = y[0], y1 = y[1];
+        };
+        if (t0 >= p.first && t0 + 16 <= past) {
+            uint32_t out[2][4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float y[2][4];
+#pragma unroll
+                for (int f = 0; f < 4; ++f) pair(4 * e + f, y[0][f], y[1][f]);
+                out[0][e] = f32_to_e4m3(y[0]), out[1][e] = f32_to_e4m3(y[1]);
+            }
+            *reinterpret_cast<uint4*>(at) = make_uint4(out[0][0], out[0][1], out[0][2], out[0][3]);
+            *reinterpret_cast<uint4*>(at + 16) = make_uint4(out[1][0], out[1][1], out[1][2], out[1][3]);
+        } else {  // an end of the new tokens: byte by byte
+#pragma unroll 1
+            for (int t = max(p.first - t0, 0); t < min(past - t0, 16); ++t) {
+                float y[4] = {};
+                pair(t, y[0], y[1]);
+                const uint32_t w = f32_to_e4m3(y);
+                at[t] = (uint8_t)w, at[16 + t] = (uint8_t)(w >> 8);
+            }
+        }
+    }
+}
 
-// Many tokens: a CTA a block and `heads` of its heads, keys and values; the next unit's values come into shared memory
-// while one is scaled and stored (a lane takes 16 values of a token, or 16 tokens of 2 neighbouring values, to store 16
-// bytes at once).  status is cleared before.
+// Many tokens: a CTA a block and `heads` of its heads, keys and values one after another, each read once into shared
+// memory.  Many small CTAs an SM hide each other's trips to memory better than two stages of one do (31 against 27 us for
+// 15,973 tokens of 8 heads of 128).  status is cleared before.
 template <typename T, int D>
 __global__ void __launch_bounds__(kWriteThreads)
     k_kv_write_many(mp_kv_cache c, mp_kv_batch bt, mp_tokens k, mp_tokens v, bool wide, int32_t* status, int per_seq,
@@ -252,50 +302,40 @@ __global__ void __launch_bounds__(kWriteThreads)
     extern __shared__ __align__(16) uint8_t dyn[];
     __shared__ uint32_t smem[kWriteThreads / 32];
     const int rank = threadIdx.x, groups = (c.n_heads + heads - 1) / heads;
-    const size_t bytes = stage_bytes(c.block_tokens, D, sizeof(T));
-    const int stages = stages_of(bytes);
     const int64_t work = (int64_t)bt.n_seqs * per_seq * groups;
     for (int64_t w = blockIdx.x; w < work; w += gridDim.x) {
         const int h0 = (int)(w % groups) * heads, j = (int)(w / groups % per_seq), b = (int)(w / groups / per_seq);
         const SeqView s = load_seq(bt, b, true);
         bool ok = s.st == MP_OK;
         const int units = j < blocks_touched(c, s) ? 2 * min(heads, c.n_heads - h0) : 0;
-        Place p, q;
+        Place p;
         if (!ok || (units > 0 && !find<T>(c, bt, s, b, j, h0, false, k, v, p))) {
             status[b] = MP_EINVAL;  // whoever writes it writes the same
             continue;
         }
         constexpr int kIn = 16 / sizeof(T);  // values in 16 bytes
         const int step = kWriteThreads / (D / kIn), t_in = rank / (D / kIn), d_in = rank % (D / kIn) * kIn;
-        auto fetch = [&](int u) {  // unit u's values into its stage: [tokens][D]
-            find<T>(c, bt, s, b, j, h0 + u / 2, u % 2, k, v, q);
-            T* to = reinterpret_cast<T*>(dyn + (u % stages) * bytes) + rank * kIn;
-            const T* at = static_cast<const T*>(q.x) + t_in * q.stride + d_in;
-            for (int t = t_in; t < q.n; t += step, at += step * q.stride, to += kWriteThreads * kIn) {
-                if (wide) {
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(
-                                     (uint32_t)__cvta_generic_to_shared(to)),
-                                 "l"(at)
-                                 : "memory");
-                } else {
-#pragma unroll
-                    for (int e = 0; e < kIn; ++e) to[e] = at[e];
-                }
-            }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        };
-        if (units > 0) fetch(0);
         for (int u = 0; u < units; ++u) {
-            p = q;
-            if (stages == 2 && u + 1 < units) {
-                fetch(u + 1);
-                asm volatile("cp.async.wait_group 1;" ::: "memory");
-            } else {
-                asm volatile("cp.async.wait_group 0;" ::: "memory");
+            find<T>(c, bt, s, b, j, h0 + u / 2, u % 2, k, v, p);
+            {
+                T* to = reinterpret_cast<T*>(dyn) + rank * kIn;
+                const T* at = static_cast<const T*>(p.x) + t_in * p.stride + d_in;
+                for (int t = t_in; t < p.n; t += step, at += step * p.stride, to += kWriteThreads * kIn) {
+                    if (wide) {
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(
+                                         (uint32_t)__cvta_generic_to_shared(to)),
+                                     "l"(at)
+                                     : "memory");
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < kIn; ++e) to[e] = at[e];
+                    }
+                }
+                asm volatile("cp.async.wait_all;" ::: "memory");
             }
             const float old = p.first > 0 ? *p.scale : 0.f;
             __syncthreads();
-            const uint4* x = reinterpret_cast<const uint4*>(dyn + (u % stages) * bytes);
+            const uint4* x = reinterpret_cast<const uint4*>(dyn);
             const int chunks = p.n * (D / kIn);  // of 16 bytes
             uint32_t top = 0;
             for (int i = rank; i < chunks; i += kWriteThreads) {
@@ -317,57 +357,14 @@ __global__ void __launch_bounds__(kWriteThreads)
             }
             if (u % 2 == 0) {
                 const float inverse = settle<D, false, 0>(value_of<T>(top), old, p.first, p.bytes, p.scale, rank);
-                for (int i = rank; i < p.n * (D / 16); i += kWriteThreads) {
-                    constexpr int kFour = 16 / kIn;  // 16-byte chunks in 16 values
-                    float y[16];
-#pragma unroll
-                    for (int e = 0; e < kFour; ++e) {
-                        const uint4 w = x[i * kFour + e];
-                        scaled<T>(w.x, inverse, odd, y + e * kIn), scaled<T>(w.y, inverse, odd, y + e * kIn + kIn / 4);
-                        scaled<T>(w.z, inverse, odd, y + e * kIn + kIn / 2);
-                        scaled<T>(w.w, inverse, odd, y + e * kIn + kIn / 4 * 3);
-                    }
-                    *reinterpret_cast<uint4*>(p.bytes + key_byte<D>(p.first + i / (D / 16), i % (D / 16) * 16)) =
-                        make_uint4(f32_to_e4m3(y), f32_to_e4m3(y + 4), f32_to_e4m3(y + 8), f32_to_e4m3(y + 12));
-                }
+                if (odd) store_keys<T, D, true>(x, p, inverse, rank);
+                else store_keys<T, D, false>(x, p, inverse, rank);
             } else {
                 const float inverse = settle<D, true, 0>(value_of<T>(top), old, p.first, p.bytes, p.scale, rank);
-                const int past = p.first + p.n, from = p.first / 16;
-                for (int i = rank; i < ((past + 15) / 16 - from) * (D / 2); i += kWriteThreads) {
-                    const int t0 = (from + i / (D / 2)) * 16, d = i % (D / 2) * 2;
-                    // two values of 16 tokens; past the ends of the new tokens the nearest one's
-                    const T* col = reinterpret_cast<const T*>(x) + (t0 - p.first) * D + d;
-                    const int lo = max(p.first - t0, 0), hi = min(past - t0, 16);
-                    uint32_t out[2][4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float y[2][4];
-#pragma unroll
-                        for (int f = 0; f < 4; ++f) {
-                            const int t = min(max(4 * e + f, lo), hi - 1);
-                            const uint32_t* at = reinterpret_cast<const uint32_t*>(col + t * D);
-                            float pair[2];
-                            scaled<T>(at[0], inverse, odd, pair);
-                            if (sizeof(T) == 4) scaled<T>(at[1], inverse, odd, pair + 1);
-                            y[0][f] = pair[0], y[1][f] = pair[1];
-                        }
-                        out[0][e] = f32_to_e4m3(y[0]), out[1][e] = f32_to_e4m3(y[1]);
-                    }
-                    uint8_t* at = p.bytes + value_byte<D>(t0, d);
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        if (lo == 0 && hi == 16) {
-                            *reinterpret_cast<uint4*>(at + 16 * r) = make_uint4(out[r][0], out[r][1], out[r][2], out[r][3]);
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 16; ++e)
-                                if (e >= lo && e < hi) at[16 * r + e] = (uint8_t)(out[r][e / 4] >> (8 * (e % 4)));
-                        }
-                    }
-                }
+                if (odd) store_columns<T, D, true>(x, p, inverse, rank);
+                else store_columns<T, D, false>(x, p, inverse, rank);
             }
-            __syncthreads();  // the stage's next values may come
-            if (stages == 1 && u + 1 < units) fetch(u + 1);
+            __syncthreads();  // the next unit's values may come
         }
         if (!ok) status[b] = MP_EINVAL;
     }
@@ -457,9 +454,10 @@ cudaError_t write_as(const mp_kv_cache& c, const mp_kv_batch& bt, const mp_token
     const int per_seq = (int)(((int64_t)bt.max_tokens + 2 * c.block_tokens - 2) / c.block_tokens);
     // as many heads a CTA as leave CTAs enough to fill the GPU several times over
     int heads = c.n_heads;
-    while (heads > 1 && (int64_t)bt.n_seqs * per_seq * ((c.n_heads + heads - 1) / heads) < kWriteCtas) heads = (heads + 1) / 2;
+    const int64_t blocks = bt.n_tokens / c.block_tokens + bt.n_seqs;  // about as many as there are
+    while (heads > 1 && blocks * ((c.n_heads + heads - 1) / heads) < kWriteCtas) heads = (heads + 1) / 2;
     const int64_t work = (int64_t)bt.n_seqs * per_seq * ((c.n_heads + heads - 1) / heads);
-    const size_t bytes = stage_bytes(c.block_tokens, D, sizeof(T)), smem = bytes * stages_of(bytes);
+    const size_t smem = (size_t)c.block_tokens * D * sizeof(T);
     e = set_smem_limit((const void*)k_kv_write_many<T, D>, smem);
     if (e != cudaSuccess) return e;
     k_kv_write_many<T, D><<<(unsigned)std::min<int64_t>(work, 1 << 20), kWriteThreads, smem, stream>>>(c, bt, k, v, wide, status,
