@@ -56,6 +56,7 @@ class KvCache:
         self._struct = _lib.MpKvCache(n_blocks, block_tokens, n_heads, head_dim, _ptr(self.k), _ptr(self.v),
                                       _ptr(self.k_scale), _ptr(self.v_scale))
         self._ref = ctypes.byref(self._struct)
+        self._key, self._index = (block_tokens, n_heads, head_dim), self.k.get_device()
 
     @staticmethod
     def block_bytes(block_tokens: int, n_heads: int, head_dim: int) -> int:
@@ -81,33 +82,37 @@ class KvBatch:
         self.max_tokens = self.n_tokens if max_tokens is None else int(max_tokens)
         self.max_len = max_len
         self.n_seqs, self.device = B, table.device
-        self._structs, self._needs = {}, {}
+        self._made = {}
 
-    def _ref(self, cache: KvCache):
-        ref = self._structs.get(cache.block_tokens)
-        if ref is None:
+    def _for(self, cache: KvCache):
+        """What calls with this batch and a cache of that shape share: the C struct, the shape of the call's keys and
+        values, and the scratch by number of query heads."""
+        made = self._made.get(cache._key)
+        if made is None:
+            if cache.device != self.device:
+                raise ValueError(f"the batch is on {self.device}, the cache on {cache.device}")
             room = self.table.shape[1] * cache.block_tokens
             s = _lib.MpKvBatch(self.n_seqs, self.table.shape[1], self.max_tokens,
                                room if self.max_len is None else int(self.max_len), self.n_tokens, _ptr(self.table),
                                _ptr(self.lens), _ptr(self.token_ptr))
-            ref = self._structs[cache.block_tokens] = ctypes.byref(s)
-        return ref
+            made = self._made[cache._key] = (ctypes.byref(s), (self.n_tokens, cache.n_heads, cache.head_dim), {})
+        return made
 
 
-def _tokens(name, t, cache, batch, n_heads=None):
-    shape, strides = t.shape, t.stride()
-    if len(shape) != 3 or shape[0] != batch.n_tokens or shape[2] != cache.head_dim or \
-            (n_heads is not None and shape[1] != n_heads):
-        raise ValueError(f"{name}: shape [{batch.n_tokens}, {n_heads or 'heads'}, {cache.head_dim}] is needed, "
-                         f"got {list(shape)}")
-    if strides[2] != 1 and shape[0] > 0:
+def _tokens(name, t, cache, shape):
+    """The C struct of a tensor, after the checks; shape: what it has to be, heads None if any number will do."""
+    have = t.shape
+    if have != shape and (shape[1] is not None or len(have) != 3 or have[0] != shape[0] or have[2] != shape[2]):
+        raise ValueError(f"{name}: shape [{shape[0]}, {shape[1] or 'heads'}, {shape[2]}] is needed, got {list(have)}")
+    token, head, last = t.stride()
+    if last != 1 and have[0] > 0:
         raise ValueError(f"{name}: the values of a head have to be dense")
     dtype = _DTYPES.get(t.dtype)
     if dtype is None:
         raise ValueError(f"{name}: float16, bfloat16 or float32 is needed, got {t.dtype}")
-    if t.device != cache.device:
+    if t.get_device() != cache._index:
         raise ValueError(f"{name} is on {t.device}, the cache on {cache.device}")
-    return _lib.MpTokens(t.data_ptr() or None, strides[0], strides[1], shape[1], dtype)
+    return _lib.MpTokens(t.data_ptr() or None, token, head, have[1], dtype)
 
 
 def _fresh(t, heads, dim):  # a dense tensor that this module has made
@@ -120,9 +125,8 @@ def _status(status, batch):
     return _tensor("status", status, torch.int32, (batch.n_seqs,), batch.device)
 
 
-def _stream(device):
-    # torch.cuda.current_stream() builds a Stream object: 5 us of a call's 22
-    return torch._C._cuda_getCurrentRawStream(device.index)
+# torch.cuda.current_stream() builds a Stream object: 5 us of a call's 22
+_stream = torch._C._cuda_getCurrentRawStream
 
 
 _workspaces = {}
@@ -143,11 +147,10 @@ def kv_write(cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tensor, s
     if stream is not None:
         with torch.cuda.stream(stream):
             return kv_write(cache, batch, k, v, status)
-    kt = _tokens("k", k, cache, batch, cache.n_heads)
-    vt = _tokens("v", v, cache, batch, cache.n_heads)
+    ref, shape, _ = batch._for(cache)
+    kt, vt = _tokens("k", k, cache, shape), _tokens("v", v, cache, shape)
     status = _status(status, batch)
-    _check("mp_kv_write", _lib.load().mp_kv_write(cache._ref, batch._ref(cache), kt, vt, status.data_ptr() or None,
-                                                  _stream(cache.device)))
+    _check("mp_kv_write", _lib.load().mp_kv_write(cache._ref, ref, kt, vt, status.data_ptr() or None, _stream(cache._index)))
     return status
 
 
@@ -156,28 +159,30 @@ def kv_read(cache: KvCache, batch: KvBatch, dtype=torch.bfloat16, k=None, v=None
     if stream is not None:
         with torch.cuda.stream(stream):
             return kv_read(cache, batch, dtype, k, v, status)
-    heads, dim = cache.n_heads, cache.head_dim
-    outs = []
-    for name, t in (("k", k), ("v", v)):
-        if t is None:
-            if dtype not in _DTYPES:
-                raise ValueError(f"float16, bfloat16 or float32 can be read, not {dtype}")
-            t = torch.empty((batch.n_tokens, heads, dim), dtype=dtype, device=cache.device)
-            outs += [t, _fresh(t, heads, dim)]
-        else:
-            outs += [t, _tokens(name, t, cache, batch, heads)]
-    k, kt, v, vt = outs
+    ref, shape, _ = batch._for(cache)
+    if k is not None:
+        kt = _tokens("k", k, cache, shape)
+    if v is not None:
+        vt = _tokens("v", v, cache, shape)
+    if k is None or v is None:
+        if dtype not in _DTYPES:
+            raise ValueError(f"float16, bfloat16 or float32 can be read, not {dtype}")
+        if k is None:
+            k = torch.empty(shape, dtype=dtype, device=cache.device)
+            kt = _fresh(k, shape[1], shape[2])
+        if v is None:
+            v = torch.empty_like(k) if k.is_contiguous() and k.dtype == dtype else torch.empty(shape, dtype=dtype, device=cache.device)
+            vt = _fresh(v, shape[1], shape[2])
     status = _status(status, batch)
-    _check("mp_kv_read", _lib.load().mp_kv_read(cache._ref, batch._ref(cache), kt, vt, status.data_ptr() or None,
-                                                _stream(cache.device)))
+    _check("mp_kv_read", _lib.load().mp_kv_read(cache._ref, ref, kt, vt, status.data_ptr() or None, _stream(cache._index)))
     return k, v, status
 
 
 def kv_attend_workspace_bytes(cache: KvCache, batch: KvBatch, n_q_heads: int) -> int:
-    key = (n_q_heads, cache.n_heads, cache.head_dim, cache.block_tokens)
-    need = batch._needs.get(key)
+    ref, _, needs = batch._for(cache)
+    need = needs.get(n_q_heads)
     if need is None:
-        need = batch._needs[key] = int(_lib.load().mp_kv_attend_workspace_bytes(cache._ref, batch._ref(cache), n_q_heads))
+        need = needs[n_q_heads] = int(_lib.load().mp_kv_attend_workspace_bytes(cache._ref, ref, n_q_heads))
     return need
 
 
@@ -190,25 +195,26 @@ def kv_attend(cache: KvCache, batch: KvBatch, q: torch.Tensor, scale: float | No
     if stream is not None:
         with torch.cuda.stream(stream):
             return kv_attend(cache, batch, q, scale, causal, window, out, lse, want_lse, status, workspace)
-    lib = _lib.load()
-    qt = _tokens("q", q, cache, batch)
-    heads = q.shape[1]
+    ref, shape, needs = batch._for(cache)
+    qt = _tokens("q", q, cache, (shape[0], None, shape[2]))
+    heads = qt.n_heads
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        ot = _fresh(out, heads, cache.head_dim)
+        ot = _fresh(out, heads, shape[2])
     else:
-        ot = _tokens("out", out, cache, batch, heads)
+        ot = _tokens("out", out, cache, (shape[0], heads, shape[2]))
     if lse is not None:
-        _tensor("lse", lse, torch.float32, (batch.n_tokens, heads), cache.device)
+        _tensor("lse", lse, torch.float32, (shape[0], heads), cache.device)
     elif want_lse:
-        lse = torch.empty((batch.n_tokens, heads), dtype=torch.float32, device=q.device)
+        lse = torch.empty((shape[0], heads), dtype=torch.float32, device=q.device)
     status = _status(status, batch)
-    stream_ptr = _stream(cache.device)
-    ref = batch._ref(cache)
-    need = kv_attend_workspace_bytes(cache, batch, heads)
+    stream_ptr = _stream(cache._index)
+    need = needs.get(heads)
+    if need is None:
+        need = kv_attend_workspace_bytes(cache, batch, heads)
     wptr, wbytes = (workspace or _workspace_of(stream_ptr, cache.device)).get(need) if need else (None, 0)
     _check("mp_kv_attend",
-           lib.mp_kv_attend(cache._ref, ref, qt, cache.head_dim ** -0.5 if scale is None else scale, 1 if causal else 0,
-                            window, ot, None if lse is None else lse.data_ptr() or None, status.data_ptr() or None, wptr,
-                            wbytes, stream_ptr))
+           _lib.load().mp_kv_attend(cache._ref, ref, qt, shape[2] ** -0.5 if scale is None else scale, 1 if causal else 0,
+                                    window, ot, None if lse is None else lse.data_ptr() or None, status.data_ptr() or None,
+                                    wptr, wbytes, stream_ptr))
     return out, lse, status
