@@ -720,6 +720,10 @@ __global__ void __launch_bounds__(kJoinThreads) k_kv_join(AttendArgs a, FewWork 
     }
 }
 
+// Sequences of few rows in a batch that also has many: k_kv_attend_many takes them at about 2.5 TB/s of cache bytes, which
+// up to this size costs less than the other kernel with its joining (8 heads of 128, GPU time without and with it:
+// 16 x 1,000 tokens 31 and 45 us, 8 x 4,000 96 and 145, 3 x 4,000-16,384 157 and 161).
+constexpr int64_t kSmallCache = 256 << 20;
 // Which kernels a batch needs, by its host scalars: sequences of at most kFewRows rows are
 // bound by the cache's bytes, which k_kv_attend_few streams; above it the products count.
 // A batch whose sequences all have max_tokens has no sequence for the first.
@@ -737,7 +741,8 @@ Route route(const mp_kv_cache& c, const mp_kv_batch& bt, int32_t group, int32_t 
         const bool brief = span <= kShortLen && (int64_t)bt.n_seqs * c.n_heads <= kShortCtas;
         return {!brief, false, brief};
     }
-    return {bt.n_tokens != (int64_t)bt.n_seqs * bt.max_tokens, true, false};
+    const int64_t bytes = (int64_t)bt.n_seqs * bt.max_len * c.n_heads * c.head_dim * 2;
+    return {bt.n_tokens != (int64_t)bt.n_seqs * bt.max_tokens && bytes > kSmallCache, true, false};
 }
 
 struct Layout {
@@ -793,11 +798,12 @@ cudaError_t attend_as(const AttendArgs& a, const FewWork& few, const ManyWork& m
         if (e != cudaSuccess) return e;
         plan.cuts = kManyCtas * (D / kJoinCols);
     }
-    // few rows in all are cut into many parts each, which a CTA's warps share (64 rows of 76 parts: 18 -> 5 us); many rows
-    // into two or three, a warp a row (2,048 rows: 12 -> 7 us)
+    // rows that are cut into many parts have a CTA each, whose warps share the parts (64 rows of 76 parts: 18 -> 5 us), the
+    // others a warp (2,048 rows of two or three: 12 -> 7 us)
     constexpr int kWarps = kJoinThreads / 32;
-    if (rows <= 4 * kFewCtas) {
-        plan.row_ctas = (int)rows;
+    const int64_t parts = kFewCtas * few_warps(NT) / ((int64_t)a.bt.n_seqs * a.c.n_heads);
+    if (rows <= 8 * kFewCtas || parts > 12) {
+        plan.row_ctas = (int)std::min<int64_t>(rows, 1 << 20);
         return launch_close(k_kv_join<T, D, NT, kWarps>, plan.cuts + plan.checks + plan.row_ctas, kJoinThreads, 0, stream, a,
                             few, many, plan);
     }
