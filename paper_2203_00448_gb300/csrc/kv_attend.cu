@@ -1,14 +1,14 @@
 // kv_attend.cu -- mp_kv_attend for few query rows a sequence and head (single
-// tokens, a few proposed ones), and the joining of split sequences.
+// tokens, a few proposed ones), the joining of split sequences, and the choice of kernels.
 //
 // A work unit is one granule (32 tokens) of one cache head under one tile of 8 * NT
-// query rows (rows = tokens x heads of a group, which share the cached head).  The
-// units of all sequences, tiles and heads lie on one line that is cut evenly among
-// the warps of the grid, so ragged batches and single long contexts keep every SM
-// at the memory alike; a warp walks its stretch with bulk copies into a ring of
+// query rows (rows = tokens x heads of a group, which share the cached head).
+// k_kv_attend_few: the units of all sequences, tiles and heads lie on one line that is cut
+// evenly among the warps of the grid, so ragged batches and single long contexts keep every
+// SM at the memory alike; a warp walks its stretch with bulk copies into a ring of
 // its own, no warp waiting for another.  A (sequence, tile, head) that one warp holds
 // whole is written at once; the others leave (sum, reference, weighted values) and
-// k_kv_join adds them up.
+// k_kv_join adds them up.  k_kv_attend_short: a CTA a (sequence, head) for short contexts.
 //
 // Per granule: scores S^T = K Q^T and O^T += V^T P^T on warp-level matrix products
 // in f16, rows of the stored tiles as the left operand, so that 8 query rows cost one
@@ -18,6 +18,11 @@
 // sum w_j byte_j / sum (w_j / value scale): the value scale costs nothing per element
 // and products stay within f16's range whatever the scales.  Sums are f32; w is
 // rounded to f16 (11 bits, down to 2^-38 of the largest).
+//
+// Measured (32 heads over 8 of 128): 64 ragged contexts of up to 8,191 tokens 97 us, 5.5
+// TB/s of the 6.8 that a copy reaches; two of 262,144 tokens 170 us, 6.1 TB/s; one of 512 6.6
+// us of GPU time.  Long contexts are bound by memory; the rest is the ramp (lengths, table,
+// queries, first bytes: four trips one after another) and the joining launch, about 12 us.
 #include <algorithm>
 #include <cmath>
 
@@ -26,9 +31,12 @@
 namespace mp {
 namespace {
 
-// Warps of a CTA, and granules that the ring of each holds: 192 KB in all (D = 128).
-constexpr int few_warps(int nt) { return nt == 1 ? 12 : 8; }
-constexpr int few_stages(int nt) { return nt == 1 ? 2 : 3; }
+// Warps of a CTA, and granules that the ring of each holds (192 KB at most in all). Registers bound the warps, an even
+// share for the four schedulers: 12 of D = 128 with 16 rows spill (64 ragged contexts 127 -> 153 us, 10 160), 12 instead of
+// 16 of D = 64 with 8 rows take 66 for 60 us. 8 with 3 granules for 12 with 2: 164 for 170 us over two of 262,144 tokens,
+// but 103 for 97 over 64 ragged ones; 3 granules for 2 never paid otherwise (130 for 127).
+constexpr int few_warps(int d, int nt) { return d == 128 ? (nt == 1 ? 12 : 8) : (nt == 1 ? 16 : 12); }
+constexpr int kFewStages = 2;
 constexpr int short_warps(int nt) { return nt == 1 ? 16 : 8; }
 constexpr int kFewRows = 16;  // most rows of a sequence and head
 constexpr int kJoinThreads = 256;
@@ -270,8 +278,8 @@ struct Tile {
 };
 
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(few_warps(NT) * 32, 1) k_kv_attend_few(AttendArgs a, FewWork work) {
-    constexpr int kFewWarps = few_warps(NT), kFewStages = few_stages(NT);
+__global__ void __launch_bounds__(few_warps(D, NT) * 32, 1) k_kv_attend_few(AttendArgs a, FewWork work) {
+    constexpr int kFewWarps = few_warps(D, NT);
     constexpr int kRows = 8 * NT;
     constexpr int kBytes = kGranule * D;  // of either array
     extern __shared__ __align__(128) uint8_t dyn[];
@@ -752,7 +760,7 @@ struct Layout {
 Layout layout(const mp_kv_cache& c, const mp_kv_batch& bt, int32_t group) {
     Layout l = {};
     const Route r = route(c, bt, group, 0);
-    const size_t warps = (size_t)kFewCtas * few_warps(1);
+    const size_t warps8 = few_warps(c.head_dim, 1), warps16 = few_warps(c.head_dim, 2);
     auto take = [&](size_t bytes) {
         const size_t at = l.bytes;
         l.bytes += align_up(bytes);
@@ -760,8 +768,8 @@ Layout layout(const mp_kv_cache& c, const mp_kv_batch& bt, int32_t group) {
     };
     if (r.few) {
         l.base = take(sizeof(int64_t) * ((size_t)bt.n_seqs + 2));
-        l.gave_up = take(sizeof(int32_t) * warps);
-        l.part = take(sizeof(float) * 2 * kFewCtas * std::max(8 * few_warps(1), 16 * few_warps(2)) * (size_t)(c.head_dim + 2));
+        l.gave_up = take(sizeof(int32_t) * kFewCtas * std::max(warps8, warps16));
+        l.part = take(sizeof(float) * 2 * kFewCtas * std::max(8 * warps8, 16 * warps16) * (size_t)(c.head_dim + 2));
     }
     if (r.many) {
         l.starts = take(sizeof(ManyStart) * kManyCtas);
@@ -786,10 +794,10 @@ cudaError_t attend_as(const AttendArgs& a, const FewWork& few, const ManyWork& m
     plan.checks = std::min(a.bt.n_seqs, 1024);
     int64_t rows = 0;
     if (few.base != nullptr) {
-        constexpr size_t smem = (size_t)few_warps(NT) * few_stages(NT) * 2 * kGranule * D;
+        constexpr size_t smem = (size_t)few_warps(D, NT) * kFewStages * 2 * kGranule * D;
         e = set_smem_limit((const void*)k_kv_attend_few<T, D, NT>, smem);
         if (e == cudaSuccess)
-            e = launch_close(k_kv_attend_few<T, D, NT>, kFewCtas, few_warps(NT) * 32, smem, stream, a, few);
+            e = launch_close(k_kv_attend_few<T, D, NT>, kFewCtas, few_warps(D, NT) * 32, smem, stream, a, few);
         if (e != cudaSuccess) return e;
         rows = (int64_t)a.bt.n_seqs * join_rows(a) * a.c.n_heads;
     }
@@ -801,7 +809,7 @@ cudaError_t attend_as(const AttendArgs& a, const FewWork& few, const ManyWork& m
     // rows that are cut into many parts have a CTA each, whose warps share the parts (64 rows of 76 parts: 18 -> 5 us), the
     // others a warp (2,048 rows of two or three: 12 -> 7 us)
     constexpr int kWarps = kJoinThreads / 32;
-    const int64_t parts = kFewCtas * few_warps(NT) / ((int64_t)a.bt.n_seqs * a.c.n_heads);
+    const int64_t parts = kFewCtas * few_warps(D, NT) / ((int64_t)a.bt.n_seqs * a.c.n_heads);
     if (rows <= 8 * kFewCtas || parts > 12) {
         plan.row_ctas = (int)std::min<int64_t>(rows, 1 << 20);
         return launch_close(k_kv_join<T, D, NT, kWarps>, plan.cuts + plan.checks + plan.row_ctas, kJoinThreads, 0, stream, a,

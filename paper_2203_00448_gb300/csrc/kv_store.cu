@@ -5,8 +5,13 @@
 // max |x| <= 448 s (448 is the largest e4m3 value).  Dividing by it is exact, so a
 // stored value carries the one rounding to e4m3's 4 significant bits, whatever the
 // scale; when a later token makes the scale grow, earlier bytes are rounded again,
-// which loses bits only among subnormals.  Both kernels move each byte once and
-// are bound by memory (prompts) or by the latency of a launch (single tokens).
+// which loses bits only among subnormals.
+//
+// Measured (8 heads of 128): a step of 253 single tokens 4.9 us of GPU time, bound by
+// three trips to memory one after another (lengths, table, values and scale); 15,973
+// prompt tokens 27 us (98 MB, 14.4 us at the rate of a copy), bound by instructions
+// (two thirds of the issue slots while CTAs run) and the uneven last CTAs; 131,071 tokens
+// read back 126 us, 94% of a copy's rate.
 #include <algorithm>
 
 #include "kv.cuh"
