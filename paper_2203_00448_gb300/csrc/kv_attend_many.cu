@@ -2,21 +2,38 @@
 // of prompts): both products on the fifth-generation tensor cores.
 //
 // Rows are tokens x heads of a group, so a tile of 128 rows shares the cached head
-// whatever the group.  A CTA works on two such tiles: while one's scores become weights
-// (a thread a row), the tensor cores work for the other.  Warps 0-3 and 4-7: softmax of
-// tile 0 and 1; warps 8-11 turn the stored bytes of 128 tokens into f16 operands in
-// shared memory (exact; two hardware conversions for 4 bytes, 8 thread operations a
-// clock less than a third of what the products leave free); one thread of warp 12 issues
-// every product.  Scores (128 x 128 f32) and sums (128 x D f32) of both tiles fill the
-// 512 columns of tensor memory; weights go back as f16 over the scores they came from
-// and are the left operand of the second product from there.  The softmax is that of the
-// kernel for few rows (the value scale in the exponent), but a row's sums are rescaled
-// only when its maximum has grown by 2^8.
+// whatever the group.  A CTA works on two such tiles against the same 128 tokens (a unit),
+// or, where there is one tile only, on two units in turn, whose sums are added up at the end.
+// Warps 0-3 and 4-7, a thread a row: softmax of tile 0 and 1.  Warps 8-11: stored bytes
+// become f16 operands in shared memory, exactly, two hardware conversions for 4 bytes
+// (59 thread operations a clock and SM; spreading bytes with integer operations: 16).
+// Warps 12 and 13: the products of tile 0 and 1.  Warp 14: the work list.  Scores (128 x 128
+// f32) and sums (128 x D f32) of both tiles fill the 512 columns of tensor memory; weights
+// go back as f16 over the scores they came from and are the left operand of the second
+// product from there, so that the next scores wait for it to end.
 //
-// (sequence, row tile pair, head, 128 tokens) units lie on a line that is cut evenly
-// among 152 CTAs, so that causal rows, ragged prompts and a short piece over a long
-// context all end together; what a CTA does not hold whole is added up by
+// x_j = scale * q.k_j * log2(e) * key scale + log2(value scale) as in kv_attend.cu; a row's
+// sums are rescaled only when its maximum has grown by 2^8, which weights as f16 (at most
+// 2^15 here, down to 2^-24) leave room for.
+//
+// (sequence, pair of row tiles, head, unit) lie on a line that is cut evenly among 152 CTAs,
+// so that causal rows, ragged prompts and a short piece over a long context all end
+// together; a pair's beginning and end count as 3 units (a prompt of 8,000 tokens with 1: 671
+// us, 2: 547, 3: 466, 5: 468).  What a CTA does not hold whole is added up by
 // k_kv_join.
+//
+// Measured: 8,000 tokens, 32 heads over 8 of 128: 470 us, 1,116 TFLOP/s counted causally; 64
+// tokens over 60,000 each for 8 sequences: 400 us, 1,260 TFLOP/s (cuBLAS bf16: 1,887); 8 tokens
+// over 64 ragged contexts of up to 8,191: 218 us (251 with one tile at work), 5 to 8 over four of
+// 60,000: 187 (217); the two ways of working cost prompts 1 to 2%.  A unit of both tiles takes
+// 3,900 cycles where its 32 products take 2,080 on their own: the converting warps are busy or
+// wait for loads through most of it, both tiles' products and both tiles' exponentials tend to
+// come together, and products, operands and loads share one shared-memory pipe (about 70% busy).
+// Dropped after measuring: the tiles taking turns at the exponentials, a quarter of the
+// exponentials as polynomials, scores of 64 tokens in columns of their own, which the next
+// scores need not wait for (466 -> 487 us: narrower products read the queries twice as often), two
+// threads a row (1,038 -> 1,059), prefetches of the units to come into L2 (480 for 465), table entries
+// and scales fetched by a warp of their own (473 for 464).
 #include <algorithm>
 #include <cmath>
 
@@ -37,7 +54,7 @@ constexpr int kLineReaders = kSoftmaxWarps + 4 + 2;  // warps that read a stretc
 constexpr int kThreads = 16 * 32;
 // Registers a thread after the roles part: 256 x 176 + 128 x 112 + 128 x 48 = 512 x 128, the launch's.
 constexpr int kSoftmaxRegs = 176, kConvertRegs = 112, kProductRegs = 48;
-constexpr int kTries = (int)(kKvSpinCycles >> 10);
+constexpr int kTries = (int)(kKvSpinCycles >> 8);  // of a wait: some tens of cycles each
 constexpr int kStrips = 1024;
 constexpr float kGrow = 8.f;
 
@@ -121,7 +138,7 @@ struct Stretch {
     int b, tile, head;
     int cnt, k;              // units of the whole, the first of this stretch
     int units;               // of this stretch; 0: the CTA has no more
-    int tiles;               // 1 or 2 of the pair have rows
+    int tiles;               // 1 or 2 of the pair have rows; 1: both work on these, tile i on the units i, i + 2, ..
     int first;               // of its CTA
     int first_gran, grans;   // granules that the pair's rows see
     int rows;                // of the sequence and head
@@ -209,6 +226,8 @@ struct Smem {
     uint8_t v[kStages][kTokens * D * 2];
     int64_t strip[kStrips];
     float scales[kScaleRing][3][kGrans];  // key scale, log2 of the value scale, 1 / value scale
+    float tops[2][kRows], sums[2][kRows];  // of rows that both tiles worked on
+    uint64_t posted, added;                // ... are there; ... have been added up
     uint64_t q_full[2], s_full[2], p_full[2], o_done[2], k_full[kStages], k_empty[kStages], v_full[kStages],
         v_empty[kStages], drained, line_full[kLineRing], line_empty[kLineRing],
         scales_full[kScaleRing];
@@ -220,8 +239,7 @@ struct Smem {
     int gave_up;
 };
 
-// Waits until the phase ends; false if some wait of the CTA has given up. A try sleeps for
-// up to 2 us, so that kTries of them are seconds.
+// Waits until the phase ends; false if some wait of the CTA has given up, which one does after kTries.
 __device__ __forceinline__ bool await(uint64_t* bar, uint32_t parity, volatile int* gave_up) {
     for (int i = 0; !mbar_try(bar, parity); ++i)
         if (i > kTries || *gave_up) {
@@ -280,19 +298,16 @@ __device__ void convert_role(const AttendArgs& a, Smem<D>& m) {
     int seg = 0, u = 0, had = 0;
     float ks = 0.f, vs = 1.f;
     // a unit's table entries are read a unit ahead, a granule a lane
-    int page = -1, in_page = 0, head = 0, next_had = 0;
-    bool more = true;  // that unit is one
+    int page = 0, in_page = 0, head = 0, next_had = 0;
+    bool more = true, there = false;  // that unit is one; it has this granule
     auto look_up = [&]() {
         if (u == 0 && !await_warp(&m.line_full[seg % kLineRing], seg / kLineRing & 1, &m.gave_up)) return false;
         const Stretch& x = m.line[seg % kLineRing];
         more = x.units > 0;
         if (!more) return true;
         const int g = (x.k + u) * kGrans + mine, gran = x.first_gran + g, col = gran / per;
-        page = -1, in_page = gran - col * per, head = x.head;
-        if (g < x.grans) {
-            page = __ldg(a.bt.table + (int64_t)x.b * a.bt.max_blocks + col);
-            if (page < 0 || page >= a.c.n_blocks) page = 0;  // k_kv_join reports it
-        }
+        in_page = gran - col * per, head = x.head, there = g < x.grans;
+        if (there) page = __ldg(a.bt.table + (int64_t)x.b * a.bt.max_blocks + col);  // looked at a unit later
         next_had = x.len - (gran - mine) * kGranule;  // tokens of the unit that are held
         if (++u == x.units) {
             release(m, seg);
@@ -303,7 +318,8 @@ __device__ void convert_role(const AttendArgs& a, Smem<D>& m) {
     auto locate = [&]() {
         int64_t here = -1;
         ks = 0.f, vs = 1.f;
-        if (page >= 0) {
+        if (there) {
+            if (page < 0 || page >= a.c.n_blocks) page = 0;  // k_kv_join reports it
             here = block_byte(a.c, page, head) + in_page * (kGranule * D);
             const int64_t sc = (int64_t)page * a.c.n_heads + head;
             ks = __ldg(a.c.k_scale + sc), vs = __ldg(a.c.v_scale + sc);
@@ -395,25 +411,21 @@ __device__ void product_role(Smem<D>& m, int tile) {
     for (;;) {
         if (!await_warp(&m.line_full[seg % kLineRing], seg / kLineRing & 1, &m.gave_up)) return;
         const int units = m.line[seg % kLineRing].units;
-        const bool has = tile < m.line[seg % kLineRing].tiles;
+        const int turns = m.line[seg % kLineRing].tiles == 1, begin = turns ? tile : 0;  // its first unit
         release(m, seg++);
         if (units == 0) return;
-        if (!has) {
+        if (begin < units && !await_warp(&m.q_full[tile], asked++ & 1, &m.gave_up)) return;
 #pragma unroll 1
-            for (int u = 0; u < units; ++u, ++it) {
-                // this tile has nothing to do with the stages: it gives its part of them back as they fill
-                if (!await_warp(&m.k_full[it & 1], it >> 1 & 1, &m.gave_up)) return;
-                if (elected()) mbar_arrive(&m.k_empty[it & 1]);
-                if (!await_warp(&m.v_full[it & 1], it >> 1 & 1, &m.gave_up)) return;
-                if (elected()) mbar_arrive(&m.v_empty[it & 1]);
-            }
-            continue;
-        }
-        if (!await_warp(&m.q_full[tile], asked++ & 1, &m.gave_up)) return;
-#pragma unroll 1
-        for (int u = 0; u < units; ++u, ++it, ++mine) {
+        for (int u = 0; u < units; ++u, ++it) {
             const uint32_t st = it & 1, round = it >> 1 & 1;
             if (!await_warp(&m.k_full[st], round, &m.gave_up)) return;
+            if (turns & (u ^ tile)) {
+                // the other tile's unit: this one gives its part of the stages back as they fill
+                if (elected()) mbar_arrive(&m.k_empty[st]);
+                if (!await_warp(&m.v_full[st], round, &m.gave_up)) return;
+                if (elected()) mbar_arrive(&m.v_empty[st]);
+                continue;
+            }
             // scores overwrite the weights that the product before reads: products of different sums are not
             // ordered among themselves
             if (mine > 0 && !await_warp(&m.o_done[tile], (mine - 1) & 1, &m.gave_up)) return;
@@ -433,11 +445,13 @@ __device__ void product_role(Smem<D>& m, int tile) {
                 const uint64_t v = v0 + st * kStep;
 #pragma unroll
                 for (int s = 0; s < kTokens / 16; ++s)
-                    mma_ts(su, sc + s * 8, v + (s / 2) * (kGranule * D * 2 >> 4) + (s % 2) * 16, kSums, u > 0 || s > 0);
+                    mma_ts(su, sc + s * 8, v + (s / 2) * (kGranule * D * 2 >> 4) + (s % 2) * 16, kSums,
+                           u > begin || s > 0);
                 commit(&m.o_done[tile]);
                 commit(&m.v_empty[st]);
             }
             __syncwarp();
+            ++mine;
         }
     }
 }
@@ -448,7 +462,7 @@ __device__ void softmax_role(const AttendArgs& a, const ManyWork& work, Smem<D>&
     const int tile = threadIdx.x / 128, in_tile = threadIdx.x % 128, warp = in_tile / 32, lane = threadIdx.x % 32;
     const uint32_t lanes = (uint32_t)(warp * 32) << 16;
     const uint32_t sc = m.tmem + lanes + kScoreCol + tile * 128, su = m.tmem + lanes + kSumCol + tile * D;
-    uint32_t it = 0, n = 0;  // units of the CTA, of this tile
+    uint32_t it = 0, n = 0, shared = 0;  // units of the CTA, of this tile; stretches that both tiles summed
     float top = -INFINITY, sum = 0.f;
     bool pending = false;
 #pragma unroll 1
@@ -458,14 +472,16 @@ __device__ void softmax_role(const AttendArgs& a, const ManyWork& work, Smem<D>&
         const Stretch& x = m.line[seg % kLineRing];
         const Stretch& done = m.line[(seg + kLineRing - 1) % kLineRing];
         const int units = x.units;
-        const bool mine = units > 0 && tile < x.tiles;
+        const bool turns = x.tiles == 1;  // the tiles take the units in turn
+        const int begin = turns ? tile : 0, first_row = x.tile * kPair + (turns ? 0 : tile * kRows);
+        const bool mine = begin < units;
         float unit = 0.f;  // what the row's scores are to be multiplied by
         if (mine) {
             // as they are into their places, 8 rows x 4 chunks of 16 bytes a step; then a thread its row
             uint4* const q = reinterpret_cast<uint4*>(m.q[tile]);
 #pragma unroll 1
             for (int g = 0; g < 4; ++g) {
-                const int at = warp * 32 + g * 8 + lane / 4, row = x.tile * kPair + tile * kRows + at;
+                const int at = warp * 32 + g * 8 + lane / 4, row = first_row + at;
                 const T* p = static_cast<const T*>(a.q.data) + (x.row + row / a.group) * a.q.token_stride +
                              (x.head * a.group + row % a.group) * a.q.head_stride + lane % 4 * 8;
                 uint4* to = q + (at / 8 * (D / 8) + lane % 4) * 8 + at % 8;
@@ -512,18 +528,42 @@ __device__ void softmax_role(const AttendArgs& a, const ManyWork& work, Smem<D>&
             if (!await_warp(&m.o_done[tile], (n - 1) & 1, &m.gave_up)) return;
             fence_after();
             const bool whole = done.units == done.cnt;
-            const int dr = done.tile * kPair + tile * kRows + in_tile;
+            const bool both = done.tiles == 1 && done.units > 1;
+            const int at = done.tiles == 1 ? in_tile : threadIdx.x, dr = done.tile * kPair + at;
             const int64_t tok = done.row + dr / a.group;
             const int qh = done.head * a.group + dr % a.group;
+            float f = 1.f, g = 0.f;  // of tile 0's and tile 1's sums
+            if (both) {
+                // both tiles have sums of the same rows, in the same lanes of tensor memory: each adds up half of the columns
+                m.tops[tile][in_tile] = top, m.sums[tile][in_tile] = sum;
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&m.posted);
+                if (!await_warp(&m.posted, shared & 1, &m.gave_up)) return;
+                fence_after();
+                const float t0 = m.tops[0][in_tile], t1 = m.tops[1][in_tile];
+                top = fmaxf(t0, t1);
+                const float ref = top == -INFINITY ? 0.f : top;
+                f = exp2_approx(t0 - ref), g = exp2_approx(t1 - ref);
+                sum = m.sums[0][in_tile] * f + m.sums[1][in_tile] * g;
+            }
             const float inv = sum == 0.f ? 0.f : __fdiv_rn(1.f, sum);
             // stretches that are not whole: at most the CTA's first and its last
-            float* part = work.part + ((int64_t)2 * blockIdx.x + (done.first ? 0 : 1)) * (kPair * (D + 2)) + tile * kRows + in_tile;
+            float* part = work.part + ((int64_t)2 * blockIdx.x + (done.first ? 0 : 1)) * (kPair * (D + 2)) + at;
             T* dst = static_cast<T*>(a.out.data) + tok * a.out.token_stride + qh * a.out.head_stride;
 #pragma unroll 1
-            for (int c = 0; c < D / 32; ++c) {
+            for (int c = both ? tile * (D / 64) : 0; c < (both ? (tile + 1) * (D / 64) : D / 32); ++c) {
                 uint32_t o[32];
-                ld32(su + c * 32, o);
+                ld32((both ? m.tmem + lanes + kSumCol : su) + c * 32, o);
                 wait_ld();
+                if (both) {
+                    uint32_t o1[32];
+                    ld32(m.tmem + lanes + kSumCol + D + c * 32, o1);
+                    wait_ld();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        o[j] = __float_as_uint(__uint_as_float(o[j]) * f + __uint_as_float(o1[j]) * g);
+                }
                 if (whole) {
                     if (dr < done.rows) {
                         float v[32];
@@ -544,31 +584,43 @@ __device__ void softmax_role(const AttendArgs& a, const ManyWork& work, Smem<D>&
                     for (int j = 0; j < 32; ++j) part[(c * 32 + j) * kPair] = __uint_as_float(o[j]);
                 }
             }
-            if (!whole) {
+            if (both && tile == 1) {
+            } else if (!whole) {
                 part[D * kPair] = top;
                 part[(D + 1) * kPair] = sum;
             } else if (dr < done.rows && a.lse != nullptr) {
                 a.lse[tok * a.q.n_heads + qh] =
                     top == -INFINITY ? -INFINITY : (top - kManyLift + log2f(sum)) * 0.6931471805599453f;
             }
+            if (both) {
+                // neither tile's next sums go over these before both have read them
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&m.added);
+                if (!await_warp(&m.added, shared++ & 1, &m.gave_up)) return;
+                fence_after();
+            }
             pending = false;
         }
         if (seg > 0) release(m, seg - 1);
         if (units == 0) return;
         if (mine) {
-            const int r = x.tile * kPair + tile * kRows + in_tile;
+            const int r = first_row + in_tile;
+            // units from one of the tile's to its next; read again where it is needed, for registers are short
+            auto step = [&]() { return 3 - *(const volatile int*)&x.tiles; };
             const int pos = x.start + r / a.group;
-            const int first_token = (x.first_gran + x.k * kGrans) * kGranule;
+            const int first_token = (x.first_gran + (x.k + begin) * kGrans) * kGranule;
             // seen: [lo, hi) counted from the unit's first score
             int hi = (r >= x.rows ? 0 : a.causal ? min(x.len, max(pos + 1, 0)) : x.len) - first_token;
             int lo = (a.window > 0 ? pos - a.window + 1 : 0) - first_token;
             top = -INFINITY, sum = 0.f;
 #pragma unroll 1
-            for (int u = 0; u < units; ++u, ++n, hi -= kTokens, lo -= kTokens) {
+            for (int u = begin; u < x.units; ++n) {
                 const float(*scale)[kGrans] = m.scales[(it + u) % kScaleRing];
                 // a tile that sat stretches out is ahead of the ring, where an old phase looks like the one to come:
                 // its first scores say that the unit is at hand
-                if (u == 0 && !await_warp(&m.s_full[tile], n & 1, &m.gave_up)) return;
+                const bool opening = u < step();
+                if (opening && !await_warp(&m.s_full[tile], n & 1, &m.gave_up)) return;
                 if (!await_warp(&m.scales_full[(it + u) % kScaleRing], (it + u) / kScaleRing & 1, &m.gave_up)) return;
                 const bool edge = __any_sync(~0u, hi < kTokens || lo > 0);
                 float mul[kGrans], add[kGrans], inverse[kGrans];
@@ -577,7 +629,7 @@ __device__ void softmax_role(const AttendArgs& a, const ManyWork& work, Smem<D>&
                     mul[c] = fmaxf(unit * scale[0][c], 0x1p-126f);  // not 0: what is not seen stays -inf
                     add[c] = scale[1][c], inverse[c] = scale[2][c];
                 }
-                if (u > 0 && !await_warp(&m.s_full[tile], n & 1, &m.gave_up)) return;
+                if (!opening && !await_warp(&m.s_full[tile], n & 1, &m.gave_up)) return;
                 fence_after();
                 uint32_t raw[kTokens];
                 float* s = reinterpret_cast<float*>(raw);
@@ -634,7 +686,7 @@ __device__ void softmax_role(const AttendArgs& a, const ManyWork& work, Smem<D>&
                     // over scores that have been read: 16 columns for 32
                     st16(sc + c * 16, p);
                 }
-                if (u > 0 && __any_sync(~0u, grows)) {
+                if (__any_sync(~0u, grows) && u >= step()) {
                     if (!await_warp(&m.o_done[tile], (n - 1) & 1, &m.gave_up)) return;
                     fence_after();
 #pragma unroll 1
@@ -651,6 +703,8 @@ __device__ void softmax_role(const AttendArgs& a, const ManyWork& work, Smem<D>&
                 fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&m.p_full[tile]);
+                const int next = step();
+                u += next, hi -= next * kTokens, lo -= next * kTokens;
             }
             pending = true;
         }
@@ -674,7 +728,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend_many(AttendArgs a, Ma
         }
         for (int i = 0; i < kScaleRing; ++i) mbar_init(&m.scales_full[i], 1);
         for (int i = 0; i < kLineRing; ++i) mbar_init(&m.line_full[i], 1), mbar_init(&m.line_empty[i], kLineReaders);
-        mbar_init(&m.drained, 2);
+        mbar_init(&m.drained, 2), mbar_init(&m.posted, kSoftmaxWarps), mbar_init(&m.added, kSoftmaxWarps);
         m.gave_up = 0;
         fence_mbar_init();
     }

@@ -233,6 +233,30 @@ def test_attend_many_ragged_prompts(cuda_lib, group, d, dtype):
             assert (np.abs(lse.double().cpu().numpy() - want_lse) <= lse_bound).all()
 
 
+@pytest.mark.parametrize("group,d,dtype,causal,window", [
+    (4, 128, BF16, True, 0), (4, 64, F16, True, 0), (3, 128, F16, False, 0), (8, 64, BF16, True, 700),
+    (1, 128, BF16, True, 130)])
+def test_attend_one_row_tile(cuda_lib, group, d, dtype, causal, window):
+    """17 to 128 rows a sequence and head, which two halves of a CTA share by the granules: contexts that give one half
+    nothing, that end in either half's turn, that are cut between CTAs, next to prompts of both row tiles."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(1000 * group + d + window)
+    heads, block = 3, 64
+    news = [17 // group + 1, 128 // group, 40 // group + 1]
+    seqs = [(max(n, length), n) for length in (1, 40, 128, 129, 256, 257, 384, 400, 640) for n in news]
+    seqs += [(int(n), news[i % 3]) for i, n in enumerate(rng.integers(1500, 6000, 12))]
+    seqs += [(900, 300), (1400, 130 // group + 1), (4000, 20)]
+    order = rng.permutation(len(seqs))
+    lens, new = [seqs[i][0] for i in order], [seqs[i][1] for i in order]
+    table, n = R.make_table(lens, block, rng)
+    pool = R.Pool(n, block, heads, d, rng)
+    pool.vs[:] = np.exp2(rng.integers(-12, 3, pool.vs.shape))
+    pool.ks[:] = np.exp2(rng.integers(-9, -5, pool.ks.shape))
+    q, qx = rows(rng, sum(new), heads * group, d, dtype)
+    check_attend(mp, pool, table, lens, new, q, qx, d ** -0.5, causal, window)
+
+
 def test_attend_sharp_and_flat_rows(cuda_lib):
     """Scores hundreds apart, one token that outweighs thousands, and queries of zeros (all weights equal)."""
     import paper_2203_00448_gb300 as mp
