@@ -55,6 +55,7 @@ constexpr int kThreads = 16 * 32;
 // Registers a thread after the roles part: 256 x 176 + 128 x 112 + 128 x 48 = 512 x 128, the launch's.
 constexpr int kSoftmaxRegs = 176, kConvertRegs = 112, kProductRegs = 48;
 constexpr int kTries = (int)(kKvSpinCycles >> 8);  // of a wait: some tens of cycles each
+constexpr int kUnitCycles = 1 << 16;               // a unit takes less by far
 constexpr int kStrips = 1024;
 constexpr float kGrow = 8.f;
 
@@ -253,6 +254,20 @@ __device__ __forceinline__ bool await_warp(uint64_t* bar, uint32_t parity, volat
     return __all_sync(~0u, await(bar, parity, gave_up));
 }
 
+// ... for as long as a stretch of that many units may take.
+__device__ __forceinline__ bool await_stretch(uint64_t* bar, uint32_t parity, int units, volatile int* gave_up) {
+    const long long t0 = clock64();
+    while (!mbar_try(bar, parity)) {
+        if (*gave_up) return false;
+        if (clock64() - t0 > kKvSpinCycles + (long long)units * kUnitCycles) {
+            *gave_up = 1;
+            return false;
+        }
+        __nanosleep(100);
+    }
+    return true;
+}
+
 constexpr uint32_t kScoreCol = 0, kSumCol = 256;  // of tile 0; tile 1 has + 128 and + D
 
 // One thread walks the CTA's part of the line ahead of the roles.
@@ -260,7 +275,7 @@ template <int D>
 __device__ void line_role(const AttendArgs& a, Smem<D>& m) {
     Stretch x = m.first;
     int64_t left = m.length;
-    int into = m.into;
+    int into = m.into, longest = 0;
     x.first = 1;
 #pragma unroll 1
     for (int seg = 0;; ++seg) {
@@ -273,7 +288,8 @@ __device__ void line_role(const AttendArgs& a, Smem<D>& m) {
             left -= span;
             if (x.units > 0) break;
         }
-        if (!await(&m.line_empty[seg % kLineRing], (seg / kLineRing & 1) ^ 1, &m.gave_up)) return;
+        if (!await_stretch(&m.line_empty[seg % kLineRing], (seg / kLineRing & 1) ^ 1, longest, &m.gave_up)) return;
+        longest = max(longest, x.units);
         m.line[seg % kLineRing] = x;
         mbar_arrive(&m.line_full[seg % kLineRing]);
         if (x.units == 0) return;

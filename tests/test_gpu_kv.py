@@ -257,6 +257,31 @@ def test_attend_one_row_tile(cuda_lib, group, d, dtype, causal, window):
     check_attend(mp, pool, table, lens, new, q, qx, d ** -0.5, causal, window)
 
 
+def test_attend_contexts_of_millions(cuda_lib):
+    """A piece of a prompt over ten million positions that share four blocks: a CTA spends a tenth of a second and more on
+    each of several heads, and no wait may take that for a fault.  As the last block is whole and every row sees each of the
+    four nearly equally often, the result is attention over the four."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(5)
+    block, heads, group, d, n = 256, 5, 8, 64, 4864
+    columns = 40000
+    pool = R.Pool(4, block, heads, d, rng)
+    q, _ = rows(rng, n, heads * group, d, BF16)
+    table = np.tile(np.arange(4, dtype=np.int32), columns // 4)[None]
+    out, _, status = mp.kv_attend(pool.cache(), batch_of(mp, table, [columns * block], [n]), q)
+    assert not status.any()
+    small = np.arange(4, dtype=np.int32)[None].repeat(n, 0)  # each row on its own over the four blocks
+    want, _, status = mp.kv_attend(pool.cache(), batch_of(mp, small, [4 * block] * n, [1] * n), q)
+    assert not status.any()
+    v = mp.kv_read(pool.cache(), batch_of(mp, small[:1], [4 * block], [4 * block]), F32)[1].double().abs().amax((0, 2))
+    # f32 sums of as many steps of 16 tokens, each cut off at 24 bits; weights as f16 and the last rows' uneven share of the
+    # four below 2^-8 together; both results rounded to bf16
+    steps = columns * block / 16
+    bound = (steps * 2.0 ** -24 + 2.0 ** -8) * v.repeat_interleave(group)[None, :, None] + 2.0 ** -7 * want.abs().double()
+    assert ((out.double() - want.double()).abs() <= bound).all()
+
+
 def test_attend_sharp_and_flat_rows(cuda_lib):
     """Scores hundreds apart, one token that outweighs thousands, and queries of zeros (all weights equal)."""
     import paper_2203_00448_gb300 as mp
