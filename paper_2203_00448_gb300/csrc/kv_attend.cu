@@ -744,6 +744,9 @@ struct Route {
     bool few, many, brief;
 };
 Route route(const mp_kv_cache& c, const mp_kv_batch& bt, int32_t group, int32_t window) {
+    // An empty pool has no block that could stand in for a bad table entry's: k_kv_join alone says which sequences are
+    // wrong (all that see a position) and writes the rows that see nothing.
+    if (c.n_blocks == 0) return {false, false, false};
     if ((int64_t)bt.max_tokens * group <= kFewRows) {
         const int32_t span = window > 0 ? std::min(bt.max_len, window + bt.max_tokens) : bt.max_len;
         const bool brief = span <= kShortLen && (int64_t)bt.n_seqs * c.n_heads <= kShortCtas;
@@ -820,8 +823,8 @@ cudaError_t attend_as(const AttendArgs& a, const FewWork& few, const ManyWork& m
                         plan);
 }
 template <typename T, int D>
-cudaError_t attend_rows(const AttendArgs& a, const FewWork& few, const ManyWork& many, cudaStream_t stream) {
-    if (few.base == nullptr && many.part == nullptr)
+cudaError_t attend_rows(const AttendArgs& a, bool brief, const FewWork& few, const ManyWork& many, cudaStream_t stream) {
+    if (brief)
         return join_rows(a) <= 8 ? short_as<T, D, 1>(a, stream) : short_as<T, D, 2>(a, stream);
     return join_rows(a) <= 8 ? attend_as<T, D, 1>(a, few, many, stream) : attend_as<T, D, 2>(a, few, many, stream);
 }
@@ -860,10 +863,10 @@ cudaError_t launch_kv_attend(const mp_kv_cache& c, const mp_kv_batch& bt, const 
         many.part = reinterpret_cast<float*>(ws + l.many_part);
     }
     if (q.dtype == MP_F16)
-        return c.head_dim == 64 ? attend_rows<__half, 64>(a, few, many, stream)
-                                : attend_rows<__half, 128>(a, few, many, stream);
-    return c.head_dim == 64 ? attend_rows<__nv_bfloat16, 64>(a, few, many, stream)
-                            : attend_rows<__nv_bfloat16, 128>(a, few, many, stream);
+        return c.head_dim == 64 ? attend_rows<__half, 64>(a, r.brief, few, many, stream)
+                                : attend_rows<__half, 128>(a, r.brief, few, many, stream);
+    return c.head_dim == 64 ? attend_rows<__nv_bfloat16, 64>(a, r.brief, few, many, stream)
+                            : attend_rows<__nv_bfloat16, 128>(a, r.brief, few, many, stream);
 }
 
 }  // namespace mp

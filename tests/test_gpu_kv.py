@@ -514,3 +514,22 @@ def test_example_serves_planned_requests(cuda_lib):
         done = serve(check=True, **kw)
         assert done["pool_blocks"] < done["blocks"] or kw["spread"] < 10
         assert 0 < done["worst"] <= 2.0 ** -9 + 2.0 ** -11
+
+
+@pytest.mark.parametrize("lens,new", [([40, 0, 33], [1, 1, 0]), ([9000, 0, 1], [1, 2, 2]), ([300, 0, 5], [100, 40, 3]),
+                                      ([120000, 0, 70000, 1], [40, 40, 1, 0])])
+@pytest.mark.parametrize("causal", [True, False])
+def test_attend_empty_pool(cuda_lib, lens, new, causal):
+    """A pool without blocks: sequences that see a position are refused by every route, the others get their zeros."""
+    import paper_2203_00448_gb300 as mp
+
+    for heads, dtype in ((1, F16), (8, BF16)):
+        cache = mp.KvCache(0, 32, heads, 128)
+        for entry in (0, -1, 7):
+            table = np.full((len(lens), -(-max(lens) // 32)), entry)
+            q = torch.ones(sum(new), 4 * heads, 128, dtype=dtype, device="cuda")
+            out = torch.full_like(q, 5)
+            _, lse, status = mp.kv_attend(cache, batch_of(mp, table, lens, new), q, causal=causal, out=out, want_lse=True)
+            assert status.tolist() == [int(n > 0 and length > 0) for length, n in zip(lens, new)]
+            at = new[0]
+            assert not out[at:at + new[1]].any() and torch.isneginf(lse[at:at + new[1]]).all()

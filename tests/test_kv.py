@@ -133,3 +133,12 @@ def test_plain_e4m3_rounding():
     assert np.array_equal(np.abs(np.clip(x, -448, 448) - got), best)
     assert R.VALUES[R.to_byte(np.array([17.0, 19.0, 2.0 ** -10, 3 * 2.0 ** -10]))].tolist() == [16.0, 20.0, 0.0, 2.0 ** -8]
     assert R.scale_of(448.0) == 1 and R.scale_of(448.1) == 2 and R.scale_of(224.0) == 0.5 and R.scale_of(0.0) == 2.0 ** -60
+
+
+def test_empty_pool_needs_no_scratch(lib):
+    """No kernel that walks a context may be launched over a pool without blocks, so none has scratch; each route's sizes."""
+    none = dict(n_blocks=0, k=None, v=None, k_scale=None, v_scale=None)
+    for sizes in (dict(max_tokens=1), dict(max_tokens=1, max_blocks=1000, max_len=32000), dict(max_tokens=40, n_tokens=160),
+                  dict(max_tokens=40, n_tokens=44, max_blocks=1 << 18, max_len=1 << 23)):
+        assert lib.mp_kv_attend_workspace_bytes(cache(**none), batch(**sizes), 4) == 0
+    assert lib.mp_kv_attend_workspace_bytes(cache(), batch(max_tokens=40, n_tokens=160), 4) > 0
