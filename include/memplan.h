@@ -470,7 +470,8 @@ size_t mp_kv_attend_workspace_bytes(const mp_kv_cache *cache, const mp_kv_batch 
  *   also j > p - window.
  * out = sum_j w_j v_j with w = softmax_j(scale * q . k_j), lse = log sum_j
  * exp(scale * q . k_j) (natural); query head h reads cache head
- * h / (q->n_heads / cache->n_heads).  A query that sees nothing gets out = 0 and
+ * h / (q->n_heads / cache->n_heads).  A v_scale below 2^-84 counts as 0 (mp_kv_write
+ * makes none below 2^-60).  A query that sees nothing gets out = 0 and
  * lse = -inf.  Products of 16-bit values are summed in 32 bits, as are the
  * softmax's sums; its weights are rounded to 16 bits (11 of precision) for the
  * second product.

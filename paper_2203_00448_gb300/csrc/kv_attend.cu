@@ -165,8 +165,8 @@ struct Tile {
         last = __reduce_max_sync(~0u, last);
     }
 
-    // The granule at position base: its keys kb and values vb as stored, and their scales.
-    __device__ __forceinline__ void add(const uint8_t* kb, const uint8_t* vb, float ks, float vs, int base) {
+    // The granule at position base: its keys kb and values vb as stored, and their scales as stored.
+    __device__ __forceinline__ void add(const uint8_t* kb, const uint8_t* vb, float ks, float stored_vs, int base) {
         const int lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
         // scores: product row r of 16 is token 4 (r % 8 / 2) + r % 2 + 2 (r / 8), the order in which a
         // lane's 4 stored value bytes meet the second product
@@ -184,7 +184,7 @@ struct Tile {
                 for (int nt = 0; nt < NT; ++nt) mma(s[nt][m], a0, a1, a2, a3, qf[nt][i][0], qf[nt][i][1]);
             }
         }
-        const float lv = log2f(vs), iv = __fdiv_rn(1.f, vs);
+        const float vs = value_scale(stored_vs), lv = log2f(vs), iv = __fdiv_rn(1.f, vs);
         uint32_t p[NT][2][2];
         bool moved = false;
         float fade[NT][2];
@@ -237,7 +237,8 @@ struct Tile {
 #pragma unroll
                     for (int k = 0; k < 4; ++k) o[nt][i][k] *= fade[nt][k % 2];
         }
-        if (base + kGranule <= last) {
+        const int meant = stored_vs < kLeastValueScale ? 0 : last;  // values from this position on are zeros
+        if (base + kGranule <= meant) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -252,7 +253,7 @@ struct Tile {
         } else {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int left = last - (base + h * 16 + t * 4);  // of this lane's 4 tokens
+                const int left = meant - (base + h * 16 + t * 4);  // of this lane's 4 tokens
                 const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) {
@@ -401,7 +402,7 @@ __global__ void __launch_bounds__(few_warps(D, NT) * 32, 1) k_kv_attend_few(Atte
                 break;
             }
             const int64_t sc = (int64_t)ring_page[st] * a.c.n_heads + head;
-            const float ks = __ldg(a.c.k_scale + sc), vs = value_scale(__ldg(a.c.v_scale + sc));
+            const float ks = __ldg(a.c.k_scale + sc), vs = __ldg(a.c.v_scale + sc);
             x.add(ring + st * 2 * kBytes, ring + st * 2 * kBytes + kBytes, ks, vs, cur.g * kGranule);
             __syncwarp();
             issue();
@@ -499,7 +500,7 @@ __global__ void __launch_bounds__(short_warps(NT) * 32, 1) k_kv_attend_short(Att
                              : "memory");
             }
             const int64_t sc = (int64_t)page * a.c.n_heads + head;
-            const float ks = __ldg(a.c.k_scale + sc), vs = value_scale(__ldg(a.c.v_scale + sc));
+            const float ks = __ldg(a.c.k_scale + sc), vs = __ldg(a.c.v_scale + sc);
             if (gran == lo + wid) x.begin(a, s.lo, rows, s.len, s.n, head, tile);
             asm volatile("cp.async.wait_all;" ::: "memory");
             __syncwarp();

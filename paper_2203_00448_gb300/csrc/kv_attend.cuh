@@ -74,9 +74,11 @@ __device__ __forceinline__ float row_factor(float most) {
     return __uint_as_float((uint32_t)min(268 - e, 254) << 23);
 }
 
-// The scale of a block of values as the kernels use it: they divide by it and take
-// its logarithm.
-__device__ __forceinline__ float value_scale(float s) { return fmaxf(s, 0x1p-100f); }
+// The scale of a block of values as the kernels use it: they divide by it and take its logarithm.  Sums of weights over
+// scales stay finite: 2^28 tokens of weight 2^15 over 2^-84 make 2^127.  A smaller scale, 0 among them, counts as 0: its
+// bytes are taken as zeros.
+constexpr float kLeastValueScale = 0x1p-84f;
+__device__ __forceinline__ float value_scale(float s) { return fmaxf(s, kLeastValueScale); }
 
 // What both kernels and the joining need of a call.
 struct AttendArgs {

@@ -364,6 +364,7 @@ __device__ void convert_role(const AttendArgs& a, Smem<D>& m) {
 #pragma unroll 1
     for (int it = 0;; ++it) {
         const int st = it % kStages, held = had;
+        const uint32_t nothing = __ballot_sync(~0u, vs < kLeastValueScale);  // bit g: granule g's values count as zeros
         const uint32_t empty = (it / kStages & 1) ^ 1;
         load(a.c.v, vr);
         if (!await_warp(&m.k_empty[st], empty, &m.gave_up)) return;
@@ -391,10 +392,10 @@ __device__ void convert_role(const AttendArgs& a, Smem<D>& m) {
         if (!await_warp(&m.v_empty[st], empty, &m.gave_up)) return;
         // stored tiles [granule][D / 8][2][8][16] become [granule][D / 8][4][8][8]
         to = reinterpret_cast<uint4*>(m.v[st]) + (tid / 8) * 16 + tid % 8;
-        if (held < kTokens) {  // bytes behind the last token mean nothing, NaN among them
+        if (held < kTokens || nothing) {  // bytes behind the last token mean nothing, NaN among them
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
-                const int left_here = held - (i / kPerGran * kGranule + (tid / 8 % 2) * 16);
+                const int left_here = nothing >> (i / kPerGran) & 1 ? 0 : held - (i / kPerGran * kGranule + (tid / 8 % 2) * 16);
                 uint32_t* p = reinterpret_cast<uint32_t*>(&vr[i]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {

@@ -533,3 +533,57 @@ def test_attend_empty_pool(cuda_lib, lens, new, causal):
             assert status.tolist() == [int(n > 0 and length > 0) for length, n in zip(lens, new)]
             at = new[0]
             assert not out[at:at + new[1]].any() and torch.isneginf(lse[at:at + new[1]]).all()
+
+
+def equal_weights(mp, rng, lens, new, vs, heads=2, group=4, d=64, dtype=BF16, blocks=4):
+    """Attention of queries of zeros over sequences that share a few blocks under value scales vs: out and lse."""
+    block = 256
+    pool = R.Pool(blocks, block, heads, d, rng)
+    pool.vs[:] = vs
+    columns = -(-max(lens) // block)
+    table = np.tile(np.arange(columns, dtype=np.int32) % blocks, (len(lens), 1))
+    cache, batch = pool.cache(), batch_of(mp, table, lens, new)
+    q = torch.zeros(sum(new), heads * group, d, dtype=dtype, device="cuda")
+    out, lse, status = mp.kv_attend(cache, batch, q, causal=False, want_lse=True)
+    assert not status.any()
+    return out, lse.double().cpu().numpy()
+
+
+@pytest.mark.parametrize("lens,new", [([1500], [1]), ([16384, 40000], [1, 2]), ([3_000_000], [1]),
+                                      ([2_500_000, 2_100_000], [40, 20])])
+@pytest.mark.parametrize("d,dtype", [(64, F16), (128, BF16)])
+def test_attend_values_all_of_scale_zero(cuda_lib, lens, new, d, dtype):
+    """Scales of 0, and below 2^-84, where they count as 0: outputs are 0 and the log-sums are those of the scores, however
+    many tokens share the weight.  A log-sum's terms are below 128 in units of log 2, where 32 bits keep 2^-18; four of them."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(41)
+    for vs in (0.0, 2.0 ** -85, 2.0 ** -149):
+        out, lse = equal_weights(mp, rng, lens, new, vs, d=d, dtype=dtype)
+        want = np.repeat(np.log(lens), new)[:, None]
+        assert not out.any()
+        assert (np.abs(lse - want) <= 2.0 ** -16 + 2.0 ** -20 * (1 + want)).all()
+
+
+@pytest.mark.parametrize("seqs", [[(300, 1), (33, 2)], [(5000, 2), (4000, 1)], [(300, 80), (65, 64)], [(4500, 300), (129, 20)]])
+def test_attend_scales_of_zero_among_others(cuda_lib, seqs):
+    """Blocks of scale 0, whose bytes are no small numbers, take part in the softmax and add nothing to the outputs."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(43)
+    lens, new = [s[0] for s in seqs], [s[1] for s in seqs]
+    table, n = R.make_table(lens, 32, rng)
+    pool = R.Pool(n, 32, 2, 128, rng)
+    pool.vs[:] = np.exp2(rng.integers(-60, -55, pool.vs.shape))
+    for b in range(2):
+        pool.vs[table[b, ::3]] = 0
+        pool.vs[table[b, 1::6]] = 2.0 ** -84 * 0.999  # counts as 0
+    q, qx = rows(rng, sum(new), 4, 128, BF16)
+    small, pool.vs = pool.vs, np.where(pool.vs < 2.0 ** -84, np.float32(0), pool.vs)
+    want = R.attend(pool, table, lens, new, qx, 0.09)
+    pool.vs = small
+    out, lse, status = mp.kv_attend(pool.cache(), batch_of(mp, table, lens, new), q, scale=0.09, want_lse=True)
+    bound, lse_bound = R.attend_bounds(BF16, *want)
+    assert not status.any()
+    assert (np.abs(out.double().cpu().numpy() - want[0]) <= bound).all()
+    assert (np.abs(lse.double().cpu().numpy() - want[1]) <= lse_bound + 2.0 ** -16).all()
