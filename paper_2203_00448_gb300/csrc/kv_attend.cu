@@ -427,8 +427,7 @@ __global__ void __launch_bounds__(few_warps(D, NT) * 32, 1) k_kv_attend_few(Atte
                             dst[i * 16 + g + 8] = from_f32<T>(x.o[nt][i][2 + k] * inv);
                         }
                         if (a.lse != nullptr && g == 0)
-                            a.lse[tok * a.q.n_heads + qh] =
-                                m == -INFINITY ? -INFINITY : (m - kLift + log2f(l)) * 0.6931471805599453f;
+                            a.lse[tok * a.q.n_heads + qh] = log_sum(m, kLift, l);
                     }
                 } else {
                     // a warp leaves at most two parts: of what began before it or with it, and of
@@ -546,7 +545,7 @@ __global__ void __launch_bounds__(short_warps(NT) * 32, 1) k_kv_attend_short(Att
             const float y[2] = {o0 * inv, o1 * inv};
             store_values<T, 2>(dst, a.wide_out, y);
             if (d == 0 && a.lse != nullptr)
-                a.lse[tok * a.q.n_heads + qh] = top == -INFINITY ? -INFINITY : (top - kLift + log2f(sum)) * 0.6931471805599453f;
+                a.lse[tok * a.q.n_heads + qh] = log_sum(top, kLift, sum);
         }
         __syncthreads();
     }
@@ -599,8 +598,7 @@ __device__ void join_cut(const AttendArgs& a, const ManyWork& work, int w, int y
     store_values<T, 8>(dst, a.wide_out, o);
     store_values<T, 8>(dst + 8, a.wide_out, o + 8);
     if (y == 0 && a.lse != nullptr)
-        a.lse[tok * a.q.n_heads + qh] =
-            top == -INFINITY ? -INFINITY : (top - kManyLift + log2f(sum)) * 0.6931471805599453f;
+        a.lse[tok * a.q.n_heads + qh] = log_sum(top, kManyLift, sum);
 }
 
 // A sequence's status, and its rows that see nothing (no kernel has units of theirs).
@@ -702,7 +700,7 @@ __device__ void join_row(const AttendArgs& a, const FewWork& work, int64_t u, bo
     for (int i = 0; i < kCols; ++i) o[i] *= inv;
     store_values<T, kCols>(dst + lane * kCols, a.wide_out, o);
     if (a.lse != nullptr && lane == 0)
-        a.lse[tok * a.q.n_heads + qh] = top == -INFINITY ? -INFINITY : (top - kLift + log2f(l)) * 0.6931471805599453f;
+        a.lse[tok * a.q.n_heads + qh] = log_sum(top, kLift, l);
 }
 
 // After both kernels: what more than one CTA or warp had of a row, and the sequences' status.  kPer: warps a row.

@@ -80,6 +80,12 @@ __device__ __forceinline__ float row_factor(float most) {
 constexpr float kLeastValueScale = 0x1p-84f;
 __device__ __forceinline__ float value_scale(float s) { return fmaxf(s, kLeastValueScale); }
 
+// A row's log-sum from its reference top, at which weights are 2^lift, and their sum.  No weight at all: the row saw
+// nothing; where no score was a number, neither is the sum.
+__device__ __forceinline__ float log_sum(float top, float lift, float sum) {
+    return sum == 0.f ? -INFINITY : (top - lift + log2f(sum)) * 0.6931471805599453f;
+}
+
 // What both kernels and the joining need of a call.
 struct AttendArgs {
     mp_kv_cache c;

@@ -606,8 +606,7 @@ __device__ void softmax_role(const AttendArgs& a, const ManyWork& work, Smem<D>&
                 part[D * kPair] = top;
                 part[(D + 1) * kPair] = sum;
             } else if (dr < done.rows && a.lse != nullptr) {
-                a.lse[tok * a.q.n_heads + qh] =
-                    top == -INFINITY ? -INFINITY : (top - kManyLift + log2f(sum)) * 0.6931471805599453f;
+                a.lse[tok * a.q.n_heads + qh] = log_sum(top, kManyLift, sum);
             }
             if (both) {
                 // neither tile's next sums go over these before both have read them

@@ -587,3 +587,27 @@ def test_attend_scales_of_zero_among_others(cuda_lib, seqs):
     assert not status.any()
     assert (np.abs(out.double().cpu().numpy() - want[0]) <= bound).all()
     assert (np.abs(lse.double().cpu().numpy() - want[1]) <= lse_bound + 2.0 ** -16).all()
+
+
+@pytest.mark.parametrize("lens,new", [([100, 50], [1, 2]), ([6000, 2500], [3, 1]), ([300, 100], [100, 70]), ([30000, 700], [90, 20])])
+@pytest.mark.parametrize("d", [64, 128])
+def test_log_sums_of_non_finite_queries(cuda_lib, lens, new, d):
+    """A query row of which no score is a number has no log-sum either: NaN, not that of a row that sees nothing, by which
+    whoever merges parts of an attention would leave it out.  All other rows keep theirs."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(19)
+    table, n = R.make_table(lens, 64, rng)
+    pool = R.Pool(n, 64, 2, d, rng)
+    cache, batch = pool.cache(), batch_of(mp, table, lens, new)
+    q, _ = rows(rng, sum(new), 8, d, F16)
+    _, clean, _ = mp.kv_attend(cache, batch, q, want_lse=True)
+    bad = [(0, 1), (new[0] - 1, 7), (sum(new) - 1, 2)]
+    for i, h in bad:
+        q[i, h, 5] = float("nan")
+    out, lse, status = mp.kv_attend(cache, batch, q, want_lse=True)
+    assert not status.any()
+    for i, h in bad:
+        assert torch.isnan(lse[i, h]) and torch.isnan(out[i, h]).all()
+        clean[i, h] = lse[i, h] = 0
+    assert torch.equal(lse, clean)
