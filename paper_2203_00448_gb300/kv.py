@@ -133,6 +133,10 @@ _workspaces = {}
 
 
 def _workspace_of(stream_ptr, device):
+    # A captured call's scratch belongs to its graph's memory: replays may overlap whatever runs on the stream of the
+    # capture, other graphs captured there among it, and go on when that stream's own scratch has been replaced.
+    if torch.cuda.is_current_stream_capturing():
+        return Workspace(device)
     # calls on different streams may overlap: each stream has its own
     key = (device.index, stream_ptr)
     ws = _workspaces.get(key)
@@ -191,7 +195,8 @@ def kv_attend(cache: KvCache, batch: KvBatch, q: torch.Tensor, scale: float | No
               workspace: Workspace | None = None, stream=None):
     """Attention of the call's queries ([n_tokens, query heads, head_dim], float16 or bfloat16) over what their
     sequences hold: causal unless told otherwise, over the last `window` positions if that is not 0, scale 1 /
-    sqrt(head_dim) unless given.  Returns (out, lse or None, status); a query that sees nothing gets 0 and -inf."""
+    sqrt(head_dim) unless given.  Returns (out, lse or None, status); a query that sees nothing gets 0 and -inf.  Scratch
+    is the stream's unless given, and the graph's own in a capture."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return kv_attend(cache, batch, q, scale, causal, window, out, lse, want_lse, status, workspace)
@@ -212,7 +217,11 @@ def kv_attend(cache: KvCache, batch: KvBatch, q: torch.Tensor, scale: float | No
     need = needs.get(heads)
     if need is None:
         need = kv_attend_workspace_bytes(cache, batch, heads)
-    wptr, wbytes = (workspace or _workspace_of(stream_ptr, cache.device)).get(need) if need else (None, 0)
+    if need:
+        scratch = workspace or _workspace_of(stream_ptr, cache.device)
+        wptr, wbytes = scratch.get(need)
+    else:
+        wptr, wbytes = None, 0
     _check("mp_kv_attend",
            _lib.load().mp_kv_attend(cache._ref, ref, qt, shape[2] ** -0.5 if scale is None else scale, 1 if causal else 0,
                                     window, ot, None if lse is None else lse.data_ptr() or None, status.data_ptr() or None,

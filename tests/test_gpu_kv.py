@@ -611,3 +611,52 @@ def test_log_sums_of_non_finite_queries(cuda_lib, lens, new, d):
         assert torch.isnan(lse[i, h]) and torch.isnan(out[i, h]).all()
         clean[i, h] = lse[i, h] = 0
     assert torch.equal(lse, clean)
+
+
+def test_captured_calls_have_scratch_of_their_own(cuda_lib):
+    """Graphs captured without scratch of the caller's: later and larger calls on the stream of the capture do not take
+    theirs away, and two that were captured on one stream run at once on two."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(47)
+    lens, new = [60000, 30000], [1, 1]
+    table, n = R.make_table(lens, 64, rng)
+    pool = R.Pool(n, 64, 2, 128, rng)
+    cache, step = pool.cache(), batch_of(mp, table, lens, new)
+    prompt = batch_of(mp, table, [60000, 700], [600, 600])
+    q, _ = rows(rng, 2, 8, 128, BF16)
+    r, _ = rows(rng, 2, 8, 128, BF16)
+    long, _ = rows(rng, 1200, 8, 128, BF16)
+    ws = mp.Workspace("cuda")
+    want = [mp.kv_attend(cache, step, x, workspace=ws)[0] for x in (q, r)]
+    want_long = mp.kv_attend(cache, prompt, long, workspace=ws)[0]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    graphs, outs = [], [torch.empty_like(q) for _ in range(2)]
+    status = [torch.empty(2, dtype=torch.int32, device="cuda") for _ in range(2)]
+    with torch.cuda.stream(side):  # an eager step first, as a warm-up
+        mp.kv_attend(cache, step, q)
+    torch.cuda.synchronize()
+    for x, out, st in zip((q, r), outs, status):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            mp.kv_attend(cache, step, x, out=out, status=st)
+    with torch.cuda.stream(side):
+        got = mp.kv_attend(cache, prompt, long)[0]
+        torch.cuda.synchronize()
+        # whatever scratch was given up on that stream is other tensors' now
+        theirs = [torch.full((size,), 3, dtype=torch.uint8, device="cuda") for size in [1 << 20] * 64 + [16 << 20] * 4]
+    torch.cuda.synchronize()
+    assert torch.equal(got, want_long)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(20):
+        for out in outs:
+            out.zero_()
+        torch.cuda.synchronize()
+        for _ in range(10):
+            for graph, stream in zip(graphs, streams):
+                with torch.cuda.stream(stream):
+                    graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    assert all(bool((x == 3).all()) for x in theirs)
