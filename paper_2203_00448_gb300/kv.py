@@ -6,8 +6,8 @@
 
 A KvCache is a pool of blocks in 8 bits (its memory may be given, e.g. views of a planned slab); a KvBatch says which
 blocks the sequences of a call have, how many tokens they hold and which rows of the call's tensors are theirs.  Its
-tensors stay on the device and may be changed there between calls.  All calls are asynchronous on the current (or given)
-CUDA stream; what they allocate belongs to that stream.
+tensors stay on the device and may be changed there between calls, not replaced by others.  All calls are asynchronous on the
+current (or given) CUDA stream; what they allocate belongs to that stream.
 """
 from __future__ import annotations
 
@@ -30,10 +30,28 @@ def _tensor(name, t, dtype, shape, device=None):
     return t
 
 
-class KvCache:
+class _Fixed:
+    """Attributes whose addresses and values the C structs hold: what they point to may change, they may not."""
+
+    _fixed = frozenset()
+
+    def __setattr__(self, name, value):
+        if name in self._fixed and name in self.__dict__ and self.__dict__[name] is not value:
+            raise AttributeError(f"{name} cannot be replaced: change its contents, or make another {type(self).__name__}")
+        object.__setattr__(self, name, value)
+
+    def __delattr__(self, name):
+        if name in self._fixed:
+            raise AttributeError(f"{name} cannot be deleted")
+        object.__delattr__(self, name)
+
+
+class KvCache(_Fixed):
     """A pool of n_blocks blocks of block_tokens tokens: e4m3 keys and values of n_heads heads of head_dim values, one
     scale for each block and head.  k, v (uint8[n_blocks, n_heads, block_tokens * head_dim], 16-byte aligned) and
     k_scale, v_scale (float32[n_blocks, n_heads]) are allocated unless given; nothing needs to be initialised."""
+
+    _fixed = frozenset(("n_blocks", "block_tokens", "n_heads", "head_dim", "k", "v", "k_scale", "v_scale", "device"))
 
     def __init__(self, n_blocks: int, block_tokens: int, n_heads: int, head_dim: int, device="cuda", k=None, v=None,
                  k_scale=None, v_scale=None):
@@ -64,11 +82,13 @@ class KvCache:
         return 2 * n_heads * (block_tokens * head_dim + 4)
 
 
-class KvBatch:
+class KvBatch(_Fixed):
     """The sequences of a call.  table int32[B, columns]: pool block of each run of block_tokens positions; lens
     int32[B]: tokens held, the call's included; token_ptr int64[B + 1]: rows of the call's tensors, the last ones that
     each sequence holds.  Host bounds: n_tokens = token_ptr[B]; max_tokens of a sequence in the call (default n_tokens);
     max_len >= lens (default what the table has room for)."""
+
+    _fixed = frozenset(("table", "lens", "token_ptr", "n_tokens", "max_tokens", "max_len", "n_seqs", "device"))
 
     def __init__(self, table: torch.Tensor, lens: torch.Tensor, token_ptr: torch.Tensor, n_tokens: int,
                  max_tokens: int | None = None, max_len: int | None = None):

@@ -142,3 +142,23 @@ def test_empty_pool_needs_no_scratch(lib):
                   dict(max_tokens=40, n_tokens=44, max_blocks=1 << 18, max_len=1 << 23)):
         assert lib.mp_kv_attend_workspace_bytes(cache(**none), batch(**sizes), 4) == 0
     assert lib.mp_kv_attend_workspace_bytes(cache(), batch(max_tokens=40, n_tokens=160), 4) > 0
+
+
+def test_attributes_are_not_replaced():
+    """The C structs hold addresses and bounds: a tensor or bound put in place of another would not be seen by any call."""
+    c = mp.KvCache(4, 32, 2, 64, "cpu")
+    b = mp.KvBatch(torch.zeros(2, 2, dtype=torch.int32), torch.zeros(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int64), 2)
+    for x, names in ((c, ("k", "v", "k_scale", "v_scale", "n_blocks", "block_tokens", "n_heads", "head_dim", "device")),
+                     (b, ("table", "lens", "token_ptr", "n_tokens", "max_tokens", "max_len", "n_seqs", "device"))):
+        for name in names:
+            had = getattr(x, name)
+            with pytest.raises(AttributeError):
+                setattr(x, name, had.clone() if isinstance(had, torch.Tensor) else 77)
+            with pytest.raises(AttributeError):
+                delattr(x, name)
+            assert getattr(x, name) is had
+    at = b.lens.data_ptr()
+    b.lens += 1  # in place: the same tensor
+    b.lens[0] = 5
+    assert b.lens.tolist() == [5, 1] and b.lens.data_ptr() == at
+    c.note = b.note = 1  # what a program hangs on them is its own
