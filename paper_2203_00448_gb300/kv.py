@@ -74,7 +74,7 @@ class KvCache(_Fixed):
         self._struct = _lib.MpKvCache(n_blocks, block_tokens, n_heads, head_dim, _ptr(self.k), _ptr(self.v),
                                       _ptr(self.k_scale), _ptr(self.v_scale))
         self._ref = ctypes.byref(self._struct)
-        self._key, self._index = (block_tokens, n_heads, head_dim), self.k.get_device()
+        self._key, self._index = (block_tokens, n_heads, head_dim, self.device), self.k.get_device()
 
     @staticmethod
     def block_bytes(block_tokens: int, n_heads: int, head_dim: int) -> int:
@@ -105,7 +105,7 @@ class KvBatch(_Fixed):
         self._made = {}
 
     def _for(self, cache: KvCache):
-        """What calls with this batch and a cache of that shape share: the C struct, the shape of the call's keys and
+        """What calls with this batch and a cache of that shape and device share: the C struct, the shape of the call's keys and
         values, and the scratch by number of query heads."""
         made = self._made.get(cache._key)
         if made is None:

@@ -162,3 +162,16 @@ def test_attributes_are_not_replaced():
     b.lens[0] = 5
     assert b.lens.tolist() == [5, 1] and b.lens.data_ptr() == at
     c.note = b.note = 1  # what a program hangs on them is its own
+
+
+def test_batch_and_cache_on_one_device():
+    """A batch that has served a cache is still refused for one of the same shape on another device."""
+    b = mp.KvBatch(torch.zeros(2, 2, dtype=torch.int32), torch.zeros(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int64), 2)
+    near, far = (mp.KvCache(4, 32, 2, 64, device) for device in ("cpu", "meta"))
+    x = torch.zeros(2, 2, 64, dtype=torch.float16)
+    mp.kv_attend_workspace_bytes(near, b, 4)
+    for _ in range(2):
+        for call in (lambda: mp.kv_attend_workspace_bytes(far, b, 4), lambda: mp.kv_write(far, b, x, x),
+                     lambda: mp.kv_read(far, b), lambda: mp.kv_attend(far, b, x)):
+            with pytest.raises(ValueError, match="batch is on cpu, the cache on meta"):
+                call()
