@@ -145,8 +145,11 @@ def _status(status, batch):
     return _tensor("status", status, torch.int32, (batch.n_seqs,), batch.device)
 
 
-# torch.cuda.current_stream() builds a Stream object: 5 us of a call's 22
-_stream = torch._C._cuda_getCurrentRawStream
+def _stream(cache):
+    if cache._index < 0:
+        raise ValueError(f"the cache is on {cache.device}: these calls run on a GPU")
+    # torch.cuda.current_stream() builds a Stream object: 5 us of a call's 22
+    return torch._C._cuda_getCurrentRawStream(cache._index)
 
 
 _workspaces = {}
@@ -173,8 +176,8 @@ def kv_write(cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tensor, s
             return kv_write(cache, batch, k, v, status)
     ref, shape, _ = batch._for(cache)
     kt, vt = _tokens("k", k, cache, shape), _tokens("v", v, cache, shape)
-    status = _status(status, batch)
-    _check("mp_kv_write", _lib.load().mp_kv_write(cache._ref, ref, kt, vt, status.data_ptr() or None, _stream(cache._index)))
+    status, stream_ptr = _status(status, batch), _stream(cache)
+    _check("mp_kv_write", _lib.load().mp_kv_write(cache._ref, ref, kt, vt, status.data_ptr() or None, stream_ptr))
     return status
 
 
@@ -197,8 +200,8 @@ def kv_read(cache: KvCache, batch: KvBatch, dtype=torch.bfloat16, k=None, v=None
         if v is None:
             v = torch.empty_like(k) if k.is_contiguous() and k.dtype == dtype else torch.empty(shape, dtype=dtype, device=cache.device)
             vt = _fresh(v, shape[1], shape[2])
-    status = _status(status, batch)
-    _check("mp_kv_read", _lib.load().mp_kv_read(cache._ref, ref, kt, vt, status.data_ptr() or None, _stream(cache._index)))
+    status, stream_ptr = _status(status, batch), _stream(cache)
+    _check("mp_kv_read", _lib.load().mp_kv_read(cache._ref, ref, kt, vt, status.data_ptr() or None, stream_ptr))
     return k, v, status
 
 
@@ -232,8 +235,7 @@ def kv_attend(cache: KvCache, batch: KvBatch, q: torch.Tensor, scale: float | No
         _tensor("lse", lse, torch.float32, (shape[0], heads), cache.device)
     elif want_lse:
         lse = torch.empty((shape[0], heads), dtype=torch.float32, device=q.device)
-    status = _status(status, batch)
-    stream_ptr = _stream(cache._index)
+    status, stream_ptr = _status(status, batch), _stream(cache)
     need = needs.get(heads)
     if need is None:
         need = kv_attend_workspace_bytes(cache, batch, heads)

@@ -175,3 +175,28 @@ def test_batch_and_cache_on_one_device():
                      lambda: mp.kv_read(far, b), lambda: mp.kv_attend(far, b, x)):
             with pytest.raises(ValueError, match="batch is on cpu, the cache on meta"):
                 call()
+
+
+def test_tensors_in_host_memory_are_refused(monkeypatch):
+    """No call hands a kernel an address of host memory: with a cache, batch and tokens on the CPU, each stops before the
+    library is called."""
+
+    class Library:
+        def __getattr__(self, name):
+            def call(*args):
+                launched.append(name)
+                return _lib.OK if name != "mp_kv_attend_workspace_bytes" else 0
+
+            return call
+
+    launched = []
+    monkeypatch.setattr(_lib, "load", Library)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 0, raising=False)
+    c = mp.KvCache(4, 32, 2, 64, "cpu")
+    b = mp.KvBatch(torch.zeros(2, 2, dtype=torch.int32), torch.zeros(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int64), 2)
+    x = torch.zeros(2, 2, 64, dtype=torch.float16)
+    for call in (lambda: mp.kv_write(c, b, x, x), lambda: mp.kv_read(c, b), lambda: mp.kv_read(c, b, x.dtype, k=x, v=x),
+                 lambda: mp.kv_attend(c, b, x), lambda: mp.kv_attend(c, b, x, out=x, want_lse=True)):
+        with pytest.raises(ValueError, match="run on a GPU"):
+            call()
+    assert not [name for name in launched if name != "mp_kv_attend_workspace_bytes"]
