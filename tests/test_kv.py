@@ -200,3 +200,15 @@ def test_tensors_in_host_memory_are_refused(monkeypatch):
         with pytest.raises(ValueError, match="run on a GPU"):
             call()
     assert not [name for name in launched if name != "mp_kv_attend_workspace_bytes"]
+
+
+def test_import_without_cuda_in_pytorch():
+    """A PyTorch built without CUDA has no raw streams; the package can be imported there all the same (its planner's
+    host-side parts and checks need no GPU)."""
+    import os
+    import subprocess
+    import sys
+
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    code = "import torch; del torch._C._cuda_getCurrentRawStream; import paper_2203_00448_gb300 as mp; mp.KvCache(1, 32, 1, 64, 'cpu')"
+    subprocess.run([sys.executable, "-c", code], cwd=root, check=True, timeout=300)
