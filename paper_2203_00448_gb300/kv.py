@@ -145,6 +145,20 @@ def _status(status, batch):
     return _tensor("status", status, torch.int32, (batch.n_seqs,), batch.device)
 
 
+def _away(cache, stream):
+    """Whether a call has to change the current stream or device first: kernels are launched on the current device."""
+    return stream is not None or (cache._index >= 0 and torch._C._cuda_getDevice() != cache._index)
+
+
+def _at(cache, stream):
+    """... the context in which it is made."""
+    if stream is None:
+        return torch.cuda.device(cache._index)
+    if stream.device_index != cache._index:
+        raise ValueError(f"the stream is on device {stream.device_index}, the cache on {cache.device}")
+    return torch.cuda.stream(stream)
+
+
 def _stream(cache):
     if cache._index < 0:
         raise ValueError(f"the cache is on {cache.device}: these calls run on a GPU")
@@ -171,8 +185,8 @@ def _workspace_of(stream_ptr, device):
 def kv_write(cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tensor, status=None, stream=None):
     """Quantises the call's keys and values ([n_tokens, n_heads, head_dim], any strides with dense values) into the
     blocks of their positions.  Returns the status of each sequence."""
-    if stream is not None:
-        with torch.cuda.stream(stream):
+    if _away(cache, stream):
+        with _at(cache, stream):
             return kv_write(cache, batch, k, v, status)
     ref, shape, _ = batch._for(cache)
     kt, vt = _tokens("k", k, cache, shape), _tokens("v", v, cache, shape)
@@ -183,8 +197,8 @@ def kv_write(cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tensor, s
 
 def kv_read(cache: KvCache, batch: KvBatch, dtype=torch.bfloat16, k=None, v=None, status=None, stream=None):
     """Reads the last n_b of the tokens that each sequence holds back.  Returns (k, v, status)."""
-    if stream is not None:
-        with torch.cuda.stream(stream):
+    if _away(cache, stream):
+        with _at(cache, stream):
             return kv_read(cache, batch, dtype, k, v, status)
     ref, shape, _ = batch._for(cache)
     if k is not None:
@@ -220,8 +234,8 @@ def kv_attend(cache: KvCache, batch: KvBatch, q: torch.Tensor, scale: float | No
     sequences hold: causal unless told otherwise, over the last `window` positions if that is not 0, scale 1 /
     sqrt(head_dim) unless given.  Returns (out, lse or None, status); a query that sees nothing gets 0 and -inf.  Scratch
     is the stream's unless given, and the graph's own in a capture."""
-    if stream is not None:
-        with torch.cuda.stream(stream):
+    if _away(cache, stream):
+        with _at(cache, stream):
             return kv_attend(cache, batch, q, scale, causal, window, out, lse, want_lse, status, workspace)
     ref, shape, needs = batch._for(cache)
     qt = _tokens("q", q, cache, (shape[0], None, shape[2]))

@@ -212,3 +212,49 @@ def test_import_without_cuda_in_pytorch():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     code = "import torch; del torch._C._cuda_getCurrentRawStream; import paper_2203_00448_gb300 as mp; mp.KvCache(1, 32, 1, 64, 'cpu')"
     subprocess.run([sys.executable, "-c", code], cwd=root, check=True, timeout=300)
+
+
+def test_calls_run_on_the_device_of_the_cache(monkeypatch):
+    """With another device current, a call makes the cache's current for its launch and puts the other back; a stream has to
+    be the cache's device's.  Two devices, both made up."""
+    from contextlib import contextmanager
+    from types import SimpleNamespace
+
+    from paper_2203_00448_gb300 import kv
+
+    now, launches = [1], []
+
+    @contextmanager
+    def device(index):
+        had, now[0] = now[0], index
+        yield
+        now[0] = had
+
+    class Library:
+        def __getattr__(self, name):
+            def call(*args):
+                if name == "mp_kv_attend_workspace_bytes":
+                    return 0
+                launches.append((name, now[0], args[-1]))
+                return _lib.OK
+
+            return call
+
+    monkeypatch.setattr(_lib, "load", Library)
+    monkeypatch.setattr(torch.cuda, "device", device)
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: device(s.device_index))
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: now[0], raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 100 + index, raising=False)
+    monkeypatch.setattr(kv, "_tokens", lambda name, t, cache, shape: _lib.MpTokens(0, 64, 64, 2, 0))
+    c = mp.KvCache(4, 32, 2, 64, "cpu")
+    c._index = 0
+    b = mp.KvBatch(torch.zeros(2, 2, dtype=torch.int32), torch.zeros(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int64), 2)
+    x = torch.zeros(2, 2, 64, dtype=torch.float16)
+    calls = [lambda **kw: mp.kv_write(c, b, x, x, **kw), lambda **kw: mp.kv_read(c, b, **kw), lambda **kw: mp.kv_attend(c, b, x, **kw)]
+    for call in calls:
+        call()
+        call(stream=SimpleNamespace(device_index=0))
+        with pytest.raises(ValueError, match="stream is on device 1"):
+            call(stream=SimpleNamespace(device_index=1))
+    assert [x[0] for x in launches] == ["mp_kv_write"] * 2 + ["mp_kv_read"] * 2 + ["mp_kv_attend"] * 2
+    assert all(x[1:] == (0, 100) for x in launches) and now == [1]
