@@ -70,6 +70,9 @@ class KvCache(_Fixed):
         self.k, self.v = make("k", k, torch.uint8, shape), make("v", v, torch.uint8, shape)
         self.k_scale = make("k_scale", k_scale, torch.float32, shape[:2])
         self.v_scale = make("v_scale", v_scale, torch.float32, shape[:2])
+        for name, t in (("k", self.k), ("v", self.v)):
+            if t.data_ptr() % 16:
+                raise ValueError(f"{name} has to start on a 16-byte boundary")
         self.device = self.k.device
         self._struct = _lib.MpKvCache(n_blocks, block_tokens, n_heads, head_dim, _ptr(self.k), _ptr(self.v),
                                       _ptr(self.k_scale), _ptr(self.v_scale))

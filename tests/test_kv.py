@@ -258,3 +258,18 @@ def test_calls_run_on_the_device_of_the_cache(monkeypatch):
             call(stream=SimpleNamespace(device_index=1))
     assert [x[0] for x in launches] == ["mp_kv_write"] * 2 + ["mp_kv_read"] * 2 + ["mp_kv_attend"] * 2
     assert all(x[1:] == (0, 100) for x in launches) and now == [1]
+
+
+def test_caches_start_on_16_byte_boundaries(lib):
+    """A pool that every call would refuse is refused at once: the size of the scratch asked for with it, 0, would otherwise
+    be kept for valid ones of its shape."""
+    shape = (4, 2, 32 * 64)
+    room = torch.zeros(4 * 2 * 32 * 64 + 64, dtype=torch.uint8)
+    start = -room.data_ptr() % 16
+    at = [room[start + i:start + i + 4 * 2 * 32 * 64].view(shape) for i in (0, 8, 1, 16)]
+    for bad in (dict(k=at[1], v=at[0]), dict(k=at[0], v=at[2]), dict(k=at[1])):
+        with pytest.raises(ValueError, match="16-byte"):
+            mp.KvCache(4, 32, 2, 64, "cpu", **bad)
+    c = mp.KvCache(4, 32, 2, 64, k=at[0], v=at[3])
+    b = mp.KvBatch(torch.zeros(2, 1000, dtype=torch.int32), torch.zeros(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int64), 2)
+    assert mp.kv_attend_workspace_bytes(c, b, 4) > 0
