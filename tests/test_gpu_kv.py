@@ -660,3 +660,48 @@ def test_captured_calls_have_scratch_of_their_own(cuda_lib):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
     assert all(bool((x == 3).all()) for x in theirs)
+
+
+@pytest.mark.parametrize("group,d,dtype,causal,window", [
+    (4, 128, BF16, True, 0), (4, 64, F16, True, 0), (3, 128, F16, True, 900), (1, 64, BF16, False, 0), (8, 128, BF16, True, 0)])
+def test_attend_by_both_long_kernels(cuda_lib, group, d, dtype, causal, window):
+    """Batches whose bound on what is cached passes 256 MB: sequences of up to 16 rows a head go to one kernel, the others to
+    the second, and the joining has rows of the first and cuts of the second at once.  On either side of the 16 rows, of one
+    row tile and of two, contexts cut between warps and between CTAs, sequences without tokens and without a past."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(100 * group + d)
+    heads, block = 2, 64
+    most = 16 // group
+    seqs = [(5000, 1), (700, most), (900, most + 1), (0, 0), (3100, 300), (0, 2), (1, 1), (2500, 128 // group), (40, 0),
+            (64, 64), (1300, 128 // group + 1), (33, most), (2, 5)]
+    seqs += [(int(n), 1) for n in rng.integers(1, 6000, 12)] + [(int(n), 18) for n in rng.integers(18, 3000, 4)]
+    order = rng.permutation(len(seqs))
+    lens, new = [seqs[i][0] for i in order], [seqs[i][1] for i in order]
+    table, n = R.make_table(lens, block, rng)
+    bound = (256 << 20) // (len(lens) * heads * d * 2) // block * block + block  # tokens a sequence might hold
+    wide = np.full((len(lens), bound // block), -1, np.int32)
+    wide[:, :table.shape[1]] = table
+    assert len(lens) * bound * heads * d * 2 > 256 << 20 and sum(new) != len(new) * max(new)
+    pool = R.Pool(n, block, heads, d, rng)
+    pool.vs[:] = np.exp2(rng.integers(-12, 3, pool.vs.shape))
+    pool.ks[:] = np.exp2(rng.integers(-9, -5, pool.ks.shape))
+    q, qx = rows(rng, sum(new), heads * group, d, dtype)
+    out = check_attend(mp, pool, wide, lens, new, q, qx, d ** -0.5, causal, window, max_len=bound)
+    # the same result from scratch that holds anything, and status of its own for either kind of sequence
+    cache = pool.cache()
+    few, many = order.tolist().index(0), order.tolist().index(4)
+    wide[few, 0], wide[many, 0] = n, -1
+    if window:  # what a window does not reach is not looked at
+        wide[few, lens[few] // block], wide[many, lens[many] // block] = n, -1
+    batch = batch_of(mp, wide, lens, new, max_len=bound)
+    ptr = np.concatenate([[0], np.cumsum(new)])
+    for fill in (0, 255):
+        ws = mp.Workspace("cuda")
+        ws.get(mp.kv_attend_workspace_bytes(cache, batch, heads * group))
+        ws.buf.fill_(fill)
+        again, _, status = mp.kv_attend(cache, batch, q, causal=causal, window=window, workspace=ws)
+        assert status.tolist() == [int(b in (few, many)) for b in range(len(lens))]
+        for b in range(len(lens)):
+            if b not in (few, many):
+                assert np.array_equal(again[ptr[b]:ptr[b + 1]].double().cpu().numpy(), out[ptr[b]:ptr[b + 1]])
