@@ -370,8 +370,10 @@ __global__ void __launch_bounds__(few_warps(D, NT) * 32, 1) k_kv_attend_few(Atte
         if (lane == 0) {
             ring_page[st] = page_ahead;
             mbar_expect(&bar[st], 2 * kBytes);
-            bulk_load(ring + st * 2 * kBytes, a.c.k + at, kBytes, &bar[st]);
-            bulk_load(ring + st * 2 * kBytes + kBytes, a.c.v + at, kBytes, &bar[st]);
+            if (!test_held(a, issued)) {
+                bulk_load(ring + st * 2 * kBytes, a.c.k + at, kBytes, &bar[st]);
+                bulk_load(ring + st * 2 * kBytes + kBytes, a.c.v + at, kBytes, &bar[st]);
+            }
         }
         if (++issued < u1) {
             next<kRows>(a, ahead);
@@ -834,6 +836,10 @@ size_t kv_attend_workspace_bytes(const mp_kv_cache& c, const mp_kv_batch& bt, in
     return bt.n_seqs == 0 ? 0 : layout(c, bt, n_q_heads / c.n_heads).bytes;
 }
 
+#ifdef MP_TEST_HOOKS
+static int64_t g_test_kv_hold = -1;
+#endif
+
 cudaError_t launch_kv_attend(const mp_kv_cache& c, const mp_kv_batch& bt, const mp_tokens& q, float scale,
                              int32_t causal, int32_t window, const mp_tokens& out, float* lse, int32_t* status,
                              void* workspace, cudaStream_t stream) {
@@ -849,6 +855,9 @@ cudaError_t launch_kv_attend(const mp_kv_cache& c, const mp_kv_batch& bt, const 
     a.group = group;
     a.few_rows = r.few || r.brief ? kFewRows : -1;
     a.wide_q = rows_aligned(q), a.wide_out = rows_aligned(out);
+#ifdef MP_TEST_HOOKS
+    a.hold = g_test_kv_hold;
+#endif
     FewWork few = {};
     ManyWork many = {};
     if (r.few) {
@@ -869,3 +878,8 @@ cudaError_t launch_kv_attend(const mp_kv_cache& c, const mp_kv_batch& bt, const 
 }
 
 }  // namespace mp
+
+#ifdef MP_TEST_HOOKS
+// Test builds only: later mp_kv_attend calls of this process hold the unit back (-1: none).
+extern "C" __attribute__((visibility("default"))) void mp_test_kv_hold(int64_t unit) { mp::g_test_kv_hold = unit; }
+#endif

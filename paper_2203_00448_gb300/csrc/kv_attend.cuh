@@ -98,7 +98,17 @@ struct AttendArgs {
     int32_t group;     // query heads a cache head
     int32_t few_rows;  // sequences of at most this many rows (tokens x group) are k_kv_attend_few's, the others k_kv_attend_many's
     bool wide_q, wide_out;
+#ifdef MP_TEST_HOOKS
+    int64_t hold;  // a unit whose bytes never come, so that waits run out (-1: none)
+#endif
 };
+// Test builds (MP_TEST_HOOKS) can hold a unit back: k_kv_attend_few's by its place on the line, k_kv_attend_many's by its
+// number in the first CTA.
+#ifdef MP_TEST_HOOKS
+__device__ __forceinline__ bool test_held(const AttendArgs& a, int64_t unit) { return unit == a.hold; }
+#else
+__device__ __forceinline__ bool test_held(const AttendArgs&, int64_t) { return false; }
+#endif
 __device__ __forceinline__ bool seq_is_few(const AttendArgs& a, const SeqView& s) {
     return (int64_t)s.n * a.group <= a.few_rows;
 }

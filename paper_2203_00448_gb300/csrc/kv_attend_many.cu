@@ -382,7 +382,7 @@ __device__ void convert_role(const AttendArgs& a, Smem<D>& m) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) widen(kr[i], to + i * 256);
         fence_smem();
-        mbar_arrive(&m.k_full[st]);
+        if (!(blockIdx.x == 0 && tid == 0 && test_held(a, it))) mbar_arrive(&m.k_full[st]);
         const bool again = more;
         if (again) {
             locate();
@@ -830,6 +830,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend_many(AttendArgs a, Ma
     if (wid < kSoftmaxWarps) {
         more_regs<kSoftmaxRegs>();
         softmax_role<T, D>(a, work, m);
+        wait_st();  // a tile that gave up may have weights on their way, and tensor memory goes below
     } else if (wid < kSoftmaxWarps + 4) {
         fewer_regs<kConvertRegs>();
         convert_role<T, D>(a, m);
