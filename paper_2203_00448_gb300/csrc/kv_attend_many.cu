@@ -54,8 +54,7 @@ constexpr int kLineReaders = kSoftmaxWarps + 4 + 2;  // warps that read a stretc
 constexpr int kThreads = 16 * 32;
 // Registers a thread after the roles part: 256 x 176 + 128 x 112 + 128 x 48 = 512 x 128, the launch's.
 constexpr int kSoftmaxRegs = 176, kConvertRegs = 112, kProductRegs = 48;
-constexpr int kTries = (int)(kKvSpinCycles >> 8);  // of a wait: some tens of cycles each
-constexpr int kUnitCycles = 1 << 16;               // a unit takes less by far
+constexpr int kUnitCycles = 1 << 16;  // a unit takes less by far
 constexpr int kStrips = 1024;
 constexpr float kGrow = 8.f;
 
@@ -240,10 +239,14 @@ struct Smem {
     int gave_up;
 };
 
-// Waits until the phase ends; false if some wait of the CTA has given up, which one does after kTries.
+// Waits until the phase ends; false if some wait of the CTA has given up, which one does after kKvSpinCycles (by the
+// clock: a try may take thousands of cycles).
 __device__ __forceinline__ bool await(uint64_t* bar, uint32_t parity, volatile int* gave_up) {
-    for (int i = 0; !mbar_try(bar, parity); ++i)
-        if (i > kTries || *gave_up) {
+    static_assert(kKvSpinCycles < 1ll << 32, "the clock's low word tells");
+    if (mbar_try(bar, parity)) return true;
+    const uint32_t t0 = clock();
+    while (!mbar_try(bar, parity))
+        if (*gave_up || (uint32_t)clock() - t0 > (uint32_t)kKvSpinCycles) {
             *gave_up = 1;
             return false;
         }

@@ -53,10 +53,15 @@ def test_attention_wait_runs_out(hooks, kernel, lens, new, units, d, dtype):
     first = new[0]
     for unit in units:
         hooks(unit)
+        start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        start.record()
         out, lse, status = mp.kv_attend(cache, batch, q, want_lse=True)
+        end.record()
         hooks(-1)
         assert status.tolist() == ([mp.ETIMEOUT, 0, 0] if kernel == "few" else [mp.ETIMEOUT] * 3)
         if kernel == "few":  # one warp gave up; the others' sequences are whole
             assert torch.equal(out[first:], want[first:]) and torch.equal(lse[first:], want_lse[first:])
+        # 2^24 cycles, twice at most (the wait, and what it leaves in flight), at 1 GHz or more, beside the call itself
+        assert start.elapsed_time(end) < 40
         out, lse, status = mp.kv_attend(cache, batch, q, want_lse=True)
         assert not status.any() and torch.equal(out, want) and torch.equal(lse, want_lse)
