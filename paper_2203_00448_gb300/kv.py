@@ -199,7 +199,8 @@ def kv_write(cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tensor, s
 
 
 def kv_read(cache: KvCache, batch: KvBatch, dtype=torch.bfloat16, k=None, v=None, status=None, stream=None):
-    """Reads the last n_b of the tokens that each sequence holds back.  Returns (k, v, status)."""
+    """Reads the last n_b of the tokens that each sequence holds back, as `dtype` or as a k or v that is given.  Returns
+    (k, v, status)."""
     if _away(cache, stream):
         with _at(cache, stream):
             return kv_read(cache, batch, dtype, k, v, status)
@@ -209,13 +210,15 @@ def kv_read(cache: KvCache, batch: KvBatch, dtype=torch.bfloat16, k=None, v=None
     if v is not None:
         vt = _tokens("v", v, cache, shape)
     if k is None or v is None:
+        if k is not None or v is not None:
+            dtype = (v if k is None else k).dtype
         if dtype not in _DTYPES:
             raise ValueError(f"float16, bfloat16 or float32 can be read, not {dtype}")
         if k is None:
             k = torch.empty(shape, dtype=dtype, device=cache.device)
             kt = _fresh(k, shape[1], shape[2])
         if v is None:
-            v = torch.empty_like(k) if k.is_contiguous() and k.dtype == dtype else torch.empty(shape, dtype=dtype, device=cache.device)
+            v = torch.empty_like(k) if k.is_contiguous() else torch.empty(shape, dtype=dtype, device=cache.device)
             vt = _fresh(v, shape[1], shape[2])
     status, stream_ptr = _status(status, batch), _stream(cache)
     _check("mp_kv_read", _lib.load().mp_kv_read(cache._ref, ref, kt, vt, status.data_ptr() or None, stream_ptr))

@@ -705,3 +705,23 @@ def test_attend_by_both_long_kernels(cuda_lib, group, d, dtype, causal, window):
         for b in range(len(lens)):
             if b not in (few, many):
                 assert np.array_equal(again[ptr[b]:ptr[b + 1]].double().cpu().numpy(), out[ptr[b]:ptr[b + 1]])
+
+
+def test_read_follows_the_tensor_that_is_given(cuda_lib):
+    """kv_read with one of k and v, whatever type and layout it has: the other comes in the same type."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(59)
+    lens, new = [100, 7], [33, 7]
+    table, n = R.make_table(lens, 32, rng)
+    pool = R.Pool(n, 32, 3, 64, rng)
+    cache, batch = pool.cache(), batch_of(mp, table, lens, new)
+    want = [np.concatenate(x) for x in zip(*(R.held(pool, table, b, lens[b] - new[b], lens[b]) for b in range(2)))]
+    for dtype in (F16, BF16, F32):
+        for how in ("plain", "heads"):
+            mine, _ = rows(rng, sum(new), 3, 64, dtype, how)
+            for name in ("k", "v"):
+                k, v, status = mp.kv_read(cache, batch, **{name: mine})
+                assert (k if name == "k" else v) is mine and k.dtype == v.dtype == dtype and not status.any()
+                for x, y in ((k, want[0]), (v, want[1])):
+                    assert torch.equal(x.cpu(), torch.from_numpy(y).to(dtype))
