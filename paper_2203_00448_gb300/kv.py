@@ -18,6 +18,7 @@ import torch
 from . import _lib
 from .api import Workspace, _check, _ptr
 
+_MOST = 1 << 28  # positions, tokens and query rows a head of a sequence
 _DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}  # mp_dtype
 
 
@@ -89,7 +90,7 @@ class KvBatch(_Fixed):
     """The sequences of a call.  table int32[B, columns]: pool block of each run of block_tokens positions; lens
     int32[B]: tokens held, the call's included; token_ptr int64[B + 1]: rows of the call's tensors, the last ones that
     each sequence holds.  Host bounds: n_tokens = token_ptr[B]; max_tokens of a sequence in the call (default n_tokens);
-    max_len >= lens (default what the table has room for)."""
+    max_len >= lens (default what the table has room for).  Either is at most 2^28."""
 
     _fixed = frozenset(("table", "lens", "token_ptr", "n_tokens", "max_tokens", "max_len", "n_seqs", "device"))
 
@@ -104,6 +105,9 @@ class KvBatch(_Fixed):
         self.n_tokens = int(n_tokens)
         self.max_tokens = self.n_tokens if max_tokens is None else int(max_tokens)
         self.max_len = max_len
+        for name, bound in (("max_tokens", self.max_tokens), ("max_len", max_len or 0)):
+            if not 0 <= bound <= _MOST:
+                raise ValueError(f"{name} is {bound}: 0 to 2^28 is possible")
         self.n_seqs, self.device = B, table.device
         self._made = {}
 
@@ -114,7 +118,7 @@ class KvBatch(_Fixed):
         if made is None:
             if cache.device != self.device:
                 raise ValueError(f"the batch is on {self.device}, the cache on {cache.device}")
-            room = self.table.shape[1] * cache.block_tokens
+            room = min(self.table.shape[1] * cache.block_tokens, _MOST)
             s = _lib.MpKvBatch(self.n_seqs, self.table.shape[1], self.max_tokens,
                                room if self.max_len is None else int(self.max_len), self.n_tokens, _ptr(self.table),
                                _ptr(self.lens), _ptr(self.token_ptr))
@@ -266,6 +270,6 @@ def kv_attend(cache: KvCache, batch: KvBatch, q: torch.Tensor, scale: float | No
         wptr, wbytes = None, 0
     _check("mp_kv_attend",
            _lib.load().mp_kv_attend(cache._ref, ref, qt, shape[2] ** -0.5 if scale is None else scale, 1 if causal else 0,
-                                    window, ot, None if lse is None else lse.data_ptr() or None, status.data_ptr() or None,
-                                    wptr, wbytes, stream_ptr))
+                                    max(-1, min(window, 0x7fffffff)), ot, None if lse is None else lse.data_ptr() or None,
+                                    status.data_ptr() or None, wptr, wbytes, stream_ptr))
     return out, lse, status

@@ -273,3 +273,39 @@ def test_caches_start_on_16_byte_boundaries(lib):
     c = mp.KvCache(4, 32, 2, 64, k=at[0], v=at[3])
     b = mp.KvBatch(torch.zeros(2, 1000, dtype=torch.int32), torch.zeros(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int64), 2)
     assert mp.kv_attend_workspace_bytes(c, b, 4) > 0
+
+
+def test_bounds_past_32_bits(monkeypatch):
+    """Numbers that 32 bits do not hold do not come out of them as others: bounds are refused, a window is as good as none."""
+    table, lens, ptr = torch.zeros(2, 2, dtype=torch.int32), torch.zeros(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int64)
+    for bad in (dict(max_tokens=(1 << 32) + 5), dict(max_tokens=-1), dict(max_len=(1 << 32) + 64), dict(max_len=-1 << 32),
+                dict(max_len=(1 << 28) + 1), dict(max_tokens=(1 << 28) + 1)):
+        with pytest.raises(ValueError, match="2\\^28"):
+            mp.KvBatch(table, lens, ptr, 2, **bad)
+    c = mp.KvCache(4, 256, 2, 64, "cpu")
+    wide = mp.KvBatch(torch.zeros(2, 1, dtype=torch.int32), lens, ptr, 2)
+    assert wide._for(c)[0]._obj.max_len == 256
+    # a table of 2^24 + 1 columns, which nobody reads here
+    long = mp.KvBatch(torch.empty(2, (1 << 24) + 1, dtype=torch.int32), lens, ptr, 2)
+    assert long._for(c)[0]._obj.max_len == 1 << 28
+
+    windows = []
+
+    class Library:
+        def __getattr__(self, name):
+            def call(*args):
+                if name == "mp_kv_attend":
+                    windows.append(args[5])
+                return _lib.OK
+
+            return call
+
+    monkeypatch.setattr(_lib, "load", Library)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 0, raising=False)
+    monkeypatch.setattr(mp.kv, "_tokens", lambda name, t, cache, shape: _lib.MpTokens(0, 64, 64, 2, 0))
+    c._index = 0
+    x = torch.zeros(2, 2, 64, dtype=torch.float16)
+    for window in (0, 7, (1 << 32) + 7, 1 << 63, -5, -(1 << 32) + 7):
+        mp.kv_attend(c, wide, x, window=window)
+    assert windows == [0, 7, (1 << 31) - 1, (1 << 31) - 1, -1, -1]
