@@ -179,7 +179,7 @@ _workspaces = {}
 def _workspace_of(stream_ptr, device):
     # A captured call's scratch belongs to its graph's memory: replays may overlap whatever runs on the stream of the
     # capture, other graphs captured there among it, and go on when that stream's own scratch has been replaced.
-    if torch.cuda.is_current_stream_capturing():
+    if torch._C._cuda_isCurrentStreamCapturing():
         return Workspace(device)
     # calls on different streams may overlap: each stream has its own
     key = (device.index, stream_ptr)
@@ -248,6 +248,8 @@ def kv_attend(cache: KvCache, batch: KvBatch, q: torch.Tensor, scale: float | No
         with _at(cache, stream):
             return kv_attend(cache, batch, q, scale, causal, window, out, lse, want_lse, status, workspace)
     ref, shape, needs = batch._for(cache)
+    if not 0 <= window <= 0x7fffffff:
+        window = -1 if window < 0 else 0x7fffffff
     qt = _tokens("q", q, cache, (shape[0], None, shape[2]))
     heads = qt.n_heads
     if out is None:
@@ -270,6 +272,6 @@ def kv_attend(cache: KvCache, batch: KvBatch, q: torch.Tensor, scale: float | No
         wptr, wbytes = None, 0
     _check("mp_kv_attend",
            _lib.load().mp_kv_attend(cache._ref, ref, qt, shape[2] ** -0.5 if scale is None else scale, 1 if causal else 0,
-                                    max(-1, min(window, 0x7fffffff)), ot, None if lse is None else lse.data_ptr() or None,
+                                    window, ot, None if lse is None else lse.data_ptr() or None,
                                     status.data_ptr() or None, wptr, wbytes, stream_ptr))
     return out, lse, status
