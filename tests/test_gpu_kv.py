@@ -725,3 +725,30 @@ def test_read_follows_the_tensor_that_is_given(cuda_lib):
                 assert (k if name == "k" else v) is mine and k.dtype == v.dtype == dtype and not status.any()
                 for x, y in ((k, want[0]), (v, want[1])):
                     assert torch.equal(x.cpu(), torch.from_numpy(y).to(dtype))
+
+
+@pytest.mark.parametrize("seqs", [[(300, 1), (90, 4)], [(6000, 3), (5000, 1)], [(400, 90), (65, 64)], [(5000, 300), (3000, 20)]])
+@pytest.mark.parametrize("d,dtype", [(64, F16), (128, BF16)])
+def test_attend_value_scales_as_far_apart_as_they_may_be(cuda_lib, seqs, d, dtype):
+    """Value scales of 2^-80 among 2^20 (2^3 with outputs in f16), the small ones' tokens holding most of the weight, before
+    and after the large ones': each weight counts in the sum although its values do not in the output."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(61)
+    lens, new = [s[0] for s in seqs], [s[1] for s in seqs]
+    table, n = R.make_table(lens, 32, rng)
+    pool = R.Pool(n, 32, 2, d, rng)
+    pool.ks[:] = 2.0 ** -8
+    large, small = (2.0 ** 3 if dtype == F16 else 2.0 ** 20), 2.0 ** -80
+    pool.vs[:] = small
+    for b in range(2):
+        pool.vs[table[b, 1::4]] = large
+        pool.vs[table[b, 0]] = (large, small)[b]
+    q, qx = rows(rng, sum(new), 4, d, dtype)
+    want, want_lse, mag, size = R.attend(pool, table, lens, new, qx, d ** -0.5)
+    out, lse, status = mp.kv_attend(pool.cache(), batch_of(mp, table, lens, new), q, want_lse=True)
+    bound, lse_bound = R.attend_bounds(dtype, want, want_lse, mag, size)
+    assert not status.any()
+    # exponents of up to 2^7 in units of log 2 keep 2^-18: twice in a weight, and in the log-sum's two terms
+    assert (np.abs(out.double().cpu().numpy() - want) <= bound + 2.0 ** -16 * mag).all()
+    assert (np.abs(lse.double().cpu().numpy() - want_lse) <= lse_bound + 2.0 ** -16).all()
