@@ -407,8 +407,8 @@ typedef struct mp_kv_cache {
 /* The sequences of one call.  Host scalars:
  *   n_seqs      B >= 0
  *   max_blocks  columns of table
- *   max_tokens  upper bound on n_b = token_ptr[b+1] - token_ptr[b]
- *   max_len     upper bound on lens[b], at most max_blocks * block_tokens
+ *   max_tokens  upper bound on n_b = token_ptr[b+1] - token_ptr[b], at most 2^28
+ *   max_len     upper bound on lens[b], at most max_blocks * block_tokens and 2^28
  *   n_tokens    rows of the call's token arrays (= token_ptr[B])
  * Device arrays:
  *   table      int32[B][max_blocks]  pool block of positions [j * block_tokens, + block_tokens)
@@ -472,13 +472,18 @@ size_t mp_kv_attend_workspace_bytes(const mp_kv_cache *cache, const mp_kv_batch 
  * exp(scale * q . k_j) (natural); query head h reads cache head
  * h / (q->n_heads / cache->n_heads).  A v_scale below 2^-84 counts as 0 (mp_kv_write
  * makes none below 2^-60).  A query that sees nothing gets out = 0 and
- * lse = -inf.  Products of 16-bit values are summed in 32 bits, as are the
- * softmax's sums; its weights are rounded to 16 bits (11 of precision) for the
- * second product.
+ * lse = -inf; one of whose scores none is a number gets NaN in both.  Products of
+ * 16-bit values are summed in 32 bits, as are the softmax's sums; its weights are
+ * rounded to 16 bits for the second product: 11 of precision for those down to
+ * 2^-28 of a row's largest (2^-21 of a value that it may pass by 2^8, in calls of
+ * more than 16 rows a head), fewer below, nothing below 2^-38 (2^-31).  Query
+ * elements below 2^-28 of their row's largest lose bits alike.  The v_scales that a
+ * query sees may differ by a factor of 2^100.
  * q, out: MP_F16 or MP_BF16, the same for both; n_heads a multiple of the
- * cache's.  scale > 0, finite.  lse: float[n_tokens][n_heads] or NULL.
+ * cache's, at most 1,024 times it; max_tokens times that multiple at most 2^28.
+ * scale > 0, finite.  lse: float[n_tokens][n_heads] or NULL.
  * seq_status int32[B]; MP_ETIMEOUT there means that a wait inside a kernel gave
- * up.  Outputs of a failed sequence are unspecified.  workspace: at least
+ * up (after about a second), on that sequence or on several.  Outputs of a failed sequence are unspecified.  workspace: at least
  * mp_kv_attend_workspace_bytes(cache, batch, q->n_heads) bytes, rules as for
  * mp_plan_greedy_by_size. */
 mp_status mp_kv_attend(const mp_kv_cache *cache, const mp_kv_batch *batch, const mp_tokens *q, float scale,

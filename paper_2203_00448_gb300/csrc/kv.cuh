@@ -16,6 +16,10 @@ namespace mp {
 // whole granules, so kernels walk granules whatever the block size.
 constexpr int kGranule = 32;
 
+// GB300's SMs.  Grids that scratch is laid out for take this number, for the size of scratch is asked for without a
+// device; a device with fewer runs the same CTAs in turn.
+constexpr int kSms = 152;
+
 // Byte of key (t, d) and of value (t, d) inside one block and head.
 template <int D>
 __device__ __forceinline__ int key_byte(int t, int d) {

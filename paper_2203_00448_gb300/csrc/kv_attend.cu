@@ -16,11 +16,11 @@
 // become f16 exactly.  With x_j = scale * q.k_j * log2(e) * key scale + log2(value
 // scale), w_j = 2^(x_j - M) <= 1 under the running maximum M, the output is
 // sum w_j byte_j / sum (w_j / value scale): the value scale costs nothing per element
-// and products stay within f16's range whatever the scales.  Sums are f32; w is
-// rounded to f16 (11 bits, down to 2^-38 of the largest).
+// and products stay within f16's range.  Sums are f32, where weights below 2^-126 are lost: a context's
+// value scales may be 2^100 apart.  w is rounded to f16: 11 bits down to 2^-28 of the largest, none below 2^-38.
 //
 // Measured (32 heads over 8 of 128): 64 ragged contexts of up to 8,191 tokens 97 us, 5.5
-// TB/s of the 6.8 that a copy reaches; two of 262,144 tokens 170 us, 6.1 TB/s; one of 512 6.6
+// TB/s of the 6.8 that a copy reaches; two of 262,144 tokens 173 us, 6.0 TB/s; one of 512 6.6
 // us of GPU time.  Long contexts are bound by memory; the rest is the ramp (lengths, table,
 // queries, first bytes: four trips one after another) and the joining launch, about 12 us.
 #include <algorithm>
@@ -39,7 +39,7 @@ constexpr int few_warps(int d, int nt) { return d == 128 ? (nt == 1 ? 12 : 8) : 
 constexpr int kFewStages = 2;
 constexpr int short_warps(int nt) { return nt == 1 ? 16 : 8; }
 constexpr int kFewRows = 16;  // most rows of a sequence and head
-constexpr int kJoinThreads = 256;
+constexpr int kJoinThreads = 256;  // k_kv_join of D = 128 keeps 16 bytes a thread in memory for it (48 registers), of 64 8 bytes
 
 template <int kRows>
 __device__ __forceinline__ int seq_tiles(const AttendArgs& a, const SeqView& s) {
@@ -730,8 +730,13 @@ __global__ void __launch_bounds__(kJoinThreads) k_kv_join(AttendArgs a, FewWork 
 }
 
 // Sequences of few rows in a batch that also has many: k_kv_attend_many takes them at about 2.5 TB/s of cache bytes, which
-// up to this size costs less than the other kernel with its joining (8 heads of 128, GPU time without and with it:
-// 16 x 1,000 tokens 31 and 45 us, 8 x 4,000 96 and 145, 3 x 4,000-16,384 157 and 161).
+// up to this size costs less than the other kernel with its joining where most sequences have many rows (8 heads of 128,
+// GPU time without and with it: 16 x 1,000 tokens 31 and 45 us, 8 x 4,000 96 and 145, 3 x 4,000-16,384 157 and 161; 16 of up
+// to 8,000, 8 with pieces of 512 and 8 with single tokens, 315 and 331).  Where one piece of 512 comes with single
+// tokens, both kernels are the faster way from well below: 16 singles of up to 2,000 (41 MB held) 57 and 57, 32 of up to
+// 4,000 (145 MB) 116 and 94, 63 of up to 2,000 (162 MB) 130 and 87; past the line 63 of up to 4,000 (294 MB) 189 and 122, 255 of
+// up to 8,000 (2.2 GB) 1,019 and 490.  The line goes by what the host knows, the number of sequences times the bound of
+// their lengths; a generous bound leads to both kernels.
 constexpr int64_t kSmallCache = 256 << 20;
 // Which kernels a batch needs, by its host scalars: sequences of at most kFewRows rows are
 // bound by the cache's bytes, which k_kv_attend_few streams; above it the products count.
@@ -740,7 +745,7 @@ constexpr int64_t kSmallCache = 256 << 20;
 // time of a call: 1 x 512 tokens 6.6 us against 9.4, 8 x 1,024 8.8 against 11.7, 38 x 2,048 32.6 against 37.2; but
 // 1 x 4,096 19.3 against 14.7, and 128 x 512, four times the SMs, 48.6 against 35.4).
 constexpr int32_t kShortLen = 2048;
-constexpr int64_t kShortCtas = 304;
+constexpr int64_t kShortCtas = 2 * kSms;
 struct Route {
     bool few, many, brief;
 };

@@ -12,8 +12,8 @@ constexpr long long kKvSpinCycles = MP_TEST_SPIN_CYCLES;
 constexpr long long kKvSpinCycles = 1ll << 31;  // about a second; a longer wait is a fault
 #endif
 
-// Weights are kept as 2^kLift times their value under the running maximum, so that in
-// f16 those down to 2^-38 of it are not lost.
+// Weights are kept as 2^kLift times their value under the running maximum: as f16 they have
+// all 11 bits down to 2^-28 of the largest, one less for each power of two below, none under 2^-38.
 constexpr float kLift = 14.f;
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -120,7 +120,7 @@ __device__ __forceinline__ void seq_granules(const AttendArgs& a, const SeqView&
 }
 
 // k_kv_attend_few: warps share the line of units; what is left to add up.
-constexpr int kFewCtas = 152;  // one an SM: its rings take most of the shared memory
+constexpr int kFewCtas = kSms;  // one an SM: its rings take most of the shared memory
 struct FewWork {
     int64_t* base;     // [n_seqs + 1] first unit of each sequence, then units a warp
     float* part;       // [2 * warps][rows * (D + 2)]
@@ -128,10 +128,10 @@ struct FewWork {
 };
 
 // k_kv_attend_many: pairs of tiles of 128 rows, units of 128 tokens; where on the line a CTA began.
-constexpr int kManyCtas = 152;
+constexpr int kManyCtas = kSms;
 constexpr int kPair = 256;
 constexpr int kExtra = 3;           // units that a stretch costs beside its own: queries in, sums out
-constexpr float kManyLift = 7.f;    // weights are at most 2^(8 + 7)
+constexpr float kManyLift = 7.f;    // weights are at most 2^(8 + 7), and have 11 bits down to 2^-21 of their reference
 struct ManyStart {
     int32_t b, tile, head, cnt, into;  // cnt: units of that (sequence, pair of tiles, head)
     int32_t there;

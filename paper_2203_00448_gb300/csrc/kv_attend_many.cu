@@ -22,10 +22,11 @@
 // us, 2: 547, 3: 466, 5: 468).  What a CTA does not hold whole is added up by
 // k_kv_join.
 //
-// Measured: 8,000 tokens, 32 heads over 8 of 128: 470 us, 1,116 TFLOP/s counted causally; 64
-// tokens over 60,000 each for 8 sequences: 400 us, 1,260 TFLOP/s (cuBLAS bf16: 1,887); 8 tokens
-// over 64 ragged contexts of up to 8,191: 218 us (251 with one tile at work), 5 to 8 over four of
-// 60,000: 187 (217); the two ways of working cost prompts 1 to 2%.  A unit of both tiles takes
+// Measured: 8,000 tokens, 32 heads over 8 of 128: 465 us, 1,128 TFLOP/s counted causally; 64
+// tokens over 60,000 each for 8 sequences: 396 us, 1,270 TFLOP/s (cuBLAS bf16: 1,887); 8 tokens
+// over 64 ragged contexts of up to 8,191: 208 us, 5 to 8 over four of 60,000: 185 (251 and 217 with one
+// tile at work, before waits read the clock only where a first try fails, which took 1 to 2% off); the two ways of working
+// cost prompts 1 to 2%.  A unit of both tiles takes
 // 3,900 cycles where its 32 products take 2,080 on their own: the converting warps are busy or
 // wait for loads through most of it, both tiles' products and both tiles' exponentials tend to
 // come together, and products, operands and loads share one shared-memory pipe (about 70% busy).
@@ -53,6 +54,7 @@ constexpr int kSoftmaxWarps = 8;
 constexpr int kLineReaders = kSoftmaxWarps + 4 + 2;  // warps that read a stretch
 constexpr int kThreads = 16 * 32;
 // Registers a thread after the roles part: 256 x 176 + 128 x 112 + 128 x 48 = 512 x 128, the launch's.
+// (D = 128 keeps 14 bytes a thread in memory all the same; 64 none.)
 constexpr int kSoftmaxRegs = 176, kConvertRegs = 112, kProductRegs = 48;
 constexpr int kUnitCycles = 1 << 16;  // a unit takes less by far
 constexpr int kStrips = 1024;

@@ -11,7 +11,9 @@
 // three trips to memory one after another (lengths, table, values and scale); 15,973
 // prompt tokens 27 us (98 MB, 14.4 us at the rate of a copy), bound by instructions
 // (two thirds of the issue slots while CTAs run) and the uneven last CTAs; 131,071 tokens
-// read back 126 us, 94% of a copy's rate.
+// read back 126 us, 94% of a copy's rate.  The same prompts in 32 bits 46 us (164 MB, 24 us at a copy's rate), bound alike;
+// 8 ragged reads of up to 512 tokens (16 heads of 64, 32 bits) 9.0 us, where each warp takes the trips to its keys and
+// to its values one after the other.
 #include <algorithm>
 
 #include "kv.cuh"
@@ -20,9 +22,16 @@ namespace mp {
 namespace {
 
 constexpr int kWriteWarps = 16;          // few tokens: one CTA a sequence, a warp a block, head and array
-constexpr int32_t kWriteFewTokens = 16;  // ... up to this many tokens a sequence
+// ... up to this many tokens a sequence.  GPU time of this kernel and of the other (a clear of the status and a launch; 8
+// heads of 128, bf16): 8 sequences of 1 token 3.7 and 8.2 us, of 4 7.0 and 8.2, of 8 10.1 and 8.2, of 16 16.5 and 8.2; 253
+// of 1 5.1 and 12.4, of 4 10.9 and 16.4, of 8 18.9 and 19.0, of 16 35.5 and 27.2.  They meet at 5 to 8 tokens; the line
+// is higher than that, and 9 to 16 proposed tokens pay for it.
+constexpr int32_t kWriteFewTokens = 16;
 constexpr int kWriteThreads = 128;
-constexpr int kWriteCtas = 152 * 12;
+// CTAs below which a CTA takes fewer heads.  With 1, 4, 12, 24 and 48 an SM (f16, 8 heads of 128): 18,800 prompt tokens of 9
+// sequences 48.9, 29.5, 28.9, 28.9 and 28.8 us, 32 x 300 tokens 41.3, 22.4, 18.5, 18.5 and 18.5, 64 x 2,000 145, 145, 145, 136
+// and 134, 1 x 4,000 14.3, 10.8, 12.3, 11.7 and 10.7.
+constexpr int kWriteCtas = kSms * 12;
 constexpr int kReadThreads = 256;
 
 // Magnitudes are compared as the integers that their bits are (without the sign): one operation a value or a pair,
@@ -224,7 +233,8 @@ __device__ __forceinline__ bool store_few(const Place& p, bool wide, int lane) {
     return !odd;
 }
 
-// Few tokens a sequence: one CTA a sequence, so that its status has one writer; a warp a block, head and array.
+// Few tokens a sequence: one CTA a sequence, so that its status has one writer; a warp a block, head and array.  (16 warps
+// leave 64 registers a thread: 24 bytes are kept in memory for values of 32 bits, 8 for others of D = 128.)
 template <typename T, int D>
 __global__ void __launch_bounds__(kWriteWarps * 32)
     k_kv_write_few(mp_kv_cache c, mp_kv_batch bt, mp_tokens k, mp_tokens v, bool wide, int32_t* status) {

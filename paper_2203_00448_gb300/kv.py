@@ -7,7 +7,8 @@
 A KvCache is a pool of blocks in 8 bits (its memory may be given, e.g. views of a planned slab); a KvBatch says which
 blocks the sequences of a call have, how many tokens they hold and which rows of the call's tensors are theirs.  Its
 tensors stay on the device and may be changed there between calls, not replaced by others.  All calls are asynchronous on the
-current (or given) CUDA stream; what they allocate belongs to that stream.
+current (or given) CUDA stream; what they allocate belongs to that stream.  No gradient passes through them: outputs are
+detached from their inputs, whatever these require.
 """
 from __future__ import annotations
 
