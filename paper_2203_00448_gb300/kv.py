@@ -79,7 +79,8 @@ class KvCache(_Fixed):
         self._struct = _lib.MpKvCache(n_blocks, block_tokens, n_heads, head_dim, _ptr(self.k), _ptr(self.v),
                                       _ptr(self.k_scale), _ptr(self.v_scale))
         self._ref = ctypes.byref(self._struct)
-        self._key, self._index = (block_tokens, n_heads, head_dim, self.device), self.k.get_device()
+        # what a batch's struct and scratch depend on
+        self._key, self._index = (n_blocks > 0, block_tokens, n_heads, head_dim, self.device), self.k.get_device()
 
     @staticmethod
     def block_bytes(block_tokens: int, n_heads: int, head_dim: int) -> int:

@@ -309,3 +309,12 @@ def test_bounds_past_32_bits(monkeypatch):
     for window in (0, 7, (1 << 32) + 7, 1 << 63, -5, -(1 << 32) + 7):
         mp.kv_attend(c, wide, x, window=window)
     assert windows == [0, 7, (1 << 31) - 1, (1 << 31) - 1, -1, -1]
+
+
+def test_scratch_of_an_empty_pool_is_not_kept_for_others(lib):
+    """An empty pool takes no scratch; a pool with blocks of the same shape, asked for with the same batch, does."""
+    b = mp.KvBatch(torch.zeros(2, 1000, dtype=torch.int32), torch.zeros(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int64), 2)
+    none, some = (mp.KvCache(n, 32, 2, 64, "cpu") for n in (0, 4))
+    for _ in range(2):
+        assert mp.kv_attend_workspace_bytes(none, b, 4) == 0
+        assert mp.kv_attend_workspace_bytes(some, b, 4) > 0
