@@ -57,7 +57,7 @@ typedef enum mp_status {
     MP_ETIMEOUT = 4, /* per-trace only: a wait of the planner on another warp or
                         CTA gave up after its bound (see mp_plan_greedy_by_size);
                         that trace's outputs are unspecified */
-    MP_ENOMEM = 5,   /* workspace smaller than the matching *_workspace_bytes */
+    MP_ENOMEM = 5,   /* workspace smaller than the matching *_workspace_bytes; of a request: no blocks left for it */
     MP_EINTERNAL = 6 /* per-trace only: a kernel found an inconsistency in its own
                         state (a library defect); that trace's outputs are unspecified */
 } mp_status;
@@ -489,6 +489,152 @@ size_t mp_kv_attend_workspace_bytes(const mp_kv_cache *cache, const mp_kv_batch 
 mp_status mp_kv_attend(const mp_kv_cache *cache, const mp_kv_batch *batch, const mp_tokens *q, float scale,
                        int32_t causal, int32_t window, const mp_tokens *out, float *lse, int32_t *seq_status,
                        void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * The same cache in 4 bits
+ *
+ * 32 consecutive values of a token and head share a scale s; a value is a code u
+ * of 4 bits and stands for (u - 8) * s.  A scale is a byte of 5 bits of exponent
+ * and 3 of fraction, the bits behind the sign of the f16 that it stands for; it is
+ * at most 240 (byte 183).  17 D bytes hold a granule: 32 tokens of a head, codes
+ * first (D = head_dim, t = token in the granule, d = value; the low half of a byte
+ * has the even d), then scales:
+ *   key    code byte   t * D / 2 + d / 2
+ *          scale byte  16 D + t % 8 * D / 8 + d / 32 * 4 + t / 8
+ *   value  code byte   ((t / 8 * 8 + d / (D / 8)) * 4 + t % 8 / 2) * D / 8 + d % (D / 8) / 4 * 4 + t % 2 * 2 + d % 4 / 2
+ *          scale byte  16 D + (d / 32 * 4 + t / 2 % 4) * 8 + t / 8 * 2 + t % 2
+ * that is, what a warp multiplies at once lies together.  Everything else is as for
+ * the cache in 8 bits. */
+
+/* The pool; limits as for mp_kv_cache.
+ *   k, v   uint8[n_blocks][n_heads][block_tokens / 32][17 * head_dim], 16-byte aligned */
+typedef struct mp_kv4_cache {
+    int32_t n_blocks;
+    int32_t block_tokens;
+    int32_t n_heads;
+    int32_t head_dim;
+    uint8_t *k;
+    uint8_t *v;
+} mp_kv4_cache;
+
+/* Quantises the call's keys and values into the blocks of their positions: for 32
+ * values of a token and head with a = max |x|, s is the least scale with a <= 7.5 s,
+ * and u - 8 the whole number of -7 .. 7 nearest to x / s (ties to even), so that no value
+ * is off by more than s / 2.  A token's codes and scales depend on no other token, and nothing
+ * but them is written.  A NaN is stored as 0, a magnitude above 1800 (infinities among
+ * them) as 1680 under the scale 240; its sequence gets MP_EINVAL.  k, v: any mp_dtype,
+ * the same for both; n_heads as the cache's.  No two sequences of a call may share a
+ * slot that it writes.  seq_status int32[B]. */
+mp_status mp_kv_four_write(const mp_kv4_cache *cache, const mp_kv_batch *batch, const mp_tokens *k, const mp_tokens *v,
+                       int32_t *seq_status, void *stream);
+
+/* As mp_kv_read.  What is read is exact in every mp_dtype. */
+mp_status mp_kv_four_read(const mp_kv4_cache *cache, const mp_kv_batch *batch, const mp_tokens *k, const mp_tokens *v,
+                      int32_t *seq_status, void *stream);
+
+/* As mp_kv_attend_workspace_bytes and mp_kv_attend; keys and values enter the products
+ * as f16 without a rounding. */
+size_t mp_kv_four_attend_workspace_bytes(const mp_kv4_cache *cache, const mp_kv_batch *batch, int32_t n_q_heads);
+mp_status mp_kv_four_attend(const mp_kv4_cache *cache, const mp_kv_batch *batch, const mp_tokens *q, float scale,
+                        int32_t causal, int32_t window, const mp_tokens *out, float *lse, int32_t *seq_status,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * Block tables from request lengths
+ *
+ * A server's requests grow by some tokens each step, and some end.  mp_kv_extend
+ * gives them their blocks and writes what the step's other calls take: the batch's
+ * lens and token_ptr, and each token's position and slot. */
+
+/* The requests' blocks.  Blocks come from a stack of free ones, or each request has a
+ * run of blocks of its own, for example by a plan (first not NULL).
+ *   table  int32[n_seqs][max_blocks]  as in mp_kv_batch, kept from step to step
+ *   free   int32[n_blocks]  the stack (entries from *n_free on mean nothing); not read with first
+ *   first  int32[n_seqs] or NULL: request b has blocks first[b], first[b] + 1, ...
+ *   room   int32[n_seqs] with first: ... of which it may have that many */
+typedef struct mp_kv_blocks {
+    int32_t n_seqs;
+    int32_t max_blocks;
+    int32_t block_tokens; /* a multiple of 32, at most 256 */
+    int32_t n_blocks;     /* of the pool */
+    int32_t *table;
+    int32_t *free;
+    const int32_t *first;
+    const int32_t *room;
+} mp_kv_blocks;
+
+/* One step.  Host scalars: n_tokens rows of positions and slots; max_tokens, max_len: upper bounds on
+ * a request's new tokens and on what it then holds (max_len at most max_blocks * block_tokens and 2^28).
+ * Device arrays, in:
+ *   lens    int32[n_seqs]  tokens held
+ *   n_free  int32[1]       height of the stack (not with first)
+ *   n_new   int32[n_seqs]  new tokens; negative: the request ends
+ * out (lens_out may be lens, n_free_out may be n_free):
+ *   lens_out    int32[n_seqs]      tokens held after the step
+ *   n_free_out  int32[1]
+ *   step_lens   int32[n_seqs]      lens of the step's mp_kv_batch: lens_out, or -1 where the request ended or got no
+ *                                  blocks (the batch's other calls then refuse it alone)
+ *   token_ptr   int64[n_seqs + 1]  sums of max(n_new, 0)
+ *   positions   int32[n_tokens]    of each row; -1 in rows of requests that take no part
+ *   slots       int64[n_tokens]    block * block_tokens + place in the block; -1 likewise
+ *   seq_status  int32[n_seqs] */
+typedef struct mp_kv_extension {
+    int64_t n_tokens;
+    int32_t max_tokens;
+    int32_t max_len;
+    const int32_t *lens;
+    const int32_t *n_free;
+    const int32_t *n_new;
+    int32_t *lens_out;
+    int32_t *n_free_out;
+    int32_t *step_lens;
+    int64_t *token_ptr;
+    int32_t *positions;
+    int64_t *slots;
+    int32_t *seq_status;
+} mp_kv_extension;
+
+/* Bytes of device workspace mp_kv_extend needs (0 for arguments that it rejects). */
+size_t mp_kv_extend_workspace_bytes(const mp_kv_blocks *blocks);
+
+/* First, requests that end push the blocks of their table rows, in the order of requests and columns.  Then
+ * the others take what ceil((lens + n_new) / block_tokens) asks for beyond ceil(lens / block_tokens), the
+ * first one from the top of the stack.  A request whose blocks, with those that all requests before it ask for,
+ * are more than there are gets MP_ENOMEM (with first: one that needs more than its room); what asks for none is always answered.
+ * MP_EINVAL: lens negative or above max_len, a bound broken, rows beyond n_tokens, a run outside the pool,
+ * blocks that come back to a stack without room for them, an *n_free outside 0 .. n_blocks (then every
+ * request).  A request with either status keeps its lens and its table.  Table entries of columns that a request
+ * does not get in the call, rows beyond token_ptr[n_seqs] and the entries of the stack below *n_free are left alone;
+ * pushed blocks stay where they were pushed even if the call pops them.  Results do not depend on how the
+ * call is run. */
+mp_status mp_kv_extend(const mp_kv_blocks *blocks, const mp_kv_extension *step, void *workspace, size_t workspace_bytes,
+                       void *stream);
+
+/* ---------------------------------------------------------------------------
+ * Rotary positions */
+
+/* Which elements of a head are a pair: i and i + dim / 2, or 2 i and 2 i + 1. */
+typedef enum mp_rotary_layout { MP_ROTARY_HALF = 0, MP_ROTARY_INTERLEAVED = 1 } mp_rotary_layout;
+
+/* dim: elements of a head that turn, even, the first ones; turns: int64[dim / 2] device, turns that a pair makes
+ * from one position to the next, times 2^64 (as an unsigned number, whole turns left out); amplitude: factor of what
+ * turns. */
+typedef struct mp_rotation {
+    int32_t dim;
+    int32_t layout; /* mp_rotary_layout */
+    const int64_t *turns;
+    float amplitude;
+} mp_rotation;
+
+/* Turns each pair (x, y) of token i's heads by the angle a = positions[i] * turns: out = amplitude * (x cos a - y sin
+ * a, x sin a + y cos a); with inverse != 0 by -a, which makes gradients with respect to the outputs into those
+ * with respect to the inputs.  Elements from dim on are copied.  The angle is reduced as an integer, exactly; products
+ * are taken in 32 bits and rounded once.  positions: int32[n_tokens] device, any value.  head_dim even, at most 1,024, dim
+ * at most head_dim.  q, k, q_out, k_out: [n_tokens] rows of any mp_dtype, the same for all; k and k_out NULL, or q and
+ * q_out.  An output may be its input (same data and strides); any other overlap is not allowed. */
+mp_status mp_rotary(const mp_rotation *rotation, const int32_t *positions, int64_t n_tokens, int32_t head_dim,
+                    const mp_tokens *q, const mp_tokens *k, const mp_tokens *q_out, const mp_tokens *k_out,
+                    int32_t inverse, void *stream);
 
 /* Static, NUL-terminated name of a status code. */
 const char *mp_status_string(mp_status status);

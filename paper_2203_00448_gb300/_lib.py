@@ -38,6 +38,13 @@ EXPORTS = (
     "mp_kv_read",
     "mp_kv_attend_workspace_bytes",
     "mp_kv_attend",
+    "mp_kv_four_write",
+    "mp_kv_four_read",
+    "mp_kv_four_attend_workspace_bytes",
+    "mp_kv_four_attend",
+    "mp_kv_extend_workspace_bytes",
+    "mp_kv_extend",
+    "mp_rotary",
     "mp_status_string",
     "mp_abi_version",
 )
@@ -88,6 +95,34 @@ class MpTokens(ctypes.Structure):
 
     _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
                 ("n_heads", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class MpKv4Cache(ctypes.Structure):
+    """Mirror of struct mp_kv4_cache."""
+
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_blocks", "block_tokens", "n_heads", "head_dim")] + \
+        [(n, ctypes.c_void_p) for n in ("k", "v")]
+
+
+class MpKvBlocks(ctypes.Structure):
+    """Mirror of struct mp_kv_blocks."""
+
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_seqs", "max_blocks", "block_tokens", "n_blocks")] + \
+        [(n, ctypes.c_void_p) for n in ("table", "free", "first", "room")]
+
+
+class MpKvExtension(ctypes.Structure):
+    """Mirror of struct mp_kv_extension."""
+
+    _fields_ = [("n_tokens", ctypes.c_int64), ("max_tokens", ctypes.c_int32), ("max_len", ctypes.c_int32)] + \
+        [(n, ctypes.c_void_p) for n in ("lens", "n_free", "n_new", "lens_out", "n_free_out", "step_lens", "token_ptr",
+                                        "positions", "slots", "seq_status")]
+
+
+class MpRotation(ctypes.Structure):
+    """Mirror of struct mp_rotation."""
+
+    _fields_ = [("dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("turns", ctypes.c_void_p), ("amplitude", ctypes.c_float)]
 
 
 HOST_PATH_MAX_CHUNKS = 64
@@ -161,6 +196,21 @@ def load(path: str = LIB_PATH):
     lib.mp_kv_attend_workspace_bytes.restype = sz
     lib.mp_kv_attend.argtypes = [CP, KP, TP, ctypes.c_float, i32, i32, TP, P, P, P, sz, P]
     lib.mp_kv_attend.restype = i32
+    CP4, XP, EP, RP = (ctypes.POINTER(t) for t in (MpKv4Cache, MpKvBlocks, MpKvExtension, MpRotation))
+    lib.mp_kv_four_write.argtypes = [CP4, KP, TP, TP, P, P]
+    lib.mp_kv_four_write.restype = i32
+    lib.mp_kv_four_read.argtypes = [CP4, KP, TP, TP, P, P]
+    lib.mp_kv_four_read.restype = i32
+    lib.mp_kv_four_attend_workspace_bytes.argtypes = [CP4, KP, i32]
+    lib.mp_kv_four_attend_workspace_bytes.restype = sz
+    lib.mp_kv_four_attend.argtypes = [CP4, KP, TP, ctypes.c_float, i32, i32, TP, P, P, P, sz, P]
+    lib.mp_kv_four_attend.restype = i32
+    lib.mp_kv_extend_workspace_bytes.argtypes = [XP]
+    lib.mp_kv_extend_workspace_bytes.restype = sz
+    lib.mp_kv_extend.argtypes = [XP, EP, P, sz, P]
+    lib.mp_kv_extend.restype = i32
+    lib.mp_rotary.argtypes = [RP, P, ctypes.c_int64, i32, TP, TP, TP, TP, i32, P]
+    lib.mp_rotary.restype = i32
     lib.mp_status_string.argtypes = [i32]
     lib.mp_status_string.restype = ctypes.c_char_p
     lib.mp_abi_version.argtypes = []

@@ -108,20 +108,27 @@ mp_status check_workspace(size_t need, const void* ws, size_t ws_bytes) {
     return MP_OK;
 }
 
-mp_status check_cache(const mp_kv_cache* c) {
+// What caches of 8 and of 4 bits have alike.
+template <typename C>
+mp_status check_pool(const C* c) {
     if (c == nullptr || c->n_blocks < 0 || c->n_heads < 1 || (c->head_dim != 64 && c->head_dim != 128) ||
         c->block_tokens < 32 || c->block_tokens > 256 || c->block_tokens % 32 != 0)
         return MP_EINVAL;
-    const int64_t n = c->n_blocks;
-    if (!array_ok(c->k_scale, n) || !array_ok(c->v_scale, n)) return MP_EINVAL;
-    for (const uint8_t* p : {c->k, c->v})
-        if ((n > 0 && p == nullptr) || reinterpret_cast<uintptr_t>(p) % 16 != 0) return MP_EINVAL;
+    const uint8_t* const arrays[2] = {c->k, c->v};
+    for (const uint8_t* p : arrays)
+        if ((c->n_blocks > 0 && p == nullptr) || reinterpret_cast<uintptr_t>(p) % 16 != 0) return MP_EINVAL;
     return MP_OK;
 }
+mp_status check_cache(const mp_kv_cache* c) {
+    if (check_pool(c) != MP_OK || !array_ok(c->k_scale, c->n_blocks) || !array_ok(c->v_scale, c->n_blocks)) return MP_EINVAL;
+    return MP_OK;
+}
+mp_status check_cache(const mp_kv4_cache* c) { return check_pool(c); }
 
 constexpr int64_t kKvMost = 1 << 28;  // positions, tokens, query rows: their sums and differences fit in 32 bits
 
-mp_status check_kv_batch(const mp_kv_cache* c, const mp_kv_batch* bt) {
+template <typename C>
+mp_status check_kv_batch(const C* c, const mp_kv_batch* bt) {
     if (bt == nullptr || bt->n_seqs < 0 || bt->max_blocks < 0 || bt->max_tokens < 0 || bt->max_len < 0 ||
         bt->n_tokens < 0 || bt->max_len > (int64_t)bt->max_blocks * c->block_tokens || bt->max_len > kKvMost ||
         bt->max_tokens > kKvMost)
@@ -141,6 +148,50 @@ mp_status check_tokens(const mp_tokens* t, const mp_kv_batch* bt, int32_t n_head
 }
 
 mp_status from_cuda(cudaError_t e) { return e == cudaSuccess ? MP_OK : MP_ECUDA; }
+
+template <typename C>
+mp_status check_stored(const C* cache, const mp_kv_batch* batch, const mp_tokens* k, const mp_tokens* v, const int32_t* seq_status) {
+    mp_status st = check_cache(cache);
+    if (st == MP_OK) st = check_kv_batch(cache, batch);
+    if (st == MP_OK) st = check_tokens(k, batch, cache->n_heads, false, MP_F32);
+    if (st == MP_OK) st = check_tokens(v, batch, cache->n_heads, false, MP_F32);
+    if (st != MP_OK) return st;
+    return k->dtype == v->dtype && array_ok(seq_status, batch->n_seqs) ? MP_OK : MP_EINVAL;
+}
+template <typename C>
+mp_status check_attend(const C* cache, const mp_kv_batch* batch, const mp_tokens* q, float scale, int32_t causal, int32_t window,
+                       const mp_tokens* out, const float* lse, const int32_t* seq_status) {
+    mp_status st = check_cache(cache);
+    if (st == MP_OK) st = check_kv_batch(cache, batch);
+    if (st == MP_OK) st = check_tokens(q, batch, cache->n_heads, true, MP_BF16);
+    if (st == MP_OK) st = check_tokens(out, batch, cache->n_heads, true, MP_BF16);
+    if (st != MP_OK) return st;
+    if (q->dtype != out->dtype || q->n_heads != out->n_heads || q->n_heads / cache->n_heads > 1024 ||
+        (int64_t)batch->max_tokens * (q->n_heads / cache->n_heads) > kKvMost || !(scale > 0.f && scale <= 3.402823466e38f) ||
+        window < 0 || (window > 0 && !causal) || !array_ok(seq_status, batch->n_seqs) ||
+        (lse != nullptr && !aligned(lse)))
+        return MP_EINVAL;
+    return MP_OK;
+}
+template <typename C>
+bool attend_needs(const C* cache, const mp_kv_batch* batch, int32_t n_q_heads) {
+    return check_cache(cache) == MP_OK && check_kv_batch(cache, batch) == MP_OK && n_q_heads >= 1 && n_q_heads % cache->n_heads == 0;
+}
+
+bool blocks_ok(const mp_kv_blocks* b) {
+    return b != nullptr && b->n_seqs >= 0 && b->max_blocks >= 0 && b->n_blocks >= 0 && b->block_tokens >= 32 &&
+           b->block_tokens <= 256 && b->block_tokens % 32 == 0 && array_ok(b->table, (int64_t)b->n_seqs * b->max_blocks) &&
+           (b->first != nullptr ? array_ok(b->first, b->n_seqs) && array_ok(b->room, b->n_seqs) : array_ok(b->free, b->n_blocks));
+}
+
+// Rows of a rotation's tensors.
+bool rows_ok(const mp_tokens* in, const mp_tokens* out, int64_t n_tokens, int32_t dtype) {
+    for (const mp_tokens* t : {in, out})
+        if (t == nullptr || t->dtype != dtype || dtype < 0 || dtype > MP_F32 || t->n_heads < 1 || t->n_heads > 1 << 16 ||
+            (n_tokens > 0 && t->data == nullptr) || reinterpret_cast<uintptr_t>(t->data) % (dtype == MP_F32 ? 4 : 2) != 0)
+            return false;
+    return in->n_heads == out->n_heads;
+}
 
 }  // namespace
 
@@ -351,34 +402,23 @@ __attribute__((visibility("default"))) mp_status mp_peak(const mp_batch* batch, 
 __attribute__((visibility("default"))) mp_status mp_kv_write(const mp_kv_cache* cache, const mp_kv_batch* batch,
                                                              const mp_tokens* k, const mp_tokens* v,
                                                              int32_t* seq_status, void* stream) {
-    mp_status st = check_cache(cache);
-    if (st == MP_OK) st = check_kv_batch(cache, batch);
-    if (st == MP_OK) st = check_tokens(k, batch, cache->n_heads, false, MP_F32);
-    if (st == MP_OK) st = check_tokens(v, batch, cache->n_heads, false, MP_F32);
+    const mp_status st = check_stored(cache, batch, k, v, seq_status);
     if (st != MP_OK) return st;
-    if (k->dtype != v->dtype || !array_ok(seq_status, batch->n_seqs)) return MP_EINVAL;
     return from_cuda(mp::launch_kv_write(*cache, *batch, *k, *v, seq_status, static_cast<cudaStream_t>(stream)));
 }
 
 __attribute__((visibility("default"))) mp_status mp_kv_read(const mp_kv_cache* cache, const mp_kv_batch* batch,
                                                             const mp_tokens* k, const mp_tokens* v,
                                                             int32_t* seq_status, void* stream) {
-    mp_status st = check_cache(cache);
-    if (st == MP_OK) st = check_kv_batch(cache, batch);
-    if (st == MP_OK) st = check_tokens(k, batch, cache->n_heads, false, MP_F32);
-    if (st == MP_OK) st = check_tokens(v, batch, cache->n_heads, false, MP_F32);
+    const mp_status st = check_stored(cache, batch, k, v, seq_status);
     if (st != MP_OK) return st;
-    if (k->dtype != v->dtype || !array_ok(seq_status, batch->n_seqs)) return MP_EINVAL;
     return from_cuda(mp::launch_kv_read(*cache, *batch, *k, *v, seq_status, static_cast<cudaStream_t>(stream)));
 }
 
 __attribute__((visibility("default"))) size_t mp_kv_attend_workspace_bytes(const mp_kv_cache* cache,
                                                                            const mp_kv_batch* batch,
                                                                            int32_t n_q_heads) {
-    if (check_cache(cache) != MP_OK || check_kv_batch(cache, batch) != MP_OK || n_q_heads < 1 ||
-        n_q_heads % cache->n_heads != 0)
-        return 0;
-    return mp::kv_attend_workspace_bytes(*cache, *batch, n_q_heads);
+    return attend_needs(cache, batch, n_q_heads) ? mp::kv_attend_workspace_bytes(*cache, *batch, n_q_heads) : 0;
 }
 
 __attribute__((visibility("default"))) mp_status mp_kv_attend(const mp_kv_cache* cache, const mp_kv_batch* batch,
@@ -386,20 +426,82 @@ __attribute__((visibility("default"))) mp_status mp_kv_attend(const mp_kv_cache*
                                                               int32_t window, const mp_tokens* out, float* lse,
                                                               int32_t* seq_status, void* workspace,
                                                               size_t workspace_bytes, void* stream) {
-    mp_status st = check_cache(cache);
-    if (st == MP_OK) st = check_kv_batch(cache, batch);
-    if (st == MP_OK) st = check_tokens(q, batch, cache->n_heads, true, MP_BF16);
-    if (st == MP_OK) st = check_tokens(out, batch, cache->n_heads, true, MP_BF16);
+    mp_status st = check_attend(cache, batch, q, scale, causal, window, out, lse, seq_status);
     if (st != MP_OK) return st;
-    if (q->dtype != out->dtype || q->n_heads != out->n_heads || q->n_heads / cache->n_heads > 1024 ||
-        (int64_t)batch->max_tokens * (q->n_heads / cache->n_heads) > kKvMost || !(scale > 0.f && scale <= 3.402823466e38f) ||
-        window < 0 || (window > 0 && !causal) || !array_ok(seq_status, batch->n_seqs) ||
-        (lse != nullptr && !aligned(lse)))
-        return MP_EINVAL;
     st = check_workspace(mp::kv_attend_workspace_bytes(*cache, *batch, q->n_heads), workspace, workspace_bytes);
     if (st != MP_OK) return st;
     return from_cuda(mp::launch_kv_attend(*cache, *batch, *q, scale, causal, window, *out, lse, seq_status, workspace,
                                           static_cast<cudaStream_t>(stream)));
+}
+
+__attribute__((visibility("default"))) mp_status mp_kv_four_write(const mp_kv4_cache* cache, const mp_kv_batch* batch,
+                                                              const mp_tokens* k, const mp_tokens* v,
+                                                              int32_t* seq_status, void* stream) {
+    const mp_status st = check_stored(cache, batch, k, v, seq_status);
+    if (st != MP_OK) return st;
+    return from_cuda(mp::launch_kv4_write(*cache, *batch, *k, *v, seq_status, static_cast<cudaStream_t>(stream)));
+}
+
+__attribute__((visibility("default"))) mp_status mp_kv_four_read(const mp_kv4_cache* cache, const mp_kv_batch* batch,
+                                                             const mp_tokens* k, const mp_tokens* v,
+                                                             int32_t* seq_status, void* stream) {
+    const mp_status st = check_stored(cache, batch, k, v, seq_status);
+    if (st != MP_OK) return st;
+    return from_cuda(mp::launch_kv4_read(*cache, *batch, *k, *v, seq_status, static_cast<cudaStream_t>(stream)));
+}
+
+__attribute__((visibility("default"))) size_t mp_kv_four_attend_workspace_bytes(const mp_kv4_cache* cache,
+                                                                            const mp_kv_batch* batch,
+                                                                            int32_t n_q_heads) {
+    return attend_needs(cache, batch, n_q_heads) ? mp::kv4_attend_workspace_bytes(*cache, *batch, n_q_heads) : 0;
+}
+
+__attribute__((visibility("default"))) mp_status mp_kv_four_attend(const mp_kv4_cache* cache, const mp_kv_batch* batch,
+                                                               const mp_tokens* q, float scale, int32_t causal,
+                                                               int32_t window, const mp_tokens* out, float* lse,
+                                                               int32_t* seq_status, void* workspace,
+                                                               size_t workspace_bytes, void* stream) {
+    mp_status st = check_attend(cache, batch, q, scale, causal, window, out, lse, seq_status);
+    if (st != MP_OK) return st;
+    st = check_workspace(mp::kv4_attend_workspace_bytes(*cache, *batch, q->n_heads), workspace, workspace_bytes);
+    if (st != MP_OK) return st;
+    return from_cuda(mp::launch_kv4_attend(*cache, *batch, *q, scale, causal, window, *out, lse, seq_status, workspace,
+                                           static_cast<cudaStream_t>(stream)));
+}
+
+__attribute__((visibility("default"))) size_t mp_kv_extend_workspace_bytes(const mp_kv_blocks* blocks) {
+    return blocks_ok(blocks) ? mp::kv_extend_workspace_bytes(*blocks) : 0;
+}
+
+__attribute__((visibility("default"))) mp_status mp_kv_extend(const mp_kv_blocks* blocks, const mp_kv_extension* step,
+                                                              void* workspace, size_t workspace_bytes, void* stream) {
+    if (!blocks_ok(blocks) || step == nullptr || step->n_tokens < 0 || step->max_tokens < 0 || step->max_tokens > kKvMost ||
+        step->max_len < 0 || step->max_len > kKvMost || step->max_len > (int64_t)blocks->max_blocks * blocks->block_tokens)
+        return MP_EINVAL;
+    const int64_t B = blocks->n_seqs, pool = blocks->first == nullptr ? 1 : 0;
+    if (!array_ok(step->lens, B) || !array_ok(step->n_new, B) || !array_ok(step->lens_out, B) || !array_ok(step->step_lens, B) ||
+        !array_ok(step->seq_status, B) || !array_ok(step->token_ptr, 1) || !array_ok(step->positions, step->n_tokens) ||
+        !array_ok(step->slots, step->n_tokens) || !array_ok(step->n_free, pool) || !array_ok(step->n_free_out, pool))
+        return MP_EINVAL;
+    const mp_status st = check_workspace(mp::kv_extend_workspace_bytes(*blocks), workspace, workspace_bytes);
+    if (st != MP_OK) return st;
+    return from_cuda(mp::launch_kv_extend(*blocks, *step, workspace, static_cast<cudaStream_t>(stream)));
+}
+
+__attribute__((visibility("default"))) mp_status mp_rotary(const mp_rotation* rotation, const int32_t* positions, int64_t n_tokens,
+                                                           int32_t head_dim, const mp_tokens* q, const mp_tokens* k,
+                                                           const mp_tokens* q_out, const mp_tokens* k_out, int32_t inverse,
+                                                           void* stream) {
+    if (rotation == nullptr || n_tokens < 0 || head_dim < 2 || head_dim > 1024 || head_dim % 2 != 0 || rotation->dim < 2 ||
+        rotation->dim > head_dim || rotation->dim % 2 != 0 || rotation->layout < MP_ROTARY_HALF ||
+        rotation->layout > MP_ROTARY_INTERLEAVED || !array_ok(rotation->turns, 1) || !array_ok(positions, n_tokens) ||
+        !(rotation->amplitude >= -3.402823466e38f && rotation->amplitude <= 3.402823466e38f) || (q == nullptr && k == nullptr))
+        return MP_EINVAL;
+    const int32_t dtype = q != nullptr ? q->dtype : k->dtype;
+    if ((q != nullptr || q_out != nullptr) && !rows_ok(q, q_out, n_tokens, dtype)) return MP_EINVAL;
+    if ((k != nullptr || k_out != nullptr) && !rows_ok(k, k_out, n_tokens, dtype)) return MP_EINVAL;
+    return from_cuda(mp::launch_rotary(*rotation, positions, n_tokens, head_dim, q, k, q_out, k_out, inverse,
+                                       static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -30,9 +30,67 @@ __device__ __forceinline__ int value_byte(int t, int d) {
     return (t >> 5) * 32 * D + (d >> 3) * 256 + ((t >> 4) & 1) * 128 + (d & 7) * 16 + (t & 15);
 }
 
+// Bytes of a granule of either array: 32 D values of 8 bits, or of 4 bits and D scales of 8 behind them.
+__host__ __device__ constexpr int granule_bytes(int bits, int d) { return bits == 8 ? kGranule * d : 17 * d; }
+
 // First byte of a block and head in either pool (64 bits: pools pass 4 GB).
+template <int kBits = 8>
 __device__ __forceinline__ int64_t block_byte(const mp_kv_cache& c, int page, int head) {
-    return ((int64_t)page * c.n_heads + head) * ((int64_t)c.block_tokens * c.head_dim);
+    return ((int64_t)page * c.n_heads + head) * ((int64_t)(c.block_tokens / kGranule) * granule_bytes(kBits, c.head_dim));
+}
+
+// 4 bits: byte of key and value (t, d) inside a granule (d even or odd: its low or high half), and byte of their scale
+// behind the codes.  A key's codes lie in a row; a warp's lanes find the D / 8 values of two neighbouring tokens that they
+// multiply in one piece, and their scales in one word.
+template <int D>
+__device__ __forceinline__ int key4_byte(int t, int d) {
+    return t * (D / 2) + d / 2;
+}
+template <int D>
+__device__ __forceinline__ int value4_byte(int t, int d) {
+    return ((t / 8 * 8 + d / (D / 8)) * 4 + t % 8 / 2) * (D / 8) + d % (D / 8) / 4 * 4 + t % 2 * 2 + d % 4 / 2;
+}
+template <int D>
+__device__ __forceinline__ int key4_scale(int t, int d) {
+    return t % 8 * (D / 8) + d / 32 * 4 + t / 8;
+}
+template <int D>
+__device__ __forceinline__ int value4_scale(int t, int d) {
+    return (d / 32 * 4 + t / 2 % 4) * 8 + t / 8 * 2 + t % 2;
+}
+
+// The 4-bit pool as the attention kernels take it.
+inline mp_kv_cache as_pool(const mp_kv4_cache& c) {
+    return {c.n_blocks, c.block_tokens, c.n_heads, c.head_dim, c.k, c.v, nullptr, nullptr};
+}
+
+// Scales (s, s') of a pair of codes as f16, and what is to be added to s times 16 + u and 256 + u so that s (u - 8) comes
+// out.  s has 4 significant bits and is at most 240: 24 s and 264 s are f16 values, and so is every s (u - 8); the fused
+// product and sum rounds nothing.
+struct Steps {
+    uint32_t s, off16, off256;
+};
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t x, uint32_t y) {
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+    return r;
+}
+__device__ __forceinline__ uint32_t fma_f16x2(uint32_t x, uint32_t y, uint32_t z) {
+    uint32_t r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(x), "r"(y), "r"(z));
+    return r;
+}
+__device__ __forceinline__ Steps steps_of(uint32_t s) {
+    return {s, mul_f16x2(s, 0xce00ce00u), mul_f16x2(s, 0xdc20dc20u)};  // -24, -264
+}
+// 8 codes of a word as f16 pairs of codes i and i + 4: a code that is moved to bits 6-9 under the exponent of 16 is 16 +
+// u, at bits 2-5 under that of 256 it is 256 + u, so that 10 operations make 8 values.
+__device__ __forceinline__ void codes_to_f16(uint32_t w, const Steps& s, uint32_t* pairs) {
+    const uint32_t lo = w << 2, hi = w >> 6;
+    pairs[0] = fma_f16x2((lo & 0x003c003cu) | 0x5c005c00u, s.s, s.off256);
+    pairs[1] = fma_f16x2((lo & 0x03c003c0u) | 0x4c004c00u, s.s, s.off16);
+    pairs[2] = fma_f16x2((hi & 0x003c003cu) | 0x5c005c00u, s.s, s.off256);
+    pairs[3] = fma_f16x2((hi & 0x03c003c0u) | 0x4c004c00u, s.s, s.off16);
 }
 
 struct SeqView {

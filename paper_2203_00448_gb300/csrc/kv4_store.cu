@@ -1,0 +1,278 @@
+// kv4_store.cu -- mp_kv_four_write and mp_kv_four_read: tokens into and out of the cache's 4-bit blocks.
+//
+// 32 values of a token and head have a scale s of 4 significant bits, the least with max |x| <= 7.5 s, and codes n =
+// x / s rounded to the nearest whole number of -7 .. 7: no value is off by more than half a step, and n s is exact in
+// f16, bf16 and f32.  A token's codes depend on no other token, so nothing that is stored is ever rounded again.
+#include <algorithm>
+
+#include "kv.cuh"
+
+namespace mp {
+namespace {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int32_t kFewTokens = 16;  // up to this many a sequence, a CTA a sequence
+constexpr float kMost = 1800.f;     // 7.5 times the largest scale
+constexpr int kMostScale = 183;     // its byte: 240
+
+__device__ __forceinline__ float scale_value(int byte) {
+    return __half2float(__ushort_as_half((unsigned short)(byte << 7)));
+}
+
+// The byte of the least scale with a <= 7.5 s.
+__device__ __forceinline__ int scale_byte(float a) {
+    const float least = a * (2.f / 15.f);
+    // what the bits below a scale's say is cut off; below 2^-14 steps are 2^-17
+    int byte = least < 0x1p-14f ? (int)(least * 0x1p17f) : (int)(__float_as_uint(least) >> 20) - (112 << 3);
+    // the product may be off by a rounding, and cutting off leaves a scale that is too small
+    if (7.5f * scale_value(byte) < a) ++byte;
+    if (7.5f * scale_value(byte) < a) ++byte;
+    return min(byte, kMostScale);
+}
+
+// x / s to the nearest whole number, ties to the even one, of -7 .. 7; as a code.  inverse: 1 / s rounded.
+__device__ __forceinline__ uint32_t code_of(float x, float s, float inverse) {
+    float n = rintf(x * inverse);
+    const float rest = fmaf(-n, s, x), off = fabsf(rest), half = 0.5f * s;  // exact: the product may lie beside a border
+    if (off > half || (off == half && ((int)n & 1))) n += copysignf(1.f, rest);
+    return (uint32_t)((int)fminf(fmaxf(n, -7.f), 7.f) + 8);
+}
+
+// A warp stores tokens [from, past) (slots of a granule) of one head and array: a lane 8 values of a token a step.
+// x: the first of them.  False if some value was not finite or too large.
+template <typename T, int D, bool kValues>
+__device__ __forceinline__ bool store_granule(const T* x, int64_t stride, bool wide, int from, int past, uint8_t* bytes) {
+    constexpr int kLanes = D / 8, kTokens = 32 / kLanes;  // lanes of a token, tokens a step
+    const int lane = threadIdx.x % 32, d = lane % kLanes * 8;
+    bool fine = true;
+#pragma unroll 4
+    for (int t0 = from / kTokens * kTokens; t0 < past; t0 += kTokens) {
+        const int t = t0 + lane / kLanes;
+        const bool mine = t >= from && t < past;
+        float v[8];
+        if (mine) load_values<T, 8>(x + (t - from) * stride + d, wide, v);
+        float most = 0.f;
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (!mine) v[i] = 0.f;
+            odd |= !(fabsf(v[i]) <= kMost);
+        }
+        if (odd) {
+            fine = false;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = v[i] != v[i] ? 0.f : fminf(fmaxf(v[i], -kMost), kMost);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(v[i]));
+        most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
+        most = fmaxf(most, __shfl_xor_sync(~0u, most, 2));
+        const int byte = scale_byte(most);
+        const float s = scale_value(byte), inverse = byte ? __fdiv_rn(1.f, s) : 0.f;
+        uint32_t w = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w |= code_of(v[i], s, inverse) << (4 * i);
+        uint8_t* const scale = bytes + 16 * D + (kValues ? value4_scale<D>(t, d) : key4_scale<D>(t, d));
+        if (mine && lane % 4 == 0) *scale = (uint8_t)byte;
+        if (!kValues) {
+            if (mine) *reinterpret_cast<uint32_t*>(bytes + key4_byte<D>(t, d)) = w;
+        } else {
+            // the neighbouring token's lane has the other half of either word
+            const uint32_t other = __shfl_xor_sync(~0u, t % 2 ? w & 0xffff : w >> 16, kLanes);
+            uint8_t* const at = bytes + value4_byte<D>(t, d);  // (of its half of the first word)
+            if (mine && (t ^ 1) >= from && (t ^ 1) < past) {
+                if (t % 2) *reinterpret_cast<uint32_t*>(at + 2) = other | (w & 0xffff0000u);
+                else *reinterpret_cast<uint32_t*>(at) = (w & 0xffffu) | other << 16;
+            } else if (mine) {
+                *reinterpret_cast<uint16_t*>(at) = (uint16_t)w;
+                *reinterpret_cast<uint16_t*>(at + 4) = (uint16_t)(w >> 16);
+            }
+        }
+    }
+    return fine;
+}
+
+// One granule, head and array of a sequence: j counts the granules that the call touches.  False if the table or a value is
+// wrong there.
+template <typename T, int D>
+__device__ __forceinline__ bool store_unit(const mp_kv_cache& c, const mp_kv_batch& bt, const SeqView& s, int b, int j, int head,
+                                           bool values, const mp_tokens& k, const mp_tokens& v, bool wide) {
+    const int start = s.len - s.n, base = (start / kGranule + j) * kGranule;
+    const int page = __ldg(bt.table + (int64_t)b * bt.max_blocks + base / c.block_tokens);
+    if (page < 0 || page >= c.n_blocks) return false;
+    const int64_t at = block_byte<4>(c, page, head) + (int64_t)(base % c.block_tokens / kGranule) * granule_bytes(4, D);
+    const int from = max(start - base, 0), past = min(s.len - base, kGranule);
+    const mp_tokens& t = values ? v : k;
+    const T* x = static_cast<const T*>(t.data) + (s.lo + (base + from - start)) * t.token_stride + head * t.head_stride;
+    return values ? store_granule<T, D, true>(x, t.token_stride, wide, from, past, c.v + at)
+                  : store_granule<T, D, false>(x, t.token_stride, wide, from, past, c.k + at);
+}
+__device__ __forceinline__ int granules_touched(const SeqView& s) {
+    return s.n == 0 ? 0 : (s.len - 1) / kGranule - (s.len - s.n) / kGranule + 1;
+}
+
+// Few tokens a sequence: one CTA a sequence, so that its status has one writer; a warp a granule, head and array.
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads)
+    k_kv4_write_few(mp_kv_cache c, mp_kv_batch bt, mp_tokens k, mp_tokens v, bool wide, int32_t* status) {
+    for (int b = blockIdx.x; b < bt.n_seqs; b += gridDim.x) {
+        const SeqView s = load_seq(bt, b, true);
+        bool ok = s.st == MP_OK;
+        const int tasks = granules_touched(s) * c.n_heads * 2;
+        for (int u = threadIdx.x / 32; u < tasks; u += kWarps)
+            ok &= store_unit<T, D>(c, bt, s, b, u / (2 * c.n_heads), u / 2 % c.n_heads, u % 2, k, v, wide);
+        const bool bad = __syncthreads_or(!ok);
+        if (threadIdx.x == 0) status[b] = bad ? MP_EINVAL : MP_OK;
+    }
+}
+
+// Many tokens: a warp a granule, head and array.  status is cleared before; whoever writes it writes the same.
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads)
+    k_kv4_write_many(mp_kv_cache c, mp_kv_batch bt, mp_tokens k, mp_tokens v, bool wide, int32_t* status, int per_seq) {
+    const int64_t units = (int64_t)bt.n_seqs * per_seq * c.n_heads * 2, warps = (int64_t)gridDim.x * kWarps;
+    for (int64_t u = (int64_t)blockIdx.x * kWarps + threadIdx.x / 32; u < units; u += warps) {
+        const int in_seq = (int)(u / 2 / c.n_heads % per_seq), b = (int)(u / 2 / c.n_heads / per_seq);
+        const SeqView s = load_seq(bt, b, true);
+        bool ok = s.st == MP_OK;
+        if (ok && in_seq < granules_touched(s))
+            ok = store_unit<T, D>(c, bt, s, b, in_seq, (int)(u / 2 % c.n_heads), u % 2, k, v, wide);
+        if (!ok) status[b] = MP_EINVAL;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void put8(T* p, bool wide, const uint32_t (&pairs)[4]) {  // pairs of values i and i + 4
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&pairs[i]));
+        x[i] = y.x, x[i + 4] = y.y;
+    }
+    store_values<T, 8>(p, wide, x);
+}
+// A warp reads a granule's tokens [from, past) of one head back, 8 values of a token (of two tokens, for values) a lane
+// and step.  x: where the granule's first token goes.
+template <typename T, int D>
+__device__ __forceinline__ void read_keys(const uint8_t* bytes, int from, int past, T* x, int64_t stride, bool wide) {
+    constexpr int kLanes = D / 8, kTokens = 32 / kLanes;
+    const int lane = threadIdx.x % 32, d = lane % kLanes * 8;
+#pragma unroll 4
+    for (int t0 = from / kTokens * kTokens; t0 < past; t0 += kTokens) {
+        const int t = t0 + lane / kLanes;
+        const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(bytes + key4_byte<D>(t, d)));
+        const uint32_t s = __ldg(bytes + 16 * D + key4_scale<D>(t, d));
+        uint32_t pairs[4];
+        codes_to_f16(w, steps_of(s * 0x00800080u), pairs);
+        if (t >= from && t < past) put8(x + t * stride + d, wide, pairs);
+    }
+}
+template <typename T, int D>
+__device__ __forceinline__ void read_values(const uint8_t* bytes, int from, int past, T* x, int64_t stride, bool wide) {
+    constexpr int kLanes = D / 8, kTokens = 2 * (32 / kLanes);
+    const int lane = threadIdx.x % 32, d = lane % kLanes * 8;
+#pragma unroll 4
+    for (int t0 = from / kTokens * kTokens; t0 < past; t0 += kTokens) {
+        const int t = t0 + lane / kLanes * 2;
+        const uint2 w = __ldg(reinterpret_cast<const uint2*>(bytes + value4_byte<D>(t, d)));
+        const uint32_t s = __ldg(reinterpret_cast<const uint16_t*>(bytes + 16 * D + value4_scale<D>(t, d)));
+        const Steps steps = steps_of(__byte_perm(s, 0, 0x4140) << 7);
+        uint32_t a[4], b[4], lo[4], hi[4];
+        codes_to_f16(w.x, steps, a), codes_to_f16(w.y, steps, b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) lo[i] = __byte_perm(a[i], b[i], 0x5410), hi[i] = __byte_perm(a[i], b[i], 0x7632);
+        if (t >= from && t < past) put8(x + t * stride + d, wide, lo);
+        if (t + 1 >= from && t + 1 < past) put8(x + (t + 1) * stride + d, wide, hi);
+    }
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads)
+    k_kv4_read(mp_kv_cache c, mp_kv_batch bt, mp_tokens k, mp_tokens v, bool wide, int32_t* status, int per_seq) {
+    const int lane = threadIdx.x % 32;
+    const int64_t units = (int64_t)bt.n_seqs * per_seq * c.n_heads * 2, warps = (int64_t)gridDim.x * kWarps;
+    for (int64_t u = (int64_t)blockIdx.x * kWarps + threadIdx.x / 32; u < units; u += warps) {
+        const int head = (int)(u / 2 % c.n_heads), j = (int)(u / 2 / c.n_heads % per_seq);
+        const int b = (int)(u / 2 / c.n_heads / per_seq);
+        const SeqView s = load_seq(bt, b, true);
+        const int start = s.len - s.n;
+        if (u % 2 == 0 && head == 0 && j == 0) {  // one warp looks the sequence's table over
+            bool ok = s.st == MP_OK;
+            if (s.n > 0)
+                for (int col = start / c.block_tokens + lane; col <= (s.len - 1) / c.block_tokens; col += 32) {
+                    const int p = __ldg(bt.table + (int64_t)b * bt.max_blocks + col);
+                    ok &= p >= 0 && p < c.n_blocks;
+                }
+            ok = __all_sync(~0u, ok);
+            if (lane == 0) status[b] = ok ? MP_OK : MP_EINVAL;
+        }
+        if (j >= granules_touched(s)) continue;
+        const int base = (start / kGranule + j) * kGranule;
+        const int page = __ldg(bt.table + (int64_t)b * bt.max_blocks + base / c.block_tokens);
+        if (page < 0 || page >= c.n_blocks) continue;
+        const int from = max(start - base, 0), past = min(s.len - base, kGranule);
+        const int64_t at = block_byte<4>(c, page, head) + (int64_t)(base % c.block_tokens / kGranule) * granule_bytes(4, D);
+        const mp_tokens& t = u % 2 ? v : k;
+        T* x = static_cast<T*>(t.data) + (s.lo + (base - start)) * t.token_stride + head * t.head_stride;
+        if (u % 2) read_values<T, D>(c.v + at, from, past, x, t.token_stride, wide);
+        else read_keys<T, D>(c.k + at, from, past, x, t.token_stride, wide);
+    }
+}
+
+// Granules that a sequence's tokens may touch.
+int granules_most(const mp_kv_batch& bt) { return std::max<int>((bt.max_tokens + 2 * kGranule - 2) / kGranule, 1); }
+
+template <typename T, int D>
+cudaError_t write_as(const mp_kv_cache& c, const mp_kv_batch& bt, const mp_tokens& k, const mp_tokens& v, int32_t* status,
+                     cudaStream_t stream) {
+    const bool wide = rows_aligned(k) && rows_aligned(v);
+    if (bt.max_tokens <= kFewTokens) {
+        k_kv4_write_few<T, D><<<(unsigned)std::min(bt.n_seqs, 1 << 20), kThreads, 0, stream>>>(c, bt, k, v, wide, status);
+        return cudaGetLastError();
+    }
+    cudaError_t e = cudaMemsetAsync(status, 0, sizeof(int32_t) * (size_t)bt.n_seqs, stream);
+    if (e != cudaSuccess) return e;
+    const int per_seq = granules_most(bt);
+    const int64_t ctas = ((int64_t)bt.n_seqs * per_seq * c.n_heads * 2 + kWarps - 1) / kWarps;
+    k_kv4_write_many<T, D><<<(unsigned)std::min<int64_t>(ctas, 1 << 20), kThreads, 0, stream>>>(c, bt, k, v, wide, status, per_seq);
+    return cudaGetLastError();
+}
+template <typename T, int D>
+cudaError_t read_as(const mp_kv_cache& c, const mp_kv_batch& bt, const mp_tokens& k, const mp_tokens& v, int32_t* status,
+                    cudaStream_t stream) {
+    const bool wide = rows_aligned(k) && rows_aligned(v);
+    const int per_seq = granules_most(bt);
+    const int64_t ctas = ((int64_t)bt.n_seqs * per_seq * c.n_heads * 2 + kWarps - 1) / kWarps;
+    k_kv4_read<T, D><<<(unsigned)std::min<int64_t>(ctas, 1 << 20), kThreads, 0, stream>>>(c, bt, k, v, wide, status, per_seq);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_kv4_write(const mp_kv4_cache& c4, const mp_kv_batch& bt, const mp_tokens& k, const mp_tokens& v,
+                             int32_t* status, cudaStream_t stream) {
+    if (bt.n_seqs == 0) return cudaSuccess;
+    const mp_kv_cache c = as_pool(c4);
+    const bool narrow = c.head_dim == 64;
+    if (k.dtype == MP_F16)
+        return narrow ? write_as<__half, 64>(c, bt, k, v, status, stream) : write_as<__half, 128>(c, bt, k, v, status, stream);
+    if (k.dtype == MP_BF16)
+        return narrow ? write_as<__nv_bfloat16, 64>(c, bt, k, v, status, stream)
+                      : write_as<__nv_bfloat16, 128>(c, bt, k, v, status, stream);
+    return narrow ? write_as<float, 64>(c, bt, k, v, status, stream) : write_as<float, 128>(c, bt, k, v, status, stream);
+}
+
+cudaError_t launch_kv4_read(const mp_kv4_cache& c4, const mp_kv_batch& bt, const mp_tokens& k, const mp_tokens& v,
+                            int32_t* status, cudaStream_t stream) {
+    if (bt.n_seqs == 0) return cudaSuccess;
+    const mp_kv_cache c = as_pool(c4);
+    const bool narrow = c.head_dim == 64;
+    if (k.dtype == MP_F16)
+        return narrow ? read_as<__half, 64>(c, bt, k, v, status, stream) : read_as<__half, 128>(c, bt, k, v, status, stream);
+    if (k.dtype == MP_BF16)
+        return narrow ? read_as<__nv_bfloat16, 64>(c, bt, k, v, status, stream)
+                      : read_as<__nv_bfloat16, 128>(c, bt, k, v, status, stream);
+    return narrow ? read_as<float, 64>(c, bt, k, v, status, stream) : read_as<float, 128>(c, bt, k, v, status, stream);
+}
+
+}  // namespace mp

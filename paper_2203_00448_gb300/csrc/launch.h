@@ -141,4 +141,19 @@ cudaError_t launch_kv_attend(const mp_kv_cache& c, const mp_kv_batch& bt, const 
                              int32_t causal, int32_t window, const mp_tokens& out, float* lse, int32_t* status,
                              void* workspace, cudaStream_t stream);
 
+cudaError_t launch_kv4_write(const mp_kv4_cache& c, const mp_kv_batch& bt, const mp_tokens& k, const mp_tokens& v,
+                             int32_t* status, cudaStream_t stream);
+cudaError_t launch_kv4_read(const mp_kv4_cache& c, const mp_kv_batch& bt, const mp_tokens& k, const mp_tokens& v,
+                            int32_t* status, cudaStream_t stream);
+size_t kv4_attend_workspace_bytes(const mp_kv4_cache& c, const mp_kv_batch& bt, int32_t n_q_heads);
+cudaError_t launch_kv4_attend(const mp_kv4_cache& c, const mp_kv_batch& bt, const mp_tokens& q, float scale, int32_t causal,
+                              int32_t window, const mp_tokens& out, float* lse, int32_t* status, void* workspace,
+                              cudaStream_t stream);
+
+size_t kv_extend_workspace_bytes(const mp_kv_blocks& b);
+cudaError_t launch_kv_extend(const mp_kv_blocks& b, const mp_kv_extension& x, void* workspace, cudaStream_t stream);
+
+cudaError_t launch_rotary(const mp_rotation& r, const int32_t* positions, int64_t n_tokens, int32_t head_dim, const mp_tokens* q,
+                          const mp_tokens* k, const mp_tokens* q_out, const mp_tokens* k_out, int32_t inverse, cudaStream_t stream);
+
 }  // namespace mp

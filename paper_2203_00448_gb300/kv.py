@@ -3,8 +3,10 @@
     kv_write(cache, batch, k, v)   -> status         new tokens quantised into their blocks
     kv_read(cache, batch)          -> k, v, status   tokens read back
     kv_attend(cache, batch, q)     -> out, lse, status   attention over the cache
+    kv_extend(blocks, new, n_tokens) -> step   blocks for a step's tokens, the step's batch, positions and slots
 
-A KvCache is a pool of blocks in 8 bits (its memory may be given, e.g. views of a planned slab); a KvBatch says which
+A KvCache is a pool of blocks in 8 bits, a KvCache4 one in 4 (its memory may be given, e.g. views of a planned slab); the three
+calls take either.  KvBlocks are the blocks that requests hold from step to step.  A KvBatch says which
 blocks the sequences of a call have, how many tokens they hold and which rows of the call's tensors are theirs.  Its
 tensors stay on the device and may be changed there between calls, not replaced by others.  All calls are asynchronous on the
 current (or given) CUDA stream; what they allocate belongs to that stream.  No gradient passes through them: outputs are
@@ -48,7 +50,32 @@ class _Fixed:
         object.__delattr__(self, name)
 
 
-class KvCache(_Fixed):
+class _Pool(_Fixed):
+    """What caches of 8 and of 4 bits have alike."""
+
+    def _begin(self, n_blocks, block_tokens, n_heads, head_dim):
+        self.n_blocks, self.block_tokens, self.n_heads, self.head_dim = n_blocks, block_tokens, n_heads, head_dim
+        if block_tokens % 32 or not 32 <= block_tokens <= 256 or head_dim not in (64, 128) or n_heads < 1:
+            raise ValueError("block_tokens is a multiple of 32 up to 256, head_dim 64 or 128, n_heads at least 1")
+
+    def _arrays(self, device, given):
+        """Makes what is not given; given: name -> (tensor or None, dtype, shape)."""
+        there = [t for t, _, _ in given.values() if t is not None]
+        device = there[0].device if there else torch.device(device)
+        for name, (t, dtype, shape) in given.items():
+            setattr(self, name, torch.empty(shape, dtype=dtype, device=device) if t is None else _tensor(name, t, dtype, shape, device))
+        for name in ("k", "v"):
+            if getattr(self, name).data_ptr() % 16:
+                raise ValueError(f"{name} has to start on a 16-byte boundary")
+        self.device = self.k.device
+
+    def _end(self, struct, calls):
+        self._struct, self._ref, self._calls = struct, ctypes.byref(struct), calls
+        # what a batch's struct and scratch depend on
+        self._key, self._index = (calls, self.n_blocks > 0, self.block_tokens, self.n_heads, self.head_dim, self.device), self.k.get_device()
+
+
+class KvCache(_Pool):
     """A pool of n_blocks blocks of block_tokens tokens: e4m3 keys and values of n_heads heads of head_dim values, one
     scale for each block and head.  k, v (uint8[n_blocks, n_heads, block_tokens * head_dim], 16-byte aligned) and
     k_scale, v_scale (float32[n_blocks, n_heads]) are allocated unless given; nothing needs to be initialised."""
@@ -57,35 +84,36 @@ class KvCache(_Fixed):
 
     def __init__(self, n_blocks: int, block_tokens: int, n_heads: int, head_dim: int, device="cuda", k=None, v=None,
                  k_scale=None, v_scale=None):
-        self.n_blocks, self.block_tokens, self.n_heads, self.head_dim = n_blocks, block_tokens, n_heads, head_dim
-        if block_tokens % 32 or not 32 <= block_tokens <= 256 or head_dim not in (64, 128) or n_heads < 1:
-            raise ValueError("block_tokens is a multiple of 32 up to 256, head_dim 64 or 128, n_heads at least 1")
+        self._begin(n_blocks, block_tokens, n_heads, head_dim)
         shape = (n_blocks, n_heads, block_tokens * head_dim)
-        given = [t for t in (k, v, k_scale, v_scale) if t is not None]
-        device = given[0].device if given else torch.device(device)
-
-        def make(name, t, dtype, shape):
-            if t is None:
-                return torch.empty(shape, dtype=dtype, device=device)
-            return _tensor(name, t, dtype, shape, device)
-
-        self.k, self.v = make("k", k, torch.uint8, shape), make("v", v, torch.uint8, shape)
-        self.k_scale = make("k_scale", k_scale, torch.float32, shape[:2])
-        self.v_scale = make("v_scale", v_scale, torch.float32, shape[:2])
-        for name, t in (("k", self.k), ("v", self.v)):
-            if t.data_ptr() % 16:
-                raise ValueError(f"{name} has to start on a 16-byte boundary")
-        self.device = self.k.device
-        self._struct = _lib.MpKvCache(n_blocks, block_tokens, n_heads, head_dim, _ptr(self.k), _ptr(self.v),
-                                      _ptr(self.k_scale), _ptr(self.v_scale))
-        self._ref = ctypes.byref(self._struct)
-        # what a batch's struct and scratch depend on
-        self._key, self._index = (n_blocks > 0, block_tokens, n_heads, head_dim, self.device), self.k.get_device()
+        self._arrays(device, {"k": (k, torch.uint8, shape), "v": (v, torch.uint8, shape),
+                              "k_scale": (k_scale, torch.float32, shape[:2]), "v_scale": (v_scale, torch.float32, shape[:2])})
+        self._end(_lib.MpKvCache(n_blocks, block_tokens, n_heads, head_dim, _ptr(self.k), _ptr(self.v), _ptr(self.k_scale),
+                                 _ptr(self.v_scale)), "kv")
 
     @staticmethod
     def block_bytes(block_tokens: int, n_heads: int, head_dim: int) -> int:
         """Bytes of one block: keys, values and their scales (what a plan counts a request's blocks at)."""
         return 2 * n_heads * (block_tokens * head_dim + 4)
+
+
+class KvCache4(_Pool):
+    """A pool in 4 bits: 32 values of a token and head share a scale of 8 bits, 4.25 bits a value.  k, v (uint8[n_blocks,
+    n_heads, block_tokens * head_dim * 17 / 32], 16-byte aligned) are allocated unless given; nothing needs to be
+    initialised.  Values are stored to half a step of a scale that is at most 240: magnitudes up to 1,800."""
+
+    _fixed = frozenset(("n_blocks", "block_tokens", "n_heads", "head_dim", "k", "v", "device"))
+
+    def __init__(self, n_blocks: int, block_tokens: int, n_heads: int, head_dim: int, device="cuda", k=None, v=None):
+        self._begin(n_blocks, block_tokens, n_heads, head_dim)
+        shape = (n_blocks, n_heads, block_tokens // 32 * 17 * head_dim)
+        self._arrays(device, {"k": (k, torch.uint8, shape), "v": (v, torch.uint8, shape)})
+        self._end(_lib.MpKv4Cache(n_blocks, block_tokens, n_heads, head_dim, _ptr(self.k), _ptr(self.v)), "kv_four")
+
+    @staticmethod
+    def block_bytes(block_tokens: int, n_heads: int, head_dim: int) -> int:
+        """Bytes of one block: keys and values with their scales."""
+        return 2 * n_heads * (block_tokens // 32 * 17 * head_dim)
 
 
 class KvBatch(_Fixed):
@@ -126,6 +154,60 @@ class KvBatch(_Fixed):
                                _ptr(self.lens), _ptr(self.token_ptr))
             made = self._made[cache._key] = (ctypes.byref(s), (self.n_tokens, cache.n_heads, cache.head_dim), {})
         return made
+
+
+class KvBlocks(_Fixed):
+    """The blocks of n_seqs requests from step to step: table int32[n_seqs, max_blocks] (columns past a request's last block mean
+    nothing), lens int32[n_seqs], tokens held, 0 to begin with.  Free blocks are a stack: free int32[n_blocks], of which the
+    first n_free[0] are free, all of them (0 on top) to begin with.  Or first, room (int32[n_seqs]) give each request a run of
+    blocks of its own, e.g. by a plan of their lifetimes; there is no stack then.  Whatever is given is used as it is."""
+
+    _fixed = frozenset(("n_seqs", "max_blocks", "block_tokens", "n_blocks", "table", "lens", "free", "n_free", "first", "room",
+                        "device"))
+
+    def __init__(self, n_seqs: int, max_blocks: int, block_tokens: int, n_blocks: int, first=None, room=None, device="cuda",
+                 table=None, lens=None, free=None, n_free=None):
+        self.n_seqs, self.max_blocks, self.block_tokens, self.n_blocks = n_seqs, max_blocks, block_tokens, n_blocks
+        if block_tokens % 32 or not 32 <= block_tokens <= 256 or min(n_seqs, max_blocks, n_blocks) < 0:
+            raise ValueError("block_tokens is a multiple of 32 up to 256, the counts are not negative")
+        if (first is None) != (room is None) or (first is not None and (free is not None or n_free is not None)):
+            raise ValueError("first and room come together, in the place of free and n_free")
+        if (free is None) != (n_free is None):
+            raise ValueError("free and n_free come together")
+        there = [t for t in (table, lens, free, n_free, first, room) if t is not None]
+        device = there[0].device if there else torch.device(device)
+        if device.type == "cuda" and device.index is None:
+            device = torch.device("cuda", torch.cuda.current_device())
+        self.device = device
+        make = dict(dtype=torch.int32, device=self.device)
+        if table is None:
+            table = torch.full((n_seqs, max_blocks), -1, **make)
+        if lens is None:
+            lens = torch.zeros(n_seqs, **make)
+        if first is None and free is None:
+            free = torch.arange(n_blocks - 1, -1, -1, **make)
+            n_free = torch.full((1,), n_blocks, **make)
+        shapes = {"table": (n_seqs, max_blocks), "lens": (n_seqs,), "free": (n_blocks,), "n_free": (1,), "first": (n_seqs,),
+                  "room": (n_seqs,)}
+        for name, t in (("table", table), ("lens", lens), ("free", free), ("n_free", n_free), ("first", first), ("room", room)):
+            setattr(self, name, t if t is None else _tensor(name, t, torch.int32, shapes[name], self.device))
+        self._struct = _lib.MpKvBlocks(n_seqs, max_blocks, block_tokens, n_blocks,
+                                       *(None if t is None else t.data_ptr() or None for t in (self.table, self.free, self.first, self.room)))
+        self._ref, self._index, self._need = ctypes.byref(self._struct), self.table.get_device(), None
+
+
+class KvStep:
+    """What kv_extend has made: the step's batch (its lens are -1 where a request takes no part), positions int32[n_tokens],
+    slots int64[n_tokens] and the status of each request."""
+
+    def __init__(self, blocks: KvBlocks, n_tokens, max_tokens, max_len):
+        dev = blocks.device
+        self.batch = KvBatch(blocks.table, torch.empty(blocks.n_seqs, dtype=torch.int32, device=dev),
+                             torch.empty(blocks.n_seqs + 1, dtype=torch.int64, device=dev), n_tokens, max_tokens, max_len)
+        self.positions = torch.empty(n_tokens, dtype=torch.int32, device=dev)
+        self.slots = torch.empty(n_tokens, dtype=torch.int64, device=dev)
+        self.status = torch.empty(blocks.n_seqs, dtype=torch.int32, device=dev)
+        self._of = blocks
 
 
 def _tokens(name, t, cache, shape):
@@ -200,7 +282,8 @@ def kv_write(cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tensor, s
     ref, shape, _ = batch._for(cache)
     kt, vt = _tokens("k", k, cache, shape), _tokens("v", v, cache, shape)
     status, stream_ptr = _status(status, batch), _stream(cache)
-    _check("mp_kv_write", _lib.load().mp_kv_write(cache._ref, ref, kt, vt, status.data_ptr() or None, stream_ptr))
+    call = "mp_" + cache._calls + "_write"
+    _check(call, getattr(_lib.load(), call)(cache._ref, ref, kt, vt, status.data_ptr() or None, stream_ptr))
     return status
 
 
@@ -227,7 +310,8 @@ def kv_read(cache: KvCache, batch: KvBatch, dtype=torch.bfloat16, k=None, v=None
             v = torch.empty_like(k) if k.is_contiguous() else torch.empty(shape, dtype=dtype, device=cache.device)
             vt = _fresh(v, shape[1], shape[2])
     status, stream_ptr = _status(status, batch), _stream(cache)
-    _check("mp_kv_read", _lib.load().mp_kv_read(cache._ref, ref, kt, vt, status.data_ptr() or None, stream_ptr))
+    call = "mp_" + cache._calls + "_read"
+    _check(call, getattr(_lib.load(), call)(cache._ref, ref, kt, vt, status.data_ptr() or None, stream_ptr))
     return k, v, status
 
 
@@ -235,7 +319,8 @@ def kv_attend_workspace_bytes(cache: KvCache, batch: KvBatch, n_q_heads: int) ->
     ref, _, needs = batch._for(cache)
     need = needs.get(n_q_heads)
     if need is None:
-        need = needs[n_q_heads] = int(_lib.load().mp_kv_attend_workspace_bytes(cache._ref, ref, n_q_heads))
+        call = getattr(_lib.load(), "mp_" + cache._calls + "_attend_workspace_bytes")
+        need = needs[n_q_heads] = int(call(cache._ref, ref, n_q_heads))
     return need
 
 
@@ -272,8 +357,48 @@ def kv_attend(cache: KvCache, batch: KvBatch, q: torch.Tensor, scale: float | No
         wptr, wbytes = scratch.get(need)
     else:
         wptr, wbytes = None, 0
-    _check("mp_kv_attend",
-           _lib.load().mp_kv_attend(cache._ref, ref, qt, shape[2] ** -0.5 if scale is None else scale, 1 if causal else 0,
-                                    window, ot, None if lse is None else lse.data_ptr() or None,
-                                    status.data_ptr() or None, wptr, wbytes, stream_ptr))
+    call = "mp_" + cache._calls + "_attend"
+    _check(call, getattr(_lib.load(), call)(cache._ref, ref, qt, shape[2] ** -0.5 if scale is None else scale,
+                                            1 if causal else 0, window, ot, None if lse is None else lse.data_ptr() or None,
+                                            status.data_ptr() or None, wptr, wbytes, stream_ptr))
     return out, lse, status
+
+
+def kv_extend(blocks: KvBlocks, new: torch.Tensor, n_tokens: int, max_tokens: int | None = None, max_len: int | None = None,
+              lens=None, n_free=None, step: KvStep | None = None, workspace: Workspace | None = None, stream=None) -> KvStep:
+    """One step of the requests: new int32[n_seqs] tokens each, negative where a request ends.  n_tokens: their sum, as the host
+    knows it; max_tokens of a request (default n_tokens), max_len that it then holds (default what the table has room for).
+    blocks.lens and blocks.n_free are advanced, or what they become is written to lens and n_free if these are given.  Returns
+    the step, or fills the one that is given (of the same blocks and bounds)."""
+    if _away(blocks, stream):
+        with _at(blocks, stream):
+            return kv_extend(blocks, new, n_tokens, max_tokens, max_len, lens, n_free, step, workspace)
+    stream_ptr = _stream(blocks)
+    _tensor("new", new, torch.int32, (blocks.n_seqs,), blocks.device)
+    room = min(blocks.max_blocks * blocks.block_tokens, _MOST)
+    max_len = room if max_len is None else int(max_len)
+    if not 0 <= max_len <= room:
+        raise ValueError(f"max_len is {max_len}: 0 to {room} is possible")
+    if n_tokens < 0:
+        raise ValueError(f"n_tokens is {n_tokens}")
+    max_tokens = min(int(n_tokens), _MOST) if max_tokens is None else int(max_tokens)
+    if step is None:
+        step = KvStep(blocks, int(n_tokens), max_tokens, max_len)
+    elif step._of is not blocks or (step.batch.n_tokens, step.batch.max_tokens, step.batch.max_len) != (n_tokens, max_tokens, max_len):
+        raise ValueError("the step that is given has other blocks or bounds")
+    lens = blocks.lens if lens is None else _tensor("lens", lens, torch.int32, (blocks.n_seqs,), blocks.device)
+    if n_free is None:
+        n_free = blocks.n_free
+    elif blocks.n_free is None:
+        raise ValueError("n_free: these blocks have no stack")
+    else:
+        _tensor("n_free", n_free, torch.int32, (1,), blocks.device)
+    b = step.batch
+    x = _lib.MpKvExtension(n_tokens, max_tokens, max_len, *(None if t is None else t.data_ptr() or None for t in (
+        blocks.lens, blocks.n_free, new, lens, n_free, b.lens, b.token_ptr, step.positions, step.slots, step.status)))
+    if blocks._need is None:
+        blocks._need = int(_lib.load().mp_kv_extend_workspace_bytes(blocks._ref))
+    scratch = workspace or _workspace_of(stream_ptr, blocks.device)
+    wptr, wbytes = scratch.get(blocks._need)
+    _check("mp_kv_extend", _lib.load().mp_kv_extend(blocks._ref, ctypes.byref(x), wptr, wbytes, stream_ptr))
+    return step

@@ -1,0 +1,321 @@
+"""The cache in 4 bits against plain 64-bit implementations: lengths of 0 and 1, blocks that end inside a granule, pairs of
+tokens of which one is new, values beside rounding borders, slots full of bytes that stand for no number."""
+import numpy as np
+import pytest
+import torch
+
+from tests import kv4_refs as R4
+from tests import kv_refs as R
+from tests.test_gpu_kv import ATTENDS, BF16, F16, F32, WRITES, batch_of, rows
+
+pytestmark = pytest.mark.gpu
+
+
+def same(cache, pool):
+    got = pool.from_stored(cache.k.cpu().numpy(), cache.v.cpu().numpy())
+    return all(np.array_equal(x, y) for x, y in zip(got, (pool.k, pool.ks, pool.v, pool.vs)))
+
+
+@pytest.mark.parametrize("block,heads,d,dtype,how,seqs", WRITES)
+def test_write_and_read(cuda_lib, block, heads, d, dtype, how, seqs):
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(11)
+    lens, new = [s[0] for s in seqs], [s[1] for s in seqs]
+    table, n = R.make_table(lens, block, rng)
+    pool = R4.Pool(n, block, heads, d, rng)
+    s = torch.from_numpy(np.exp2(rng.integers(-20, 7, (sum(new), heads, 1)))).cuda()
+    k, _ = rows(rng, sum(new), heads, d, dtype, how)
+    v, _ = rows(rng, sum(new), heads, d, dtype, how)
+    k.copy_(k.double() * s)
+    v.copy_(v.double() * s * 0.03)
+    cache, batch = pool.cache(), batch_of(mp, table, lens, new)
+    status = mp.kv_write(cache, batch, k, v)
+    assert np.array_equal(R4.write(pool, table, lens, new, k.double().cpu().numpy(), v.double().cpu().numpy()), status.cpu().numpy())
+    assert same(cache, pool)  # what is not written is as it was
+    for out_dtype in (F16, BF16, F32):
+        ko, _ = rows(rng, sum(new), heads, d, out_dtype, how)
+        vo, _ = rows(rng, sum(new), heads, d, out_dtype, how)
+        _, _, st = mp.kv_read(cache, batch, out_dtype, k=ko, v=vo)
+        assert not st.any()
+        want = [np.concatenate(x) for x in zip(*(R4.held(pool, table, b, lens[b] - new[b], lens[b]) for b in range(len(lens))))]
+        for x, y in ((ko, want[0]), (vo, want[1])):  # exact in every type
+            assert torch.equal(x.double().cpu(), torch.from_numpy(y))
+    mp.kv_write(cache, batch, k, v)  # a second call with the same tokens changes nothing
+    assert same(cache, pool)
+
+
+@pytest.mark.parametrize("tokens", [9, 40])
+def test_write_beside_borders(cuda_lib, tokens):
+    """Largest magnitudes and values a rounding of 32 bits around 7.5 s and (n + 1/2) s, for every scale; zeros; the smallest."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(tokens)
+    every = np.concatenate([R4.SCALES[1:], [2.0 ** -30, 1e-40, 240.0]])
+    x = np.zeros((tokens * 4 * 4, 32), np.float32)
+    for row in range(len(x)):
+        s = every[(row * 7 + tokens) % len(every)]
+        n = rng.integers(-8, 8, 32) + 0.5
+        x[row] = np.clip(n, -7.5, 7.5) * s
+        x[row, 0] = 7.5 * s
+        off = rng.integers(-1, 2, 32)
+        x[row] = np.where(off == 0, x[row], np.nextafter(x[row], np.float32(np.inf) * np.where(off > 0, 1, -1).astype(np.float32)))
+        x[row, 0] = min(x[row, 0], np.float32(1800))
+    x[5], x[6, 1:] = 0, 0
+    k = torch.from_numpy(np.clip(x, -1800, 1800).reshape(tokens, 4, 128)).cuda()
+    table, n = R.make_table([tokens + 3], 64, rng)
+    pool = R4.Pool(n, 64, 4, 128, rng)
+    cache, batch = pool.cache(), batch_of(mp, table, [tokens + 3], [tokens])
+    assert not mp.kv_write(cache, batch, k, k.flip(0)).any()
+    R4.write(pool, table, [tokens + 3], [tokens], k.double().cpu().numpy(), k.flip(0).double().cpu().numpy())
+    assert same(cache, pool)
+
+
+def test_write_non_finite_and_large_values(cuda_lib):
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(5)
+    lens, new = [40, 40, 3, 40, 35], [8, 40, 3, 40, 20]
+    for dtype, few in ((BF16, False), (F32, True), (F16, False)):
+        if few:
+            new = [8, 5, 3, 4, 16]
+        at = np.concatenate([[0], np.cumsum(new)])
+        table, n = R.make_table(lens, 32, rng)
+        pool = R4.Pool(n, 32, 2, 64, rng)
+        k, _ = rows(rng, sum(new), 2, 64, dtype)
+        v, _ = rows(rng, sum(new), 2, 64, dtype)
+        k[3, 0, 5], k[at[1] + 1, 1, 6] = float("nan"), float("inf")
+        v[at[1], 1, 7] = float("-inf")
+        v[at[2]:at[3]] = 1800.0
+        k[at[3]] = 1808.0  # in every type the next number above
+        cache, batch = pool.cache(), batch_of(mp, table, lens, new)
+        status = mp.kv_write(cache, batch, k, v)
+        want = R4.write(pool, table, lens, new, k.double().cpu().numpy(), v.double().cpu().numpy())
+        assert want.tolist() == [1, 1, 0, 1, 0] and np.array_equal(want, status.cpu().numpy())
+        assert same(cache, pool)
+
+
+def check_attend(mp, pool, table, lens, new, q, qx, scale, causal, window, **kw):
+    cache, batch = pool.cache(), batch_of(mp, table, lens, new, **kw)
+    out, lse, status = mp.kv_attend(cache, batch, q, scale=scale, causal=causal, window=window, want_lse=True)
+    want, want_lse, mag, size = R4.attend(pool, table, lens, new, qx, scale, causal, window)
+    bound, lse_bound = R.attend_bounds(q.dtype, want, want_lse, mag, size)
+    assert not status.any()
+    out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    assert np.array_equal(np.isneginf(lse), np.isneginf(want_lse))
+    assert (out[np.isneginf(want_lse)] == 0).all()
+    assert (np.abs(out - want) <= bound).all(), np.max(np.abs(out - want) / bound)
+    fine = np.isfinite(want_lse)
+    assert (np.abs(lse[fine] - want_lse[fine]) <= lse_bound[fine]).all()
+
+
+@pytest.mark.parametrize("block,hq,heads,d,dtype,how,causal,window,seqs", ATTENDS)
+def test_attend(cuda_lib, block, hq, heads, d, dtype, how, causal, window, seqs):
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(7)
+    lens, new = [s[0] for s in seqs], [s[1] for s in seqs]
+    table, n = R.make_table(lens, block, rng)
+    pool = R4.Pool(n, block, heads, d, rng)
+    for b, length in enumerate(lens):  # slots past the end hold bytes that stand for no number
+        if length % block:
+            for scales in (pool.ks, pool.vs):
+                scales[table[b, length // block], :, length % block:] = 0xFF
+    q, qx = rows(rng, sum(new), hq, d, dtype, how)
+    check_attend(mp, pool, table, lens, new, q, qx, d ** -0.5, causal, window)
+
+
+@pytest.mark.parametrize("group,d,dtype", [(4, 128, BF16), (4, 64, F16), (3, 128, F16), (1, 64, BF16), (8, 128, BF16)])
+@pytest.mark.parametrize("kind", ["prompts", "few", "singles"])
+def test_attend_ragged(cuda_lib, group, d, dtype, kind):
+    """Batches whose work is cut between CTAs, from scratch memory that holds anything; the definition in 64 bits on the GPU."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(group * d)
+    heads, block = 3, 32
+    most = {"prompts": 700, "few": 128 // group + 1, "singles": 2}[kind]
+    for count in (3, 24):
+        new = [int(n) for n in rng.integers(1, most, count)]
+        lens = [n + int(x) for n, x in zip(new, rng.integers(0, 900 if kind == "prompts" else 6000, count))]
+        lens[0] = new[0]
+        table, n = R.make_table(lens, block, rng)
+        pool = R4.Pool(n, block, heads, d, rng)
+        pool.vs[:] = rng.integers(40, 150, pool.vs.shape)
+        cache, batch = pool.cache(), batch_of(mp, table, lens, new)
+        q, qx = rows(rng, sum(new), heads * group, d, dtype)
+        k, v, _ = mp.kv_read(cache, batch_of(mp, table, lens, lens), F32)
+        want, mag, want_lse, size, row, past = [], [], [], [], 0, 0
+        for length, m in zip(lens, new):
+            kk, vv = (x[past:past + length].double().repeat_interleave(group, 1).transpose(0, 1) for x in (k, v))
+            qq = q[row:row + m].double().transpose(0, 1)
+            x = qq @ kk.transpose(1, 2) * d ** -0.5
+            j = torch.arange(length, device="cuda")
+            x = x.masked_fill(j > (length - m + torch.arange(m, device="cuda"))[:, None], -torch.inf)
+            w = torch.softmax(x, -1)
+            want.append((w @ vv).transpose(0, 1)), mag.append((w @ vv.abs()).transpose(0, 1))
+            want_lse.append(torch.logsumexp(x, -1).transpose(0, 1))
+            size.append(((qq.abs() @ kk.abs().transpose(1, 2)).amax(-1) * d ** -0.5).transpose(0, 1))
+            row, past = row + m, past + length
+        want, mag, want_lse, size = (torch.cat(x).cpu().numpy() for x in (want, mag, want_lse, size))
+        bound, lse_bound = R.attend_bounds(dtype, want, want_lse, mag, size)
+        first = None
+        for fill in (0, 255, 0, 255):
+            ws = mp.Workspace("cuda")
+            ws.get(max(mp.kv_attend_workspace_bytes(cache, batch, heads * group), 1))
+            ws.buf.fill_(fill)
+            out, lse, status = mp.kv_attend(cache, batch, q, want_lse=True, workspace=ws)
+            assert not status.any()
+            assert (np.abs(out.double().cpu().numpy() - want) <= bound).all()
+            assert (np.abs(lse.double().cpu().numpy() - want_lse) <= lse_bound).all()
+            first = out if first is None else first
+            assert torch.equal(out, first)
+
+
+def test_attend_sharp_and_flat_rows_and_scales_far_apart(cuda_lib):
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(9)
+    for new in ([1, 90], [2, 3]):
+        lens = [3000, 700]
+        table, n = R.make_table(lens, 64, rng)
+        pool = R4.Pool(n, 64, 2, 128, rng)
+        pool.vs[:] = rng.integers(0, 184, pool.vs.shape)  # every scale there is, zeros among them
+        pool.ks[table[1, 3]] = 0
+        q, _ = rows(rng, sum(new), 4, 128, F16)
+        q[0] *= 60
+        q[1] = 0
+        q[2, 1] *= 1e-6
+        q[-1, 2:] *= 100
+        check_attend(mp, pool, table, lens, new, q, q.double().cpu().numpy(), 128 ** -0.5, True, 0)
+
+
+def test_non_finite_queries_stay_in_their_rows(cuda_lib):
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(19)
+    for lens, new in (([100, 50], [1, 2]), ([300, 100], [100, 70]), ([5000, 100], [2, 2])):
+        table, n = R.make_table(lens, 64, rng)
+        pool = R4.Pool(n, 64, 2, 64, rng)
+        cache, batch = pool.cache(), batch_of(mp, table, lens, new)
+        q, _ = rows(rng, sum(new), 4, 64, F16)
+        clean, _, _ = mp.kv_attend(cache, batch, q)
+        q[1, 2, 3], q[0, 1, 5] = float("nan"), float("inf")
+        out, _, status = mp.kv_attend(cache, batch, q)
+        assert torch.isnan(out[1, 2]).all() and torch.isnan(out[0, 1]).all() and not status.any()
+        clean[1, 2] = clean[0, 1] = out[1, 2] = out[0, 1] = 0
+        assert torch.equal(out, clean)
+
+
+def test_pools_past_32_bit_offsets(cuda_lib):
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(29)
+    block, heads, d = 128, 8, 128
+    n = (1 << 32) // (block * heads * d * 17 // 32) + 40
+    cache = mp.KvCache4(n, block, heads, d)
+    lens = [200, 300]
+    ids, local = np.array([[n - 1, n - 3, -1], [n - 2, n - 7, n - 5]], np.int32), np.array([[7, 5, -1], [6, 1, 3]], np.int32)
+    small = R4.Pool(8, block, heads, d, rng)
+    for x, y in zip((cache.k, cache.v), small.stored()):
+        x[n - 8:] = torch.from_numpy(y).cuda()
+    for new in ([200, 1], [1, 2]):
+        batch = batch_of(mp, ids, lens, new)
+        k, kx = rows(rng, sum(new), heads, d, BF16)
+        v, vx = rows(rng, sum(new), heads, d, BF16)
+        assert not mp.kv_write(cache, batch, k, v).any()
+        R4.write(small, local, lens, new, kx, vx)
+        got = small.from_stored(cache.k[n - 8:].cpu().numpy(), cache.v[n - 8:].cpu().numpy())
+        assert all(np.array_equal(x, y) for x, y in zip(got, (small.k, small.ks, small.v, small.vs)))
+        ko, vo, _ = mp.kv_read(cache, batch, F32)
+        want = R4.held(small, local, 0, 200 - new[0], 200)
+        assert torch.equal(ko[:new[0]].double().cpu(), torch.from_numpy(want[0]))
+        q, qx = rows(rng, sum(new), heads, d, BF16)
+        out, lse, status = mp.kv_attend(cache, batch, q, want_lse=True)
+        want, want_lse, mag, size = R4.attend(small, local, lens, new, qx, d ** -0.5)
+        bound, _ = R.attend_bounds(BF16, want, want_lse, mag, size)
+        assert not status.any() and (np.abs(out.double().cpu().numpy() - want) <= bound).all()
+
+
+def test_bad_sequences_are_reported_and_leave_others_alone(cuda_lib):
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(31)
+    lens = [100, 90, 80, 70, 64, 60]
+    table, n = R.make_table(lens, 32, rng)
+    for count in (3, 40):
+        new = [count] * 6
+        pool = R4.Pool(n, 32, 2, 64, rng)
+        cache = pool.cache()
+        q, _ = rows(rng, sum(new), 4, 64, F16)
+        k, kx = rows(rng, sum(new), 2, 64, F16)
+        bad_lens, bad_table = list(lens), table.copy()
+        bad_lens[1], bad_lens[2] = 101, -1  # past max_len, negative
+        bad_table[3, 1:], bad_table[4, 1:] = n, -1  # outside the pool
+        bad = batch_of(mp, bad_table, bad_lens, new, max_len=100)
+        clean, _, _ = mp.kv_attend(cache, batch_of(mp, table, lens, new, max_len=100), q)
+        out, _, status = mp.kv_attend(cache, bad, q)
+        assert status.tolist() == [0, 1, 1, 1, 1, 0]
+        for s in (slice(0, count), slice(5 * count, 6 * count)):
+            assert torch.equal(out[s], clean[s])
+        before_k, _, st = mp.kv_read(cache, bad, F32)
+        assert st.tolist() == [0, 1, 1, 1, 1, 0]
+        assert mp.kv_write(cache, bad, k, k).tolist() == [0, 1, 1, 1, 1, 0]
+        for b in (0, 5):
+            part = [x[b:b + 1] for x in (table, np.array(lens), np.array(new))]
+            R4.write(pool, *part, kx[b * count:(b + 1) * count], kx[b * count:(b + 1) * count])
+        got = pool.from_stored(cache.k.cpu().numpy(), cache.v.cpu().numpy())
+        for b in (0, 5):
+            pages = table[b, :-(-lens[b] // 32)]
+            for x, y in zip(got, (pool.k, pool.ks, pool.v, pool.vs)):
+                assert np.array_equal(x[pages], y[pages])
+
+
+def test_empty_pool_and_empty_batch(cuda_lib):
+    import paper_2203_00448_gb300 as mp
+
+    none = mp.KvCache4(0, 32, 2, 64)
+    q = torch.ones(3, 4, 64, dtype=F16, device="cuda")
+    batch = batch_of(mp, np.zeros((2, 2)), [0, 40], [1, 2])
+    out, lse, status = mp.kv_attend(none, batch, q, want_lse=True)
+    assert status.tolist() == [0, 1] and (out[0] == 0).all() and torch.isneginf(lse[0]).all()
+    cache = mp.KvCache4(3, 32, 2, 64)
+    empty = batch_of(mp, np.zeros((0, 2)), [], [])
+    assert mp.kv_write(cache, empty, q[:0, :2], q[:0, :2]).numel() == 0
+    assert mp.kv_attend(cache, empty, q[:0])[0].numel() == 0
+
+
+def test_captured_calls_and_other_streams(cuda_lib):
+    """Graphs replayed after their inputs have changed, two of them at once, beside eager calls on another stream."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(41)
+    lens, new = [6000, 333, 64], [1, 2, 1]
+    table, n = R.make_table(lens, 64, rng)
+    pool = R4.Pool(n, 64, 2, 128, rng)
+    cache, batch = pool.cache(), batch_of(mp, table, lens, new)
+    q, _ = rows(rng, 4, 8, 128, BF16)
+    k, _ = rows(rng, 4, 2, 128, BF16)
+    other, _ = rows(rng, 4, 8, 128, BF16)
+    mp.kv_write(cache, batch, k, k)
+    mp.kv_attend(cache, batch, q)
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for x in (q, other):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            mp.kv_write(cache, batch, k, k)
+            outs.append(mp.kv_attend(cache, batch, x)[0])
+        graphs.append(g)
+    k.mul_(2)
+    q.mul_(0.5)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        eager = mp.kv_read(cache, batch, F32, stream=streams[2])[0]
+    torch.cuda.synchronize()
+    assert eager.shape == (4, 2, 128)
+    for x, y in zip(outs, (q, other)):
+        assert torch.equal(x, mp.kv_attend(cache, batch, y)[0])
