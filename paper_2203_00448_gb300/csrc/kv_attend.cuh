@@ -1,4 +1,4 @@
-// kv_attend.cuh -- what the attention kernels over the 8-bit cache share: barriers
+// kv_attend.cuh -- what the attention kernels over the caches share: barriers
 // with bounded waits, bulk copies, and the scaling that both products use.
 #pragma once
 
@@ -167,6 +167,7 @@ inline cudaError_t launch_close(void (*kernel)(K...), int grid, int threads, siz
 }
 
 size_t kv_many_part_bytes(const mp_kv_cache& c);
-cudaError_t launch_kv_many(const AttendArgs& a, const ManyWork& w, cudaStream_t stream);
+cudaError_t launch_kv_many(const AttendArgs& a, const ManyWork& w, cudaStream_t stream);   // over 8 bits
+cudaError_t launch_kv4_many(const AttendArgs& a, const ManyWork& w, cudaStream_t stream);  // over 4
 
 }  // namespace mp

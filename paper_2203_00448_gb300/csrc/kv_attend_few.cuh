@@ -865,8 +865,7 @@ Route route(const mp_kv_cache& c, const mp_kv_batch& bt, int32_t group, int32_t 
         const bool brief = span <= kShortLen && (int64_t)bt.n_seqs * c.n_heads <= kShortCtas;
         return {!brief, false, brief};
     }
-    if (kBits == 4) return {true, false, false};
-    const int64_t bytes = (int64_t)bt.n_seqs * bt.max_len * c.n_heads * c.head_dim * 2;
+    const int64_t bytes = (int64_t)bt.n_seqs * bt.max_len * c.n_heads * granule_bytes(kBits, c.head_dim) / (kGranule / 2);
     return {bt.n_tokens != (int64_t)bt.n_seqs * bt.max_tokens && bytes > kSmallCache, true, false};
 }
 
@@ -920,7 +919,7 @@ cudaError_t attend_as(const AttendArgs& a, const FewWork& few, const ManyWork& m
         rows = (int64_t)a.bt.n_seqs * join_rows(a) * a.c.n_heads;
     }
     if (many.part != nullptr) {
-        e = launch_kv_many(a, many, stream);
+        e = kBits == 8 ? launch_kv_many(a, many, stream) : launch_kv4_many(a, many, stream);
         if (e != cudaSuccess) return e;
         plan.cuts = kManyCtas * (D / kJoinCols);
     }
@@ -964,7 +963,7 @@ cudaError_t launch_attend(const mp_kv_cache& c, const mp_kv_batch& bt, const mp_
     a.c = c, a.bt = bt, a.q = q, a.out = out, a.lse = lse, a.status = status;
     a.scale = scale, a.causal = causal, a.window = window;
     a.group = group;
-    a.few_rows = kBits == 4 ? 1 << 30 : r.few || r.brief ? kFewRows : -1;
+    a.few_rows = r.few || r.brief ? kFewRows : -1;
     a.wide_q = rows_aligned(q), a.wide_out = rows_aligned(out);
 #ifdef MP_TEST_HOOKS
     a.hold = hold;
