@@ -83,14 +83,21 @@ __device__ __forceinline__ uint32_t fma_f16x2(uint32_t x, uint32_t y, uint32_t z
 __device__ __forceinline__ Steps steps_of(uint32_t s) {
     return {s, mul_f16x2(s, 0xce00ce00u), mul_f16x2(s, 0xdc20dc20u)};  // -24, -264
 }
+// x & mask | bits in one operation (written with & and | it became two, for both constants would be immediate ones: 774
+// instructions a granule of k_kv_attend_few for 646).
+__device__ __forceinline__ uint32_t masked_or(uint32_t x, uint32_t mask, uint32_t bits) {
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(x), "r"(mask), "r"(bits));
+    return r;
+}
 // 8 codes of a word as f16 pairs of codes i and i + 4: a code that is moved to bits 6-9 under the exponent of 16 is 16 +
 // u, at bits 2-5 under that of 256 it is 256 + u, so that 10 operations make 8 values.
 __device__ __forceinline__ void codes_to_f16(uint32_t w, const Steps& s, uint32_t* pairs) {
     const uint32_t lo = w << 2, hi = w >> 6;
-    pairs[0] = fma_f16x2((lo & 0x003c003cu) | 0x5c005c00u, s.s, s.off256);
-    pairs[1] = fma_f16x2((lo & 0x03c003c0u) | 0x4c004c00u, s.s, s.off16);
-    pairs[2] = fma_f16x2((hi & 0x003c003cu) | 0x5c005c00u, s.s, s.off256);
-    pairs[3] = fma_f16x2((hi & 0x03c003c0u) | 0x4c004c00u, s.s, s.off16);
+    pairs[0] = fma_f16x2(masked_or(lo, 0x003c003cu, 0x5c005c00u), s.s, s.off256);
+    pairs[1] = fma_f16x2(masked_or(lo, 0x03c003c0u, 0x4c004c00u), s.s, s.off16);
+    pairs[2] = fma_f16x2(masked_or(hi, 0x003c003cu, 0x5c005c00u), s.s, s.off256);
+    pairs[3] = fma_f16x2(masked_or(hi, 0x03c003c0u, 0x4c004c00u), s.s, s.off16);
 }
 
 struct SeqView {

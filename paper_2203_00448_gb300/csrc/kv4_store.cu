@@ -30,12 +30,86 @@ __device__ __forceinline__ int scale_byte(float a) {
     return min(byte, kMostScale);
 }
 
-// x / s to the nearest whole number, ties to the even one, of -7 .. 7; as a code.  inverse: 1 / s rounded.
-__device__ __forceinline__ uint32_t code_of(float x, float s, float inverse) {
-    float n = rintf(x * inverse);
-    const float rest = fmaf(-n, s, x), off = fabsf(rest), half = 0.5f * s;  // exact: the product may lie beside a border
-    if (off > half || (off == half && ((int)n & 1))) n += copysignf(1.f, rest);
-    return (uint32_t)((int)fminf(fmaxf(n, -7.f), 7.f) + 8);
+// 8 values of a token as they are in memory.
+template <typename T>
+struct Raw {
+    uint4 w[sizeof(T) / 2];
+};
+template <typename T>
+__device__ __forceinline__ Raw<T> load_raw(const T* p, bool wide) {
+    Raw<T> r;
+    if (wide) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = *(reinterpret_cast<const uint4*>(p) + i);
+    } else {
+        T* e = reinterpret_cast<T*>(&r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = p[i];
+    }
+    return r;
+}
+
+constexpr float kWhole = 12582912.f;  // 1.5 * 2^23: a sum with it is a whole number in its low bits
+// x / s to the nearest whole number, ties to the even one, in the low bits.  For values of 16 bits a quotient that is no tie
+// is further from one than 2^-15 of itself, so products with the neighbours of 1 / s on either side agree unless it is a
+// tie, and then they are the two that it lies between.
+__device__ __forceinline__ uint32_t nearest16(float x, float below, float above) {
+    const uint32_t lo = __float_as_uint(fmaf(x, below, kWhole)), hi = __float_as_uint(fmaf(x, above, kWhole));
+    return lo & 1 ? hi : lo;
+}
+// ... of 32 bits: what the product leaves of x is exact and says whether it was off.
+__device__ __forceinline__ uint32_t nearest32(float x, float s, float inverse) {
+    const float y = fmaf(x, inverse, kWhole), rest = fmaf(-(y - kWhole), s, x);
+    const uint32_t bits = __float_as_uint(y);
+    // half a step, or the number before it where a tie has to move from an odd number
+    const float most = __uint_as_float(__float_as_uint(0.5f * s) - (bits & 1));
+    return fabsf(rest) > most ? bits + (rest < 0.f ? ~0u : 1u) : bits;
+}
+
+// Codes of 8 values of a token (32 of 4 neighbouring lanes share a scale) and their scale's byte; fine: becomes false if some
+// value is not finite or too large.
+template <typename T>
+__device__ __forceinline__ uint32_t quantise(const Raw<T>& raw, int& byte, bool& fine) {
+    float v[8], most = 0.f;
+    const T* e = reinterpret_cast<const T*>(&raw);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = to_f32(e[i]);
+    if (sizeof(T) == 2) {
+        // magnitudes as the integers that their bits are, two at a time; infinities and NaN come out on top
+        const uint32_t m = __vmaxu2(__vmaxu2(raw.w[0].x & 0x7fff7fffu, raw.w[0].y & 0x7fff7fffu),
+                                    __vmaxu2(raw.w[0].z & 0x7fff7fffu, raw.w[0].w & 0x7fff7fffu));
+        const uint16_t bits = (uint16_t)max(m & 0xffffu, m >> 16);
+        most = to_f32(*reinterpret_cast<const T*>(&bits));
+    } else {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+        most = __uint_as_float(m);
+    }
+    if (!(most <= kMost)) {
+        fine = false;
+        most = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            v[i] = v[i] != v[i] ? 0.f : fminf(fmaxf(v[i], -kMost), kMost);
+            most = fmaxf(most, fabsf(v[i]));
+        }
+    }
+    most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
+    most = fmaxf(most, __shfl_xor_sync(~0u, most, 2));
+    byte = scale_byte(most);
+    const float s = scale_value(byte), inverse = byte ? __fdiv_rn(1.f, s) : 0.f;
+    const float below = __uint_as_float(max(__float_as_uint(inverse), 1u) - 1), above = __uint_as_float(__float_as_uint(inverse) + (byte ? 1 : 0));
+    uint32_t n[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) n[i] = sizeof(T) == 2 ? nearest16(v[i], below, above) : nearest32(v[i], s, inverse);
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t two = __vmins2(__vmaxs2(__byte_perm(n[i], n[i + 4], 0x5410), 0xfff9fff9u), 0x00070007u);
+        w |= (two & 0x000f000fu) << (4 * i);
+    }
+    return w ^ 0x88888888u;  // two's complement of 4 bits, 8 more
 }
 
 // A warp stores tokens [from, past) (slots of a granule) of one head and array: a lane 8 values of a token a step.
@@ -43,49 +117,38 @@ __device__ __forceinline__ uint32_t code_of(float x, float s, float inverse) {
 template <typename T, int D, bool kValues>
 __device__ __forceinline__ bool store_granule(const T* x, int64_t stride, bool wide, int from, int past, uint8_t* bytes) {
     constexpr int kLanes = D / 8, kTokens = 32 / kLanes;  // lanes of a token, tokens a step
+    constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;        // steps whose values are on their way together
     const int lane = threadIdx.x % 32, d = lane % kLanes * 8;
     bool fine = true;
-#pragma unroll 4
-    for (int t0 = from / kTokens * kTokens; t0 < past; t0 += kTokens) {
-        const int t = t0 + lane / kLanes;
-        const bool mine = t >= from && t < past;
-        float v[8];
-        if (mine) load_values<T, 8>(x + (t - from) * stride + d, wide, v);
-        float most = 0.f;
-        bool odd = false;
+    x += d - from * stride;
+    for (int t0 = from / kTokens * kTokens; t0 < past; t0 += kAhead * kTokens) {
+        Raw<T> raw[kAhead] = {};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (!mine) v[i] = 0.f;
-            odd |= !(fabsf(v[i]) <= kMost);
-        }
-        if (odd) {
-            fine = false;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = v[i] != v[i] ? 0.f : fminf(fmaxf(v[i], -kMost), kMost);
+        for (int e = 0; e < kAhead; ++e) {
+            const int t = t0 + e * kTokens + lane / kLanes;
+            if (t >= from && t < past) raw[e] = load_raw(x + t * stride, wide);
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(v[i]));
-        most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
-        most = fmaxf(most, __shfl_xor_sync(~0u, most, 2));
-        const int byte = scale_byte(most);
-        const float s = scale_value(byte), inverse = byte ? __fdiv_rn(1.f, s) : 0.f;
-        uint32_t w = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w |= code_of(v[i], s, inverse) << (4 * i);
-        uint8_t* const scale = bytes + 16 * D + (kValues ? value4_scale<D>(t, d) : key4_scale<D>(t, d));
-        if (mine && lane % 4 == 0) *scale = (uint8_t)byte;
-        if (!kValues) {
-            if (mine) *reinterpret_cast<uint32_t*>(bytes + key4_byte<D>(t, d)) = w;
-        } else {
-            // the neighbouring token's lane has the other half of either word
-            const uint32_t other = __shfl_xor_sync(~0u, t % 2 ? w & 0xffff : w >> 16, kLanes);
-            uint8_t* const at = bytes + value4_byte<D>(t, d);  // (of its half of the first word)
-            if (mine && (t ^ 1) >= from && (t ^ 1) < past) {
-                if (t % 2) *reinterpret_cast<uint32_t*>(at + 2) = other | (w & 0xffff0000u);
-                else *reinterpret_cast<uint32_t*>(at) = (w & 0xffffu) | other << 16;
-            } else if (mine) {
-                *reinterpret_cast<uint16_t*>(at) = (uint16_t)w;
-                *reinterpret_cast<uint16_t*>(at + 4) = (uint16_t)(w >> 16);
+        for (int e = 0; e < kAhead; ++e) {
+            if (t0 + e * kTokens >= past) break;
+            const int t = t0 + e * kTokens + lane / kLanes;
+            const bool mine = t >= from && t < past;
+            int byte;
+            const uint32_t w = quantise<T>(raw[e], byte, fine);
+            if (mine && lane % 4 == 0) bytes[16 * D + (kValues ? value4_scale<D>(t, d) : key4_scale<D>(t, d))] = (uint8_t)byte;
+            if (!kValues) {
+                if (mine) *reinterpret_cast<uint32_t*>(bytes + key4_byte<D>(t, d)) = w;
+            } else {
+                // the neighbouring token's lane has the other half of either word
+                const uint32_t other = __shfl_xor_sync(~0u, t % 2 ? w & 0xffff : w >> 16, kLanes);
+                uint8_t* const at = bytes + value4_byte<D>(t, d);  // (of its half of the first word)
+                if (mine && (t ^ 1) >= from && (t ^ 1) < past) {
+                    if (t % 2) *reinterpret_cast<uint32_t*>(at + 2) = other | (w & 0xffff0000u);
+                    else *reinterpret_cast<uint32_t*>(at) = (w & 0xffffu) | other << 16;
+                } else if (mine) {
+                    *reinterpret_cast<uint16_t*>(at) = (uint16_t)w;
+                    *reinterpret_cast<uint16_t*>(at + 4) = (uint16_t)(w >> 16);
+                }
             }
         }
     }

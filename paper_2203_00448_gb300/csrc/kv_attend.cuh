@@ -15,6 +15,10 @@ constexpr long long kKvSpinCycles = 1ll << 31;  // about a second; a longer wait
 // Weights are kept as 2^kLift times their value under the running maximum: as f16 they have
 // all 11 bits down to 2^-28 of the largest, one less for each power of two below, none under 2^-38.
 constexpr float kLift = 14.f;
+// k_kv_attend_few over 4 bits keeps its reference until a score passes it by 2^5, so weights are 2^10 times theirs: 11 bits
+// down to 2^-24 of the reference.
+constexpr float kFewGrow = 5.f;
+constexpr float lift_of(int bits) { return bits == 8 ? kLift : 10.f; }
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 

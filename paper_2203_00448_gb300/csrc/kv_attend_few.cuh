@@ -38,8 +38,8 @@ namespace {
 // share for the four schedulers: 12 of D = 128 with 16 rows spill (64 ragged contexts 127 -> 153 us, 10 160), 12 instead of
 // 16 of D = 64 with 8 rows take 66 for 60 us. 8 with 3 granules for 12 with 2: 164 for 170 us over two of 262,144 tokens,
 // but 103 for 97 over 64 ragged ones; 3 granules for 2 never paid otherwise (130 for 127).
-constexpr int few_warps(int, int d, int nt) { return d == 128 ? (nt == 1 ? 12 : 8) : (nt == 1 ? 16 : 12); }
-constexpr int few_stages(int bits) { return bits == 8 ? 2 : 4; }
+constexpr int few_warps(int d, int nt) { return d == 128 ? (nt == 1 ? 12 : 8) : (nt == 1 ? 16 : 12); }
+constexpr int kFewStages = 2;
 constexpr int short_warps(int nt) { return nt == 1 ? 16 : 8; }
 constexpr int kFewRows = 16;  // most rows of a sequence and head
 constexpr int kJoinThreads = 256;  // k_kv_join of D = 128 keeps 16 bytes a thread in memory for it (48 registers), of 64 8 bytes
@@ -60,13 +60,20 @@ __device__ __forceinline__ int64_t seq_units(const AttendArgs& a, int b) {
 // A position on the line of units.
 struct Cursor {
     int b, lo, hi, g;    // sequence, its granules, the granule
+    int col, in_block;   // g as a column of the table and a granule of its block
     int slots, slot;     // tiles x heads, tile * heads + head
+    int tile, head;
     int64_t row;         // first row of the token arrays
     int n, len;          // the call's tokens, tokens held
-    __device__ __forceinline__ void seek(int lo_, int hi_, int slots_, int64_t unit) {
+    __device__ __forceinline__ void at(const AttendArgs& a, int gran) {
+        const int per = a.c.block_tokens / kGranule;
+        g = gran, col = gran / per, in_block = gran - col * per;
+    }
+    __device__ __forceinline__ void seek(const AttendArgs& a, int lo_, int hi_, int slots_, int64_t unit) {
         lo = lo_, hi = hi_, slots = slots_;
         slot = (int)quotient(unit, hi - lo);
-        g = lo + (int)(unit - (int64_t)slot * (hi - lo));
+        tile = slot / a.c.n_heads, head = slot - tile * a.c.n_heads;
+        at(a, lo + (int)(unit - (int64_t)slot * (hi - lo)));
     }
 };
 template <int kRows>
@@ -78,20 +85,25 @@ __device__ __forceinline__ bool enter(const AttendArgs& a, Cursor& c, int64_t un
     const int slots = a.c.n_heads * seq_tiles<kRows>(a, s);
     if (hi <= lo || slots == 0) return false;
     c.row = s.lo, c.n = s.n, c.len = s.len;
-    c.seek(lo, hi, slots, unit);
+    c.seek(a, lo, hi, slots, unit);
     return true;
 }
 template <int kRows>
 __device__ __forceinline__ void next(const AttendArgs& a, Cursor& c) {
-    if (++c.g < c.hi) return;
-    c.g = c.lo;
-    if (++c.slot < c.slots) return;
+    if (++c.g < c.hi) {
+        if (++c.in_block == a.c.block_tokens / kGranule) c.in_block = 0, ++c.col;
+        return;
+    }
+    if (++c.slot < c.slots) {
+        if (++c.head == a.c.n_heads) c.head = 0, ++c.tile;
+        return c.at(a, c.lo);
+    }
     do ++c.b;
     while (c.b < a.bt.n_seqs && !enter<kRows>(a, c, 0));
 }
 __device__ __forceinline__ int page_of(const AttendArgs& a, const Cursor& c) {
-    const int p = __ldg(a.bt.table + (int64_t)c.b * a.bt.max_blocks + c.g / (a.c.block_tokens / kGranule));
-    return p >= 0 && p < a.c.n_blocks ? p : 0;  // k_kv_join reports it; nothing outside the pool is read
+    const int p = __ldg(a.bt.table + (int64_t)c.b * a.bt.max_blocks + c.col);
+    return (uint32_t)p < (uint32_t)a.c.n_blocks ? p : 0;  // k_kv_join reports it; nothing outside the pool is read
 }
 
 __device__ __forceinline__ void mma(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -116,11 +128,14 @@ struct Tile {
     float o[NT][D / 16][4];
     int see_lo[NT][2], see_hi[NT][2];  // positions that the column's row sees
     int last;                          // stored bytes from this position on mean nothing
+    int all_lo, all_hi;                // positions that every row sees
+    // 4 bits: weights are 2^(score * unit + off); a score above limit moves the reference
+    float off[NT][2], limit[NT][2];
 
     // rows: of the sequence and head, at least 1; row: the sequence's first in the token arrays
     __device__ __forceinline__ void begin(const AttendArgs& a, int64_t row, int rows, int len, int n, int head, int tile) {
         const int lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
-        last = 0;
+        last = all_lo = 0, all_hi = len;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int r = tile * 8 * NT + nt * 8 + g, there = min(r, rows - 1);
@@ -171,29 +186,33 @@ struct Tile {
                 see_hi[nt][k] = col < rows && a.causal ? min(len, pos + 1) : len;
                 see_lo[nt][k] = col < rows && a.window > 0 ? pos - a.window + 1 : 0;
                 last = max(last, see_hi[nt][k]);
-                top[nt][k] = -INFINITY, sum[nt][k] = 0.f;
+                all_lo = max(all_lo, see_lo[nt][k]), all_hi = min(all_hi, see_hi[nt][k]);
+                top[nt][k] = limit[nt][k] = -INFINITY, sum[nt][k] = off[nt][k] = 0.f;
+                if (kBits == 4) unit[nt][k] = fmaxf(unit[nt][k], 0x1p-126f);  // not 0: what is not seen stays -inf
             }
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
         }
         last = __reduce_max_sync(~0u, last);
+        if (kBits == 4) all_lo = __reduce_max_sync(~0u, all_lo), all_hi = __reduce_min_sync(~0u, all_hi);
     }
 
-    // The granule at position base: its keys kb and values vb as stored, and their scales as stored (8 bits; of 4 they lie
-    // with the codes).
-    __device__ __forceinline__ void add(const uint8_t* kb, const uint8_t* vb, float ks, float stored_vs, int base) {
+    // The granule at position base: its keys kb and values vb as stored, and their scales as stored.
+    __device__ __forceinline__ void add8(const uint8_t* kb, const uint8_t* vb, float ks, float stored_vs, int base) {
         float s[NT][2][4] = {};
-        if constexpr (kBits == 8) scores8(kb, s);
-        else scores4(kb, s);
+        scores8(kb, s);
+        const float vs = value_scale(stored_vs);
         uint32_t p[NT][2][2];
-        if constexpr (kBits == 8) {
-            const float vs = value_scale(stored_vs);
-            weigh(s, ks, log2f(vs), __fdiv_rn(1.f, vs), base, p);
-            values8(vb, stored_vs < kLeastValueScale ? 0 : last, base, p);
-        } else {
-            weigh(s, 1.f, 0.f, 1.f, base, p);
-            values4(vb, base, p);
-        }
+        weigh(s, ks, log2f(vs), __fdiv_rn(1.f, vs), base, p);
+        values8(vb, stored_vs < kLeastValueScale ? 0 : last, base, p);
+    }
+    // ... of 4 bits, whose scales lie with the codes.
+    __device__ __forceinline__ void add4(const uint8_t* kb, const uint8_t* vb, int base) {
+        float s[NT][2][4] = {};
+        scores4(kb, s);
+        uint32_t p[NT][2][2];
+        weigh4(s, base, p);
+        values4(vb, base, p);
     }
 
     // Of the 32 tokens, product row r of 16 is token token_of(r): of 8 bits the order in which a lane's 4 stored value
@@ -300,6 +319,70 @@ struct Tile {
         }
     }
 
+    // ... of 4 bits: no scales are left, and a reference stays until a score passes it by 2^kFewGrow, which weights have
+    // room for: one vote a granule in the place of a maximum over lanes.
+    __device__ __forceinline__ void weigh4(float (&s)[NT][2][4], int base, uint32_t (&p)[NT][2][2]) {
+        const int lane = threadIdx.x % 32, g = lane / 4;
+        if (base < all_lo || base + kGranule > all_hi) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int j = base + i / 2 * 16 + token_of(g, i % 2);
+                        if (!(j < see_hi[nt][k] && j >= see_lo[nt][k])) s[nt][i / 2][i % 2 * 2 + k] = -INFINITY;
+                    }
+        }
+        float most[NT][2];
+        bool over = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                most[nt][k] = fmaxf(fmaxf(s[nt][0][k], s[nt][0][2 + k]), fmaxf(s[nt][1][k], s[nt][1][2 + k]));
+                over |= most[nt][k] > limit[nt][k];
+            }
+        if (__any_sync(~0u, over)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    float x = most[nt][k];
+                    x = fmaxf(x, __shfl_xor_sync(~0u, x, 4));
+                    x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
+                    x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
+                    if (x > limit[nt][k]) {
+                        const float now = x * unit[nt][k], fade = exp2_approx(top[nt][k] - now);
+                        top[nt][k] = now, off[nt][k] = lift_of(4) - now;
+                        limit[nt][k] = __fdiv_rn(now + kFewGrow, unit[nt][k]);
+                        sum[nt][k] *= fade;
+#pragma unroll
+                        for (int i = 0; i < D / 16; ++i) o[nt][i][k] *= fade, o[nt][i][2 + k] *= fade;
+                    }
+                }
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                float part[2] = {};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float& x = s[nt][i / 2][i % 2 * 2 + k];
+                    x = exp2_approx(fmaf(x, unit[nt][k], off[nt][k]));
+                    part[i % 2] += x;
+                }
+                sum[nt][k] += part[0] + part[1];
+            }
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                p[nt][m][0] = transposed(pack_f16(s[nt][m][0], s[nt][m][1]));
+                p[nt][m][1] = transposed(pack_f16(s[nt][m][2], s[nt][m][3]));
+            }
+        }
+    }
+
     // Values from position `meant` on are zeros.
     __device__ __forceinline__ void values8(const uint8_t* vb, int meant, int base, const uint32_t (&p)[NT][2][2]) {
         const int lane = threadIdx.x % 32, t = lane % 4;
@@ -375,9 +458,35 @@ struct Tile {
     }
 };
 
+// Copies a granule's keys and values (of kBytes each) into shared memory, 16 bytes a lane and step.
+template <int kBytes>
+struct GranuleCopy {
+    static constexpr int kSteps = kBytes / 512, kRest = kBytes % 512;  // the rest of both in one step
+    static_assert(kRest <= 256, "a lane has one of the rest");
+    const uint8_t *k, *v, *rest;  // this lane's of the pools' first granule
+    int rest_to;
+    __device__ __forceinline__ explicit GranuleCopy(const mp_kv_cache& c) {
+        const int lane = threadIdx.x % 32;
+        const bool values = lane >= kRest / 16;
+        const int o = kSteps * 512 + (lane - (values ? kRest / 16 : 0)) * 16;
+        k = c.k + lane * 16, v = c.v + lane * 16, rest = (values ? c.v : c.k) + o, rest_to = (values ? kBytes : 0) + o;
+    }
+    // to: shared address of the stage; at: the granule's place in either pool
+    __device__ __forceinline__ void operator()(uint32_t to, int64_t at) const {
+        const int lane = threadIdx.x % 32;
+        const uint32_t mine = to + lane * 16;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(mine + i * 512), "l"(k + at + i * 512) : "memory");
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(mine + kBytes + i * 512), "l"(v + at + i * 512) : "memory");
+        }
+        if (lane < kRest / 8) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + rest_to), "l"(rest + at) : "memory");
+    }
+};
+
 template <typename T, int D, int NT, int kBits>
-__global__ void __launch_bounds__(few_warps(kBits, D, NT) * 32, 1) k_kv_attend_few(AttendArgs a, FewWork work) {
-    constexpr int kFewWarps = few_warps(kBits, D, NT), kFewStages = few_stages(kBits);
+__global__ void __launch_bounds__(few_warps(D, NT) * 32, 1) k_kv_attend_few(AttendArgs a, FewWork work) {
+    constexpr int kFewWarps = few_warps(D, NT);
     constexpr int kRows = 8 * NT;
     constexpr int kBytes = granule_bytes(kBits, D);  // of either array
     extern __shared__ __align__(128) uint8_t dyn[];
@@ -459,13 +568,28 @@ __global__ void __launch_bounds__(few_warps(kBits, D, NT) * 32, 1) k_kv_attend_f
     Cursor ahead = cur;
     int64_t issued = u0;
     int page_ahead = page_of(a, ahead);
+    const GranuleCopy<kBytes> copy(a.c);  // of 4 bits
+    const uint32_t first_stage = smem_addr(ring), last_stage = first_stage + (kFewStages - 1) * 2 * kBytes;
+    uint32_t next_stage = first_stage;
+    int to_come = (int)(u1 - u0);
     auto issue = [&]() {  // the next unit's bytes into its stage
+        if constexpr (kBits == 4) {
+            if (to_come > 0) {
+                copy(next_stage, block_byte<kBits>(a.c, page_ahead, ahead.head) + ahead.in_block * kBytes);
+                next_stage = next_stage == last_stage ? first_stage : next_stage + 2 * kBytes;
+                if (--to_come > 0) {
+                    next<kRows>(a, ahead);
+                    page_ahead = page_of(a, ahead);
+                }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            return;
+        }
         if (issued >= u1) return;
         const int st = (int)((issued - u0) % kFewStages);
-        const int64_t at = block_byte<kBits>(a.c, page_ahead, ahead.slot % a.c.n_heads) +
-                           (int64_t)(ahead.g % (a.c.block_tokens / kGranule)) * kBytes;
+        const int64_t at = block_byte<kBits>(a.c, page_ahead, ahead.head) + ahead.in_block * kBytes;
         if (lane == 0) {
-            ring_page[st] = page_ahead;
+            if (kBits == 8) ring_page[st] = page_ahead;
             mbar_expect(&bar[st], 2 * kBytes);
             if (!test_held(a, issued)) {
                 bulk_load(ring + st * 2 * kBytes, a.c.k + at, kBytes, &bar[st]);
@@ -487,27 +611,36 @@ __global__ void __launch_bounds__(few_warps(kBits, D, NT) * 32, 1) k_kv_attend_f
 
     for (int left = (int)(u1 - u0); left > 0 && !up;) {
         // one (sequence, tile, head) or what this warp has of it
-        const int head = cur.slot % a.c.n_heads, tile = cur.slot / a.c.n_heads;
+        const int head = cur.head, tile = cur.tile;
         const int rows = cur.n * a.group, units = min(cur.hi - cur.g, left);
         const bool whole = units == cur.hi - cur.lo;
         const bool first = done == 0;
         left -= units;
         x.begin(a, cur.row, rows, cur.len, cur.n, head, tile);
+        if constexpr (kBits == 4) {
 #pragma unroll 1
-        for (int i = 0; i < units; ++i, ++done, ++cur.g) {
-            const int st = done % kFewStages;
-            if (!__all_sync(~0u, mbar_wait(&bar[st], (uint32_t)(done / kFewStages & 1)))) {
-                up = true;
-                break;
+            for (int i = 0; i < units; ++i, ++done, ++cur.g) {
+                asm volatile("cp.async.wait_group %0;" ::"n"(kFewStages - 1) : "memory");
+                __syncwarp();
+                const uint8_t* kv = ring + done % kFewStages * (2 * kBytes);
+                x.add4(kv, kv + kBytes, cur.g * kGranule);
+                __syncwarp();
+                issue();
             }
-            float ks = 1.f, vs = 1.f;
-            if constexpr (kBits == 8) {
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < units; ++i, ++done, ++cur.g) {
+                const int st = done % kFewStages;
+                if (!__all_sync(~0u, mbar_wait(&bar[st], (uint32_t)(done / kFewStages & 1)))) {
+                    up = true;
+                    break;
+                }
                 const int64_t sc = (int64_t)ring_page[st] * a.c.n_heads + head;
-                ks = __ldg(a.c.k_scale + sc), vs = __ldg(a.c.v_scale + sc);
+                const float ks = __ldg(a.c.k_scale + sc), vs = __ldg(a.c.v_scale + sc);
+                x.add8(ring + st * 2 * kBytes, ring + st * 2 * kBytes + kBytes, ks, vs, cur.g * kGranule);
+                __syncwarp();
+                issue();
             }
-            x.add(ring + st * 2 * kBytes, ring + st * 2 * kBytes + kBytes, ks, vs, cur.g * kGranule);
-            __syncwarp();
-            issue();
         }
         if (up) break;
 #pragma unroll
@@ -529,7 +662,7 @@ __global__ void __launch_bounds__(few_warps(kBits, D, NT) * 32, 1) k_kv_attend_f
                             dst[x.value_of(i, g, 1)] = from_f32<T>(x.o[nt][i][2 + k] * inv);
                         }
                         if (a.lse != nullptr && g == 0)
-                            a.lse[tok * a.q.n_heads + qh] = log_sum(m, kLift, l);
+                            a.lse[tok * a.q.n_heads + qh] = log_sum(m, lift_of(kBits), l);
                     }
                 } else {
                     // a warp leaves at most two parts: of what began before it or with it, and of
@@ -548,7 +681,7 @@ __global__ void __launch_bounds__(few_warps(kBits, D, NT) * 32, 1) k_kv_attend_f
                 }
             }
         --cur.g;
-        if (left > 0) next<kRows>(a, cur);
+        if (left > 0) next<kRows>(a, cur);  // (a new slot or sequence: it sets col and in_block, which no one read here)
     }
     if (up) {
         if (lane == 0) work.gave_up[w] = 1;
@@ -611,7 +744,11 @@ __global__ void __launch_bounds__(short_warps(NT) * 32, 1) k_kv_attend_short(Att
             if (gran == lo + wid) x.begin(a, s.lo, rows, s.len, s.n, head, tile);
             asm volatile("cp.async.wait_all;" ::: "memory");
             __syncwarp();
-            x.add(mine, mine + kBytes, ks, vs, gran * kGranule);
+            if constexpr (kBits == 8) {
+                x.add8(mine, mine + kBytes, ks, vs, gran * kGranule);
+            } else {
+                x.add4(mine, mine + kBytes, gran * kGranule);
+            }
             __syncwarp();
         }
         const bool any = lo + wid < hi;
@@ -653,7 +790,7 @@ __global__ void __launch_bounds__(short_warps(NT) * 32, 1) k_kv_attend_short(Att
             const float y[2] = {o0 * inv, o1 * inv};
             store_values<T, 2>(dst, a.wide_out, y);
             if (d == 0 && a.lse != nullptr)
-                a.lse[tok * a.q.n_heads + qh] = log_sum(top, kLift, sum);
+                a.lse[tok * a.q.n_heads + qh] = log_sum(top, lift_of(kBits), sum);
         }
         __syncthreads();
     }
@@ -744,7 +881,7 @@ __device__ void check_seq(const AttendArgs& a, const FewWork& few, bool late, in
 }
 
 // kPer warps a query row add up what several warps of k_kv_attend_few had of it.
-template <typename T, int D, int NT, int kPer>
+template <typename T, int D, int NT, int kPer, int kBits>
 __device__ void join_row(const AttendArgs& a, const FewWork& work, int64_t u, bool there) {
     constexpr int kRows = 8 * NT, kCols = D / 32, kAhead = 4;
     __shared__ float acc[kJoinThreads / 32][D + 2];
@@ -808,11 +945,11 @@ __device__ void join_row(const AttendArgs& a, const FewWork& work, int64_t u, bo
     for (int i = 0; i < kCols; ++i) o[i] *= inv;
     store_values<T, kCols>(dst + lane * kCols, a.wide_out, o);
     if (a.lse != nullptr && lane == 0)
-        a.lse[tok * a.q.n_heads + qh] = log_sum(top, kLift, l);
+        a.lse[tok * a.q.n_heads + qh] = log_sum(top, lift_of(kBits), l);
 }
 
 // After both kernels: what more than one CTA or warp had of a row, and the sequences' status.  kPer: warps a row.
-template <typename T, int D, int NT, int kPer>
+template <typename T, int D, int NT, int kPer, int kBits>
 __global__ void __launch_bounds__(kJoinThreads) k_kv_join(AttendArgs a, FewWork few, ManyWork many, JoinPlan plan) {
     after_previous();
     let_next_begin();
@@ -831,7 +968,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_kv_join(AttendArgs a, FewWork 
     const int64_t rows = (int64_t)a.bt.n_seqs * join_rows(a) * a.c.n_heads;
     for (int64_t u = (int64_t)cta * kRowsCta; u < rows; u += (int64_t)plan.row_ctas * kRowsCta) {
         const int64_t mine = u + threadIdx.x / 32 / kPer;
-        join_row<T, D, NT, kPer>(a, few, mine < rows ? mine : 0, mine < rows);
+        join_row<T, D, NT, kPer, kBits>(a, few, mine < rows ? mine : 0, mine < rows);
     }
 }
 
@@ -877,7 +1014,7 @@ template <int kBits>
 Layout layout(const mp_kv_cache& c, const mp_kv_batch& bt, int32_t group) {
     Layout l = {};
     const Route r = route<kBits>(c, bt, group, 0);
-    const size_t warps8 = few_warps(kBits, c.head_dim, 1), warps16 = few_warps(kBits, c.head_dim, 2);
+    const size_t warps8 = few_warps(c.head_dim, 1), warps16 = few_warps(c.head_dim, 2);
     auto take = [&](size_t bytes) {
         const size_t at = l.bytes;
         l.bytes += align_up(bytes);
@@ -911,10 +1048,10 @@ cudaError_t attend_as(const AttendArgs& a, const FewWork& few, const ManyWork& m
     plan.checks = std::min(a.bt.n_seqs, 1024);
     int64_t rows = 0;
     if (few.base != nullptr) {
-        constexpr size_t smem = (size_t)few_warps(kBits, D, NT) * few_stages(kBits) * 2 * granule_bytes(kBits, D);
+        constexpr size_t smem = (size_t)few_warps(D, NT) * kFewStages * 2 * granule_bytes(kBits, D);
         e = set_smem_limit((const void*)k_kv_attend_few<T, D, NT, kBits>, smem);
         if (e == cudaSuccess)
-            e = launch_close(k_kv_attend_few<T, D, NT, kBits>, kFewCtas, few_warps(kBits, D, NT) * 32, smem, stream, a, few);
+            e = launch_close(k_kv_attend_few<T, D, NT, kBits>, kFewCtas, few_warps(D, NT) * 32, smem, stream, a, few);
         if (e != cudaSuccess) return e;
         rows = (int64_t)a.bt.n_seqs * join_rows(a) * a.c.n_heads;
     }
@@ -926,14 +1063,14 @@ cudaError_t attend_as(const AttendArgs& a, const FewWork& few, const ManyWork& m
     // rows that are cut into many parts have a CTA each, whose warps share the parts (64 rows of 76 parts: 18 -> 5 us), the
     // others a warp (2,048 rows of two or three: 12 -> 7 us)
     constexpr int kWarps = kJoinThreads / 32;
-    const int64_t parts = kFewCtas * few_warps(kBits, D, NT) / ((int64_t)a.bt.n_seqs * a.c.n_heads);
+    const int64_t parts = kFewCtas * few_warps(D, NT) / ((int64_t)a.bt.n_seqs * a.c.n_heads);
     if (rows <= 8 * kFewCtas || parts > 12) {
         plan.row_ctas = (int)std::min<int64_t>(rows, 1 << 20);
-        return launch_close(k_kv_join<T, D, NT, kWarps>, plan.cuts + plan.checks + plan.row_ctas, kJoinThreads, 0, stream, a,
+        return launch_close(k_kv_join<T, D, NT, kWarps, kBits>, plan.cuts + plan.checks + plan.row_ctas, kJoinThreads, 0, stream, a,
                             few, many, plan);
     }
     plan.row_ctas = (int)std::min<int64_t>((rows + kWarps - 1) / kWarps, 1 << 20);
-    return launch_close(k_kv_join<T, D, NT, 1>, plan.cuts + plan.checks + plan.row_ctas, kJoinThreads, 0, stream, a, few, many,
+    return launch_close(k_kv_join<T, D, NT, 1, kBits>, plan.cuts + plan.checks + plan.row_ctas, kJoinThreads, 0, stream, a, few, many,
                         plan);
 }
 template <typename T, int D, int kBits>
