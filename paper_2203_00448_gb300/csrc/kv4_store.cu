@@ -19,14 +19,16 @@ __device__ __forceinline__ float scale_value(int byte) {
     return __half2float(__ushort_as_half((unsigned short)(byte << 7)));
 }
 
-// The byte of the least scale with a <= 7.5 s.
+// The byte of the least scale with a <= 7.5 s, a a value of type T.
+template <typename T>
 __device__ __forceinline__ int scale_byte(float a) {
-    const float least = a * (2.f / 15.f);
-    // what the bits below a scale's say is cut off; below 2^-14 steps are 2^-17
-    int byte = least < 0x1p-14f ? (int)(least * 0x1p17f) : (int)(__float_as_uint(least) >> 20) - (112 << 3);
-    // the product may be off by a rounding, and cutting off leaves a scale that is too small
-    if (7.5f * scale_value(byte) < a) ++byte;
-    if (7.5f * scale_value(byte) < a) ++byte;
+    // a little less than a / 7.5, so that a = 7.5 s does not come out above s; no other value of 16 bits is as near
+    float least = a * (2.f / 15.f * (1.f - 0x1p-18f));
+    // up to the next number of 4 significant bits, or, below 2^-14, to the next multiple of 2^-17
+    const bool small = least < 0x1p-14f;
+    if (small) least = __fadd_ru(least, 0x1p-14f);
+    int byte = (int)((__float_as_uint(least) + 0xfffffu) >> 20) - (small ? 113 << 3 : 112 << 3);
+    if (sizeof(T) == 4 && 7.5f * scale_value(byte) < a) ++byte;  // a value of 32 bits may be as near
     return min(byte, kMostScale);
 }
 
@@ -51,11 +53,10 @@ __device__ __forceinline__ Raw<T> load_raw(const T* p, bool wide) {
 
 constexpr float kWhole = 12582912.f;  // 1.5 * 2^23: a sum with it is a whole number in its low bits
 // x / s to the nearest whole number, ties to the even one, in the low bits.  For values of 16 bits a quotient that is no tie
-// is further from one than 2^-15 of itself, so products with the neighbours of 1 / s on either side agree unless it is a
-// tie, and then they are the two that it lies between.
+// is further from one than 2^-15 of itself, so products with numbers on either side of 1 / s (2^-21 of it away) agree, unless
+// it is a tie: then they are the two that it lies between, and the sum of both, an odd number of 25 bits, is rounded to even.
 __device__ __forceinline__ uint32_t nearest16(float x, float below, float above) {
-    const uint32_t lo = __float_as_uint(fmaf(x, below, kWhole)), hi = __float_as_uint(fmaf(x, above, kWhole));
-    return lo & 1 ? hi : lo;
+    return __float_as_uint(fmaf(x, below, kWhole) + fmaf(x, above, kWhole));
 }
 // ... of 32 bits: what the product leaves of x is exact and says whether it was off.
 __device__ __forceinline__ uint32_t nearest32(float x, float s, float inverse) {
@@ -97,9 +98,12 @@ __device__ __forceinline__ uint32_t quantise(const Raw<T>& raw, int& byte, bool&
     }
     most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
     most = fmaxf(most, __shfl_xor_sync(~0u, most, 2));
-    byte = scale_byte(most);
-    const float s = scale_value(byte), inverse = byte ? __fdiv_rn(1.f, s) : 0.f;
-    const float below = __uint_as_float(max(__float_as_uint(inverse), 1u) - 1), above = __uint_as_float(__float_as_uint(inverse) + (byte ? 1 : 0));
+    byte = scale_byte<T>(most);
+    const float s = scale_value(byte);
+    float inverse;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(inverse) : "f"(s));
+    if (byte == 0) inverse = 0.f;
+    const float below = inverse * (1.f - 0x1p-21f), above = inverse * (1.f + 0x1p-21f);
     uint32_t n[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) n[i] = sizeof(T) == 2 ? nearest16(v[i], below, above) : nearest32(v[i], s, inverse);
@@ -112,27 +116,29 @@ __device__ __forceinline__ uint32_t quantise(const Raw<T>& raw, int& byte, bool&
     return w ^ 0x88888888u;  // two's complement of 4 bits, 8 more
 }
 
-// A warp stores tokens [from, past) (slots of a granule) of one head and array: a lane 8 values of a token a step.
-// x: the first of them.  False if some value was not finite or too large.
-template <typename T, int D, bool kValues>
-__device__ __forceinline__ bool store_granule(const T* x, int64_t stride, bool wide, int from, int past, uint8_t* bytes) {
+// A warp stores tokens [from, past) (slots of a granule; all of them, from wide rows, with kAll) of one head and array: a
+// lane 8 values of a token a step.  x: the first of them.  False if some value was not finite or too large.
+template <typename T, int D, bool kValues, bool kAll>
+__device__ __forceinline__ bool store_tokens(const T* x, int64_t stride, bool wide, int from, int past, uint8_t* bytes) {
     constexpr int kLanes = D / 8, kTokens = 32 / kLanes;  // lanes of a token, tokens a step
     constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;        // steps whose values are on their way together
     const int lane = threadIdx.x % 32, d = lane % kLanes * 8;
     bool fine = true;
+    if (kAll) from = 0, past = kGranule;
     x += d - from * stride;
+#pragma unroll 1
     for (int t0 = from / kTokens * kTokens; t0 < past; t0 += kAhead * kTokens) {
         Raw<T> raw[kAhead] = {};
 #pragma unroll
         for (int e = 0; e < kAhead; ++e) {
             const int t = t0 + e * kTokens + lane / kLanes;
-            if (t >= from && t < past) raw[e] = load_raw(x + t * stride, wide);
+            if (kAll || (t >= from && t < past)) raw[e] = load_raw(x + t * stride, kAll || wide);
         }
 #pragma unroll
         for (int e = 0; e < kAhead; ++e) {
-            if (t0 + e * kTokens >= past) break;
+            if (!kAll && t0 + e * kTokens >= past) break;
             const int t = t0 + e * kTokens + lane / kLanes;
-            const bool mine = t >= from && t < past;
+            const bool mine = kAll || (t >= from && t < past);
             int byte;
             const uint32_t w = quantise<T>(raw[e], byte, fine);
             if (mine && lane % 4 == 0) bytes[16 * D + (kValues ? value4_scale<D>(t, d) : key4_scale<D>(t, d))] = (uint8_t)byte;
@@ -142,7 +148,7 @@ __device__ __forceinline__ bool store_granule(const T* x, int64_t stride, bool w
                 // the neighbouring token's lane has the other half of either word
                 const uint32_t other = __shfl_xor_sync(~0u, t % 2 ? w & 0xffff : w >> 16, kLanes);
                 uint8_t* const at = bytes + value4_byte<D>(t, d);  // (of its half of the first word)
-                if (mine && (t ^ 1) >= from && (t ^ 1) < past) {
+                if (kAll || (mine && (t ^ 1) >= from && (t ^ 1) < past)) {
                     if (t % 2) *reinterpret_cast<uint32_t*>(at + 2) = other | (w & 0xffff0000u);
                     else *reinterpret_cast<uint32_t*>(at) = (w & 0xffffu) | other << 16;
                 } else if (mine) {
@@ -153,6 +159,12 @@ __device__ __forceinline__ bool store_granule(const T* x, int64_t stride, bool w
         }
     }
     return fine;
+}
+
+template <typename T, int D, bool kValues>
+__device__ __forceinline__ bool store_granule(const T* x, int64_t stride, bool wide, int from, int past, uint8_t* bytes) {
+    return wide && past - from == kGranule ? store_tokens<T, D, kValues, true>(x, stride, true, 0, kGranule, bytes)
+                                           : store_tokens<T, D, kValues, false>(x, stride, wide, from, past, bytes);
 }
 
 // One granule, head and array of a sequence: j counts the granules that the call touches.  False if the table or a value is
@@ -215,37 +227,52 @@ __device__ __forceinline__ void put8(T* p, bool wide, const uint32_t (&pairs)[4]
     store_values<T, 8>(p, wide, x);
 }
 // A warp reads a granule's tokens [from, past) of one head back, 8 values of a token (of two tokens, for values) a lane
-// and step.  x: where the granule's first token goes.
+// and step; four steps, 8 tokens apart, have their scales in one word and their codes on the way together.  x: where the granule's first
+// token goes.
 template <typename T, int D>
 __device__ __forceinline__ void read_keys(const uint8_t* bytes, int from, int past, T* x, int64_t stride, bool wide) {
     constexpr int kLanes = D / 8, kTokens = 32 / kLanes;
     const int lane = threadIdx.x % 32, d = lane % kLanes * 8;
-#pragma unroll 4
-    for (int t0 = from / kTokens * kTokens; t0 < past; t0 += kTokens) {
-        const int t = t0 + lane / kLanes;
-        const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(bytes + key4_byte<D>(t, d)));
-        const uint32_t s = __ldg(bytes + 16 * D + key4_scale<D>(t, d));
-        uint32_t pairs[4];
-        codes_to_f16(w, steps_of(s * 0x00800080u), pairs);
-        if (t >= from && t < past) put8(x + t * stride + d, wide, pairs);
+    x += d;
+#pragma unroll(8 / kTokens >= 4 ? 2 : 1)
+    for (int t0 = 0; t0 < 8; t0 += kTokens) {
+        const int t1 = t0 + lane / kLanes;
+        const uint32_t scales = __ldg(reinterpret_cast<const uint32_t*>(bytes + 16 * D + key4_scale<D>(t1, d)));
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = __ldg(reinterpret_cast<const uint32_t*>(bytes + key4_byte<D>(t1 + 8 * e, d)));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int t = t1 + 8 * e;
+            uint32_t pairs[4];
+            codes_to_f16(w[e], steps_of((scales >> (8 * e) & 0xff) * 0x00800080u), pairs);
+            if (t >= from && t < past) put8(x + t * stride, wide, pairs);
+        }
     }
 }
 template <typename T, int D>
 __device__ __forceinline__ void read_values(const uint8_t* bytes, int from, int past, T* x, int64_t stride, bool wide) {
     constexpr int kLanes = D / 8, kTokens = 2 * (32 / kLanes);
     const int lane = threadIdx.x % 32, d = lane % kLanes * 8;
-#pragma unroll 4
-    for (int t0 = from / kTokens * kTokens; t0 < past; t0 += kTokens) {
-        const int t = t0 + lane / kLanes * 2;
-        const uint2 w = __ldg(reinterpret_cast<const uint2*>(bytes + value4_byte<D>(t, d)));
-        const uint32_t s = __ldg(reinterpret_cast<const uint16_t*>(bytes + 16 * D + value4_scale<D>(t, d)));
-        const Steps steps = steps_of(__byte_perm(s, 0, 0x4140) << 7);
-        uint32_t a[4], b[4], lo[4], hi[4];
-        codes_to_f16(w.x, steps, a), codes_to_f16(w.y, steps, b);
+    x += d;
+#pragma unroll 1
+    for (int t0 = 0; t0 < 8; t0 += kTokens) {
+        const int t1 = t0 + lane / kLanes * 2;
+        const uint2 scales = __ldg(reinterpret_cast<const uint2*>(bytes + 16 * D + value4_scale<D>(t1, d)));
+        uint2 w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) lo[i] = __byte_perm(a[i], b[i], 0x5410), hi[i] = __byte_perm(a[i], b[i], 0x7632);
-        if (t >= from && t < past) put8(x + t * stride + d, wide, lo);
-        if (t + 1 >= from && t + 1 < past) put8(x + (t + 1) * stride + d, wide, hi);
+        for (int e = 0; e < 4; ++e) w[e] = __ldg(reinterpret_cast<const uint2*>(bytes + value4_byte<D>(t1 + 8 * e, d)));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int t = t1 + 8 * e;
+            const Steps steps = steps_of(__byte_perm(e < 2 ? scales.x : scales.y, 0, e % 2 ? 0x4342 : 0x4140) << 7);
+            uint32_t a[4], b[4], lo[4], hi[4];
+            codes_to_f16(w[e].x, steps, a), codes_to_f16(w[e].y, steps, b);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) lo[i] = __byte_perm(a[i], b[i], 0x5410), hi[i] = __byte_perm(a[i], b[i], 0x7632);
+            if (t >= from && t < past) put8(x + t * stride, wide, lo);
+            if (t + 1 >= from && t + 1 < past) put8(x + (t + 1) * stride, wide, hi);
+        }
     }
 }
 
