@@ -25,27 +25,36 @@ struct ExtendArgs {
 
 __device__ __forceinline__ int blocks_of(int tokens, int block) { return (tokens + block - 1) / block; }
 
-// Sum over the threads before this one; total: over all.
-__device__ int64_t scan(int64_t mine, int64_t* smem, int64_t& total) {
+// Rows, and blocks that come back and are needed.
+struct Sums {
+    int64_t rows, back, need;
+    __device__ __forceinline__ void add(const Sums& x) { rows += x.rows, back += x.back, need += x.need; }
+};
+__device__ __forceinline__ Sums shuffled(const Sums& x, int lane) {
+    return {__shfl_sync(~0u, x.rows, lane), __shfl_sync(~0u, x.back, lane), __shfl_sync(~0u, x.need, lane)};
+}
+__device__ __forceinline__ Sums scan_warp(Sums x) {
+    const int lane = threadIdx.x % 32;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const Sums y = {__shfl_up_sync(~0u, x.rows, o), __shfl_up_sync(~0u, x.back, o), __shfl_up_sync(~0u, x.need, o)};
+        if (lane >= o) x.add(y);
+    }
+    return x;
+}
+// Sums over the threads before this one; total: over all.
+__device__ Sums scan(const Sums& mine, Sums* smem, Sums& total) {
     const int lane = threadIdx.x % 32, wid = threadIdx.x / 32;
-    int64_t sum = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int64_t y = __shfl_up_sync(~0u, sum, o);
-        if (lane >= o) sum += y;
-    }
+    const Sums x = scan_warp(mine);
     __syncthreads();  // smem's last use
-    if (lane == 31) smem[wid] = sum;
+    if (lane == 31) smem[wid] = x;
     __syncthreads();
-    int64_t w = smem[lane];
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int64_t y = __shfl_up_sync(~0u, w, o);
-        if (lane >= o) w += y;
-    }
-    total = __shfl_sync(~0u, w, 31);
-    const int64_t base = __shfl_sync(~0u, w, wid) - __shfl_sync(~0u, sum, 31);
-    return base + sum - mine;
+    const Sums w = scan_warp(smem[lane]);
+    total = shuffled(w, 31);
+    Sums base = shuffled(w, wid);
+    const Sums last = shuffled(x, 31);
+    return {base.rows - last.rows + x.rows - mine.rows, base.back - last.back + x.back - mine.back,
+            base.need - last.need + x.need - mine.need};
 }
 
 struct Request {
@@ -81,47 +90,58 @@ __device__ __forceinline__ void skip_row(const ExtendArgs& a, int64_t row) { a.x
 
 template <bool kRows>
 __global__ void __launch_bounds__(kThreads) k_kv_extend(ExtendArgs a) {
-    __shared__ int64_t smem[32];
+    __shared__ Sums smem[32];
     __shared__ unsigned long long pushed, popped;
     const int tid = threadIdx.x, lane = tid % 32, B = a.b.n_seqs;
     after_previous();
     let_next_begin();
+    const int strip = (B + kThreads - 1) / kThreads;
+    Request held = {};
+    if (strip == 1 && tid < B) held = request(a, tid);  // read once where a thread has one request
+    auto of = [&](int b) { return strip == 1 ? held : request(a, b); };
     const bool pool = a.b.first == nullptr;
     const int64_t n_free = pool ? *a.x.n_free : 0;
     const bool stack = n_free >= 0 && n_free <= a.b.n_blocks;  // else no request is answered
-    if (tid == 0) pushed = popped = 0;
-    const int strip = (B + kThreads - 1) / kThreads;
-    // rows, and blocks that come back
-    int64_t rows = 0, back = 0, total;
-    for (int i = 0; i < strip; ++i) {
-        const int b = tid * strip + i;
-        if (b >= B) break;
-        const Request r = request(a, b);
-        rows += r.n;
-        if (pool && r.done && r.sound) back += blocks_of(r.len, a.b.block_tokens);
+    // what a request adds, if its rows are there
+    auto sums_of = [&](const Request& r) {
+        Sums x = {r.n, 0, 0};
+        if (pool && stack && r.done && r.sound) x.back = blocks_of(r.len, a.b.block_tokens);
+        if (r.sound) x.need = need_of(a, r);
+        return x;
+    };
+    Sums mine = {}, total;
+    for (int b = tid * strip; b < min((tid + 1) * strip, B); ++b) mine.add(sums_of(of(b)));
+    Sums from0 = scan(mine, smem, total);
+    if (tid == 0) a.x.token_ptr[B] = total.rows;
+    if (total.rows > a.x.n_tokens) {  // requests whose rows are not there need nothing
+        mine = {};
+        int64_t rows = from0.rows;
+        for (int b = tid * strip; b < min((tid + 1) * strip, B); ++b) {
+            const Request r = of(b);
+            rows += r.n;
+            if (rows <= a.x.n_tokens) mine.need += sums_of(r).need;
+        }
+        Sums needs;
+        from0.need = scan(mine, smem, needs).need, total.need = needs.need;
     }
-    const int64_t row0 = scan(rows, smem, total);
-    if (tid == 0) a.x.token_ptr[B] = total;
-    const int64_t back0 = scan(back, smem, total);
-    // a request's rows have to be there; done requests push their blocks as long as the stack has room
-    int64_t need = 0;
-    rows = row0, back = back0;
-    for (int i = 0; i < strip; ++i) {
-        const int b = tid * strip + i;
-        if (b >= B) break;
-        const Request r = request(a, b);
-        if (pool && r.done && r.sound && stack) {
-            back += blocks_of(r.len, a.b.block_tokens);
+    // done requests push their blocks as long as the stack has room for them
+    if (tid == 0) pushed = n_free + total.back <= a.b.n_blocks ? total.back : 0, popped = 0;
+    __syncthreads();
+    if (n_free + total.back > a.b.n_blocks) {
+        int64_t back = from0.back;
+        for (int b = tid * strip; b < min((tid + 1) * strip, B); ++b) {
+            back += sums_of(of(b)).back;
             if (n_free + back <= a.b.n_blocks) atomicMax(&pushed, (unsigned long long)back);
         }
-        rows += r.n;
-        if (r.sound && rows <= a.x.n_tokens) need += need_of(a, r);
+        __syncthreads();
     }
-    const int64_t need0 = scan(need, smem, total);
-    __syncthreads();
     const int64_t top = n_free + (int64_t)pushed;
-    if (tid == 0) *a.top = top;
-    rows = row0, back = back0, need = need0;
+    const bool enough = total.need <= top;
+    if (tid == 0) {
+        *a.top = top;
+        if (enough) popped = total.need;
+    }
+    int64_t rows = from0.rows, back = from0.back, need = from0.need;
     for (int i = 0; i < strip; ++i) {
         const int b = tid * strip + i;
         const unsigned there = __ballot_sync(~0u, b < B);
@@ -130,7 +150,7 @@ __global__ void __launch_bounds__(kThreads) k_kv_extend(ExtendArgs a) {
         int status = MP_EINVAL, take = 0;
         int64_t from = back;
         if (b < B) {
-            r = request(a, b);
+            r = of(b);
             take = r.sound && rows + r.n <= a.x.n_tokens ? need_of(a, r) : 0;
             a.x.token_ptr[b] = rows;
             a.had[b] = r.len, a.before[b] = need;
@@ -144,7 +164,7 @@ __global__ void __launch_bounds__(kThreads) k_kv_extend(ExtendArgs a) {
                 } else if (pool) {
                     if (take > 0) {
                         if (need + take > top) status = MP_ENOMEM;
-                        else atomicMax(&popped, (unsigned long long)(need + take));
+                        else if (!enough) atomicMax(&popped, (unsigned long long)(need + take));
                     }
                 } else {
                     const int blocks = blocks_of(r.len + r.n, a.b.block_tokens);
@@ -171,7 +191,7 @@ __global__ void __launch_bounds__(kThreads) k_kv_extend(ExtendArgs a) {
     if (tid == 0 && pool) *a.x.n_free_out = (int32_t)(stack ? top - (int64_t)popped : n_free);
     if (!kRows) return;
     // rows: a lane those of its request where there are few, else the warp those of one request after another
-    rows = row0;
+    rows = from0.rows;
     for (int i = 0; i < strip; ++i) {
         const int b = tid * strip + i;
         if (!__any_sync(~0u, b < B)) break;
@@ -201,17 +221,46 @@ __global__ void __launch_bounds__(kThreads) k_kv_extend(ExtendArgs a) {
     }
 }
 
+// The last request that begins at or before the row; the lanes of a warp have rows in a row.  A search among 32 requests a
+// step finds the first lane's; the others' are mostly among the 32 after it.
+__device__ __forceinline__ int request_of(const ExtendArgs& a, int64_t row, int64_t past) {
+    const int lane = threadIdx.x % 32, B = a.b.n_seqs;
+    const int64_t* const ptr = a.x.token_ptr;
+    int lo = 0, span = B;  // among lo, ..., lo + span - 1
+    if (row - lane + 31 < past) {  // every lane has one
+        const int64_t first = __shfl_sync(~0u, row, 0);
+        while (span > 1) {
+            const int step = (span + 31) / 32, at = lo + lane * step;
+            const int before = __popc(__ballot_sync(~0u, at < lo + span && ptr[min(at, B - 1)] <= first));
+            const int next = lo + (before - 1) * step;
+            span = min(step, lo + span - next), lo = next;
+        }
+        const int64_t begins = ptr[min(lo + 1 + lane, B)];  // of the 32 after it
+        if (lo + 33 > B || __shfl_sync(~0u, begins, 31) > __shfl_sync(~0u, row, 31)) {
+            int more = 0;  // how many of them begin at or before the row
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                const int64_t x = __shfl_sync(~0u, begins, more + o - 1);
+                if (lo + more + o < B && x <= row) more += o;
+            }
+            return lo + more;
+        }
+        span = B - lo;
+    }
+    while (span > 1) {
+        const int half = span / 2;
+        if (ptr[lo + half] <= row) lo += half, span -= half;
+        else span = half;
+    }
+    return lo;
+}
+
 __global__ void __launch_bounds__(kRowThreads) k_kv_extend_rows(ExtendArgs a) {
     after_previous();
     let_next_begin();
     const int64_t past = min(a.x.n_tokens, a.x.token_ptr[a.b.n_seqs]), top = *a.top;
     for (int64_t row = (int64_t)blockIdx.x * kRowThreads + threadIdx.x; row < past; row += (int64_t)gridDim.x * kRowThreads) {
-        int lo = 0, hi = a.b.n_seqs;  // the last request that begins at or before the row
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (a.x.token_ptr[mid] <= row) lo = mid;
-            else hi = mid;
-        }
+        const int lo = request_of(a, row, past);
         if (a.x.step_lens[lo] >= 0) write_row(a, lo, a.had[lo], a.before[lo], top, (int)(row - a.x.token_ptr[lo]), row);
         else skip_row(a, row);
     }

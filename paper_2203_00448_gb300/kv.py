@@ -70,7 +70,8 @@ class _Pool(_Fixed):
         self.device = self.k.device
 
     def _end(self, struct, calls):
-        self._struct, self._ref, self._calls = struct, ctypes.byref(struct), calls
+        self._struct, self._ref = struct, ctypes.byref(struct)
+        self._write, self._read, self._attend = (f"mp_{calls}_{name}" for name in ("write", "read", "attend"))
         # what a batch's struct and scratch depend on
         self._key, self._index = (calls, self.n_blocks > 0, self.block_tokens, self.n_heads, self.head_dim, self.device), self.k.get_device()
 
@@ -196,18 +197,31 @@ class KvBlocks(_Fixed):
         self._ref, self._index, self._need = ctypes.byref(self._struct), self.table.get_device(), None
 
 
-class KvStep:
+class KvStep(_Fixed):
     """What kv_extend has made: the step's batch (its lens are -1 where a request takes no part), positions int32[n_tokens],
     slots int64[n_tokens] and the status of each request."""
 
+    _fixed = frozenset(("batch", "positions", "slots", "status"))
+
     def __init__(self, blocks: KvBlocks, n_tokens, max_tokens, max_len):
-        dev = blocks.device
-        self.batch = KvBatch(blocks.table, torch.empty(blocks.n_seqs, dtype=torch.int32, device=dev),
-                             torch.empty(blocks.n_seqs + 1, dtype=torch.int64, device=dev), n_tokens, max_tokens, max_len)
-        self.positions = torch.empty(n_tokens, dtype=torch.int32, device=dev)
-        self.slots = torch.empty(n_tokens, dtype=torch.int64, device=dev)
-        self.status = torch.empty(blocks.n_seqs, dtype=torch.int32, device=dev)
-        self._of = blocks
+        for name, bound in (("max_tokens", max_tokens), ("max_len", max_len)):
+            if not 0 <= bound <= _MOST:
+                raise ValueError(f"{name} is {bound}: 0 to 2^28 is possible")
+        if max_len > blocks.max_blocks * blocks.block_tokens or n_tokens < 0:
+            raise ValueError(f"max_len is {max_len}, n_tokens {n_tokens}: the table has room for {blocks.max_blocks * blocks.block_tokens}")
+        n, i32, dev = blocks.n_seqs, torch.int32, blocks.device
+        lens, status = torch.empty_like(blocks.lens), torch.empty_like(blocks.lens)
+        token_ptr = torch.empty(n + 1, dtype=torch.int64, device=dev)
+        positions, slots = torch.empty(n_tokens, dtype=i32, device=dev), torch.empty(n_tokens, dtype=torch.int64, device=dev)
+        batch = KvBatch.__new__(KvBatch)  # (what KvBatch checks of its arguments is so of these)
+        batch.__dict__.update(table=blocks.table, lens=lens, token_ptr=token_ptr, n_tokens=n_tokens, max_tokens=max_tokens,
+                              max_len=max_len, n_seqs=n, device=dev, _made={})
+        old, free = blocks.lens.data_ptr() or None, None if blocks.n_free is None else blocks.n_free.data_ptr()
+        struct = _lib.MpKvExtension(n_tokens, max_tokens, max_len, old, free, None, old, free, lens.data_ptr() or None,
+                                    token_ptr.data_ptr(), positions.data_ptr() or None, slots.data_ptr() or None,
+                                    status.data_ptr() or None)
+        self.__dict__.update(batch=batch, positions=positions, slots=slots, status=status, _of=blocks, _struct=struct,
+                             _ref=ctypes.byref(struct))
 
 
 def _tokens(name, t, cache, shape):
@@ -282,8 +296,7 @@ def kv_write(cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tensor, s
     ref, shape, _ = batch._for(cache)
     kt, vt = _tokens("k", k, cache, shape), _tokens("v", v, cache, shape)
     status, stream_ptr = _status(status, batch), _stream(cache)
-    call = "mp_" + cache._calls + "_write"
-    _check(call, getattr(_lib.load(), call)(cache._ref, ref, kt, vt, status.data_ptr() or None, stream_ptr))
+    _check(cache._write, getattr(_lib.load(), cache._write)(cache._ref, ref, kt, vt, status.data_ptr() or None, stream_ptr))
     return status
 
 
@@ -310,8 +323,7 @@ def kv_read(cache: KvCache, batch: KvBatch, dtype=torch.bfloat16, k=None, v=None
             v = torch.empty_like(k) if k.is_contiguous() else torch.empty(shape, dtype=dtype, device=cache.device)
             vt = _fresh(v, shape[1], shape[2])
     status, stream_ptr = _status(status, batch), _stream(cache)
-    call = "mp_" + cache._calls + "_read"
-    _check(call, getattr(_lib.load(), call)(cache._ref, ref, kt, vt, status.data_ptr() or None, stream_ptr))
+    _check(cache._read, getattr(_lib.load(), cache._read)(cache._ref, ref, kt, vt, status.data_ptr() or None, stream_ptr))
     return k, v, status
 
 
@@ -319,8 +331,7 @@ def kv_attend_workspace_bytes(cache: KvCache, batch: KvBatch, n_q_heads: int) ->
     ref, _, needs = batch._for(cache)
     need = needs.get(n_q_heads)
     if need is None:
-        call = getattr(_lib.load(), "mp_" + cache._calls + "_attend_workspace_bytes")
-        need = needs[n_q_heads] = int(call(cache._ref, ref, n_q_heads))
+        need = needs[n_q_heads] = int(getattr(_lib.load(), cache._attend + "_workspace_bytes")(cache._ref, ref, n_q_heads))
     return need
 
 
@@ -357,10 +368,9 @@ def kv_attend(cache: KvCache, batch: KvBatch, q: torch.Tensor, scale: float | No
         wptr, wbytes = scratch.get(need)
     else:
         wptr, wbytes = None, 0
-    call = "mp_" + cache._calls + "_attend"
-    _check(call, getattr(_lib.load(), call)(cache._ref, ref, qt, shape[2] ** -0.5 if scale is None else scale,
-                                            1 if causal else 0, window, ot, None if lse is None else lse.data_ptr() or None,
-                                            status.data_ptr() or None, wptr, wbytes, stream_ptr))
+    _check(cache._attend, getattr(_lib.load(), cache._attend)(
+        cache._ref, ref, qt, shape[2] ** -0.5 if scale is None else scale, 1 if causal else 0, window, ot,
+        None if lse is None else lse.data_ptr() or None, status.data_ptr() or None, wptr, wbytes, stream_ptr))
     return out, lse, status
 
 
@@ -373,32 +383,23 @@ def kv_extend(blocks: KvBlocks, new: torch.Tensor, n_tokens: int, max_tokens: in
     if _away(blocks, stream):
         with _at(blocks, stream):
             return kv_extend(blocks, new, n_tokens, max_tokens, max_len, lens, n_free, step, workspace)
-    stream_ptr = _stream(blocks)
-    _tensor("new", new, torch.int32, (blocks.n_seqs,), blocks.device)
-    room = min(blocks.max_blocks * blocks.block_tokens, _MOST)
-    max_len = room if max_len is None else int(max_len)
-    if not 0 <= max_len <= room:
-        raise ValueError(f"max_len is {max_len}: 0 to {room} is possible")
-    if n_tokens < 0:
-        raise ValueError(f"n_tokens is {n_tokens}")
+    stream_ptr, n, device = _stream(blocks), blocks.n_seqs, blocks.device
+    _tensor("new", new, torch.int32, (n,), device)
+    max_len = min(blocks.max_blocks * blocks.block_tokens, _MOST) if max_len is None else int(max_len)
     max_tokens = min(int(n_tokens), _MOST) if max_tokens is None else int(max_tokens)
     if step is None:
         step = KvStep(blocks, int(n_tokens), max_tokens, max_len)
     elif step._of is not blocks or (step.batch.n_tokens, step.batch.max_tokens, step.batch.max_len) != (n_tokens, max_tokens, max_len):
         raise ValueError("the step that is given has other blocks or bounds")
-    lens = blocks.lens if lens is None else _tensor("lens", lens, torch.int32, (blocks.n_seqs,), blocks.device)
-    if n_free is None:
-        n_free = blocks.n_free
-    elif blocks.n_free is None:
+    if n_free is not None and blocks.n_free is None:
         raise ValueError("n_free: these blocks have no stack")
-    else:
-        _tensor("n_free", n_free, torch.int32, (1,), blocks.device)
-    b = step.batch
-    x = _lib.MpKvExtension(n_tokens, max_tokens, max_len, *(None if t is None else t.data_ptr() or None for t in (
-        blocks.lens, blocks.n_free, new, lens, n_free, b.lens, b.token_ptr, step.positions, step.slots, step.status)))
+    x = step._struct
+    x.n_new = new.data_ptr() or None
+    x.lens_out = x.lens if lens is None else _tensor("lens", lens, torch.int32, (n,), device).data_ptr() or None
+    x.n_free_out = x.n_free if n_free is None else _tensor("n_free", n_free, torch.int32, (1,), device).data_ptr()
+    lib = _lib.load()
     if blocks._need is None:
-        blocks._need = int(_lib.load().mp_kv_extend_workspace_bytes(blocks._ref))
-    scratch = workspace or _workspace_of(stream_ptr, blocks.device)
-    wptr, wbytes = scratch.get(blocks._need)
-    _check("mp_kv_extend", _lib.load().mp_kv_extend(blocks._ref, ctypes.byref(x), wptr, wbytes, stream_ptr))
+        blocks._need = int(lib.mp_kv_extend_workspace_bytes(blocks._ref))
+    wptr, wbytes = (workspace or _workspace_of(stream_ptr, device)).get(blocks._need)
+    _check("mp_kv_extend", lib.mp_kv_extend(blocks._ref, step._ref, wptr, wbytes, stream_ptr))
     return step

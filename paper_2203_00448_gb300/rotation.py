@@ -130,28 +130,33 @@ def rotary(rotation: Rotary, positions: torch.Tensor, q: torch.Tensor | None, k:
     if _away(rotation, stream):
         with _at(rotation, stream):
             return rotary(rotation, positions, q, k, q_out, k_out, inverse)
-    stream_ptr = _stream(rotation)
+    stream_ptr, index = _stream(rotation), rotation._index
     some = q if q is not None else k
     if some is None or (q is None and q_out is not None) or (k is None and k_out is not None):
         raise ValueError("q or k is needed, and an output only for what is there")
     _tensor("positions", positions, torch.int32, some.shape[:1], rotation.device)
-    structs, outs = [], []
+    structs, outs, empty = [], [], some.shape[0] == 0
     for name, x, out in (("q", q, q_out), ("k", k, k_out)):
         if x is None:
-            structs.append((None, None))
+            structs += (None, None)
             outs.append(None)
             continue
-        a = _rows(name, x, None, rotation._index)
-        if x.shape[0] != some.shape[0] or x.shape[2] != some.shape[2] or x.dtype != some.dtype:
+        a = _rows(name, x, None, index)
+        tokens, heads, dim = x.shape
+        if x is not some and (tokens != some.shape[0] or dim != some.shape[2] or x.dtype != some.dtype):
             raise ValueError("q and k have as many tokens, heads of one size and one type")
         if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        structs.append((a, _rows(name + "_out", out, x, rotation._index)))
+            out = torch.empty_like(x, memory_format=torch.contiguous_format)
+            b = _lib.MpTokens(out.data_ptr() or None, heads * dim, dim, heads, a.dtype)
+        else:
+            b = _rows(name + "_out", out, x, index)
+        structs += (a, b)
         outs.append(out)
+        empty = empty or heads == 0
     if rotation.dim > some.shape[2]:
         raise ValueError(f"dim is {rotation.dim}, heads have {some.shape[2]} values")
-    if some.shape[0] and all(x is None or x.shape[1] for x in (q, k)):
-        (qi, qo), (ki, ko) = structs
+    if not empty:
+        qi, qo, ki, ko = structs
         _check("mp_rotary", _lib.load().mp_rotary(rotation._ref, positions.data_ptr(), some.shape[0], some.shape[2], qi, ki, qo, ko,
                                                   1 if inverse else 0, stream_ptr))
     return tuple(outs)
