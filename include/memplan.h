@@ -564,7 +564,8 @@ typedef struct mp_kv_blocks {
 } mp_kv_blocks;
 
 /* One step.  Host scalars: n_tokens rows of positions and slots; max_tokens, max_len: upper bounds on
- * a request's new tokens and on what it then holds (max_len at most max_blocks * block_tokens and 2^28).
+ * a request's new tokens and on what it then holds (max_len at most max_blocks * block_tokens and 2^28); one that ends may
+ * have held more.
  * Device arrays, in:
  *   lens    int32[n_seqs]  tokens held
  *   n_free  int32[1]       height of the stack (not with first)
@@ -601,7 +602,7 @@ size_t mp_kv_extend_workspace_bytes(const mp_kv_blocks *blocks);
  * the others take what ceil((lens + n_new) / block_tokens) asks for beyond ceil(lens / block_tokens), the
  * first one from the top of the stack.  A request whose blocks, with those that all requests before it ask for,
  * are more than there are gets MP_ENOMEM (with first: one that needs more than its room); what asks for none is always answered.
- * MP_EINVAL: lens negative or above max_len, a bound broken, rows beyond n_tokens, a run outside the pool,
+ * MP_EINVAL: lens negative or more than the table has room for, a bound broken, rows beyond n_tokens, a run outside the pool,
  * blocks that come back to a stack without room for them, an *n_free outside 0 .. n_blocks (then every
  * request).  A request with either status keeps its lens and its table.  Table entries of columns that a request
  * does not get in the call, rows beyond token_ptr[n_seqs] and the entries of the stack below *n_free are left alone;

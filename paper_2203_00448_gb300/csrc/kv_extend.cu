@@ -66,7 +66,9 @@ __device__ __forceinline__ Request request(const ExtendArgs& a, int b) {
     r.len = a.x.lens[b];
     const int n = a.x.n_new[b];
     r.done = n < 0, r.n = max(n, 0);
-    r.sound = r.len >= 0 && r.len <= a.x.max_len && r.n <= a.x.max_tokens && (int64_t)r.len + r.n <= a.x.max_len;
+    // one that ends may have held more than the others may
+    const int64_t most = r.done ? min((int64_t)a.b.max_blocks * a.b.block_tokens, (int64_t)1 << 28) : a.x.max_len;
+    r.sound = r.len >= 0 && r.n <= a.x.max_tokens && (int64_t)r.len + r.n <= most;
     return r;
 }
 __device__ __forceinline__ int need_of(const ExtendArgs& a, const Request& r) {

@@ -121,7 +121,8 @@ def extend(table, lens, new, block, n_tokens, max_tokens, max_len, free=None, n_
     status, out, step = [1] * B, list(lens), [-1] * B
     ptr = np.concatenate([[0], np.cumsum([max(n, 0) for n in new])]).astype(np.int64)
     positions, slots = np.full(n_tokens, -77, np.int32), np.full(n_tokens, -77, np.int64)
-    sound = [0 <= a <= max_len and max(n, 0) <= max_tokens and a + max(n, 0) <= max_len for a, n in zip(lens, new)]
+    room_for = len(table[0]) * block if B else 0
+    sound = [0 <= a and max(n, 0) <= max_tokens and a + max(n, 0) <= (room_for if n < 0 else max_len) for a, n in zip(lens, new)]
     stack = first is not None or 0 <= n_free <= n_blocks
     top = back = n_free
     if first is None and stack:

@@ -101,6 +101,13 @@ def test_extend_refuses_requests_one_by_one(cuda_lib, many):
     for bad in (-1, n_blocks + 1, 2 ** 31 - 1, -2 ** 31):  # a stack of no such height: nobody is answered
         want = run_extend(mp, table, lens, new, *args[:4], free, bad, n_blocks)
         assert set(want["status"]) == {1}
+    # a request that ends may have held more than the step's others may
+    new[7] = 0
+    long, gone = [a if 0 <= a <= 640 else 0 for a in lens], list(new)
+    most = max(range(60), key=lambda b: long[b])
+    gone[most] = -1
+    want = run_extend(mp, table, long, gone, 32, sum(max(n, 0) for n in gone), 200 if many else 5, long[most] - 1, free, n_free, n_blocks)
+    assert want["status"][most] == 0 and want["lens"][most] == 0
     # blocks that come back to a stack that is full already
     done = [-1 if a > 0 else 0 for a in lens]
     want = run_extend(mp, table, lens, done, *args[:4], free, n_blocks - 3, n_blocks)
@@ -292,3 +299,11 @@ def test_steps_together(cuda_lib, bits):
                 bound, _ = R.attend_bounds(torch.bfloat16, want, lse, mag, size)
                 assert (np.abs(out[row:row + m].double().cpu().numpy() - want) <= bound).all()
             row, past = row + m, past + held[b]
+
+
+def test_example_serves_from_four_bits(cuda_lib):
+    """The example's loop over the 4-bit cache; bounds as for 8 bits: bf16's last rounding, 2^-9, and the weights' 2^-11."""
+    from examples.serve_requests import serve
+
+    done = serve(n=12, prompt=150, generate=8, spread=15, heads=2, group=4, dim=64, block_tokens=32, check=True, bits=4)
+    assert done["pool_blocks"] < done["blocks"] and 0 < done["worst"] <= 2.0 ** -9 + 2.0 ** -11
