@@ -41,6 +41,7 @@ namespace {
 constexpr int few_warps(int d, int nt) { return d == 128 ? (nt == 1 ? 12 : 8) : (nt == 1 ? 16 : 12); }
 constexpr int kFewStages = 2;
 constexpr int short_warps(int nt) { return nt == 1 ? 16 : 8; }
+constexpr int kLeastUnits = 4;
 constexpr int kFewRows = 16;  // most rows of a sequence and head
 constexpr int kJoinThreads = 256;  // k_kv_join of D = 128 keeps 16 bytes a thread in memory for it (48 registers), of 64 8 bytes
 
@@ -128,14 +129,16 @@ struct Tile {
     float o[NT][D / 16][4];
     int see_lo[NT][2], see_hi[NT][2];  // positions that the column's row sees
     int last;                          // stored bytes from this position on mean nothing
-    int all_lo, all_hi;                // positions that every row sees
-    // 4 bits: weights are 2^(score * unit + off); a score above limit moves the reference
+    // 4 bits: positions that every row sees; the columns' own positions (kNoEnd: all that is held is seen, or no one reads
+    // the column); weights are 2^(score * unit + off), and a score above limit moves the reference
+    int all_lo, all_hi, held, window, pos[NT][2];
     float off[NT][2], limit[NT][2];
+    static constexpr int kNoEnd = 1 << 30;
 
     // rows: of the sequence and head, at least 1; row: the sequence's first in the token arrays
     __device__ __forceinline__ void begin(const AttendArgs& a, int64_t row, int rows, int len, int n, int head, int tile) {
         const int lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
-        last = all_lo = 0, all_hi = len;
+        last = all_lo = 0, all_hi = held = len, window = a.window;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int r = tile * 8 * NT + nt * 8 + g, there = min(r, rows - 1);
@@ -181,10 +184,11 @@ struct Tile {
             for (int k = 0; k < 2; ++k) {
                 unit[nt][k] = __shfl_sync(~0u, mine, (2 * t + k) * 4);
                 const int col = tile * 8 * NT + nt * 8 + 2 * t + k;
-                const int pos = len - n + col / a.group;
+                const int at = len - n + col / a.group;
                 // columns past the last row repeat it and see all that is held: no one reads them
-                see_hi[nt][k] = col < rows && a.causal ? min(len, pos + 1) : len;
-                see_lo[nt][k] = col < rows && a.window > 0 ? pos - a.window + 1 : 0;
+                see_hi[nt][k] = col < rows && a.causal ? min(len, at + 1) : len;
+                see_lo[nt][k] = col < rows && a.window > 0 ? at - a.window + 1 : 0;
+                pos[nt][k] = col < rows && a.causal ? at : kNoEnd;
                 last = max(last, see_hi[nt][k]);
                 all_lo = max(all_lo, see_lo[nt][k]), all_hi = min(all_hi, see_hi[nt][k]);
                 top[nt][k] = limit[nt][k] = -INFINITY, sum[nt][k] = off[nt][k] = 0.f;
@@ -330,8 +334,8 @@ struct Tile {
                 for (int k = 0; k < 2; ++k)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int j = base + i / 2 * 16 + token_of(g, i % 2);
-                        if (!(j < see_hi[nt][k] && j >= see_lo[nt][k])) s[nt][i / 2][i % 2 * 2 + k] = -INFINITY;
+                        const int j = base + i / 2 * 16 + token_of(g, i % 2), before = pos[nt][k] - j;
+                        if (j >= held || before < 0 || (window > 0 && before >= window)) s[nt][i / 2][i % 2 * 2 + k] = -INFINITY;
                     }
         }
         float most[NT][2];
@@ -353,9 +357,9 @@ struct Tile {
                     x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
                     x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
                     if (x > limit[nt][k]) {
-                        const float now = x * unit[nt][k], fade = exp2_approx(top[nt][k] - now);
-                        top[nt][k] = now, off[nt][k] = lift_of(4) - now;
-                        limit[nt][k] = __fdiv_rn(now + kFewGrow, unit[nt][k]);
+                        const float now = x * unit[nt][k], next = lift_of(4) - now;
+                        const float fade = limit[nt][k] == -INFINITY ? 0.f : exp2_approx(next - off[nt][k]);
+                        off[nt][k] = next, limit[nt][k] = __fdiv_rn(now + kFewGrow, unit[nt][k]);
                         sum[nt][k] *= fade;
 #pragma unroll
                         for (int i = 0; i < D / 16; ++i) o[nt][i][k] *= fade, o[nt][i][2 + k] *= fade;
@@ -448,6 +452,11 @@ struct Tile {
         }
     }
 
+    // The reference of a column's weights, which are 2^lift_of(kBits) there.
+    __device__ __forceinline__ float reference(int nt, int k) const {
+        return kBits == 8 ? top[nt][k] : limit[nt][k] == -INFINITY ? -INFINITY : lift_of(4) - off[nt][k];
+    }
+
     // This lane's part of a column's sum becomes the column's.
     __device__ __forceinline__ float total(int nt, int k) const {
         float l = sum[nt][k];
@@ -535,7 +544,9 @@ __global__ void __launch_bounds__(few_warps(D, NT) * 32, 1) k_kv_attend_few(Atte
     }
     const int warps = gridDim.x * kFewWarps;
     const int64_t total = strip_base[kFewWarps * 32];
-    const int64_t per_warp = quotient(total + warps - 1, warps);
+    // of 4 bits at least so many that what is left to add up is worth it (one context of 8,000 tokens 22 us with 1, 18 with 4, 20
+    // with 6; four of 4,000 22, 20 and 20)
+    const int64_t per_warp = max(quotient(total + warps - 1, warps), kBits == 8 ? (int64_t)0 : min(total, (int64_t)kLeastUnits));
     // consecutive warps of the line are on different SMs: short lines reach them all
     const int w = wid * gridDim.x + blockIdx.x;
     if (w == 0 && lane == 0) work.base[a.bt.n_seqs + 1] = per_warp;
@@ -649,7 +660,7 @@ __global__ void __launch_bounds__(few_warps(D, NT) * 32, 1) k_kv_attend_few(Atte
             for (int k = 0; k < 2; ++k) {
                 const float l = x.total(nt, k);
                 const int in_tile = nt * 8 + 2 * t + k, r = tile * kRows + in_tile;
-                const float m = x.top[nt][k];
+                const float m = x.reference(nt, k);
                 if (whole) {
                     if (r < rows) {
                         const int64_t tok = cur.row + r / a.group;
@@ -766,7 +777,7 @@ __global__ void __launch_bounds__(short_warps(NT) * 32, 1) k_kv_attend_short(Att
                         acc[r * D + x.value_of(i, g, 1)] = x.o[nt][i][2 + k];
                     }
                 }
-                if (g == 0) ref[wid][r] = any ? x.top[nt][k] : -INFINITY, weight[wid][r] = l;
+                if (g == 0) ref[wid][r] = any ? x.reference(nt, k) : -INFINITY, weight[wid][r] = l;
             }
         __syncthreads();
         for (int i = threadIdx.x; i < kRows * (D / 2); i += kWarps * 32) {
@@ -883,7 +894,7 @@ __device__ void check_seq(const AttendArgs& a, const FewWork& few, bool late, in
 // kPer warps a query row add up what several warps of k_kv_attend_few had of it.
 template <typename T, int D, int NT, int kPer, int kBits>
 __device__ void join_row(const AttendArgs& a, const FewWork& work, int64_t u, bool there) {
-    constexpr int kRows = 8 * NT, kCols = D / 32, kAhead = 4;
+    constexpr int kRows = 8 * NT, kCols = D / 32, kAhead = kPer == 1 ? 4 : 8;
     __shared__ float acc[kJoinThreads / 32][D + 2];
     const int lane = threadIdx.x % 32, wid = threadIdx.x / 32;
     const int head = (int)(u % a.c.n_heads), rows_max = join_rows(a);

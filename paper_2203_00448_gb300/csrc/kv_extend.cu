@@ -90,10 +90,21 @@ __device__ __forceinline__ void write_row(const ExtendArgs& a, int b, int len, i
 }
 __device__ __forceinline__ void skip_row(const ExtendArgs& a, int64_t row) { a.x.positions[row] = -1, a.x.slots[row] = -1; }
 
+// Blocks of a request that ends, and where on the stack they go; a warp pushes them.
+struct Ended {
+    int32_t b, blocks, to;
+};
+__device__ __forceinline__ void push(const ExtendArgs& a, const Ended& e) {
+#pragma unroll 4
+    for (int j = threadIdx.x % 32; j < e.blocks; j += 32) a.b.free[e.to + j] = a.b.table[(int64_t)e.b * a.b.max_blocks + j];
+}
+
 template <bool kRows>
 __global__ void __launch_bounds__(kThreads) k_kv_extend(ExtendArgs a) {
     __shared__ Sums smem[32];
     __shared__ unsigned long long pushed, popped;
+    __shared__ Ended ended[kThreads];
+    __shared__ int n_ended;
     const int tid = threadIdx.x, lane = tid % 32, B = a.b.n_seqs;
     after_previous();
     let_next_begin();
@@ -127,7 +138,7 @@ __global__ void __launch_bounds__(kThreads) k_kv_extend(ExtendArgs a) {
         from0.need = scan(mine, smem, needs).need, total.need = needs.need;
     }
     // done requests push their blocks as long as the stack has room for them
-    if (tid == 0) pushed = n_free + total.back <= a.b.n_blocks ? total.back : 0, popped = 0;
+    if (tid == 0) pushed = n_free + total.back <= a.b.n_blocks ? total.back : 0, popped = 0, n_ended = 0;
     __syncthreads();
     if (n_free + total.back > a.b.n_blocks) {
         int64_t back = from0.back;
@@ -179,15 +190,22 @@ __global__ void __launch_bounds__(kThreads) k_kv_extend(ExtendArgs a) {
             a.x.step_lens[b] = part ? r.len + r.n : -1;
             a.x.lens_out[b] = status != MP_OK ? r.len : r.done ? 0 : r.len + r.n;
         }
-        // the blocks of done requests, a warp a request
-        unsigned gone = __ballot_sync(~0u, b < B && pool && r.done && status == MP_OK);
-        for (; gone; gone &= gone - 1) {
-            const int l = __ffs(gone) - 1;
-            const int who = __shfl_sync(~0u, b, l), n = blocks_of(__shfl_sync(~0u, r.len, l), a.b.block_tokens);
-            const int64_t to = n_free + __shfl_sync(~0u, from, l);
-            for (int j = lane; j < n; j += 32) a.b.free[to + j] = a.b.table[(int64_t)who * a.b.max_blocks + j];
+        // the blocks of done requests, a warp a request: all at once where a thread has one request
+        const bool gone = b < B && pool && r.done && status == MP_OK && r.len > 0;
+        if (strip == 1) {
+            if (gone) ended[atomicAdd(&n_ended, 1)] = {b, blocks_of(r.len, a.b.block_tokens), (int32_t)(n_free + from)};
+        } else {
+            for (unsigned left = __ballot_sync(~0u, gone); left; left &= left - 1) {
+                const int l = __ffs(left) - 1;
+                push(a, {__shfl_sync(~0u, b, l), blocks_of(__shfl_sync(~0u, r.len, l), a.b.block_tokens),
+                         (int32_t)(n_free + __shfl_sync(~0u, from, l))});
+            }
         }
         rows += r.n, need += take;
+    }
+    if (strip == 1) {
+        __syncthreads();
+        for (int i = tid / 32; i < n_ended; i += kThreads / 32) push(a, ended[i]);
     }
     __syncthreads();
     if (tid == 0 && pool) *a.x.n_free_out = (int32_t)(stack ? top - (int64_t)popped : n_free);
