@@ -3,6 +3,11 @@
 // 32 values of a token and head have a scale s of 4 significant bits, the least with max |x| <= 7.5 s, and codes n =
 // x / s rounded to the nearest whole number of -7 .. 7: no value is off by more than half a step, and n s is exact in
 // f16, bf16 and f32.  A token's codes depend on no other token, so nothing that is stored is ever rounded again.
+//
+// Measured (8 heads of 128, GPU time): 253 single tokens written 5 us and read 6; 15,973 prompt tokens written 28 us (83 MB of them and
+// 17 of codes: 12 us at a copy's rate) and read back 16; 131,071 read back 105 us (6.4 TB/s, 95% of a copy's rate);
+// 32 x 300 tokens written 20, the prompts in 32 bits 43.  Writes are bound by instructions, 145 for 8 values of each lane
+// (with rintf and conversions to integers, which run on a slow unit, and divisions it was 60 us).
 #include <algorithm>
 
 #include "kv.cuh"

@@ -24,6 +24,15 @@
 // TB/s of the 6.8 that a copy reaches; two of 262,144 tokens 173 us, 6.0 TB/s; one of 512 6.6
 // us of GPU time.  Long contexts are bound by memory; the rest is the ramp (lengths, table,
 // queries, first bytes: four trips one after another) and the joining launch, about 12 us.
+//
+// 4 bits.  A code times its scale is exact in f16, so both products take the values themselves: w_j = 2^(x_j - M), no value
+// scale in the sum.  The reference M stays until a score passes it by 2^5 (kFewGrow), which one vote a granule says; w
+// has 11 bits down to 2^-24 of it.  A granule is 4.4 KB where it is 8.2 KB of 8 bits, and takes as many products and more
+// operations on codes: 600 instructions, of which 136 pick codes out of words, 128 scale them and 32 are products.
+// Measured: the 64 contexts 80 us (3.6 TB/s; 64 us without any operation on the bytes), the two long ones 119 us (4.6 TB/s;
+// 99): half of the cycles are integer operations, a quarter each f16 operations and products, and hardly any of the three
+// come at the same time.  Dropped: 64 tokens a step, products in two chains, 8 and 16 warps, four
+// granules ahead (89 and 128 us for 85 and 126), bulk copies for the ring (93 and 130).
 #pragma once
 
 #include <algorithm>
@@ -41,7 +50,7 @@ namespace {
 constexpr int few_warps(int d, int nt) { return d == 128 ? (nt == 1 ? 12 : 8) : (nt == 1 ? 16 : 12); }
 constexpr int kFewStages = 2;
 constexpr int short_warps(int nt) { return nt == 1 ? 16 : 8; }
-constexpr int kLeastUnits = 4;
+constexpr int kLeastUnits = 4;  // of 4 bits, that a warp takes where there are more
 constexpr int kFewRows = 16;  // most rows of a sequence and head
 constexpr int kJoinThreads = 256;  // k_kv_join of D = 128 keeps 16 bytes a thread in memory for it (48 registers), of 64 8 bytes
 
@@ -584,7 +593,7 @@ __global__ void __launch_bounds__(few_warps(D, NT) * 32, 1) k_kv_attend_few(Atte
     uint32_t next_stage = first_stage;
     int to_come = (int)(u1 - u0);
     auto issue = [&]() {  // the next unit's bytes into its stage
-        if constexpr (kBits == 4) {
+        if constexpr (kBits == 4) {  // (these copies end by themselves: there is no wait to give up)
             if (to_come > 0) {
                 copy(next_stage, block_byte<kBits>(a.c, page_ahead, ahead.head) + ahead.in_block * kBytes);
                 next_stage = next_stage == last_stage ? first_stage : next_stage + 2 * kBytes;
@@ -600,7 +609,7 @@ __global__ void __launch_bounds__(few_warps(D, NT) * 32, 1) k_kv_attend_few(Atte
         const int st = (int)((issued - u0) % kFewStages);
         const int64_t at = block_byte<kBits>(a.c, page_ahead, ahead.head) + ahead.in_block * kBytes;
         if (lane == 0) {
-            if (kBits == 8) ring_page[st] = page_ahead;
+            ring_page[st] = page_ahead;
             mbar_expect(&bar[st], 2 * kBytes);
             if (!test_held(a, issued)) {
                 bulk_load(ring + st * 2 * kBytes, a.c.k + at, kBytes, &bar[st]);
@@ -990,14 +999,17 @@ __global__ void __launch_bounds__(kJoinThreads) k_kv_join(AttendArgs a, FewWork 
 // tokens, both kernels are the faster way from well below: 16 singles of up to 2,000 (41 MB held) 57 and 57, 32 of up to
 // 4,000 (145 MB) 116 and 94, 63 of up to 2,000 (162 MB) 130 and 87; past the line 63 of up to 4,000 (294 MB) 189 and 122, 255 of
 // up to 8,000 (2.2 GB) 1,019 and 490.  The line goes by what the host knows, the number of sequences times the bound of
-// their lengths; a generous bound leads to both kernels.
-constexpr int64_t kSmallCache = 256 << 20;
+// their lengths; a generous bound leads to both kernels.  Of 4 bits the first kernel reads half of the bytes, and the second
+// takes as long: 16 singles of up to 2,000 with a piece of 512 (37 MB) 64 us without the first and 70 with it, 32 of up to 4,000 (143
+// MB) 115 and 91, 8 pieces of 512 and 8 singles over up to 8,000 (139 MB) 471 and 470.
+constexpr int64_t small_cache(int bits) { return bits == 8 ? 256 << 20 : 64 << 20; }
 // Which kernels a batch needs, by its host scalars: sequences of at most kFewRows rows are
 // bound by the cache's bytes, which k_kv_attend_few streams; above it the products count.
 // A batch whose sequences all have max_tokens has no sequence for the first.
 // Few rows of short contexts in batches that fill the GPU at most twice over go to k_kv_attend_short (8 heads, the GPU's
 // time of a call: 1 x 512 tokens 6.6 us against 9.4, 8 x 1,024 8.8 against 11.7, 38 x 2,048 32.6 against 37.2; but
-// 1 x 4,096 19.3 against 14.7, and 128 x 512, four times the SMs, 48.6 against 35.4).
+// 1 x 4,096 19.3 against 14.7, and 128 x 512, four times the SMs, 48.6 against 35.4).  Of 4 bits the same lines hold: 1 x 512 7
+// against 11, 8 x 1,024 9 against 15, 38 x 2,048 27 against 38, but 2 x 4,000 21 against 17.
 constexpr int32_t kShortLen = 2048;
 constexpr int64_t kShortCtas = 2 * kSms;
 struct Route {
@@ -1014,7 +1026,7 @@ Route route(const mp_kv_cache& c, const mp_kv_batch& bt, int32_t group, int32_t 
         return {!brief, false, brief};
     }
     const int64_t bytes = (int64_t)bt.n_seqs * bt.max_len * c.n_heads * granule_bytes(kBits, c.head_dim) / (kGranule / 2);
-    return {bt.n_tokens != (int64_t)bt.n_seqs * bt.max_tokens && bytes > kSmallCache, true, false};
+    return {bt.n_tokens != (int64_t)bt.n_seqs * bt.max_tokens && bytes > small_cache(kBits), true, false};
 }
 
 struct Layout {

@@ -36,6 +36,13 @@
 // scores need not wait for (466 -> 487 us: narrower products read the queries twice as often), two
 // threads a row (1,038 -> 1,059), prefetches of the units to come into L2 (480 for 465), table entries
 // and scales fetched by a warp of their own (473 for 464).
+//
+// 4 bits: codes times scales become the operands (10 operations for 8 of them), and nothing is left of scales for the
+// softmax.  Measured: 8,000 tokens 468 us, pieces of 300 to 512 over up to 16,384 156 us, 16 tokens over 60,000 each for 8
+// sequences 335 us, 8 tokens over the 64 ragged contexts 222 us.  Neither the exponentials nor the conversion bound prompts
+// (without the one 468 -> 466, without the other 461): a unit is a chain of product, scores out, weights in, product, whose four
+// hand-overs take 1,900 cycles before any work is done in them.  With few rows the trip of the units' bytes is the bound (335 -> 250
+// without it).  Dropped: tile 1's scores only once tile 0 has its weights, or its scores (468 -> 515 and 490).
 #pragma once
 
 #include <algorithm>

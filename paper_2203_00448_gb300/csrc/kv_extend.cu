@@ -4,6 +4,9 @@
 // back, and of the blocks that the others need.  One CTA takes them (a thread a strip of requests) and writes what there
 // is one of for each request; rows (position, slot, and the table's entry where a row opens a block) need no more than
 // their request's sums, so in large steps a second kernel has them, a thread a row.
+//
+// Measured (GPU time): 64 requests with a token each 5 us, 509 requests of which 484 get 125,000 tokens and 25 end 13 us: trips to
+// memory one after another (lengths, the ended requests' table rows, then sums, tables and stacks for the rows).
 #include <algorithm>
 
 #include "kv_attend.cuh"
@@ -12,7 +15,7 @@ namespace mp {
 namespace {
 
 constexpr int kThreads = 1024, kRowThreads = 256;
-// Rows up to which the first kernel writes them too, a warp a request.
+// Rows up to which the first kernel writes them too, a warp a request; the second launch costs 2 us.
 constexpr int64_t kFewRows = 4096;
 
 struct ExtendArgs {

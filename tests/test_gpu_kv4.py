@@ -7,6 +7,7 @@ import torch
 from tests import kv4_refs as R4
 from tests import kv_refs as R
 from tests.test_gpu_kv import ATTENDS, BF16, F16, F32, WRITES, batch_of, rows
+from tests.test_gpu_kv_timeout import hooks  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -319,3 +320,62 @@ def test_captured_calls_and_other_streams(cuda_lib):
     assert eager.shape == (4, 2, 128)
     for x, y in zip(outs, (q, other)):
         assert torch.equal(x, mp.kv_attend(cache, batch, y)[0])
+
+
+@pytest.mark.parametrize("d,lens,new", [(128, [6000, 700, 3000], [600, 40, 200]), (64, [60000, 700, 30000], [30, 20, 25])])
+def test_attention_wait_runs_out(hooks, d, lens, new):  # noqa: F811
+    """A unit held back in the kernel for many rows, as in tests/test_gpu_kv_timeout.py: the call ends, says so, and the next is
+    right."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(53)
+    table, n = R.make_table(lens, 64, rng)
+    pool = R4.Pool(n, 64, 2, d, rng)
+    cache, batch = pool.cache(), batch_of(mp, table, lens, new)
+    q, _ = rows(rng, sum(new), 8, d, BF16)
+    want, _, status = mp.kv_attend(cache, batch, q)
+    assert not status.any()
+    for unit in (0, 2):
+        hooks(unit)
+        _, _, status = mp.kv_attend(cache, batch, q)
+        torch.cuda.synchronize()
+        hooks(-1)
+        assert status.tolist() == [mp.ETIMEOUT] * 3
+        out, _, status = mp.kv_attend(cache, batch, q)
+        assert not status.any() and torch.equal(out, want)
+
+
+@pytest.mark.parametrize("group,d", [(4, 128), (1, 64)])
+def test_attend_by_both_long_kernels(cuda_lib, group, d):
+    """A batch of single tokens over long contexts with pieces of prompts, large enough for both kernels, one joining launch, and one
+    that the second takes alone; the definition in 64 bits on the GPU."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(d)
+    heads, block = 4, 64
+    for lens in ([30000, 17, 40000, 300, 0, 25000, 64, 900], [3000, 17, 4000, 300, 0, 2500, 64, 900]):
+        new = [1, 2, 100, 290, 1, 2, 33, 1]
+        table, n = R.make_table(lens, block, rng)
+        pool = R4.Pool(n, block, heads, d, rng)
+        cache, batch = pool.cache(), batch_of(mp, table, lens, new)
+        q, _ = rows(rng, sum(new), heads * group, d, BF16)
+        out, lse, status = mp.kv_attend(cache, batch, q, want_lse=True)
+        assert not status.any()
+        k, v, _ = mp.kv_read(cache, batch_of(mp, table, lens, lens), F32)
+        row = past = 0
+        for length, m in zip(lens, new):
+            mine, mine_lse = out[row:row + m].double().cpu().numpy(), lse[row:row + m].double().cpu().numpy()
+            kk, vv = (x[past:past + length].double().repeat_interleave(group, 1).transpose(0, 1) for x in (k, v))
+            qq = q[row:row + m].double().transpose(0, 1)
+            row, past = row + m, past + length
+            if length == 0:
+                assert (mine == 0).all() and np.isneginf(mine_lse).all()
+                continue
+            x = qq @ kk.transpose(1, 2) * d ** -0.5
+            x = x.masked_fill(torch.arange(length, device="cuda") > (length - m + torch.arange(m, device="cuda"))[:, None], -torch.inf)
+            w = torch.softmax(x, -1)
+            want, mag = (w @ vv).transpose(0, 1).cpu().numpy(), (w @ vv.abs()).transpose(0, 1).cpu().numpy()
+            want_lse = torch.logsumexp(x, -1).transpose(0, 1).cpu().numpy()
+            size = ((qq.abs() @ kk.abs().transpose(1, 2)).amax(-1) * d ** -0.5).transpose(0, 1).cpu().numpy()
+            bound, lse_bound = R.attend_bounds(BF16, want, want_lse, mag, size)
+            assert (np.abs(mine - want) <= bound).all() and (np.abs(mine_lse - want_lse) <= lse_bound).all()
