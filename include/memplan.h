@@ -533,7 +533,9 @@ mp_status mp_kv_four_read(const mp_kv4_cache *cache, const mp_kv_batch *batch, c
                       int32_t *seq_status, void *stream);
 
 /* As mp_kv_attend_workspace_bytes and mp_kv_attend; keys and values enter the products
- * as f16 without a rounding. */
+ * as f16 without a rounding.  Weights have 11 bits of precision down to 2^-24 of a value
+ * that a row's largest may pass by 2^5, and vanish below 2^-34 of it; in calls of more than 16 rows a head
+ * 2^-21, 2^8 and 2^-31, as there, where scale * q . k has to stay below 2^23 in magnitude. */
 size_t mp_kv_four_attend_workspace_bytes(const mp_kv4_cache *cache, const mp_kv_batch *batch, int32_t n_q_heads);
 mp_status mp_kv_four_attend(const mp_kv4_cache *cache, const mp_kv_batch *batch, const mp_tokens *q, float scale,
                         int32_t causal, int32_t window, const mp_tokens *out, float *lse, int32_t *seq_status,
@@ -553,7 +555,7 @@ mp_status mp_kv_four_attend(const mp_kv4_cache *cache, const mp_kv_batch *batch,
  *   first  int32[n_seqs] or NULL: request b has blocks first[b], first[b] + 1, ...
  *   room   int32[n_seqs] with first: ... of which it may have that many */
 typedef struct mp_kv_blocks {
-    int32_t n_seqs;
+    int32_t n_seqs;       /* at most 2^28 */
     int32_t max_blocks;
     int32_t block_tokens; /* a multiple of 32, at most 256 */
     int32_t n_blocks;     /* of the pool */

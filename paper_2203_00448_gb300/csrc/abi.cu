@@ -179,7 +179,7 @@ bool attend_needs(const C* cache, const mp_kv_batch* batch, int32_t n_q_heads) {
 }
 
 bool blocks_ok(const mp_kv_blocks* b) {
-    return b != nullptr && b->n_seqs >= 0 && b->max_blocks >= 0 && b->n_blocks >= 0 && b->block_tokens >= 32 &&
+    return b != nullptr && b->n_seqs >= 0 && b->n_seqs <= kKvMost && b->max_blocks >= 0 && b->n_blocks >= 0 && b->block_tokens >= 32 &&
            b->block_tokens <= 256 && b->block_tokens % 32 == 0 && array_ok(b->table, (int64_t)b->n_seqs * b->max_blocks) &&
            (b->first != nullptr ? array_ok(b->first, b->n_seqs) && array_ok(b->room, b->n_seqs) : array_ok(b->free, b->n_blocks));
 }

@@ -139,9 +139,10 @@ struct Tile {
     int see_lo[NT][2], see_hi[NT][2];  // positions that the column's row sees
     int last;                          // stored bytes from this position on mean nothing
     // 4 bits: positions that every row sees; the columns' own positions (kNoEnd: all that is held is seen, or no one reads
-    // the column); weights are 2^(score * unit + off), and a score above limit moves the reference
+    // the column); weights are 2^((score - mark) * unit + lift) -- the difference first, so that they stay in their range
+    // however large scores are -- and a score above limit moves the mark
     int all_lo, all_hi, held, window, pos[NT][2];
-    float off[NT][2], limit[NT][2];
+    float mark[NT][2], limit[NT][2];
     static constexpr int kNoEnd = 1 << 30;
 
     // rows: of the sequence and head, at least 1; row: the sequence's first in the token arrays
@@ -200,7 +201,7 @@ struct Tile {
                 pos[nt][k] = col < rows && a.causal ? at : kNoEnd;
                 last = max(last, see_hi[nt][k]);
                 all_lo = max(all_lo, see_lo[nt][k]), all_hi = min(all_hi, see_hi[nt][k]);
-                top[nt][k] = limit[nt][k] = -INFINITY, sum[nt][k] = off[nt][k] = 0.f;
+                top[nt][k] = limit[nt][k] = -INFINITY, sum[nt][k] = mark[nt][k] = 0.f;
                 if (kBits == 4) unit[nt][k] = fmaxf(unit[nt][k], 0x1p-126f);  // not 0: what is not seen stays -inf
             }
 #pragma unroll
@@ -366,9 +367,8 @@ struct Tile {
                     x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
                     x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
                     if (x > limit[nt][k]) {
-                        const float now = x * unit[nt][k], next = lift_of(4) - now;
-                        const float fade = limit[nt][k] == -INFINITY ? 0.f : exp2_approx(next - off[nt][k]);
-                        off[nt][k] = next, limit[nt][k] = __fdiv_rn(now + kFewGrow, unit[nt][k]);
+                        const float fade = limit[nt][k] == -INFINITY ? 0.f : exp2_approx((mark[nt][k] - x) * unit[nt][k]);
+                        mark[nt][k] = x, limit[nt][k] = x + __fdiv_rn(kFewGrow, unit[nt][k]);
                         sum[nt][k] *= fade;
 #pragma unroll
                         for (int i = 0; i < D / 16; ++i) o[nt][i][k] *= fade, o[nt][i][2 + k] *= fade;
@@ -383,7 +383,7 @@ struct Tile {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float& x = s[nt][i / 2][i % 2 * 2 + k];
-                    x = exp2_approx(fmaf(x, unit[nt][k], off[nt][k]));
+                    x = exp2_approx(fmaf(x - mark[nt][k], unit[nt][k], lift_of(4)));
                     part[i % 2] += x;
                 }
                 sum[nt][k] += part[0] + part[1];
@@ -463,7 +463,7 @@ struct Tile {
 
     // The reference of a column's weights, which are 2^lift_of(kBits) there.
     __device__ __forceinline__ float reference(int nt, int k) const {
-        return kBits == 8 ? top[nt][k] : limit[nt][k] == -INFINITY ? -INFINITY : lift_of(4) - off[nt][k];
+        return kBits == 8 ? top[nt][k] : limit[nt][k] == -INFINITY ? -INFINITY : mark[nt][k] * unit[nt][k];
     }
 
     // This lane's part of a column's sum becomes the column's.

@@ -379,3 +379,31 @@ def test_attend_by_both_long_kernels(cuda_lib, group, d):
             size = ((qq.abs() @ kk.abs().transpose(1, 2)).amax(-1) * d ** -0.5).transpose(0, 1).cpu().numpy()
             bound, lse_bound = R.attend_bounds(BF16, want, want_lse, mag, size)
             assert (np.abs(mine - want) <= bound).all() and (np.abs(mine_lse - want_lse) <= lse_bound).all()
+
+
+@pytest.mark.parametrize("new,size", [(1, 1e4), (1, 1e7), (1, 1e12), (40, 1e3), (40, 1e5)])
+def test_attend_scores_of_any_size(cuda_lib, new, size):
+    """Scores of up to 1e12 and more (2^23 in calls of many rows): one token of each row outweighs all others by far, so the row is
+    that token's values, but for rounding to the output's type and for the others, whose weights are e^-40 at most each; in every
+    kernel."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(3)
+    for lens in ([100, 60], [5000, 60]):
+        table, n = R.make_table(lens, 64, rng)
+        pool = R4.Pool(n, 64, 2, 64, rng)
+        q = torch.from_numpy(rng.standard_normal((2 * new, 4, 64))).to(BF16).cuda()
+        assert new == 1 or size * 64 * 8 * float(R4.SCALES[pool.ks.max()]) * 0.2 < 2.0 ** 23  # |q| |k| of 64 values, a fifth of the most
+        out, lse, status = mp.kv_attend(pool.cache(), batch_of(mp, table, lens, [new, new]), q, scale=size, want_lse=True)
+        assert not status.any() and torch.isfinite(lse).all()
+        for b, length in enumerate(lens):
+            k, v = R4.held(pool, table, b, 0, length)
+            for i in range(new):
+                for h in range(4):
+                    x = k[:length - new + i + 1, h // 2] @ q[b * new + i, h].double().cpu().numpy()
+                    order = np.sort(x)
+                    if len(x) > 1 and (order[-1] - order[-2]) * size < 40 + 2.0 ** -16 * order[-1] * size:
+                        continue  # two that rounding may bring together
+                    want = v[np.argmax(x), h // 2]
+                    others = len(x) * np.exp(-40.0) * np.abs(v).max()
+                    assert (np.abs(out[b * new + i, h].double().cpu().numpy() - want) <= 2.0 ** -8 * np.abs(want) + others).all()

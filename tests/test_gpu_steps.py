@@ -114,6 +114,16 @@ def test_extend_refuses_requests_one_by_one(cuda_lib, many):
     assert want["n_free"] <= n_blocks and 1 in want["status"]
 
 
+def test_extend_of_nothing(cuda_lib):
+    """No requests, requests without tokens or columns, and a pool without blocks."""
+    import paper_2203_00448_gb300 as mp
+
+    run_extend(mp, np.zeros((0, 3), np.int32), [], [], 32, 0, 0, 96, np.zeros(0, np.int32), 0, 0)
+    for n_tokens in (0, 5, 5000):
+        run_extend(mp, np.zeros((3, 0), np.int32), [0, 0, 0], [0, -1, 2], 32, n_tokens, 2, 0, np.zeros(0, np.int32), 0, 0)
+        run_extend(mp, np.zeros((3, 2), np.int32), [0, 0, 0], [0, -1, 2], 32, n_tokens, 2, 64, np.zeros(0, np.int32), 0, 0)
+
+
 def test_extend_step_after_step(cuda_lib):
     """Requests come, grow and go in a pool that is sometimes short; no block is ever anybody's twice."""
     import paper_2203_00448_gb300 as mp

@@ -75,7 +75,7 @@ def test_extend_argument_errors(lib):
     def call(b, s, ws=P, room=1 << 40):
         return lib.mp_kv_extend(b, s, ws, room, None)
 
-    for bad in (dict(n_seqs=-1), dict(max_blocks=-1), dict(n_blocks=-1), dict(block_tokens=0), dict(block_tokens=40), dict(block_tokens=288),
+    for bad in (dict(n_seqs=-1), dict(n_seqs=(1 << 28) + 1), dict(max_blocks=-1), dict(n_blocks=-1), dict(block_tokens=0), dict(block_tokens=40), dict(block_tokens=288),
                 dict(table=None), dict(table=P + 2), dict(free=None), dict(first=P), dict(first=P + 1, room=P), dict(first=P, room=P + 2)):
         assert call(blocks(**bad), step()) == E and lib.mp_kv_extend_workspace_bytes(blocks(**bad)) == 0
     names = ("lens", "n_free", "n_new", "lens_out", "n_free_out", "step_lens", "token_ptr", "positions", "slots", "seq_status")
