@@ -26,10 +26,10 @@
 // queries, first bytes: four trips one after another) and the joining launch, about 12 us.
 //
 // 4 bits.  A code times its scale is exact in f16, so both products take the values themselves: w_j = 2^(x_j - M), no value
-// scale in the sum.  The reference M stays until a score passes it by 2^5 (kFewGrow), which one vote a granule says; w
+// scale in the sum (they take sixteenths, which cost one shift a word less).  The reference M stays until a score passes it by 2^5 (kFewGrow), which one vote a granule says; w
 // has 11 bits down to 2^-24 of it.  A granule is 4.4 KB where it is 8.2 KB of 8 bits, and takes as many products and more
-// operations on codes: 600 instructions, of which 136 pick codes out of words, 128 scale them and 32 are products.
-// Measured: the 64 contexts 80 us (3.6 TB/s; 64 us without any operation on the bytes), the two long ones 119 us (4.6 TB/s;
+// operations on codes: about 580 instructions, of which 136 pick codes out of words, 128 scale them and 32 are products.
+// Measured: the 64 contexts 79 us (3.6 TB/s; 64 us without any operation on the bytes), the two long ones 118 us (4.7 TB/s;
 // 99): half of the cycles are integer operations, a quarter each f16 operations and products, and hardly any of the three
 // come at the same time.  Dropped: 64 tokens a step, products in two chains, 8 and 16 warps, four
 // granules ahead (89 and 128 us for 85 and 126), bulk copies for the ring (93 and 130).
@@ -118,7 +118,7 @@ __device__ __forceinline__ int page_of(const AttendArgs& a, const Cursor& c) {
 
 __device__ __forceinline__ void mma(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                     uint32_t b1) {
-    asm volatile(
+    asm(
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
@@ -202,7 +202,7 @@ struct Tile {
                 last = max(last, see_hi[nt][k]);
                 all_lo = max(all_lo, see_lo[nt][k]), all_hi = min(all_hi, see_hi[nt][k]);
                 top[nt][k] = limit[nt][k] = -INFINITY, sum[nt][k] = mark[nt][k] = 0.f;
-                if (kBits == 4) unit[nt][k] = fmaxf(unit[nt][k], 0x1p-126f);  // not 0: what is not seen stays -inf
+                if (kBits == 4) unit[nt][k] = fmaxf(unit[nt][k] * kSixteenth, 0x1p-126f);  // not 0: what is not seen stays -inf
             }
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
@@ -251,30 +251,29 @@ struct Tile {
             }
         }
     }
-    // A lane has D / 4 consecutive values of its two tokens of 16, of one group's scale.
+    // A lane has D / 4 consecutive values of its four tokens, of one group's scale; the two products of 16 tokens take turns.
     __device__ __forceinline__ void scores4(const uint8_t* kb, float (&s)[NT][2][4]) {
         const int lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
         const uint32_t scales = *reinterpret_cast<const uint32_t*>(kb + 16 * D + key4_scale<D>(g, t * (D / 4)));
+        Pack<uint32_t, D / 32> w[4];
+        Sixteenths x[4];
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            Pack<uint32_t, D / 32> w[2];
-            Steps x[2];
+        for (int r = 0; r < 4; ++r) {
+            w[r] = *reinterpret_cast<const Pack<uint32_t, D / 32>*>(kb + key4_byte<D>(r * 8 + g, t * (D / 4)));
+            x[r] = sixteenths_of((scales >> (8 * r) & 0xff) * 0x00800080u);
+        }
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                w[r] = *reinterpret_cast<const Pack<uint32_t, D / 32>*>(kb + key4_byte<D>(m * 16 + r * 8 + g, t * (D / 4)));
-                x[r] = steps_of((scales >> (8 * (2 * m + r)) & 0xff) * 0x00800080u);
-            }
+        for (int j = 0; j < D / 32; ++j)
 #pragma unroll
-            for (int j = 0; j < D / 32; ++j) {
+            for (int m = 0; m < 2; ++m) {
                 uint32_t a[2][4];
-                codes_to_f16(w[0].x[j], x[0], a[0]), codes_to_f16(w[1].x[j], x[1], a[1]);
+                codes_to_sixteenths(w[2 * m].x[j], x[2 * m], a[0]), codes_to_sixteenths(w[2 * m + 1].x[j], x[2 * m + 1], a[1]);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     mma(s[nt][m], a[0][0], a[1][0], a[0][1], a[1][1], qf[nt][2 * j][0], qf[nt][2 * j][1]);
                     mma(s[nt][m], a[0][2], a[1][2], a[0][3], a[1][3], qf[nt][2 * j + 1][0], qf[nt][2 * j + 1][1]);
                 }
             }
-        }
     }
 
     // Scores become weights p of the second product; lv, iv: log2 and inverse of the values' scale.
@@ -437,7 +436,7 @@ struct Tile {
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
             Pack<uint32_t, D / 32> w[2];
-            Steps x[2];
+            Sixteenths x[2];
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 w[r] = *reinterpret_cast<const Pack<uint32_t, D / 32>*>(vb + (2 * m + r) * 4 * D + lane * (D / 8));
@@ -446,12 +445,12 @@ struct Tile {
                     const int left = last - (base + m * 16 + r * 8 + 2 * t);
                     s2 &= left >= 2 ? ~0u : left == 1 ? 0xffffu : 0u;
                 }
-                x[r] = steps_of(s2);
+                x[r] = sixteenths_of(s2);
             }
 #pragma unroll
             for (int j = 0; j < D / 32; ++j) {
                 uint32_t a[2][4];
-                codes_to_f16(w[0].x[j], x[0], a[0]), codes_to_f16(w[1].x[j], x[1], a[1]);
+                codes_to_sixteenths(w[0].x[j], x[0], a[0]), codes_to_sixteenths(w[1].x[j], x[1], a[1]);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     mma(o[nt][2 * j], a[0][0], a[0][1], a[1][0], a[1][1], p[nt][m][0], p[nt][m][1]);
@@ -675,7 +674,7 @@ __global__ void __launch_bounds__(few_warps(D, NT) * 32, 1) k_kv_attend_few(Atte
                         const int64_t tok = cur.row + r / a.group;
                         const int qh = head * a.group + r % a.group;
                         T* dst = static_cast<T*>(a.out.data) + tok * a.out.token_stride + qh * a.out.head_stride;
-                        const float inv = l == 0.f ? 0.f : __fdiv_rn(1.f, l);
+                        const float inv = l == 0.f ? 0.f : __fdiv_rn(kBits == 8 ? 1.f : kSixteenth, l);
 #pragma unroll
                         for (int i = 0; i < D / 16; ++i) {
                             dst[x.value_of(i, g, 0)] = from_f32<T>(x.o[nt][i][k] * inv);
@@ -803,7 +802,7 @@ __global__ void __launch_bounds__(short_warps(NT) * 32, 1) k_kv_attend_short(Att
                 const float2 y = *reinterpret_cast<const float2*>(dyn + w * kMine + (in_tile * D + d) * sizeof(float));
                 sum += weight[w][in_tile] * f, o0 += y.x * f, o1 += y.y * f;
             }
-            const float inv = sum == 0.f ? 0.f : __fdiv_rn(1.f, sum);
+            const float inv = sum == 0.f ? 0.f : __fdiv_rn(kBits == 8 ? 1.f : kSixteenth, sum);
             const int64_t tok = s.lo + r / a.group;
             const int qh = head * a.group + r % a.group;
             T* dst = static_cast<T*>(a.out.data) + tok * a.out.token_stride + qh * a.out.head_stride + d;
@@ -960,7 +959,7 @@ __device__ void join_row(const AttendArgs& a, const FewWork& work, int64_t u, bo
     const int64_t tok = s.lo + r / a.group;
     const int qh = head * a.group + r % a.group;
     T* dst = static_cast<T*>(a.out.data) + tok * a.out.token_stride + qh * a.out.head_stride;
-    const float inv = l == 0.f ? 0.f : __fdiv_rn(1.f, l);
+    const float inv = l == 0.f ? 0.f : __fdiv_rn(kBits == 8 ? 1.f : kSixteenth, l);
 #pragma unroll
     for (int i = 0; i < kCols; ++i) o[i] *= inv;
     store_values<T, kCols>(dst + lane * kCols, a.wide_out, o);
