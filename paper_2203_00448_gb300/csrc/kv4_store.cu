@@ -4,9 +4,9 @@
 // x / s rounded to the nearest whole number of -7 .. 7: no value is off by more than half a step, and n s is exact in
 // f16, bf16 and f32.  A token's codes depend on no other token, so nothing that is stored is ever rounded again.
 //
-// Measured (8 heads of 128, GPU time): 253 single tokens written 5 us and read 6; 15,973 prompt tokens written 28 us (83 MB of them and
-// 17 of codes: 12 us at a copy's rate) and read back 16; 131,071 read back 105 us (6.4 TB/s, 95% of a copy's rate);
-// 32 x 300 tokens written 20, the prompts in 32 bits 43.  Writes are bound by instructions, 145 for 8 values of each lane
+// Measured (8 heads of 128, GPU time): 253 single tokens written 5 us and read 6; 15,973 prompt tokens written 27 us (66 MB of them and
+// 17 of codes: 12 us at a copy's rate) and read back 15; 131,071 read back 101 us (6.7 TB/s, a copy's rate);
+// 32 x 300 tokens written 19, the prompts in 32 bits 39.  Writes are bound by instructions, 145 for 8 values of each lane
 // (with rintf and conversions to integers, which run on a slow unit, and divisions it was 60 us).
 #include <algorithm>
 
@@ -15,7 +15,8 @@
 namespace mp {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kFewThreads = 512;  // few tokens: a CTA a sequence (253 of them: 128 threads 13.2, 256 11.1, 512 9.7 us with the timing)
+constexpr int kThreads = 128, kWarps = kThreads / 32;  // else (64, 128 and 256: prompts written 28.8, 26.8 and 28.8 us)
 constexpr int32_t kFewTokens = 16;  // up to this many a sequence, a CTA a sequence
 constexpr float kMost = 1800.f;     // 7.5 times the largest scale
 constexpr int kMostScale = 183;     // its byte: 240
@@ -193,13 +194,13 @@ __device__ __forceinline__ int granules_touched(const SeqView& s) {
 
 // Few tokens a sequence: one CTA a sequence, so that its status has one writer; a warp a granule, head and array.
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kFewThreads)
     k_kv4_write_few(mp_kv_cache c, mp_kv_batch bt, mp_tokens k, mp_tokens v, bool wide, int32_t* status) {
     for (int b = blockIdx.x; b < bt.n_seqs; b += gridDim.x) {
         const SeqView s = load_seq(bt, b, true);
         bool ok = s.st == MP_OK;
         const int tasks = granules_touched(s) * c.n_heads * 2;
-        for (int u = threadIdx.x / 32; u < tasks; u += kWarps)
+        for (int u = threadIdx.x / 32; u < tasks; u += kFewThreads / 32)
             ok &= store_unit<T, D>(c, bt, s, b, u / (2 * c.n_heads), u / 2 % c.n_heads, u % 2, k, v, wide);
         const bool bad = __syncthreads_or(!ok);
         if (threadIdx.x == 0) status[b] = bad ? MP_EINVAL : MP_OK;
@@ -282,7 +283,7 @@ __device__ __forceinline__ void read_values(const uint8_t* bytes, int from, int 
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 12)  // (131,071 tokens 101.5 us, 102.5 with as many registers as it likes)
     k_kv4_read(mp_kv_cache c, mp_kv_batch bt, mp_tokens k, mp_tokens v, bool wide, int32_t* status, int per_seq) {
     const int lane = threadIdx.x % 32;
     const int64_t units = (int64_t)bt.n_seqs * per_seq * c.n_heads * 2, warps = (int64_t)gridDim.x * kWarps;
@@ -322,7 +323,7 @@ cudaError_t write_as(const mp_kv_cache& c, const mp_kv_batch& bt, const mp_token
                      cudaStream_t stream) {
     const bool wide = rows_aligned(k) && rows_aligned(v);
     if (bt.max_tokens <= kFewTokens) {
-        k_kv4_write_few<T, D><<<(unsigned)std::min(bt.n_seqs, 1 << 20), kThreads, 0, stream>>>(c, bt, k, v, wide, status);
+        k_kv4_write_few<T, D><<<(unsigned)std::min(bt.n_seqs, 1 << 20), kFewThreads, 0, stream>>>(c, bt, k, v, wide, status);
         return cudaGetLastError();
     }
     cudaError_t e = cudaMemsetAsync(status, 0, sizeof(int32_t) * (size_t)bt.n_seqs, stream);

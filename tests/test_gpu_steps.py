@@ -225,6 +225,20 @@ def test_rotary_gradient(cuda_lib):
             assert abs(difference - grad[i]) <= 192 * 3 * 4 * 2.0 ** -24
 
 
+def test_rotary_past_32_bit_offsets(cuda_lib):
+    """Rows that are 2^30 values apart."""
+    import paper_2203_00448_gb300 as mp
+
+    wide = torch.empty(3, 1 << 30, dtype=torch.bfloat16, device="cuda")
+    x = wide[:, 40:104].view(3, 1, 64)
+    x.copy_(torch.randn(3, 1, 64, device="cuda"))
+    r, at = mp.Rotary(64), torch.tensor([3, 4, 5], dtype=torch.int32, device="cuda")
+    want = mp.rotary(r, at, x.contiguous())[0]
+    assert torch.equal(mp.rotary(r, at, x)[0], want)
+    mp.rotary(r, at, x, q_out=x)
+    assert torch.equal(x, want)
+
+
 def test_rotary_captured_and_on_another_stream(cuda_lib):
     import paper_2203_00448_gb300 as mp
 
