@@ -30,8 +30,9 @@
 // has 11 bits down to 2^-24 of it.  A granule is 4.4 KB where it is 8.2 KB of 8 bits, and takes as many products and more
 // operations on codes: about 580 instructions, of which 136 pick codes out of words, 128 scale them and 32 are products.
 // Measured: the 64 contexts 79 us (3.6 TB/s; 64 us without any operation on the bytes), the two long ones 118 us (4.7 TB/s;
-// 99): half of the cycles are integer operations, a quarter each f16 operations and products, and hardly any of the three
-// come at the same time.  Dropped: 64 tokens a step, products in two chains, 8 and 16 warps, four
+// 99).  The time goes by the number of instructions, at 0.6 a clock and scheduler: the work alone, without loads, takes 118 us of
+// the long ones' 127 (GPU time with the timing), 93 without the 128 operations that scale codes, 122 with integer ones in their
+// place.  Dropped: 64 tokens a step, products in two chains, 8 and 16 warps, four
 // granules ahead (89 and 128 us for 85 and 126), bulk copies for the ring (93 and 130).
 #pragma once
 
