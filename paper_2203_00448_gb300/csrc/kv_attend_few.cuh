@@ -368,7 +368,8 @@ struct Tile {
                     x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
                     if (x > limit[nt][k]) {
                         const float fade = limit[nt][k] == -INFINITY ? 0.f : exp2_approx((mark[nt][k] - x) * unit[nt][k]);
-                        mark[nt][k] = x, limit[nt][k] = x + __fdiv_rn(kFewGrow, unit[nt][k]);
+                        // rounded down: where scores are large a step of 32 bits is several powers of two of weight
+                        mark[nt][k] = x, limit[nt][k] = __fadd_rd(x, __fdiv_rd(kFewGrow, unit[nt][k]));
                         sum[nt][k] *= fade;
 #pragma unroll
                         for (int i = 0; i < D / 16; ++i) o[nt][i][k] *= fade, o[nt][i][2 + k] *= fade;

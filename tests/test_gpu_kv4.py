@@ -407,3 +407,40 @@ def test_attend_scores_of_any_size(cuda_lib, new, size):
                     want = v[np.argmax(x), h // 2]
                     others = len(x) * np.exp(-40.0) * np.abs(v).max()
                     assert (np.abs(out[b * new + i, h].double().cpu().numpy() - want) <= 2.0 ** -8 * np.abs(want) + others).all()
+
+
+@pytest.mark.parametrize("rows_a_head", [4, 12])
+@pytest.mark.parametrize("length,later", [(1000, 16), (2560, 1)])
+@pytest.mark.parametrize("unit,ahead", [(3.2, 2), (6.5, 1), (9.0, 1)])
+def test_attend_large_scores_a_step_apart(cuda_lib, unit, ahead, length, later, rows_a_head):
+    """Two tokens whose scores of 13,762,560 and `ahead` more (as the kernels for few rows multiply them, one step of 32 bits is 1
+    there) are a few powers of two apart, the larger one in a later granule of the same warp: the larger score may not pass the
+    reference by more than weights of 16 bits have room for.  Weights are off by 2^-11, the exponential and its argument by less
+    than 2^-18; the log-sum has seven roundings of 2^-24 of itself."""
+    import paper_2203_00448_gb300 as mp
+
+    heads, group, d = 2, 4, 64
+    new = rows_a_head // group
+    table = np.arange(-(-length // 64), dtype=np.int32)[None]
+    pool = R4.Pool(table.size, 64, heads, d, np.random.default_rng(61))
+    pool.k[:], pool.ks[:] = 8, 120  # zeros under the scale 1
+    for granule, more in ((0, 0), (later, ahead)):
+        at = (granule * 32 // 64, slice(None), granule * 32 % 64 + 5)
+        pool.k[at][:, :8], pool.ks[at][:, 0] = 15, 183  # 8 values of 7 * 240
+        pool.k[at][:, 32] = 8 + more
+    cache, batch = pool.cache(), batch_of(mp, table, [length], [new])
+    for dtype in (BF16, F16):
+        q = torch.zeros(new, heads * group, d, dtype=dtype, device="cuda")
+        q[..., :8], q[..., 32] = 1.0, 2.0 ** -10  # times 2^14 in the kernels, and keys a sixteenth
+        scale = float(np.float32(unit * 2.0 ** 10 / np.log2(np.e)))
+        out, lse, status = mp.kv_attend(cache, batch, q, scale=scale, want_lse=True)
+        assert not status.any()
+        w = np.exp(-scale * ahead * 2.0 ** -10)
+        _, v = R4.held(pool, table, 0, 0, length)
+        low, high = (v[granule * 32 + 5].repeat(group, 0) for granule in (0, later))
+        want, mag = (w * low + high) / (w + 1), (w * np.abs(low) + np.abs(high)) / (w + 1)
+        near = mag * (2.0 ** -11 + 2.0 ** -18)
+        bound = near + (np.abs(want) + near) * torch.finfo(dtype).eps / 2
+        assert (np.abs(out.double().cpu().numpy() - want) <= bound).all()
+        want_lse = scale * (13762560 + ahead) * 2.0 ** -10 + np.log1p(w)
+        assert (np.abs(lse.double().cpu().numpy() - want_lse) <= want_lse * 2.0 ** -21).all()
