@@ -135,7 +135,7 @@ def rotary(rotation: Rotary, positions: torch.Tensor, q: torch.Tensor | None, k:
     if some is None or (q is None and q_out is not None) or (k is None and k_out is not None):
         raise ValueError("q or k is needed, and an output only for what is there")
     _tensor("positions", positions, torch.int32, some.shape[:1], rotation.device)
-    structs, outs, empty = [], [], some.shape[0] == 0
+    structs, outs = [], []
     for name, x, out in (("q", q, q_out), ("k", k, k_out)):
         if x is None:
             structs += (None, None)
@@ -150,13 +150,12 @@ def rotary(rotation: Rotary, positions: torch.Tensor, q: torch.Tensor | None, k:
             b = _lib.MpTokens(out.data_ptr() or None, heads * dim, dim, heads, a.dtype)
         else:
             b = _rows(name + "_out", out, x, index)
-        structs += (a, b)
+        structs += (a, b) if heads else (None, None)  # nothing of a tensor without heads turns
         outs.append(out)
-        empty = empty or heads == 0
     if rotation.dim > some.shape[2]:
         raise ValueError(f"dim is {rotation.dim}, heads have {some.shape[2]} values")
-    if not empty:
-        qi, qo, ki, ko = structs
+    qi, qo, ki, ko = structs
+    if some.shape[0] > 0 and (qi is not None or ki is not None):
         _check("mp_rotary", _lib.load().mp_rotary(rotation._ref, positions.data_ptr(), some.shape[0], some.shape[2], qi, ki, qo, ko,
                                                   1 if inverse else 0, stream_ptr))
     return tuple(outs)

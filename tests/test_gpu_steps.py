@@ -260,6 +260,25 @@ def test_rotary_captured_and_on_another_stream(cuda_lib):
     assert mp.rotary(r, at[:0], x[:0])[0].shape == (0, 4, 64)
 
 
+@pytest.mark.parametrize("inverse", [False, True])
+def test_rotary_of_no_heads(cuda_lib, inverse):
+    """Queries or keys without heads leave the other to be turned, as a call without them does."""
+    import paper_2203_00448_gb300 as mp
+
+    r, at = mp.Rotary(64, layout="interleaved"), torch.arange(5, 12, dtype=torch.int32, device="cuda")
+    x = torch.randn(7, 3, 64, device="cuda")
+    want = mp.rotary(r, at, x, inverse=inverse)[0]
+    assert not torch.equal(want, x)
+    none = x[:, :0]
+    for q, k in ((none, x), (x, none)):
+        outs = mp.rotary(r, at, q, k, inverse=inverse)
+        assert [y.shape for y in outs] == [q.shape, k.shape] and torch.equal(outs[0] if k is none else outs[1], want)
+    y = x.clone()
+    mp.rotary(r, at, none, y, q_out=none, k_out=y, inverse=inverse)
+    assert torch.equal(y, want)
+    assert [y.shape for y in mp.rotary(r, at, none, none)] == [none.shape] * 2
+
+
 @pytest.mark.parametrize("bits", [4, 8])
 def test_steps_together(cuda_lib, bits):
     """What a server does each step: blocks, positions, rotated queries and keys, the cache, attention; against plain attention

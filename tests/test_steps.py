@@ -173,6 +173,38 @@ def test_calls_check_their_tensors(monkeypatch):
         mp.kv_extend(mp.KvBlocks(4, 3, 32, 20, device="cpu"), new, 4, step=first, workspace=ws)
 
 
+@pytest.mark.parametrize("inverse", [False, True])
+@pytest.mark.parametrize("hq,hk", [(0, 3), (3, 0), (0, 0), (2, 3)])
+def test_rotary_of_no_heads(monkeypatch, hq, hk, inverse):
+    """A tensor without heads has nothing to turn; the other one is turned all the same."""
+    from paper_2203_00448_gb300 import rotation
+
+    reached = []
+
+    class Library:
+        def mp_rotary(self, *args):
+            reached.append(args[4:8])
+            return 0
+
+    monkeypatch.setattr(_lib, "load", Library)
+    monkeypatch.setattr(rotation, "_away", lambda *args: False)
+    monkeypatch.setattr(rotation, "_stream", lambda *args: 0)
+    at, q, k = torch.zeros(2, dtype=torch.int32), torch.zeros(2, hq, 64), torch.zeros(2, hk, 64)
+    for given in ({}, dict(q_out=q, k_out=k)):
+        reached.clear()
+        outs = mp.rotary(mp.Rotary(32, device="cpu"), at, q, k, inverse=inverse, **given)
+        assert [x.shape for x in outs] == [q.shape, k.shape]
+        if hq == hk == 0:
+            assert not reached
+            continue
+        (qi, ki, qo, ko), = reached
+        for heads, x, i, o in ((hq, q, qi, qo), (hk, k, ki, ko)):
+            assert (i is None) == (o is None) == (heads == 0)
+            assert heads == 0 or i.data == x.data_ptr()
+        for o, out in ((qo, outs[0]), (ko, outs[1])):
+            assert o is None or o.data == out.data_ptr()
+
+
 def test_frequencies():
     """Each kind against its definition at single pairs, and what the integer turns stand for."""
     f, a = mp.rotary_frequencies(128)
