@@ -124,6 +124,7 @@ class KvBatch(_Fixed):
     max_len >= lens (default what the table has room for).  Either is at most 2^28."""
 
     _fixed = frozenset(("table", "lens", "token_ptr", "n_tokens", "max_tokens", "max_len", "n_seqs", "device"))
+    _block_tokens = None  # of the table's blocks, where it is known
 
     def __init__(self, table: torch.Tensor, lens: torch.Tensor, token_ptr: torch.Tensor, n_tokens: int,
                  max_tokens: int | None = None, max_len: int | None = None):
@@ -149,6 +150,8 @@ class KvBatch(_Fixed):
         if made is None:
             if cache.device != self.device:
                 raise ValueError(f"the batch is on {self.device}, the cache on {cache.device}")
+            if self._block_tokens not in (None, cache.block_tokens):
+                raise ValueError(f"the step has blocks of {self._block_tokens} tokens, the cache of {cache.block_tokens}")
             room = min(self.table.shape[1] * cache.block_tokens, _MOST)
             s = _lib.MpKvBatch(self.n_seqs, self.table.shape[1], self.max_tokens,
                                room if self.max_len is None else int(self.max_len), self.n_tokens, _ptr(self.table),
@@ -198,8 +201,8 @@ class KvBlocks(_Fixed):
 
 
 class KvStep(_Fixed):
-    """What kv_extend has made: the step's batch (its lens are -1 where a request takes no part), positions int32[n_tokens],
-    slots int64[n_tokens] and the status of each request."""
+    """What kv_extend has made: the step's batch (its lens are -1 where a request takes no part; for caches of the blocks' size),
+    positions int32[n_tokens], slots int64[n_tokens] and the status of each request."""
 
     _fixed = frozenset(("batch", "positions", "slots", "status"))
 
@@ -215,7 +218,7 @@ class KvStep(_Fixed):
         positions, slots = torch.empty(n_tokens, dtype=i32, device=dev), torch.empty(n_tokens, dtype=torch.int64, device=dev)
         batch = KvBatch.__new__(KvBatch)  # (what KvBatch checks of its arguments is so of these)
         batch.__dict__.update(table=blocks.table, lens=lens, token_ptr=token_ptr, n_tokens=n_tokens, max_tokens=max_tokens,
-                              max_len=max_len, n_seqs=n, device=dev, _made={})
+                              max_len=max_len, n_seqs=n, device=dev, _made={}, _block_tokens=blocks.block_tokens)
         old, free = blocks.lens.data_ptr() or None, None if blocks.n_free is None else blocks.n_free.data_ptr()
         struct = _lib.MpKvExtension(n_tokens, max_tokens, max_len, old, free, None, old, free, lens.data_ptr() or None,
                                     token_ptr.data_ptr(), positions.data_ptr() or None, slots.data_ptr() or None,

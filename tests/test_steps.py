@@ -173,6 +173,21 @@ def test_calls_check_their_tensors(monkeypatch):
         mp.kv_extend(mp.KvBlocks(4, 3, 32, 20, device="cpu"), new, 4, step=first, workspace=ws)
 
 
+@pytest.mark.parametrize("kind", [mp.KvCache, mp.KvCache4])
+def test_steps_go_with_caches_of_their_block_size(kind):
+    """Blocks of another size are other tokens' places, even where the step's lengths fit into the table's columns."""
+    blocks = mp.KvBlocks(2, 4, 64, 10, device="cpu")
+    step = mp.KvStep(blocks, 3, 2, 100)
+    assert step.batch._for(kind(10, 64, 2, 64, "cpu"))[1] == (3, 2, 64)
+    for other in (32, 96, 128):
+        with pytest.raises(ValueError, match="blocks of 64 tokens"):
+            step.batch._for(kind(10, other, 2, 64, "cpu"))
+    # a batch of the user's own tables may be of any
+    own = mp.KvBatch(blocks.table, blocks.lens, step.batch.token_ptr, 3, 2, 100)
+    for other in (32, 64):
+        own._for(kind(10, other, 2, 64, "cpu"))
+
+
 @pytest.mark.parametrize("inverse", [False, True])
 @pytest.mark.parametrize("hq,hk", [(0, 3), (3, 0), (0, 0), (2, 3)])
 def test_rotary_of_no_heads(monkeypatch, hq, hk, inverse):
