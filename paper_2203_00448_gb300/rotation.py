@@ -29,7 +29,7 @@ def rotary_frequencies(dim: int, base: float = 10000.0, scaling: dict | None = N
     base    factor                          base times factor ** (dim / (dim - 2)): the slowest pair is divided by factor
     parts   factor, original, fast, slow    pairs that turn `fast` times over the original length stay, those that turn `slow`
                                             times are divided by factor, a ramp over the pairs' indexes between; amplitude 0.1
-                                            ln(factor) + 1
+                                            ln(factor) + 1, 1 for factors below 1
     bands   factor, original, low, high     the same with a ramp over the number of turns, from low (divided) to high (as they
                                             are); amplitude 1
     """
@@ -64,7 +64,7 @@ def rotary_frequencies(dim: int, base: float = 10000.0, scaling: dict | None = N
     place = [dim * math.log(original / (2 * math.pi * turns)) / (2 * math.log(base)) for turns in (hi, lo)]
     first, last = max(0, math.floor(place[0])), min(dim - 1, math.ceil(place[1]))
     scaled = ((index - first) / max(last - first, 1e-3)).clamp(0, 1)
-    return f * (1 - scaled) + f / factor * scaled, 0.1 * math.log(factor) + 1
+    return f * (1 - scaled) + f / factor * scaled, 0.1 * math.log(max(factor, 1.0)) + 1
 
 
 def _turns(frequencies):

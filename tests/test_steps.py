@@ -239,6 +239,13 @@ def test_frequencies():
     assert [int(t) % (1 << 64) for t in r.turns] == [1 << 63, 3 << 62]
 
 
+def test_amplitude_of_parts_is_1_up_to_a_factor_of_1():
+    """Only longer contexts need the larger amplitude: ln of a factor below 1 would make it less than 1."""
+    for factor, want in ((0.25, 1.0), (1.0, 1.0), (1.5, 0.1 * math.log(1.5) + 1), (16.0, 0.1 * math.log(16) + 1)):
+        scaling = {"kind": "parts", "factor": factor, "original": 4096, "fast": 32.0, "slow": 1.0}
+        assert mp.rotary_frequencies(64, scaling=scaling)[1] == want and mp.Rotary(64, scaling=scaling, device="cpu").amplitude == want
+
+
 def test_plain_quantisation():
     rng = np.random.default_rng(0)
     assert R4.SCALES[183] == 240 and (np.diff(R4.SCALES) > 0).all()
