@@ -631,10 +631,11 @@ typedef struct mp_rotation {
 
 /* Turns each pair (x, y) of token i's heads by the angle a = positions[i] * turns: out = amplitude * (x cos a - y sin
  * a, x sin a + y cos a); with inverse != 0 by -a, which makes gradients with respect to the outputs into those
- * with respect to the inputs.  Elements from dim on are copied.  The angle is reduced as an integer, exactly; products
- * are taken in 32 bits and rounded once.  positions: int32[n_tokens] device, any value.  head_dim even, at most 1,024, dim
- * at most head_dim.  q, k, q_out, k_out: [n_tokens] rows of any mp_dtype, the same for all; k and k_out NULL, or q and
- * q_out.  An output may be its input (same data and strides); any other overlap is not allowed. */
+ * with respect to the inputs.  Elements from dim on are copied.  The angle is reduced as an integer, exactly (an error of
+ * turns itself counts as often as the position says); products are taken in 32 bits and rounded once.  positions:
+ * int32[n_tokens] device, any value.  head_dim even, at most 1,024, dim at most head_dim.  q, k, q_out, k_out: [n_tokens]
+ * rows of any mp_dtype, the same for all; k and k_out NULL, or q and q_out.  An output may be its input (same data and
+ * strides); any other overlap is not allowed. */
 mp_status mp_rotary(const mp_rotation *rotation, const int32_t *positions, int64_t n_tokens, int32_t head_dim,
                     const mp_tokens *q, const mp_tokens *k, const mp_tokens *q_out, const mp_tokens *k_out,
                     int32_t inverse, void *stream);

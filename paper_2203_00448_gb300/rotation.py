@@ -68,7 +68,8 @@ def rotary_frequencies(dim: int, base: float = 10000.0, scaling: dict | None = N
 
 
 def _turns(frequencies):
-    """Turns a position, times 2^64, whole turns left out: int64 with the bits of the unsigned number."""
+    """Turns a position, times 2^64, whole turns left out: int64 with the bits of the unsigned number; as exact as doubles,
+    2^-52 of a frequency's turns."""
     out = []
     for f in frequencies.tolist():
         if not math.isfinite(f):

@@ -1,6 +1,7 @@
 """Checks of arguments of the 4-bit cache, of kv_extend and of rotary, and the tests' own plain forms, without a GPU."""
 import ctypes
 import math
+from fractions import Fraction
 
 import numpy as np
 import pytest
@@ -244,6 +245,30 @@ def test_amplitude_of_parts_is_1_up_to_a_factor_of_1():
     for factor, want in ((0.25, 1.0), (1.0, 1.0), (1.5, 0.1 * math.log(1.5) + 1), (16.0, 0.1 * math.log(16) + 1)):
         scaling = {"kind": "parts", "factor": factor, "original": 4096, "fast": 32.0, "slow": 1.0}
         assert mp.rotary_frequencies(64, scaling=scaling)[1] == want and mp.Rotary(64, scaling=scaling, device="cpu").amplitude == want
+
+
+def test_turns_are_as_near_as_doubles():
+    """Turns a position times 2^64, against pi from its series 16 atan(1/5) - 4 atan(1/239) in whole numbers of 400 bits: the
+    division in doubles and the double of 2 pi leave less than 2^-52 of a frequency's turns, the last rounding half a unit."""
+    one = 1 << 400
+
+    def atan(n):
+        total, power, k = 0, one // n, 0
+        while power:
+            total += (-1) ** k * (power // (2 * k + 1))
+            power //= n * n
+            k += 1
+        return total
+
+    two_pi = 2 * (16 * atan(5) - 4 * atan(239))
+    given = mp.rotary_frequencies(128)[0].tolist() + [-f for f in mp.rotary_frequencies(40, base=500000.0)[0].tolist()] + \
+        [0.0, 3.0, math.pi, -math.pi / 2, 1e-300, 2.0 ** -70, 12345.678]
+    r = mp.Rotary(2 * len(given), frequencies=given, device="cpu")
+    for f, t in zip(given, r.turns.tolist()):
+        n, d = f.as_integer_ratio()
+        want = Fraction(n << 464, d * two_pi)
+        off = abs((t - want + (1 << 63)) % (1 << 64) - (1 << 63))
+        assert off <= abs(want) / 2 ** 52 + Fraction(1, 2), f
 
 
 def test_plain_quantisation():
