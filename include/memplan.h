@@ -478,7 +478,8 @@ size_t mp_kv_attend_workspace_bytes(const mp_kv_cache *cache, const mp_kv_batch 
  * 2^-28 of a row's largest (2^-21 of a value that it may pass by 2^8, in calls of
  * more than 16 rows a head), fewer below, nothing below 2^-38 (2^-31).  Query
  * elements below 2^-28 of their row's largest lose bits alike.  The v_scales that a
- * query sees may differ by a factor of 2^100.
+ * query sees may differ by a factor of 2^100.  scale * q . k has to stay below 2^23 in
+ * magnitude: the weights of larger ones may leave the range of 16 bits.
  * q, out: MP_F16 or MP_BF16, the same for both; n_heads a multiple of the
  * cache's, at most 1,024 times it; max_tokens times that multiple at most 2^28.
  * scale > 0, finite.  lse: float[n_tokens][n_heads] or NULL.
@@ -535,7 +536,8 @@ mp_status mp_kv_four_read(const mp_kv4_cache *cache, const mp_kv_batch *batch, c
 /* As mp_kv_attend_workspace_bytes and mp_kv_attend; keys and values enter the products
  * as f16 without a rounding.  Weights have 11 bits of precision down to 2^-24 of a value
  * that a row's largest may pass by 2^5, and vanish below 2^-34 of it; in calls of more than 16 rows a head
- * 2^-21, 2^8 and 2^-31, as there, where scale * q . k has to stay below 2^23 in magnitude. */
+ * 2^-21, 2^8 and 2^-31, as there.  In these scale * q . k has to stay below 2^23 in magnitude; in calls of up to 16 rows
+ * a head it may be as large as 32 bits hold (below 2^127). */
 size_t mp_kv_four_attend_workspace_bytes(const mp_kv4_cache *cache, const mp_kv_batch *batch, int32_t n_q_heads);
 mp_status mp_kv_four_attend(const mp_kv4_cache *cache, const mp_kv_batch *batch, const mp_tokens *q, float scale,
                         int32_t causal, int32_t window, const mp_tokens *out, float *lse, int32_t *seq_status,

@@ -343,8 +343,9 @@ def kv_attend(cache: KvCache, batch: KvBatch, q: torch.Tensor, scale: float | No
               workspace: Workspace | None = None, stream=None):
     """Attention of the call's queries ([n_tokens, query heads, head_dim], float16 or bfloat16) over what their
     sequences hold: causal unless told otherwise, over the last `window` positions if that is not 0, scale 1 /
-    sqrt(head_dim) unless given.  Returns (out, lse or None, status); a query that sees nothing gets 0 and -inf.  Scratch
-    is the stream's unless given, and the graph's own in a capture."""
+    sqrt(head_dim) unless given.  Returns (out, lse or None, status); a query that sees nothing gets 0 and -inf.  Scores
+    (scale * q . k) have to stay below 2^23 in magnitude (over 4 bits in calls of more than 16 rows a head; in smaller ones
+    they may be of any size).  Scratch is the stream's unless given, and the graph's own in a capture."""
     if _away(cache, stream):
         with _at(cache, stream):
             return kv_attend(cache, batch, q, scale, causal, window, out, lse, want_lse, status, workspace)

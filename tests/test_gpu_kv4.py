@@ -444,3 +444,42 @@ def test_attend_large_scores_a_step_apart(cuda_lib, unit, ahead, length, later, 
         assert (np.abs(out.double().cpu().numpy() - want) <= bound).all()
         want_lse = scale * (13762560 + ahead) * 2.0 ** -10 + np.log1p(w)
         assert (np.abs(lse.double().cpu().numpy() - want_lse) <= want_lse * 2.0 ** -21).all()
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("new,lens", [(1, [100, 90]), (1, [5000, 4000]), (3, [900, 2600]), (40, [900, 5000])])
+def test_attend_scores_near_the_limit(cuda_lib, bits, new, lens):
+    """Scores of just under 2^23, all of a row's within 4.5 of each other: 32 bits leave them off by less than 1 each (1.45 as powers of
+    two), so weights are off by e at most and outputs are means of the values all the same, whichever value of a row is the
+    reference: between the least and the largest, but for the weights' 2^-11 and the output's rounding."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(67)
+    heads, group, d, block = 2, 4, 64, 64
+    table, n = R.make_table(lens, block, rng)
+    kind = R4 if bits == 4 else R
+    pool = kind.Pool(n, block, heads, d, rng)
+    code = rng.integers(0, 8, pool.k.shape[:3])
+    if bits == 4:
+        pool.k[:], pool.ks[:] = 8, 120  # zeros under the scale 1
+        pool.k[..., :8], pool.ks[..., 0] = 15, 183  # 8 values of 7 * 240
+        pool.k[..., 32] = 8 + code
+        most, step = 8 * 1680.0, 2.0 ** -10
+    else:
+        pool.k[:], pool.ks[:] = 0, 4.0
+        pool.k[..., :8] = 0x7e  # 448
+        pool.k[..., 32] = R.to_byte(code.astype(float))
+        most, step = 8 * 1792.0, 2.0 ** -12
+    scale = (2.0 ** 23 - 8) / most
+    assert 7 * step * float(pool.ks.flat[0] if bits == 8 else 1) * scale < 4.5
+    q = torch.zeros(2 * new, heads * group, d, dtype=BF16, device="cuda")
+    q[..., :8], q[..., 32] = 1.0, step
+    out, lse, status = mp.kv_attend(pool.cache(), batch_of(mp, table, lens, [new, new]), q, scale=scale, want_lse=True)
+    assert not status.any() and (torch.abs(lse / 2.0 ** 23 - 1) < 2.0 ** -18).all()
+    out = out.double().cpu().numpy()
+    for b, length in enumerate(lens):
+        _, v = kind.held(pool, table, b, 0, length)
+        low, high, size = (x.repeat(group, 0) for x in (v.min(0), v.max(0), np.abs(v).max(0)))
+        for i in range(new):
+            mine = out[b * new + i]
+            assert (mine >= low - size * 2.0 ** -7).all() and (mine <= high + size * 2.0 ** -7).all()
