@@ -78,6 +78,12 @@ __device__ __forceinline__ float row_factor(float most) {
     return __uint_as_float((uint32_t)min(268 - e, 254) << 23);
 }
 
+// What a row's products with keys are multiplied by, as powers of two.  Finite, so that products of 0 stay 0 under the largest
+// scales; where the bound is met, other scores over 4 bits are of 2^77 and more anyway.
+__device__ __forceinline__ float row_unit(float scale, float factor) {
+    return fminf(__fdiv_rn(scale * 1.4426950408889634f, factor), 0x1p122f);
+}
+
 // The scale of a block of values as the kernels use it: they divide by it and take its logarithm.  Sums of weights over
 // scales stay finite: 2^28 tokens of weight 2^15 over 2^-84 make 2^127.  A smaller scale, 0 among them, counts as 0: its
 // bytes are taken as zeros.

@@ -190,7 +190,7 @@ struct Tile {
                     for (int k = 0; k < 2; ++k)
                         qf[nt][i][k] = pack_f16(to_f32(raw[i & ~1].x[i % 2 * 2 + k]) * f, to_f32(raw[i | 1].x[i % 2 * 2 + k]) * f);
             }
-            const float mine = __fdiv_rn(a.scale * 1.4426950408889634f, f);
+            const float mine = row_unit(a.scale, f);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 unit[nt][k] = __shfl_sync(~0u, mine, (2 * t + k) * 4);

@@ -653,7 +653,7 @@ __device__ void softmax_role(const AttendArgs& a, const ManyWork& work, Smem<D>&
                 for (int j = 0; j < 8; j += 2) most = max3(most, fabsf(to_f32(e[j])), fabsf(to_f32(e[j + 1])));
             }
             const float f = row_factor(most);
-            unit = __fdiv_rn(a.scale * 1.4426950408889634f, f);
+            unit = row_unit(a.scale, f);
 #pragma unroll 2
             for (int i = 0; i < D / 8; ++i) {
                 const uint4 v = row[i * 8];

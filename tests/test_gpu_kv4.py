@@ -483,3 +483,29 @@ def test_attend_scores_near_the_limit(cuda_lib, bits, new, lens):
         for i in range(new):
             mine = out[b * new + i]
             assert (mine >= low - size * 2.0 ** -7).all() and (mine <= high + size * 2.0 ** -7).all()
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("new,lens", [(1, [100, 90]), (1, [5000, 4000]), (3, [900, 2600]), (40, [900, 5000])])
+def test_attend_zero_queries_under_any_scale(cuda_lib, bits, new, lens):
+    """Scores of 0 are 0 under the largest scale too: every value that a row sees weighs the same.  Sums of 5,000 values under
+    equal weights in 32 bits, 16 at a time, each off by 2^-22 of the sum of magnitudes: 2^-13."""
+    import paper_2203_00448_gb300 as mp
+
+    rng = np.random.default_rng(71)
+    heads, group, d = 2, 4, 64
+    table, n = R.make_table(lens, 64, rng)
+    kind = R4 if bits == 4 else R
+    pool = kind.Pool(n, 64, heads, d, rng)
+    q = torch.zeros(2 * new, heads * group, d, dtype=BF16, device="cuda")
+    for scale in (1e36, 1e38, 3.4e38):
+        out, lse, status = mp.kv_attend(pool.cache(), batch_of(mp, table, lens, [new, new]), q, scale=scale, want_lse=True)
+        assert not status.any()
+        out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+        for b, length in enumerate(lens):
+            _, v = kind.held(pool, table, b, 0, length)
+            for i in range(new):
+                seen = v[:length - new + i + 1].repeat(group, 1)
+                want, size = seen.mean(0), np.abs(seen).mean(0)
+                assert (np.abs(out[b * new + i] - want) <= size * (2.0 ** -13 + 2.0 ** -20) + np.abs(want) * 2.0 ** -8).all()
+                assert (np.abs(lse[b * new + i] - np.log(len(seen))) <= 2.0 ** -18).all()
