@@ -90,7 +90,8 @@ __device__ __forceinline__ uint32_t masked_or(uint32_t x, uint32_t mask, uint32_
     asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(x), "r"(mask), "r"(bits));
     return r;
 }
-// 8 codes of a word as f16 pairs of codes i and i + 4: a code that is moved to bits 6-9 under the exponent of 16 is 16 +
+// 8 codes of a word as f16 pairs of codes i and i + 4, by the well-known way of widening small whole numbers, their bits placed in the
+// fraction under a fixed exponent: a code that is moved to bits 6-9 under the exponent of 16 is 16 +
 // u, at bits 2-5 under that of 256 it is 256 + u, so that 10 operations make 8 values.
 __device__ __forceinline__ void codes_to_f16(uint32_t w, const Steps& s, uint32_t* pairs) {
     const uint32_t lo = w << 2, hi = w >> 6;

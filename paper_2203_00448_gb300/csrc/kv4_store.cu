@@ -6,8 +6,10 @@
 //
 // Measured (8 heads of 128, GPU time): 253 single tokens written 5 us and read 6; 15,973 prompt tokens written 27 us (66 MB of them and
 // 17 of codes: 12 us at a copy's rate) and read back 15; 131,071 read back 101 us (6.7 TB/s, a copy's rate);
-// 32 x 300 tokens written 19, the prompts in 32 bits 39.  Writes are bound by instructions, 145 for 8 values of each lane
-// (with rintf and conversions to integers, which run on a slow unit, and divisions it was 60 us).
+// 32 x 300 tokens written 19, the prompts in 32 bits 39.  Writes take 145 instructions for 8 values of each lane, which issue in 68% of
+// the cycles (with rintf and conversions to integers, which run on a slow unit, and divisions it was 60 us); the others go to
+// the trips for values, four steps (of 32 bits two) at a time with none on its way under the arithmetic.  One prompt of 8,192 tokens
+// with 255 single tokens takes 194 us to write and 156 to read back (16 and 12 in two calls): units are laid out for the longest sequence.
 #include <algorithm>
 
 #include "kv.cuh"
@@ -17,7 +19,10 @@ namespace {
 
 constexpr int kFewThreads = 512;  // few tokens: a CTA a sequence (253 of them: 128 threads 13.2, 256 11.1, 512 9.7 us with the timing)
 constexpr int kThreads = 128, kWarps = kThreads / 32;  // else (64, 128 and 256: prompts written 28.8, 26.8 and 28.8 us)
-constexpr int32_t kFewTokens = 16;  // up to this many a sequence, a CTA a sequence
+// Up to this many tokens a sequence, a CTA a sequence (GPU time with it and without: 8 sequences of 1 token 2.0 and 2.1 us, of 16 6.1
+// and 6.1, of 24 8.3 and 8.1; 64 of 1 token 1.8 and 3.1, of 8 4.1 and 4.1, of 16 7.5 and 6.1; 253 of 1 token 2.0 and 4.1, of 8 6.1 and
+// 8.2, of 16 10.2 and 12.3): what few sequences of many tokens lose by it many of one token gain.
+constexpr int32_t kFewTokens = 16;
 constexpr float kMost = 1800.f;     // 7.5 times the largest scale
 constexpr int kMostScale = 183;     // its byte: 240
 

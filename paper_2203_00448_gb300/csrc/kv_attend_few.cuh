@@ -29,11 +29,12 @@
 // scale in the sum (they take sixteenths, which cost one shift a word less).  The reference M stays until a score passes it by 2^5 (kFewGrow), which one vote a granule says; w
 // has 11 bits down to 2^-24 of it.  A granule is 4.4 KB where it is 8.2 KB of 8 bits, and takes as many products and more
 // operations on codes: about 580 instructions, of which 136 pick codes out of words, 128 scale them and 32 are products.
-// Measured: the 64 contexts 79 us (3.6 TB/s; 64 us without any operation on the bytes), the two long ones 118 us (4.7 TB/s;
-// 99).  The time goes by the number of instructions, at 0.6 a clock and scheduler: the work alone, without loads, takes 118 us of
-// the long ones' 127 (GPU time with the timing), 93 without the 128 operations that scale codes, 122 with integer ones in their
-// place.  Dropped: 64 tokens a step, products in two chains, 8 and 16 warps, four
-// granules ahead (89 and 128 us for 85 and 126), bulk copies for the ring (93 and 130).
+// Measured: the 64 contexts 80 us (3.6 TB/s; 64 us without any operation on the bytes), the two long ones 119 us (4.7 TB/s;
+// 99).  What grows with the granules does so at 5.7 TB/s, 84% of a copy: 64 contexts of one length take 22 us (GPU time) and 50 for
+// each 4,096 tokens of all of them; ragged ones of the same bytes 7 more.  The growing part goes by the number of instructions,
+// at 0.6 a clock and scheduler: the work alone, without loads, takes 118 us of the long ones' 127 (GPU time with the timing), 93
+// without the 128 operations that scale codes, 122 with integer ones in their place.  Dropped: 64 tokens a step, 8 and 16
+// warps, four granules ahead (89 and 128 us for 85 and 126), bulk copies for the ring (93 and 130).
 #pragma once
 
 #include <algorithm>
@@ -45,15 +46,18 @@ namespace mp {
 namespace {
 
 // Warps of a CTA, and granules that the ring of each holds (192 KB at most in all). Registers bound the warps, an even
-// share for the four schedulers: 12 of D = 128 with 16 rows spill (64 ragged contexts 127 -> 153 us, 10 160), 12 instead of
-// 16 of D = 64 with 8 rows take 66 for 60 us. 8 with 3 granules for 12 with 2: 164 for 170 us over two of 262,144 tokens,
-// but 103 for 97 over 64 ragged ones; 3 granules for 2 never paid otherwise (130 for 127).
+// share for the four schedulers: 12 of D = 128 with 16 rows spill (64 ragged contexts 127 -> 153 us, 10 160; D = 64 with 16 rows
+// over 8 bits keeps 8 bytes a thread in memory), 12 instead of 16 of D = 64 with 8 rows take 66 for 60 us. 8 with 3 granules for
+// 12 with 2: 164 for 170 us over two of 262,144 tokens, but 103 for 97 over 64 ragged ones; 3 granules for 2 never paid otherwise
+// (130 for 127).
 constexpr int few_warps(int d, int nt) { return d == 128 ? (nt == 1 ? 12 : 8) : (nt == 1 ? 16 : 12); }
 constexpr int kFewStages = 2;
 constexpr int short_warps(int nt) { return nt == 1 ? 16 : 8; }
 constexpr int kLeastUnits = 4;  // of 4 bits, that a warp takes where there are more
 constexpr int kFewRows = 16;  // most rows of a sequence and head
-constexpr int kJoinThreads = 256;  // k_kv_join of D = 128 keeps 16 bytes a thread in memory for it (48 registers), of 64 8 bytes
+// k_kv_join with a warp a row has 48 registers and keeps 16 bytes a thread in memory (D = 128, 8 bits) or 8 (D = 64), or has 64 and
+// keeps none (D = 128, 4 bits); with 8 warps a row it has 63 or 64 and keeps none.
+constexpr int kJoinThreads = 256;
 
 template <int kRows>
 __device__ __forceinline__ int seq_tiles(const AttendArgs& a, const SeqView& s) {

@@ -13,7 +13,7 @@
 // go back as f16 over the scores they came from and are the left operand of the second
 // product from there, so that the next scores wait for it to end.
 //
-// x_j = scale * q.k_j * log2(e) * key scale + log2(value scale) as in kv_attend.cu; a row's
+// x_j = scale * q.k_j * log2(e) * key scale + log2(value scale) as in kv_attend_few.cuh; a row's
 // sums are rescaled only when its maximum has grown by 2^8, which weights as f16 (at most
 // 2^15 here, down to 2^-24) leave room for.
 //
