@@ -559,7 +559,7 @@ mp_status mp_kv_four_attend(const mp_kv4_cache *cache, const mp_kv_batch *batch,
 typedef struct mp_kv_blocks {
     int32_t n_seqs;       /* at most 2^28 */
     int32_t max_blocks;
-    int32_t block_tokens; /* a multiple of 32, at most 256 */
+    int32_t block_tokens; /* as the caches that the step is for have: a multiple of 32, at most 256 */
     int32_t n_blocks;     /* of the pool */
     int32_t *table;
     int32_t *free;

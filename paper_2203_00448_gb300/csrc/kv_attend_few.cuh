@@ -26,8 +26,8 @@
 // queries, first bytes: four trips one after another) and the joining launch, about 12 us.
 //
 // 4 bits.  A code times its scale is exact in f16, so both products take the values themselves: w_j = 2^(x_j - M), no value
-// scale in the sum (they take sixteenths, which cost one shift a word less).  The reference M stays until a score passes it by 2^5 (kFewGrow), which one vote a granule says; w
-// has 11 bits down to 2^-24 of it.  A granule is 4.4 KB where it is 8.2 KB of 8 bits, and takes as many products and more
+// scale in the sum (they take sixteenths, which cost one shift a word less).  The reference M stays until a score passes it by
+// 2^5 (kFewGrow), which one vote a granule says; w has 11 bits down to 2^-24 of it.  A granule is 4.4 KB where it is 8.2 KB of 8 bits, and takes as many products and more
 // operations on codes: about 580 instructions, of which 136 pick codes out of words, 128 scale them and 32 are products.
 // Measured: the 64 contexts 80 us (3.6 TB/s; 64 us without any operation on the bytes), the two long ones 119 us (4.7 TB/s;
 // 99).  What grows with the granules does so at 5.7 TB/s, 84% of a copy: 64 contexts of one length take 22 us (GPU time) and 50 for
